@@ -454,6 +454,120 @@ int pkv_decode_attention_layers(int32_t L, const pkv_decode_desc* descs,
                                 void* workspace, size_t workspace_bytes,
                                 void* stream);
 
+/*
+ * Element types of the operators below (rotary positions, prompt attention,
+ * attention over long caches).  The compression calls take bf16.
+ */
+typedef enum { PKV_BF16 = 0, PKV_FP16 = 1 } pkv_dtype;
+
+/* Which elements of a head turn together: (i, i + rot/2), or (2i, 2i + 1). */
+typedef enum { PKV_ROTARY_HALF = 0, PKV_ROTARY_INTERLEAVED = 1 } pkv_rotary_layout;
+
+/*
+ * Frequencies of rotary positions, for contexts longer than the trained one
+ * too.  HOST only, pure; in 64 bits.  With f_i = base^(-2i/rot), i < rot/2:
+ *   PKV_ROTARY_PLAIN   f_i
+ *   PKV_ROTARY_LINEAR  f_i / factor (positions are interpolated)
+ *   PKV_ROTARY_BANDS   by the turns u_i = trained * f_i / 2 pi that fit into
+ *                      the trained context: f_i / factor up to `low` turns,
+ *                      f_i from `high` turns on, between them the blend
+ *                      (1 - s) f_i / factor + s f_i, s = (u_i - low)/(high - low)
+ *   PKV_ROTARY_RAMP    with c(u) = rot ln(trained / 2 pi u) / (2 ln base), the
+ *                      pair that makes u turns: f_i / factor above
+ *                      ceil(c(low)), f_i below floor(c(high)) (both clamped to
+ *                      0 .. rot - 1), a ramp over the pairs' numbers between;
+ *                      magnitude 0.1 ln(factor) + 1 where factor > 1
+ * inv_freq_out  HOST, double[rot/2], written: radians per position.
+ * magnitude_out HOST, written: factor for cosine and sine (1 but for RAMP).
+ * Errors: rot odd or outside 2..256, base <= 1, factor < 1 or trained, low or
+ * high not positive or low >= high where they are used, any of them not
+ * finite, NULL -> PKV_ERR_INVALID_ARG.
+ */
+typedef enum {
+  PKV_ROTARY_PLAIN = 0,
+  PKV_ROTARY_LINEAR = 1,
+  PKV_ROTARY_BANDS = 2,
+  PKV_ROTARY_RAMP = 3
+} pkv_rotary_scaling;
+
+int pkv_rotary_frequencies(int32_t rot, int32_t scaling, double base,
+                           double factor, double trained, double low,
+                           double high, double* inv_freq_out,
+                           float* magnitude_out);
+
+/*
+ * Rotary positions of new tokens, and their append to a cache: the step in
+ * front of the compression (all tokens of a prompt; the calls above take
+ * rotated queries and keys) and in front of each decoding step (one token per
+ * sequence behind the rows that were kept; Sec. 3).
+ *   y_a = m (x_a cos(p f_i) - x_b sin(p f_i)),
+ *   y_b = m (x_b cos(p f_i) + x_a sin(p f_i))
+ * for the pairs (a, b) of the first `rot` elements of a head; the other
+ * elements are copied.  The angle is formed in 64 bits, the sums in fp32, one
+ * rounding to the type at the end.
+ * Token t < new_b of sequence b has row r = count_b - new_b + t of the cache
+ * and position p = positions[b][t], or r if positions is NULL.  Its rotated
+ * keys and its values go to row r of K_cache and V_cache.  A row outside
+ * [0, k_cap), or one whose page number is out of range, is never written: it
+ * is dropped and counted.  Nothing else of the caches is written.
+ */
+typedef struct {
+  int32_t B, Hq, Hkv; /* sequences, query heads, key/value heads, >= 1       */
+  int32_t d;          /* 64 or 128                                           */
+  int32_t T;          /* tokens per sequence in q, k and v, >= 1             */
+  int32_t rot;        /* elements of a head that turn: 8 .. d, a multiple
+                         of 8                                                */
+  int32_t layout;     /* pkv_rotary_layout                                   */
+  int32_t dtype;      /* pkv_dtype                                           */
+  int32_t k_cap;      /* rows per sequence the cache can hold                */
+  int32_t page_size;  /* 0: compact cache; > 0: pages                        */
+  int32_t num_pages;  /* pages in the pool                                   */
+  int32_t max_pages;  /* entries per sequence in the block table,
+                         >= ceil(k_cap / page_size)                          */
+  float magnitude;    /* m, finite                                           */
+  int32_t reserved;   /* must be 0                                           */
+  int64_t q_sb, q_sh, q_st; /* element strides of q [B,Hq,T,d]               */
+  int64_t k_sb, k_sh, k_st; /* of k [B,Hkv,T,d]                              */
+  int64_t v_sb, v_sh, v_st; /* of v [B,Hkv,T,d]                              */
+  int64_t o_sb, o_sh, o_st; /* of q_out [B,Hq,T,d]                           */
+  int64_t c_sb, c_sh, c_st; /* of a compact K_cache and V_cache
+                               [B,Hkv,k_cap,d]                               */
+  int64_t p_sb, p_sh;       /* of pos_cache [B,Hkv,k_cap]                    */
+} pkv_rotary_desc;
+
+/*
+ * desc        HOST.  Strides are >= 0 and multiples of 8 (p_*: any); those of
+ *             tensors that are not given are not looked at.
+ * q, q_out    DEVICE, 16-byte aligned, both or neither NULL.  q_out may be q
+ *             with the same strides, and overlaps it in no other way.  Rows
+ *             t >= new_b are neither read nor written.
+ * k, v, K_cache, V_cache
+ *             DEVICE, 16-byte aligned, all or none NULL; compact caches with
+ *             strides c_*, or pools [num_pages,Hkv,page_size,d] contiguous.
+ *             They overlap in one way at most: a compact cache may be k (and
+ *             v) itself, same strides, where every row r is t.
+ * inv_freq    DEVICE double[rot/2]: radians per position.
+ * positions   DEVICE int32 [B,T] contiguous, or NULL.  Any value.
+ * new_lens    DEVICE int32 [B]: new_b, clamped to 0..T; NULL: T.
+ * count       DEVICE int32 [B]: rows of the cache that are valid once the new
+ *             tokens are there (never written: a decoder adds 1 to all layers'
+ *             counts before a step); NULL: new_b.
+ * block_table DEVICE int32 [B,max_pages] contiguous (paged) or NULL.
+ * pos_cache   DEVICE int32 [B,Hkv,k_cap] or NULL: the positions of the cache's
+ *             rows (idx_out of a compression call, with room behind it);
+ *             pos_cache[b][g][r] = p is written for every g.
+ * dropped_out DEVICE int32 [B] or NULL, written: tokens of b that were dropped.
+ * Asynchronous on `stream`, needs no workspace, never allocates.
+ * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, rot not a
+ * multiple of 8, more than 2^31 - 1 tokens or workgroups), PKV_ERR_HIP.
+ */
+int pkv_rotary_append(const pkv_rotary_desc* desc, const void* q,
+                      const void* k, const void* v, const double* inv_freq,
+                      const int32_t* positions, const int32_t* new_lens,
+                      const int32_t* count, const int32_t* block_table,
+                      void* q_out, void* K_cache, void* V_cache,
+                      int32_t* pos_cache, int32_t* dropped_out, void* stream);
+
 /* Static, NUL-terminated description of a pkv_status value.  HOST only. */
 const char* pkv_status_string(int status);
 

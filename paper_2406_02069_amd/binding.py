@@ -28,7 +28,8 @@ DESC_FLAGS = 0
 EXPORTS = ["pkv_budgets", "pkv_workspace_bytes", "pkv_compress_layer", "pkv_compress_layer_noalloc", "pkv_compress_layers",
            "pkv_compress_layers_lse", "pkv_compress_layers_paged", "pkv_compress_layers_profiled",
            "pkv_budgets_schedule", "pkv_attention_recall", "pkv_decode_attention", "pkv_decode_workspace_bytes", "pkv_decode_attention_layers",
-           "pkv_decode_layers_workspace_bytes", "pkv_probe_read", "pkv_scoring_route", "pkv_scoring_sweeps", "pkv_status_string"]
+           "pkv_decode_layers_workspace_bytes", "pkv_rotary_frequencies", "pkv_rotary_append", "pkv_probe_read", "pkv_scoring_route",
+           "pkv_scoring_sweeps", "pkv_status_string"]
 
 
 class PkvError(RuntimeError):
@@ -48,6 +49,14 @@ class DecodeDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "k_cap", "page_size", "num_pages", "max_pages",
                                               "reserved", "reserved2")] + \
                [(n, ctypes.c_int64) for n in ("c_sb", "c_sh", "c_st")]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "T", "rot", "layout", "dtype", "k_cap", "page_size",
+                                              "num_pages", "max_pages")] + \
+               [("magnitude", ctypes.c_float), ("reserved", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "q_st", "k_sb", "k_sh", "k_st", "v_sb", "v_sh", "v_st",
+                                              "o_sb", "o_sh", "o_st", "c_sb", "c_sh", "c_st", "p_sb", "p_sh")]
 
 
 class PagedDesc(ctypes.Structure):
@@ -92,6 +101,11 @@ def load() -> ctypes.CDLL:
         lib.pkv_decode_layers_workspace_bytes.restype = ctypes.c_size_t
         lib.pkv_decode_attention_layers.argtypes = [i32, ctypes.POINTER(DecodeDesc)] + [vp] * 8 + [ctypes.c_size_t, vp]
         lib.pkv_decode_attention_layers.restype = ctypes.c_int
+        dbl = ctypes.c_double
+        lib.pkv_rotary_frequencies.argtypes = [i32, i32, dbl, dbl, dbl, dbl, dbl, vp, vp]
+        lib.pkv_rotary_frequencies.restype = ctypes.c_int
+        lib.pkv_rotary_append.argtypes = [ctypes.POINTER(RotaryDesc)] + [vp] * 14
+        lib.pkv_rotary_append.restype = ctypes.c_int
         lib.pkv_status_string.argtypes = [ctypes.c_int]
         lib.pkv_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -407,6 +421,134 @@ def compress_layers_paged(Q_win, K, V, k_ls, pool, pool_w, K_pages, V_pages, blo
     """pkv_compress_layers_paged: kept rows written into per-layer page pools through per-layer block tables."""
     return LayersCall(Q_win, K, V, k_ls, pool, pool_w, seq_lens, want_scores, lse=lse,
                       paged=(K_pages, V_pages, block_tables, page_size)).run()
+
+
+# ---- rotary positions, prompt attention, attention over long caches ----
+
+DTYPES = {torch.bfloat16: 0, torch.float16: 1}            # pkv_dtype
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}            # pkv_rotary_layout
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "bands": 2, "ramp": 3}
+
+
+def _on_device(device, function, *args):
+    """function(*args) with `device` current: a stream takes launches only while its device is the current one."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        return function(*args)
+    with torch.cuda.device(device):
+        return function(*args)
+
+
+def _need(t: Optional[torch.Tensor], name: str, dtype, shape, device, contiguous: bool = True):
+    """Raise unless t is None or a tensor of this type, shape and device (contiguous, or with contiguous rows)."""
+    if t is None:
+        return
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: need {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the first argument on {device}")
+    if (not t.is_contiguous()) if contiguous else (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise ValueError(f"{name}: need a contiguous {'tensor' if contiguous else 'last dimension'}")
+
+
+def _gpu(t: torch.Tensor, name: str, dims: int) -> int:
+    """The type code of a GPU tensor with `dims` dimensions, the last one contiguous."""
+    code = DTYPES.get(t.dtype)
+    if code is None or t.dim() != dims or t.stride(-1) != 1:
+        raise ValueError(f"{name}: need a {dims}-d bf16 or fp16 tensor with a contiguous last dimension")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: need a GPU tensor")
+    return code
+
+
+def _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, device):
+    """(k_cap, page_size, num_pages, max_pages, c_sb, c_sh, c_st) of a compact cache or of page pools."""
+    if block_table is None:
+        if k_cap is None:
+            k_cap = K_cache.shape[2]
+        if K_cache.dim() != 4 or k_cap > K_cache.shape[2]:
+            raise ValueError("K_cache: need [B, Hkv, k_cap, d]")
+        shape = (B, Hkv, K_cache.shape[2], d)
+        _need(K_cache, "K_cache", dtype, shape, device, False)
+        _need(V_cache, "V_cache", dtype, shape, device, False)
+        if K_cache.stride() != V_cache.stride():
+            raise ValueError("K_cache and V_cache must have the same strides")
+        return (k_cap, 0, 0, 0) + K_cache.stride()[:3]
+    if K_cache.dim() != 4 or block_table.dim() != 2:
+        raise ValueError("need pools [num_pages, Hkv, page_size, d] and a block table [B, max_pages]")
+    shape = (K_cache.shape[0], Hkv, K_cache.shape[2], d)
+    _need(K_cache, "K_cache", dtype, shape, device)
+    _need(V_cache, "V_cache", dtype, shape, device)
+    _need(block_table, "block_table", torch.int32, (B, block_table.shape[1]), device)
+    if k_cap is None:
+        k_cap = block_table.shape[1] * shape[2]
+    return k_cap, shape[2], shape[0], block_table.shape[1], 0, 0, 0
+
+
+def rotary_frequencies(rot: int, scaling: str = "plain", base: float = 10000.0, factor: float = 1.0,
+                       trained: float = 0.0, low: float = 0.0, high: float = 0.0, device=None):
+    """pkv_rotary_frequencies: (radians per position of each pair, fp64 [rot / 2] on `device`; magnitude)."""
+    out, magnitude = (ctypes.c_double * max(rot // 2, 1))(), ctypes.c_float()
+    rc = load().pkv_rotary_frequencies(rot, ROTARY_SCALINGS[scaling], base, factor, trained, low, high, out,
+                                       ctypes.byref(magnitude))
+    if rc != OK:
+        raise PkvError(rc, "pkv_rotary_frequencies")
+    return torch.tensor(list(out), dtype=torch.float64, device=device), float(magnitude.value)
+
+
+def rotary_append(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optional[torch.Tensor], inv_freq: torch.Tensor,
+                  K_cache: Optional[torch.Tensor] = None, V_cache: Optional[torch.Tensor] = None,
+                  count: Optional[torch.Tensor] = None, layout: str = "half", magnitude: float = 1.0,
+                  positions: Optional[torch.Tensor] = None, new_lens: Optional[torch.Tensor] = None,
+                  block_table: Optional[torch.Tensor] = None, k_cap: Optional[int] = None,
+                  pos_cache: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                  dropped: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """pkv_rotary_append on the current stream.  q [B,Hq,T,d] (None: keys and values only) and k, v [B,Hkv,T,d] (None:
+    queries only) with any strides; inv_freq fp64 [rot / 2] turns the first rot elements of a head.  The new tokens are
+    the last rows of the cache's count[b] (compact [B,Hkv,k_cap,d], or pools with a block table).  Returns the rotated
+    queries: q_out (which may be q), or a new contiguous tensor whose rows beyond new_lens are zero."""
+    first = q if q is not None else k
+    if first is None or (k is None) != (v is None) or (k is None) != (K_cache is None) or (k is None) != (V_cache is None):
+        raise ValueError("need q, or k and v with their caches, or both")
+    code, device = _gpu(first, "q" if q is not None else "k", 4), first.device
+    B, H, T, d = first.shape
+    Hkv = H if k is None else k.shape[1]
+    rot = 2 * inv_freq.numel()
+    _need(inv_freq, "inv_freq", torch.float64, (rot // 2,), device)
+    qs = os_ = ks = vs = ps = (0, 0, 0)
+    cache = (1, 0, 0, 0, 0, 0, 0)
+    if q is not None:
+        if q_out is None:
+            q_out = (torch.empty if new_lens is None else torch.zeros)((B, H, T, d), dtype=q.dtype, device=device)
+        else:
+            _need(q_out, "q_out", q.dtype, q.shape, device, False)
+        qs, os_ = q.stride(), q_out.stride()
+    if k is not None:
+        _need(k, "k", first.dtype, (B, Hkv, T, d), device, False)
+        _need(v, "v", first.dtype, (B, Hkv, T, d), device, False)
+        ks, vs = k.stride(), v.stride()
+        cache = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, first.dtype, device)
+    if pos_cache is not None:
+        _need(pos_cache, "pos_cache", torch.int32, (B, Hkv, pos_cache.shape[2]), device, False)
+        if pos_cache.shape[2] < cache[0]:
+            raise ValueError("pos_cache: shorter than the cache")
+        ps = pos_cache.stride()
+    _need(positions, "positions", torch.int32, (B, T), device)
+    _need(new_lens, "new_lens", torch.int32, (B,), device)
+    _need(count, "count", torch.int32, (B,), device)
+    _need(dropped, "dropped", torch.int32, (B,), device)
+    desc = RotaryDesc(B, H if q is not None else Hkv, Hkv, d, T, rot, ROTARY_LAYOUTS[layout], code, cache[0], cache[1], cache[2],
+                      cache[3], magnitude, 0, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                      os_[0], os_[1], os_[2], cache[4], cache[5], cache[6], ps[0], ps[1])
+    rc = _on_device(device, load().pkv_rotary_append, ctypes.byref(desc), _a(q), _a(k), _a(v), inv_freq.data_ptr(),
+                    _a(positions), _a(new_lens), _a(count), _a(block_table), _a(q_out), _a(K_cache), _a(V_cache),
+                    _a(pos_cache), _a(dropped), _stream_ptr(device))
+    if rc != OK:
+        raise PkvError(rc, "pkv_rotary_append")
+    return q_out
+
+
+def _a(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 def probe_read(buf: torch.Tensor, sink: torch.Tensor) -> None:
