@@ -568,6 +568,71 @@ int pkv_rotary_append(const pkv_rotary_desc* desc, const void* q,
                       void* q_out, void* K_cache, void* V_cache,
                       int32_t* pos_cache, int32_t* dropped_out, void* stream);
 
+/*
+ * pkv_decode_attention for caches of any length and any number of query heads
+ * per KV head: the single-token form of pkv_prefill_attention.  Rows of the
+ * cache are keys 0 .. count_b - 1 with the positions positions[b][g][j] (the
+ * kept rows of a compression call: its idx_out), or j if positions is NULL;
+ * the query's position is q_pos_b, or count_b - 1 if q_pos is NULL.  A row is
+ * seen if 0 <= position <= q's and, with a window, position > q's - window.
+ * Scores, softmax and lse as pkv_prefill_attention's; the softmax weights keep
+ * 16 bits and more.  A page number out of range makes its rows count as
+ * absent.
+ */
+typedef struct {
+  int32_t B, Hq, Hkv; /* Hq % Hkv == 0                                       */
+  int32_t d;          /* 64 or 128                                           */
+  int32_t k_cap;      /* rows per sequence the cache can hold                */
+  int32_t page_size;  /* 0: compact cache; > 0: paged                        */
+  int32_t num_pages;  /* paged: pages in the pool                            */
+  int32_t max_pages;  /* paged: entries per sequence in the block table,
+                         >= ceil(k_cap / page_size)                          */
+  int32_t dtype;      /* pkv_dtype                                           */
+  int32_t window;     /* 0: none; > 0                                        */
+  float scale;        /* > 0; 0: 1/sqrt(d)                                   */
+  float cap;          /* 0: none; > 0                                        */
+  int64_t q_sb, q_sh;       /* element strides of q [B,Hq,d]                 */
+  int64_t c_sb, c_sh, c_st; /* compact: of K_cache and V_cache
+                               [B,Hkv,k_cap,d]                               */
+  int64_t p_sb, p_sh;       /* of positions [B,Hkv,k_cap]                    */
+} pkv_decode_long_desc;
+
+/*
+ * Bytes of DEVICE workspace pkv_decode_attention_long needs for this shape (0
+ * for shapes it serves with one workgroup per sequence and head; 0 as well if
+ * the descriptor is invalid).  HOST only, pure.
+ */
+size_t pkv_decode_long_workspace_bytes(const pkv_decode_long_desc* desc);
+
+/*
+ * desc        HOST.  Strides are >= 0 and multiples of 8 (p_*: any).
+ * q           DEVICE, of the descriptor's type, 16-byte aligned.
+ * K_cache, V_cache
+ *             DEVICE, 16-byte aligned: compact with strides c_*, or pools
+ *             [num_pages,Hkv,page_size,d] contiguous.
+ * block_table DEVICE int32 [B,max_pages] contiguous (paged) or NULL.
+ * count       DEVICE int32 [B], clamped to 0..k_cap.
+ * positions   DEVICE int32 or NULL.
+ * q_pos       DEVICE int32 [B] or NULL.
+ * slopes      DEVICE fp32 [Hq] or NULL.  Finite.
+ * out         DEVICE [B,Hq,d] contiguous, of the descriptor's type, 16-byte
+ *             aligned, written (zero where no row is seen).
+ * lse_out     DEVICE fp32 [B,Hq] contiguous, or NULL (-inf where no row is
+ *             seen).
+ * workspace   as pkv_decode_attention's, pkv_decode_long_workspace_bytes.
+ * Asynchronous on `stream`, never allocates.
+ * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv >
+ * 128, B > 65535, k_cap > 2^30, too many workgroups), PKV_ERR_WORKSPACE,
+ * PKV_ERR_HIP.
+ */
+int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q,
+                              const void* K_cache, const void* V_cache,
+                              const int32_t* block_table,
+                              const int32_t* count, const int32_t* positions,
+                              const int32_t* q_pos, const float* slopes,
+                              void* out, float* lse_out, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
 /* Static, NUL-terminated description of a pkv_status value.  HOST only. */
 const char* pkv_status_string(int status);
 

@@ -28,7 +28,8 @@ DESC_FLAGS = 0
 EXPORTS = ["pkv_budgets", "pkv_workspace_bytes", "pkv_compress_layer", "pkv_compress_layer_noalloc", "pkv_compress_layers",
            "pkv_compress_layers_lse", "pkv_compress_layers_paged", "pkv_compress_layers_profiled",
            "pkv_budgets_schedule", "pkv_attention_recall", "pkv_decode_attention", "pkv_decode_workspace_bytes", "pkv_decode_attention_layers",
-           "pkv_decode_layers_workspace_bytes", "pkv_rotary_frequencies", "pkv_rotary_append", "pkv_probe_read", "pkv_scoring_route",
+           "pkv_decode_layers_workspace_bytes", "pkv_rotary_frequencies", "pkv_rotary_append", "pkv_decode_attention_long",
+           "pkv_decode_long_workspace_bytes", "pkv_probe_read", "pkv_scoring_route",
            "pkv_scoring_sweeps", "pkv_status_string"]
 
 
@@ -57,6 +58,13 @@ class RotaryDesc(ctypes.Structure):
                [("magnitude", ctypes.c_float), ("reserved", ctypes.c_int32)] + \
                [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "q_st", "k_sb", "k_sh", "k_st", "v_sb", "v_sh", "v_st",
                                               "o_sb", "o_sh", "o_st", "c_sb", "c_sh", "c_st", "p_sb", "p_sh")]
+
+
+class DecodeLongDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "k_cap", "page_size", "num_pages", "max_pages", "dtype",
+                                              "window")] + \
+               [("scale", ctypes.c_float), ("cap", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "c_sb", "c_sh", "c_st", "p_sb", "p_sh")]
 
 
 class PagedDesc(ctypes.Structure):
@@ -106,6 +114,10 @@ def load() -> ctypes.CDLL:
         lib.pkv_rotary_frequencies.restype = ctypes.c_int
         lib.pkv_rotary_append.argtypes = [ctypes.POINTER(RotaryDesc)] + [vp] * 14
         lib.pkv_rotary_append.restype = ctypes.c_int
+        lib.pkv_decode_attention_long.argtypes = [ctypes.POINTER(DecodeLongDesc)] + [vp] * 11 + [ctypes.c_size_t, vp]
+        lib.pkv_decode_attention_long.restype = ctypes.c_int
+        lib.pkv_decode_long_workspace_bytes.argtypes = [ctypes.POINTER(DecodeLongDesc)]
+        lib.pkv_decode_long_workspace_bytes.restype = ctypes.c_size_t
         lib.pkv_status_string.argtypes = [ctypes.c_int]
         lib.pkv_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -545,6 +557,63 @@ def rotary_append(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optio
     if rc != OK:
         raise PkvError(rc, "pkv_rotary_append")
     return q_out
+
+
+def decode_attention_long(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch.Tensor, count: torch.Tensor,
+                          block_table: Optional[torch.Tensor] = None, k_cap: Optional[int] = None,
+                          positions: Optional[torch.Tensor] = None, q_pos: Optional[torch.Tensor] = None,
+                          slopes: Optional[torch.Tensor] = None, cap: float = 0.0, window: int = 0,
+                          scale: Optional[float] = None, want_lse: bool = False, out: Optional[torch.Tensor] = None,
+                          lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """pkv_decode_attention_long on the current stream.  q [B,Hq,d]; compact cache [B,Hkv,k_cap,d] (any row strides) or
+    pools [num_pages,Hkv,page_size,d] with block_table int32 [B,max_pages]; count int32 [B]; positions int32
+    [B,Hkv,>= k_cap] of the cache's rows and q_pos int32 [B]; slopes fp32 [Hq].
+    Returns (out [B,Hq,d] of q's type, lse fp32 [B,Hq] or None)."""
+    code, device = _gpu(q, "q", 3), q.device
+    B, Hq, d = q.shape
+    if K_cache.dim() != 4:
+        raise ValueError("K_cache: need four dimensions")
+    Hkv = K_cache.shape[1]
+    cache = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, q.dtype, device)
+    _need(count, "count", torch.int32, (B,), device)
+    _need(q_pos, "q_pos", torch.int32, (B,), device)
+    _need(slopes, "slopes", torch.float32, (Hq,), device)
+    ps = (0, 0)
+    if positions is not None:
+        _need(positions, "positions", torch.int32, (B, Hkv, positions.shape[2]), device, False)
+        if positions.shape[2] < cache[0]:
+            raise ValueError("positions: shorter than the cache")
+        ps = positions.stride()
+    if out is None:
+        out = torch.empty((B, Hq, d), dtype=q.dtype, device=device)
+    else:
+        _need(out, "out", q.dtype, (B, Hq, d), device)
+    if want_lse and lse is None:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=device)
+    _need(lse, "lse", torch.float32, (B, Hq), device)
+    desc = DecodeLongDesc(B, Hq, Hkv, d, cache[0], cache[1], cache[2], cache[3], code, window, _scale(scale), cap,
+                          q.stride(0), q.stride(1), cache[4], cache[5], cache[6], ps[0], ps[1])
+    ref = ctypes.byref(desc)
+    lib = load()
+    if workspace is None:  # (a workspace that is handed over is checked by the call)
+        need = lib.pkv_decode_long_workspace_bytes(ref)
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    rc = _on_device(device, lib.pkv_decode_attention_long, ref, q.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(),
+                    _a(block_table), count.data_ptr(), _a(positions), _a(q_pos), _a(slopes), out.data_ptr(), _a(lse),
+                    _a(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(device))
+    if rc != OK:
+        raise PkvError(rc, "pkv_decode_attention_long")
+    return out, lse
+
+
+def _scale(scale: Optional[float]) -> float:
+    """The descriptors' scale, where 0 stands for 1 / sqrt(d): a scale that is given is a positive number."""
+    if scale is None:
+        return 0.0
+    if not scale > 0:
+        raise ValueError("scale must be positive")
+    return float(scale)
 
 
 def _a(t: Optional[torch.Tensor]):
