@@ -569,6 +569,76 @@ int pkv_rotary_append(const pkv_rotary_desc* desc, const void* q,
                       int32_t* pos_cache, int32_t* dropped_out, void* stream);
 
 /*
+ * Attention of a prompt, or of the last part of one, over its keys: where the
+ * window queries' softmax denominators that pkv_compress_layers_lse takes
+ * come from, and the prompt's attention itself.
+ * Query row t of sequence b has position p = q_start_b + t.  It is there if
+ * 0 <= p < n_b, and sees the keys j with lo <= j <= hi,
+ *   lo = max(doc_start[b][p], p - window + 1, 0),
+ *   hi = max(p, prefix_end[b][p] - 1), and j < n_b
+ * (without doc_start, window or prefix_end: without their part).
+ *   s_j = q_p . k_j * scale;  cap > 0: s_j = cap tanh(s_j / cap);
+ *   slopes: s_j -= slopes[h] |p - j|
+ *   out[b][h][t] = sum_j softmax_j(s) V_j,  lse[b][h][t] = ln sum_j exp(s_j)
+ * Rows that are not there, or see no key: zero and -inf.
+ * fp32 scores, sums and accumulation; the softmax weights are rounded to the
+ * input's type for the product with V.  Rows >= n_b of K and V are never
+ * read.  A key that a query does not see has no influence on its row,
+ * whatever it holds (NaN and infinities included).
+ */
+typedef struct {
+  int32_t B, Hq, Hkv; /* Hq % Hkv == 0                                       */
+  int32_t d;          /* 64 or 128                                           */
+  int32_t T;          /* query rows per sequence, >= 1                       */
+  int32_t N;          /* (padded) length of K and V, >= 1                    */
+  int32_t dtype;      /* pkv_dtype                                           */
+  int32_t window;     /* 0: none; > 0: keys a query sees, itself included    */
+  float scale;        /* > 0; 0: 1/sqrt(d)                                   */
+  float cap;          /* 0: none; > 0                                        */
+  int64_t q_sb, q_sh, q_st;    /* element strides of q [B,Hq,T,d]            */
+  int64_t kv_sb, kv_sh, kv_st; /* of K and of V [B,Hkv,N,d]                  */
+  int64_t o_sb, o_sh, o_st;    /* of out [B,Hq,T,d]                          */
+} pkv_prefill_desc;
+
+/*
+ * Bytes of DEVICE workspace pkv_prefill_attention needs for this shape (0
+ * where the query rows alone fill the device; 0 as well if the descriptor is
+ * invalid).  HOST only, pure.
+ */
+size_t pkv_prefill_workspace_bytes(const pkv_prefill_desc* desc);
+
+/*
+ * desc       HOST.  Strides are >= 0 and multiples of 8.
+ * q, K, V, out
+ *            DEVICE, of the descriptor's type, 16-byte aligned; out overlaps
+ *            nothing.
+ * seq_lens   DEVICE int32 [B]: n_b, clamped to 0..N; NULL: N.
+ * q_start    DEVICE int32 [B] or NULL (0).  Any value.
+ * doc_start  DEVICE int32 [B,N] contiguous or NULL: where the document of
+ *            position p begins.  Any value.
+ * prefix_end DEVICE int32 [B,N] contiguous or NULL: the position behind the
+ *            keys that p sees although they lie behind it.  Any value.
+ * slopes     DEVICE fp32 [Hq] or NULL.  Finite.
+ * lse_out    DEVICE fp32 [B,Hq,T] contiguous, or NULL.  With scale 0 and
+ *            neither cap, slopes, window, doc_start nor prefix_end, the rows
+ *            of the last alpha tokens are what pkv_compress_layers_lse takes.
+ * workspace  DEVICE, 256-byte aligned, >= pkv_prefill_workspace_bytes(desc)
+ *            bytes (may be NULL when that is 0); contents irrelevant on
+ *            entry, undefined on exit; concurrent calls need distinct ones.
+ * Asynchronous on `stream`, never allocates.
+ * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv >
+ * 128, B > 65535, N or T > 2^30, T * Hq/Hkv > 2^31 - 256, too many workgroups),
+ * PKV_ERR_WORKSPACE, PKV_ERR_HIP.
+ */
+int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q,
+                          const void* K, const void* V,
+                          const int32_t* seq_lens, const int32_t* q_start,
+                          const int32_t* doc_start, const int32_t* prefix_end,
+                          const float* slopes, void* out, float* lse_out,
+                          void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
  * pkv_decode_attention for caches of any length and any number of query heads
  * per KV head: the single-token form of pkv_prefill_attention.  Rows of the
  * cache are keys 0 .. count_b - 1 with the positions positions[b][g][j] (the

@@ -28,7 +28,7 @@ DESC_FLAGS = 0
 EXPORTS = ["pkv_budgets", "pkv_workspace_bytes", "pkv_compress_layer", "pkv_compress_layer_noalloc", "pkv_compress_layers",
            "pkv_compress_layers_lse", "pkv_compress_layers_paged", "pkv_compress_layers_profiled",
            "pkv_budgets_schedule", "pkv_attention_recall", "pkv_decode_attention", "pkv_decode_workspace_bytes", "pkv_decode_attention_layers",
-           "pkv_decode_layers_workspace_bytes", "pkv_rotary_frequencies", "pkv_rotary_append", "pkv_decode_attention_long",
+           "pkv_decode_layers_workspace_bytes", "pkv_rotary_frequencies", "pkv_rotary_append", "pkv_prefill_attention", "pkv_prefill_workspace_bytes", "pkv_decode_attention_long",
            "pkv_decode_long_workspace_bytes", "pkv_probe_read", "pkv_scoring_route",
            "pkv_scoring_sweeps", "pkv_status_string"]
 
@@ -58,6 +58,12 @@ class RotaryDesc(ctypes.Structure):
                [("magnitude", ctypes.c_float), ("reserved", ctypes.c_int32)] + \
                [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "q_st", "k_sb", "k_sh", "k_st", "v_sb", "v_sh", "v_st",
                                               "o_sb", "o_sh", "o_st", "c_sb", "c_sh", "c_st", "p_sb", "p_sh")]
+
+
+class PrefillDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "T", "N", "dtype", "window")] + \
+               [("scale", ctypes.c_float), ("cap", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "q_st", "kv_sb", "kv_sh", "kv_st", "o_sb", "o_sh", "o_st")]
 
 
 class DecodeLongDesc(ctypes.Structure):
@@ -114,6 +120,10 @@ def load() -> ctypes.CDLL:
         lib.pkv_rotary_frequencies.restype = ctypes.c_int
         lib.pkv_rotary_append.argtypes = [ctypes.POINTER(RotaryDesc)] + [vp] * 14
         lib.pkv_rotary_append.restype = ctypes.c_int
+        lib.pkv_prefill_attention.argtypes = [ctypes.POINTER(PrefillDesc)] + [vp] * 11 + [ctypes.c_size_t, vp]
+        lib.pkv_prefill_attention.restype = ctypes.c_int
+        lib.pkv_prefill_workspace_bytes.argtypes = [ctypes.POINTER(PrefillDesc)]
+        lib.pkv_prefill_workspace_bytes.restype = ctypes.c_size_t
         lib.pkv_decode_attention_long.argtypes = [ctypes.POINTER(DecodeLongDesc)] + [vp] * 11 + [ctypes.c_size_t, vp]
         lib.pkv_decode_attention_long.restype = ctypes.c_int
         lib.pkv_decode_long_workspace_bytes.argtypes = [ctypes.POINTER(DecodeLongDesc)]
@@ -557,6 +567,53 @@ def rotary_append(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optio
     if rc != OK:
         raise PkvError(rc, "pkv_rotary_append")
     return q_out
+
+
+def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_lens: Optional[torch.Tensor] = None,
+                      q_start: Optional[torch.Tensor] = None, doc_start: Optional[torch.Tensor] = None,
+                      prefix_end: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None, cap: float = 0.0,
+                      window: int = 0, scale: Optional[float] = None, want_lse: bool = False,
+                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None):
+    """pkv_prefill_attention on the current stream.  q [B,Hq,T,d] at positions q_start[b] (0) and on, K and V [B,Hkv,N,d]
+    of the same strides; seq_lens, q_start int32 [B]; doc_start, prefix_end int32 [B,N]; slopes fp32 [Hq].
+    Returns (out [B,Hq,T,d] of q's type, lse fp32 [B,Hq,T] or None)."""
+    code, device = _gpu(q, "q", 4), q.device
+    B, Hq, T, d = q.shape
+    if K.dim() != 4:
+        raise ValueError("K: need four dimensions")
+    Hkv, N = K.shape[1], K.shape[2]
+    _need(K, "K", q.dtype, (B, Hkv, N, d), device, False)
+    _need(V, "V", q.dtype, (B, Hkv, N, d), device, False)
+    if K.stride() != V.stride():
+        raise ValueError("K and V must have the same strides")
+    _need(seq_lens, "seq_lens", torch.int32, (B,), device)
+    _need(q_start, "q_start", torch.int32, (B,), device)
+    _need(doc_start, "doc_start", torch.int32, (B, N), device)
+    _need(prefix_end, "prefix_end", torch.int32, (B, N), device)
+    _need(slopes, "slopes", torch.float32, (Hq,), device)
+    if out is None:
+        out = torch.empty((B, Hq, T, d), dtype=q.dtype, device=device)
+    else:
+        _need(out, "out", q.dtype, q.shape, device, False)
+    if want_lse and lse is None:
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=device)
+    _need(lse, "lse", torch.float32, (B, Hq, T), device)
+    qs, ks, os_ = q.stride(), K.stride(), out.stride()
+    desc = PrefillDesc(B, Hq, Hkv, d, T, N, code, window, _scale(scale), cap, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
+                       os_[0], os_[1], os_[2])
+    ref = ctypes.byref(desc)
+    lib = load()
+    if workspace is None:  # (a workspace that is handed over is checked by the call)
+        need = lib.pkv_prefill_workspace_bytes(ref)
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    rc = _on_device(device, lib.pkv_prefill_attention, ref, q.data_ptr(), K.data_ptr(), V.data_ptr(), _a(seq_lens), _a(q_start),
+                    _a(doc_start), _a(prefix_end), _a(slopes), out.data_ptr(), _a(lse), _a(workspace),
+                    0 if workspace is None else workspace.numel(), _stream_ptr(device))
+    if rc != OK:
+        raise PkvError(rc, "pkv_prefill_attention")
+    return out, lse
 
 
 def decode_attention_long(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch.Tensor, count: torch.Tensor,

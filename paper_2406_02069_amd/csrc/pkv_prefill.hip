@@ -1,0 +1,509 @@
+// Attention of a prompt over its keys (include/pkv.h: pkv_prefill_attention).
+//
+// Matrix-bound: 4 d products-and-sums per (query row, seen key), for which K and V come from LDS.
+// Work split: the G T query rows of a KV head (row = token * G + head, so that a tile of rows covers few tokens and hardly more
+// keys than its rows see) in tiles of 128, a workgroup of four waves each, 32 rows a wave; the longest tiles first.  Workgroups
+// that follow one another take different KV heads: with eight of them each XCD's cache holds the keys of one.  Few rows: the
+// keys of a tile are cut into S ranges, whose un-normalised results a second kernel joins in order.
+//   keys    64 at a time, K and V straight from memory into LDS, double-buffered: the next step's are requested when a step
+//           begins, one barrier per step.  16-byte pieces of a row are swapped (through the lanes' addresses in memory) so that
+//           neither way of reading them meets the same bank twice.
+//   scores  S^T = K Q^T in v_mfma_f32_32x32x16: a lane ends with 32 keys of one query row (column), the other half of the wave
+//           with the other 32, so that maxima and sums stay in the lane.
+//   softmax a reference exponent per row, moved only when a score exceeds it by a factor of 2^6.  The weights are rounded to the
+//           type (as the result is), their sum is not.
+//   values  O^T += V^T P^T: the weights are in B's layout already if the 16 keys of a step are taken in the order in which the
+//           lanes hold them; V^T is read column-wise.
+// Masks leave each row an interval of keys.  Steps that no row of a wave sees are skipped, those that all of its rows see whole
+// take no comparisons.  In the others hidden keys have the weight 0; a value that is not finite would still spoil their product,
+// so the waves look over the rows that they fetched for such a step, put zeros in LDS for such values, and add them afterwards for
+// the rows that see them.
+#include <math.h>
+#include <string.h>
+
+#include <type_traits>
+
+#include "pkv_attn.h"
+#include "pkv_lds.h"
+
+namespace pkv {
+namespace {
+
+constexpr int kRows = 128;   // query rows of a workgroup
+constexpr int kKeys = 64;    // keys per step
+constexpr int kMaxParts = 64;  // ranges of keys
+
+struct PrefillArgs {
+  const uint16_t *q, *K, *V;
+  const int32_t *seq_lens, *q_start, *doc_start, *prefix_end;
+  const float* slopes;
+  uint16_t* out;
+  float* lse;
+  float* part_o;   // [B * Hkv][T * G][S][d]
+  float* part_mz;  // [B * Hkv][T * G][S][2]
+  int32_t B, Hq, Hkv, G, T, N, window, S, tiles;
+  int64_t q_sb, q_sh, q_st, kv_sb, kv_sh, kv_st, o_sb, o_sh, o_st;
+  float scale;               // of the products; with a cap: natural units, without: log2
+  float cap2, two_over_cap;  // cap in log2 units (0: none); 2 log2(e) / cap
+};
+
+// What the masks leave a query row: keys lo .. hi (none: lo > hi).
+struct Seen {
+  int32_t lo, hi, p;
+};
+__device__ __forceinline__ Seen seen_keys(const PrefillArgs& a, int b, int t, int n) {
+  Seen s;
+  const int64_t p = (int64_t)(a.q_start ? a.q_start[b] : 0) + t;
+  s.p = (int32_t)p;
+  s.lo = 1;
+  s.hi = 0;
+  if (p >= 0 && p < n) {
+    int lo = 0, hi = s.p;
+    if (a.window) lo = max(lo, s.p - a.window + 1);
+    if (a.doc_start) lo = max(lo, a.doc_start[(int64_t)b * a.N + p]);
+    if (a.prefix_end) hi = max(hi, max(min(a.prefix_end[(int64_t)b * a.N + p], n), 0) - 1);
+    if (lo <= hi) {
+      s.lo = lo;
+      s.hi = hi;
+    }
+  }
+  return s;
+}
+
+__device__ __forceinline__ int wave_max(int x) {
+  for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
+  return x;
+}
+
+// 16 bytes per lane from base + at into LDS, lane after lane from byte `to` on.  Asynchronous: wait_loads.  (Written out because
+// the compiler lets every later read of LDS wait for such a load, though it goes to another buffer; nothing is returned in
+// registers.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is a register that the compiler keeps to itself; nothing else here uses it)
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
+// Halves of a word whose exponent is all ones (bit 15, bit 31 set).
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t u);
+template <>
+__device__ __forceinline__ uint32_t not_finite<__bf16>(uint32_t u) {
+  return ((u & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+template <>
+__device__ __forceinline__ uint32_t not_finite<_Float16>(uint32_t u) {
+  return ((u & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+}
+
+// The first key of register i of a 32 x 32 product, in the lower half of the wave (the upper half: 4 more).
+__device__ __forceinline__ constexpr int key_of(int i) { return 8 * (i >> 2) + (i & 3); }
+
+template <int D>
+__device__ __forceinline__ int swizzle_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int swizzle_v(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
+
+// MODE 1: scores are capped or biased.
+template <typename T, int D, int MODE>
+__global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
+  constexpr int STEPS = D / 16, MB = D / 32, PIECES = D / 8, ROWS_PER_LOAD = 64 / PIECES, LOADS = 16 / ROWS_PER_LOAD;
+  constexpr int ROW = D * 2, BUF = kKeys * ROW;
+  constexpr float SHIFT = sizeof(T) == 2 && __is_same(T, _Float16) ? 8.0f : 0.0f;  // fp16 weights: away from its subnormals
+  __shared__ __align__(1024) char lds[4 * BUF];  // [buffer][K, V]
+  __shared__ int lds_range[4][4];
+  __shared__ uint32_t lds_bad[2][4];             // [buffer][wave]: rows of V (16 per wave) that hold a value that is not finite
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  const int units = a.B * a.Hkv;
+  const int unit = blockIdx.x % units, rest = blockIdx.x / units;
+  const int part = rest % a.S, tile = a.tiles - 1 - rest / a.S;
+  const int b = unit / a.Hkv, g = unit % a.Hkv;
+  const int n = a.seq_lens ? min(max(a.seq_lens[b], 0), a.N) : a.N;
+
+  const int64_t rows = (int64_t)a.T * a.G;
+  const int64_t row = (int64_t)tile * kRows + 32 * wave + col;
+  const bool there = row < rows;
+  const int t = there ? (int)(row / a.G) : 0, h = g * a.G + (there ? (int)(row % a.G) : 0);
+  Seen seen = {1, 0, 0};
+  if (there) seen = seen_keys(a, b, t, n);
+  const bool some = seen.lo <= seen.hi;
+
+  // Keys of the wave and of the workgroup: the span that some row sees, and the span that all rows see whole.
+  const int first_w = -wave_max(some ? -seen.lo : -0x7FFFFFFF), last_w = wave_max(some ? seen.hi : -1);
+  const int lo_w = wave_max(some ? seen.lo : 0), hi_w = -wave_max(some ? -seen.hi : -0x7FFFFFFF);
+  if (lane == 0) {
+    lds_range[wave][0] = first_w;
+    lds_range[wave][1] = last_w;
+    lds_range[wave][2] = lo_w;
+    lds_range[wave][3] = hi_w;
+  }
+  __syncthreads();
+  int first = 0x7FFFFFFF, last = -1, lo_g = 0, hi_g = 0x7FFFFFFF;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    first = min(first, __builtin_amdgcn_readfirstlane(lds_range[w][0]));
+    last = max(last, __builtin_amdgcn_readfirstlane(lds_range[w][1]));
+    lo_g = max(lo_g, __builtin_amdgcn_readfirstlane(lds_range[w][2]));
+    hi_g = min(hi_g, __builtin_amdgcn_readfirstlane(lds_range[w][3]));
+  }
+  int step = 0, step_end = 0;
+  if (last >= 0) {
+    step = first / kKeys;
+    step_end = last / kKeys + 1;
+  }
+  if (a.S > 1) {
+    const int per = (step_end - step + a.S - 1) / a.S;
+    const int s0 = step + part * per;
+    step_end = min(step_end, s0 + per);
+    step = min(s0, step_end);
+  }
+
+  // Fetching a step: wave w rows 16 w .. 16 w + 15 of K and of V, a row's pieces swapped.
+  const char* const Kb = reinterpret_cast<const char*>(a.K + b * a.kv_sb + g * a.kv_sh);
+  const char* const Vb = reinterpret_cast<const char*>(a.V + b * a.kv_sb + g * a.kv_sh);
+  const uint32_t stride = (uint32_t)(a.kv_st * 2);
+  uint32_t at_k[LOADS], at_v[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int r = 16 * wave + i * ROWS_PER_LOAD + lane / PIECES, piece = lane % PIECES;
+    at_k[i] = r * stride + 16 * (piece ^ swizzle_k<D>(r));
+    at_v[i] = r * stride + 16 * (piece ^ swizzle_v<D>(r));
+  }
+  auto fetch = [&](int st, int buf) {
+    const int64_t base = (int64_t)st * kKeys * stride;
+    const int most = n - 1 - st * kKeys;  // rows behind the last one are taken as the last
+    const uint32_t to = lds_base + buf * 2 * BUF + 16 * wave * ROW;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      uint32_t back = 0;
+      if (most < kKeys - 1) {
+        const int r = 16 * wave + i * ROWS_PER_LOAD + lane / PIECES;
+        back = (uint32_t)max(r - most, 0) * stride;
+      }
+      load_to_lds(Kb + base, at_k[i] - back, to + i * 1024);
+      load_to_lds(Vb + base, at_v[i] - back, to + i * 1024 + BUF);
+    }
+  };
+  if (step < step_end) fetch(step, 0);
+
+  u32x4 qf[STEPS];
+  {
+    const uint16_t* qp = a.q + b * a.q_sb + h * a.q_sh + t * a.q_st + 8 * half;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) qf[i] = some ? *reinterpret_cast<const u32x4*>(qp + 16 * i) : (u32x4)(0);
+  }
+  const float slope = MODE == 1 && a.slopes ? a.slopes[h] * kLog2e : 0.0f;
+
+  float m = kNone, z = 0.0f;
+  f32x16 o[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) o[i] = (f32x16)(0.0f);
+
+  // Places in a step's rows: for scores this lane's row (K, and 32 rows on), for values its place in a block of 8 keys x 32
+  // columns.  What is added to them is known at compile time.
+  const int k_at = col * ROW + ((half ^ swizzle_k<D>(col)) << 4);
+  const int v_row = 4 * half + ((lane & 15) >> 2), v_piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const int v_at = v_row * ROW + ((v_piece ^ swizzle_v<D>(v_row)) << 4) + 8 * (lane & 1);
+
+  auto one_step = [&](auto buffer) {
+    constexpr int buf = decltype(buffer)::value;
+    const char* const Kl = lds + buf * 2 * BUF;
+    char* const Vl = lds + buf * 2 * BUF + BUF;
+    const int key0 = step * kKeys;
+    const bool cut = key0 < lo_g || key0 + kKeys - 1 > hi_g;  // some row of the workgroup does not see all of the step
+    wait_loads();
+    if (cut) {  // the rows of V that this wave fetched
+      uint32_t bad = 0;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        u32x4* const at = reinterpret_cast<u32x4*>(Vl + (16 * wave + i * ROWS_PER_LOAD) * ROW + 16 * lane);
+        u32x4 v = *at;
+        uint32_t any = 0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t nf = not_finite<T>(v[x]);
+          any |= nf;
+          v[x] &= ~((nf >> 15) * 0xFFFFu);
+        }
+        if (any) {
+          *at = v;
+          bad |= 1u << (i * ROWS_PER_LOAD + lane / PIECES);
+        }
+      }
+      uint32_t all = 0;
+      if (__any(bad != 0)) {
+        for (int i = 0; i < 16; ++i) all |= __any((bad >> i) & 1) ? 1u << i : 0u;
+      }
+      if (lane == 0) lds_bad[buf][wave] = all;
+    }
+    lds_barrier();
+    if (step + 1 < step_end) fetch(step + 1, buf ^ 1);
+    if (key0 > last_w || key0 + kKeys - 1 < first_w) return;
+    f32x16 sc[2];
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const u32x4 kf = *reinterpret_cast<const u32x4*>(Kl + (k_at ^ (i << 5)) + 32 * kt * ROW);
+        sc[kt] = Elem<T>::mfma32(kf, qf[i], i == 0 ? (f32x16)(0.0f) : sc[kt]);
+      }
+    }
+    if constexpr (MODE == 1) {
+      if (a.cap2 != 0.0f) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sc[e >> 4][e & 15] = capped(sc[e >> 4][e & 15] * a.scale, a.two_over_cap, a.cap2);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sc[e >> 4][e & 15] *= a.scale;
+      }
+      if (a.slopes) {
+        const float far = (float)(seen.p - key0 - 4 * half);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sc[e >> 4][e & 15] = fmaf(-slope, fabsf(far - (float)(32 * (e >> 4) + key_of(e & 15))), sc[e >> 4][e & 15]);
+      }
+    }
+    if (key0 < lo_w || key0 + kKeys - 1 > hi_w) {
+      const uint32_t from = (uint32_t)(seen.lo - key0 - 4 * half), width = (uint32_t)(seen.hi - seen.lo);
+#pragma unroll
+      for (int e = 0; e < 32; ++e)
+        if (!some || (uint32_t)(32 * (e >> 4) + key_of(e & 15)) - from > width) sc[e >> 4][e & 15] = kNone;
+    }
+    const float f1 = MODE == 1 ? 1.0f : a.scale;
+    float top = sc[0][0];
+#pragma unroll
+    for (int e = 1; e < 32; ++e) top = fmaxf(top, sc[e >> 4][e & 15]);
+    top *= f1;
+    if (__any(top > m + 6.0f)) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m1 = fmaxf(m, top);
+      const float f = m1 == kNone ? 1.0f : exp2_(m - m1);
+      m = m1;
+      z *= f;
+#pragma unroll
+      for (int i = 0; i < MB; ++i) o[i] *= f;
+    }
+    const float ref = (m == kNone ? 0.0f : m) - SHIFT;
+    u32x4 pf[2][2];
+    float z0 = 0.0f, z1 = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      const float p0 = exp2_(fmaf(sc[e >> 4][e & 15], f1, -ref)), p1 = exp2_(fmaf(sc[e >> 4][(e & 15) + 1], f1, -ref));
+      z0 += p0;
+      z1 += p1;
+      pf[e >> 4][(e >> 3) & 1][(e >> 1) & 3] = pack2<T>(p0, p1);
+    }
+    z += z0 + z1;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        const char* const at = Vl + (v_at ^ (mb << 6)) + 16 * ks * ROW;
+        const u32x2 x = read_columns(at), y = read_columns(at + 8 * ROW);
+        const u32x4 vf = {x[0], x[1], y[0], y[1]};
+        o[mb] = Elem<T>::mfma32(vf, pf[ks >> 1][ks & 1], o[mb]);
+      }
+    }
+    if (!cut) return;
+    // Values that are not finite, key by key, for the rows that see it (from memory: the copy in LDS holds zeros there).
+#pragma unroll 1
+    for (int w = 0; w < 4; ++w) {
+#pragma unroll 1
+      for (uint32_t bad = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_bad[buf][w]); bad != 0; bad &= bad - 1) {
+        const int k = 16 * w + __builtin_ctz(bad), kr = k & 31, word = 8 * (k >> 5) + 2 * (kr >> 3) + ((kr & 3) >> 1);
+        uint32_t u = 0;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) u = x == word ? pf[x >> 3][(x >> 2) & 1][x & 3] : u;
+        u = (uint32_t)__shfl((int)u, col + 32 * ((kr >> 2) & 1));
+        const float p = (kr & 1) ? unpack<T>(u, 1) : unpack<T>(u, 0);
+        const bool sees = some && key0 + k >= seen.lo && key0 + k <= seen.hi;
+        const char* const from = Vb + (int64_t)min(key0 + k, n - 1) * stride + 8 * half;
+#pragma unroll
+        for (int x = 0; x < MB * 4; ++x) {
+          const u32x2 v = *reinterpret_cast<const u32x2*>(from + 16 * x);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const uint32_t nf = not_finite<T>(v[y >> 1]) & ((y & 1) ? 0x80000000u : 0x8000u);
+            if (sees && nf) o[x >> 2][4 * (x & 3) + y] += p * unpack<T>(v[y >> 1], y & 1);
+          }
+        }
+      }
+    }
+  };
+  while (step < step_end) {
+    one_step(std::integral_constant<int, 0>());
+    if (++step >= step_end) break;
+    one_step(std::integral_constant<int, 1>());
+    ++step;
+  }
+
+  z += __shfl_xor(z, 32);
+  if (!there) return;
+  const int64_t out_row = ((int64_t)b * a.Hq + h) * a.T + t;
+  if (a.S > 1) {
+    const int64_t at = ((int64_t)unit * rows + row) * a.S + part;
+    float* po = a.part_o + at * D + 4 * half;
+    if (!some) m = kNone, z = 0.0f;
+#pragma unroll
+    for (int x = 0; x < MB * 4; ++x) {
+      f32x4 v;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) v[y] = some ? o[x >> 2][4 * (x & 3) + y] : 0.0f;
+      *reinterpret_cast<f32x4*>(po + 8 * x) = v;
+    }
+    if (half == 0) {
+      a.part_mz[at * 2] = m;
+      a.part_mz[at * 2 + 1] = z;
+    }
+    return;
+  }
+  const bool none = !some || z == 0.0f;
+  const float inv = none ? 0.0f : 1.0f / z;
+  uint16_t* op = a.out + b * a.o_sb + h * a.o_sh + t * a.o_st + 4 * half;
+#pragma unroll
+  for (int x = 0; x < MB * 4; ++x) {
+    u32x2 w;
+    w[0] = none ? 0 : pack2<T>(o[x >> 2][4 * (x & 3)] * inv, o[x >> 2][4 * (x & 3) + 1] * inv);
+    w[1] = none ? 0 : pack2<T>(o[x >> 2][4 * (x & 3) + 2] * inv, o[x >> 2][4 * (x & 3) + 3] * inv);
+    *reinterpret_cast<u32x2*>(op + 8 * x) = w;
+  }
+  if (a.lse && half == 0) a.lse[out_row] = none ? kNone : (m - SHIFT + log2_(z)) * kLn2;
+}
+
+// The ranges' results in order: d / 4 threads per query row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void prefill_join_kernel(const PrefillArgs a) {
+  constexpr int LANES = D / 4;
+  constexpr float SHIFT = __is_same(T, _Float16) ? 8.0f : 0.0f;
+  const int64_t rows = (int64_t)a.T * a.G, at = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const int d4 = threadIdx.x % LANES;
+  if (at >= rows * a.B * a.Hkv) return;
+  const int unit = (int)(at / rows);
+  const int64_t row = at - unit * rows;
+  const int b = unit / a.Hkv, g = unit % a.Hkv, t = (int)(row / a.G), h = g * a.G + (int)(row % a.G);
+  const float* mz = a.part_mz + at * a.S * 2;
+  float top = kNone;
+  for (int i = 0; i < a.S; ++i) top = fmaxf(top, mz[2 * i]);
+  const float ref = top == kNone ? 0.0f : top;
+  float sum = 0.0f;
+  f32x4 acc = (f32x4)(0.0f);
+  for (int i = 0; i < a.S; ++i) {
+    const float f = exp2_(mz[2 * i] - ref);
+    sum += f * mz[2 * i + 1];
+    if (f != 0.0f) acc += f * *reinterpret_cast<const f32x4*>(a.part_o + (at * a.S + i) * D + 4 * d4);
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  u32x2 w;
+  w[0] = pack2<T>(acc[0] * inv, acc[1] * inv);
+  w[1] = pack2<T>(acc[2] * inv, acc[3] * inv);
+  *reinterpret_cast<u32x2*>(a.out + b * a.o_sb + h * a.o_sh + t * a.o_st + 4 * d4) = w;
+  if (d4 == 0 && a.lse) a.lse[((int64_t)b * a.Hq + h) * a.T + t] = sum == 0.0f ? kNone : (top - SHIFT + log2_(sum)) * kLn2;
+}
+
+template <typename T, int D>
+hipError_t launch(const PrefillArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.tiles * a.S * a.B * a.Hkv)), block(256);
+  if (a.cap2 != 0.0f || a.slopes)
+    hipLaunchKernelGGL((prefill_kernel<T, D, 1>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((prefill_kernel<T, D, 0>), grid, block, 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.S == 1) return e;
+  const int64_t rows = (int64_t)a.T * a.G * a.B * a.Hkv, per = 256 / (D / 4);
+  hipLaunchKernelGGL((prefill_join_kernel<T, D>), dim3((unsigned)((rows + per - 1) / per)), block, 0, s, a);
+  return hipGetLastError();
+}
+
+int64_t row_tiles(const pkv_prefill_desc& d) { return ((int64_t)d.T * (d.Hq / d.Hkv) + kRows - 1) / kRows; }
+
+// Ranges of keys per tile of rows: one where the tiles alone give every compute unit its two workgroups, otherwise as many as
+// do, but none below 512 keys.
+int parts(const pkv_prefill_desc& d) {
+  const int64_t wgs = row_tiles(d) * d.B * d.Hkv;
+  int64_t S = wgs >= 384 ? 1 : (512 + wgs - 1) / wgs;
+  const int64_t most = ((int64_t)d.N + 511) / 512;
+  if (S > most) S = most;
+  if (S > kMaxParts) S = kMaxParts;
+  return (int)(S < 1 ? 1 : S);
+}
+
+bool aligned(const void* p, int n) { return ((uintptr_t)p & (n - 1)) == 0; }
+bool good_strides(int64_t sb, int64_t sh, int64_t st) {
+  return sb >= 0 && sh >= 0 && st >= 0 && sb % 8 == 0 && sh % 8 == 0 && st % 8 == 0;
+}
+
+int check_prefill_desc(const pkv_prefill_desc* desc) {
+  if (!desc) return PKV_ERR_INVALID_ARG;
+  const pkv_prefill_desc& d = *desc;
+  if (d.B < 1 || d.Hq < 1 || d.Hkv < 1 || d.Hq % d.Hkv != 0 || d.T < 1 || d.N < 1 || d.window < 0) return PKV_ERR_INVALID_ARG;
+  if (d.dtype != PKV_BF16 && d.dtype != PKV_FP16) return PKV_ERR_INVALID_ARG;
+  if (!(d.scale >= 0.0f) || !(d.cap >= 0.0f) || !isfinite(d.scale) || !isfinite(d.cap)) return PKV_ERR_INVALID_ARG;
+  if (!good_strides(d.q_sb, d.q_sh, d.q_st) || !good_strides(d.kv_sb, d.kv_sh, d.kv_st) || !good_strides(d.o_sb, d.o_sh, d.o_st))
+    return PKV_ERR_INVALID_ARG;
+  if (d.d != 64 && d.d != 128) return PKV_ERR_UNSUPPORTED;
+  if (d.Hq / d.Hkv > 128 || d.B > 65535 || d.N > (1 << 30) || d.T > (1 << 30)) return PKV_ERR_UNSUPPORTED;
+  if ((int64_t)d.T * (d.Hq / d.Hkv) > 0x7FFFFF00ll) return PKV_ERR_UNSUPPORTED;
+  if (d.kv_st > (1 << 23)) return PKV_ERR_UNSUPPORTED;  // (offsets inside a step of 64 keys: 32 bits)
+  // (a product of at most 2^24 * 2^16 * 2^31 does not fit 64 bits: the head count is bounded first)
+  if ((int64_t)d.B * d.Hkv > 0x7FFFFFFF || row_tiles(d) * parts(d) > 0x7FFFFFFFll / ((int64_t)d.B * d.Hkv)) return PKV_ERR_UNSUPPORTED;
+  if ((double)d.T * d.Hq * d.B > 8e9) return PKV_ERR_UNSUPPORTED;  // (workgroups of the joining kernel)
+  return PKV_OK;
+}
+
+}  // namespace
+}  // namespace pkv
+
+using namespace pkv;
+
+extern "C" {
+
+size_t pkv_prefill_workspace_bytes(const pkv_prefill_desc* desc) {
+  if (check_prefill_desc(desc) != PKV_OK) return 0;
+  const int S = parts(*desc);
+  return S == 1 ? 0 : (size_t)desc->B * desc->Hq * desc->T * S * (desc->d + 2) * sizeof(float);
+}
+
+int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q, const void* K, const void* V, const int32_t* seq_lens,
+                          const int32_t* q_start, const int32_t* doc_start, const int32_t* prefix_end, const float* slopes,
+                          void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!desc || !q || !K || !V || !out) return PKV_ERR_INVALID_ARG;
+  const int rc = check_prefill_desc(desc);
+  if (rc != PKV_OK) return rc;
+  const pkv_prefill_desc& d = *desc;
+  if (!aligned(q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(seq_lens, 4) || !aligned(q_start, 4) ||
+      !aligned(doc_start, 4) || !aligned(prefix_end, 4) || !aligned(slopes, 4) || !aligned(lse_out, 4))
+    return PKV_ERR_INVALID_ARG;
+  const size_t need = pkv_prefill_workspace_bytes(desc);
+  if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PKV_ERR_WORKSPACE;
+  PrefillArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = static_cast<const uint16_t*>(q);
+  a.K = static_cast<const uint16_t*>(K);
+  a.V = static_cast<const uint16_t*>(V);
+  a.seq_lens = seq_lens; a.q_start = q_start; a.doc_start = doc_start; a.prefix_end = prefix_end; a.slopes = slopes;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse_out;
+  a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.T = d.T; a.N = d.N; a.window = d.window;
+  a.S = parts(d);
+  a.tiles = (int32_t)row_tiles(d);
+  a.part_o = static_cast<float*>(workspace);
+  a.part_mz = a.part_o ? a.part_o + (size_t)d.B * d.Hq * d.T * a.S * d.d : nullptr;
+  a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.q_st = d.q_st; a.kv_sb = d.kv_sb; a.kv_sh = d.kv_sh; a.kv_st = d.kv_st;
+  a.o_sb = d.o_sb; a.o_sh = d.o_sh; a.o_st = d.o_st;
+  const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d);
+  // without a cap the scores are taken to log2 units at once (with slopes before these are subtracted)
+  a.scale = (float)(d.cap > 0.0f ? scale : scale * 1.4426950408889634);
+  a.cap2 = d.cap * kLog2e;
+  a.two_over_cap = d.cap > 0.0f ? 2.0f * kLog2e / d.cap : 0.0f;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  if (d.dtype == PKV_BF16)
+    e = d.d == 128 ? launch<__bf16, 128>(a, st) : launch<__bf16, 64>(a, st);
+  else
+    e = d.d == 128 ? launch<_Float16, 128>(a, st) : launch<_Float16, 64>(a, st);
+  return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+}
+
+}  // extern "C"
