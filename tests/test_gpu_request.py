@@ -1,0 +1,89 @@
+"""A request from its projections to the tokens behind it: rotary positions into the prompt's cache, the prompt's attention
+with its softmax denominators, the compression that takes them, and decoding steps over the kept rows, to which each new
+token is added at its own position.  Every stage is compared with a plain implementation of what it has in hand."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pkv_oracle
+from paper_2406_02069_amd import binding
+from tests.attention_ref import attend, check
+from tests.parity import compare_layer
+from tests.test_gpu_prefill import _compare
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("page,window,slopes", [(0, 0, False), (16, 0, False), (0, 600, True)])
+def test_request(page, window, slopes):
+    B, Hq, Hkv, d, N, alpha, k_l, steps = 2, 8, 2, 128, 1100, 16, 96, 5
+    g = torch.Generator(device=DEV).manual_seed(page + window)
+    lens = torch.tensor([1100, 700], dtype=torch.int32, device=DEV)
+    qkv = torch.randn(B, N, Hq + 2 * Hkv, d, generator=g, device=DEV).to(torch.bfloat16).transpose(1, 2)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+    inv, m = binding.rotary_frequencies(d, "bands", base=500000.0, factor=8.0, trained=512, low=1, high=4, device=DEV)
+
+    # the prompt: rotated queries, rotated keys and values in a cache of their own, attention with denominators
+    K, V = (torch.zeros(B, Hkv, N, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    qr = binding.rotary_append(q, k, v, inv, K, V, count=lens, magnitude=m, new_lens=lens)
+    out, lse = binding.prefill_attention(qr, K, V, seq_lens=lens, want_lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, qr, K, V, lens, heads=[1, 6])
+
+    # the compression, with the denominators of the last alpha rows, against the oracle with its own softmax
+    last = (lens.long()[:, None] - alpha + torch.arange(alpha, device=DEV))[:, None]
+    Qw = qr.gather(2, last[..., None].expand(B, Hq, alpha, d)).contiguous()
+    lw = lse.gather(2, last.expand(B, Hq, alpha)).contiguous()
+    room = k_l + steps
+    host = lens.cpu().numpy()
+    if page:
+        per = -(-room // page)
+        table = torch.randperm(B * per, generator=g, device=DEV).to(torch.int32).view(B, per).contiguous()
+        Kc, Vc = (torch.zeros(B * per, Hkv, page, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        got = binding.compress_layers_paged([Qw], [K], [V], [k_l], binding.POOL_MAX, 7, [Kc], [Vc], [table], page, seq_lens=lens,
+                                            want_scores=True, lse=[lw])[0]
+        torch.cuda.synchronize()
+        j = torch.arange(room, device=DEV)
+        rows = lambda x: torch.stack([x[table[b].long()[j // page], :, j % page].transpose(0, 1) for b in range(B)])
+        compared = (rows(Kc)[:, :, :k_l], rows(Vc)[:, :, :k_l]) + tuple(got[2:])
+    else:
+        table = None
+        got = binding.compress_layers_lse([Qw], [K], [V], [lw], [k_l], binding.POOL_MAX, 7, seq_lens=lens, want_scores=True)[0]
+        torch.cuda.synchronize()
+        compared = got
+        Kc, Vc = (torch.zeros(B, Hkv, room, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        Kc[:, :, :k_l], Vc[:, :, :k_l] = got[0], got[1]
+        rows = lambda x: x
+    compare_layer(Qw, K, V, k_l, alpha, binding.POOL_MAX, 7, host, compared)
+    pos = torch.full((B, Hkv, room), -1, dtype=torch.int32, device=DEV)
+    pos[:, :, :k_l] = got[2]
+    count = got[3].clone()
+
+    # decoding: the new token's row goes behind the kept ones, at the position that it has in the text
+    sl = torch.linspace(0.01, 0.2, Hq, device=DEV) if slopes else None
+    at = lens.clone()
+    for step in range(steps):
+        x = torch.randn(B, 1, Hq + 2 * Hkv, d, generator=g, device=DEV).to(torch.bfloat16).transpose(1, 2)
+        count += 1
+        dropped = torch.full((B,), 9, dtype=torch.int32, device=DEV)
+        before = rows(Kc).clone()
+        qn = binding.rotary_append(x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], inv, Kc, Vc, count, magnitude=m,
+                                   positions=at.view(B, 1), block_table=table, k_cap=room, pos_cache=pos, dropped=dropped)
+        out, lse = binding.decode_attention_long(qn[:, :, 0], Kc, Vc, count, block_table=table, k_cap=room, positions=pos, q_pos=at,
+                                                 slopes=sl, window=window, want_lse=True)
+        torch.cuda.synchronize()
+        assert not dropped.any()
+        for b in range(B):
+            n = int(count[b])
+            assert n == k_l + step + 1 and bool((pos[b, :, n - 1] == at[b]).all()) and bool((pos[b, :, n:] == -1).all())
+            assert torch.equal(rows(Kc)[b, :, :n - 1], before[b, :, :n - 1])
+            assert torch.equal(rows(Vc)[b, :, n - 1], x[b, Hq + Hkv:, 0])
+            for h in range(Hq):
+                p = pos[b, h // (Hq // Hkv), :n].long()
+                dist = int(at[b]) - p
+                seen = dist < window if window else torch.ones_like(p, dtype=torch.bool)
+                want = attend(qn[b, h], rows(Kc)[b, h // (Hq // Hkv), :n], rows(Vc)[b, h // (Hq // Hkv), :n], seen[None], dist[None],
+                              d ** -0.5, 0.0, None if sl is None else float(sl[h]))
+                check(out[b, h][None], lse[b, h][None], *want, torch.bfloat16)
+        at += 1
