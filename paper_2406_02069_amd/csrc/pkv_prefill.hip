@@ -5,11 +5,13 @@
 // keys than its rows see) in tiles of 128, a workgroup of four waves each, 32 rows a wave; the longest tiles first.  Workgroups
 // that follow one another take different KV heads: with eight of them each XCD's cache holds the keys of one.  Few rows: the
 // keys of a tile are cut into S ranges, whose un-normalised results a second kernel joins in order.
-//   keys    64 at a time, K and V straight from memory into LDS, double-buffered: the next step's are requested when a step
-//           begins, one barrier per step.  16-byte pieces of a row are swapped (through the lanes' addresses in memory) so that
+//   keys    32 at a time, K and V straight from memory into LDS, double-buffered: the next step's are requested when a step
+//           begins, one barrier per step.  With 32 keys three workgroups share a compute unit (168 registers), with 64 two: the
+//           third is worth more than half the barriers (32k prompt 8.00 against 8.20 ms, 300 rows of 50k keys 0.34 against 0.36).
+//           16-byte pieces of a row are swapped (through the lanes' addresses in memory) so that
 //           neither way of reading them meets the same bank twice.
-//   scores  S^T = K Q^T in v_mfma_f32_32x32x16: a lane ends with 32 keys of one query row (column), the other half of the wave
-//           with the other 32, so that maxima and sums stay in the lane.
+//   scores  S^T = K Q^T in v_mfma_f32_32x32x16: a lane ends with 16 keys of one query row (column), the other half of the wave
+//           with the other 16, so that maxima and sums stay in the lane.
 //   softmax a reference exponent per row, moved only when a score exceeds it by a factor of 2^6.  The weights are rounded to the
 //           type (as the result is), their sum is not.
 //   values  O^T += V^T P^T: the weights are in B's layout already if the 16 keys of a step are taken in the order in which the
@@ -30,7 +32,7 @@ namespace pkv {
 namespace {
 
 constexpr int kRows = 128;   // query rows of a workgroup
-constexpr int kKeys = 64;    // keys per step
+constexpr int kKeys = 32;    // keys per step
 constexpr int kMaxParts = 64;  // ranges of keys
 
 struct PrefillArgs {
@@ -72,7 +74,7 @@ __device__ __forceinline__ Seen seen_keys(const PrefillArgs& a, int b, int t, in
 
 __device__ __forceinline__ int wave_max(int x) {
   for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
-  return x;
+  return __builtin_amdgcn_readfirstlane(x);
 }
 
 // 16 bytes per lane from base + at into LDS, lane after lane from byte `to` on.  Asynchronous: wait_loads.  (Written out because
@@ -84,7 +86,10 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t at, uint3
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
 }
 #pragma clang diagnostic pop
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  asm volatile("" : : : "memory");
+}
 
 // Halves of a word whose exponent is all ones (bit 15, bit 31 set).
 template <typename T>
@@ -108,13 +113,14 @@ __device__ __forceinline__ int swizzle_v(int row) { return D == 128 ? 4 * (row &
 
 // MODE 1: scores are capped or biased.
 template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
-  constexpr int STEPS = D / 16, MB = D / 32, PIECES = D / 8, ROWS_PER_LOAD = 64 / PIECES, LOADS = 16 / ROWS_PER_LOAD;
+__global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
+  constexpr int STEPS = D / 16, MB = D / 32, PIECES = D / 8, ROWS_PER_LOAD = 64 / PIECES;
+  constexpr int OWN = kKeys / 4, LOADS = OWN / ROWS_PER_LOAD;  // rows of a step that a wave fetches, loads of K (and of V) for them
   constexpr int ROW = D * 2, BUF = kKeys * ROW;
   constexpr float SHIFT = sizeof(T) == 2 && __is_same(T, _Float16) ? 8.0f : 0.0f;  // fp16 weights: away from its subnormals
   __shared__ __align__(1024) char lds[4 * BUF];  // [buffer][K, V]
   __shared__ int lds_range[4][4];
-  __shared__ uint32_t lds_bad[2][4];             // [buffer][wave]: rows of V (16 per wave) that hold a value that is not finite
+  __shared__ uint32_t lds_bad[2][4];             // [buffer][wave]: rows of V (eight per wave) that hold a value that is not finite
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int units = a.B * a.Hkv;
@@ -161,26 +167,26 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
     step = min(s0, step_end);
   }
 
-  // Fetching a step: wave w rows 16 w .. 16 w + 15 of K and of V, a row's pieces swapped.
+  // Fetching a step: wave w rows 8 w .. 8 w + 7 of K and of V, a row's pieces swapped.
   const char* const Kb = reinterpret_cast<const char*>(a.K + b * a.kv_sb + g * a.kv_sh);
   const char* const Vb = reinterpret_cast<const char*>(a.V + b * a.kv_sb + g * a.kv_sh);
   const uint32_t stride = (uint32_t)(a.kv_st * 2);
   uint32_t at_k[LOADS], at_v[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
-    const int r = 16 * wave + i * ROWS_PER_LOAD + lane / PIECES, piece = lane % PIECES;
+    const int r = OWN * wave + i * ROWS_PER_LOAD + lane / PIECES, piece = lane % PIECES;
     at_k[i] = r * stride + 16 * (piece ^ swizzle_k<D>(r));
     at_v[i] = r * stride + 16 * (piece ^ swizzle_v<D>(r));
   }
   auto fetch = [&](int st, int buf) {
     const int64_t base = (int64_t)st * kKeys * stride;
     const int most = n - 1 - st * kKeys;  // rows behind the last one are taken as the last
-    const uint32_t to = lds_base + buf * 2 * BUF + 16 * wave * ROW;
+    const uint32_t to = lds_base + buf * 2 * BUF + OWN * wave * ROW;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       uint32_t back = 0;
       if (most < kKeys - 1) {
-        const int r = 16 * wave + i * ROWS_PER_LOAD + lane / PIECES;
+        const int r = OWN * wave + i * ROWS_PER_LOAD + lane / PIECES;
         back = (uint32_t)max(r - most, 0) * stride;
       }
       load_to_lds(Kb + base, at_k[i] - back, to + i * 1024);
@@ -202,7 +208,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
 #pragma unroll
   for (int i = 0; i < MB; ++i) o[i] = (f32x16)(0.0f);
 
-  // Places in a step's rows: for scores this lane's row (K, and 32 rows on), for values its place in a block of 8 keys x 32
+  // Places in a step's rows: for scores this lane's row, for values its place in a block of 8 keys x 32
   // columns.  What is added to them is known at compile time.
   const int k_at = col * ROW + ((half ^ swizzle_k<D>(col)) << 4);
   const int v_row = 4 * half + ((lane & 15) >> 2), v_piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
@@ -219,7 +225,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
       uint32_t bad = 0;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
-        u32x4* const at = reinterpret_cast<u32x4*>(Vl + (16 * wave + i * ROWS_PER_LOAD) * ROW + 16 * lane);
+        u32x4* const at = reinterpret_cast<u32x4*>(Vl + (OWN * wave + i * ROWS_PER_LOAD) * ROW + 16 * lane);
         u32x4 v = *at;
         uint32_t any = 0;
 #pragma unroll
@@ -235,46 +241,44 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
       }
       uint32_t all = 0;
       if (__any(bad != 0)) {
-        for (int i = 0; i < 16; ++i) all |= __any((bad >> i) & 1) ? 1u << i : 0u;
+        for (int i = 0; i < OWN; ++i) all |= __any((bad >> i) & 1) ? 1u << i : 0u;
       }
       if (lane == 0) lds_bad[buf][wave] = all;
     }
     lds_barrier();
     if (step + 1 < step_end) fetch(step + 1, buf ^ 1);
     if (key0 > last_w || key0 + kKeys - 1 < first_w) return;
-    f32x16 sc[2];
+    f32x16 sc;
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(Kl + (k_at ^ (i << 5)) + 32 * kt * ROW);
-        sc[kt] = Elem<T>::mfma32(kf, qf[i], i == 0 ? (f32x16)(0.0f) : sc[kt]);
-      }
+      const u32x4 kf = *reinterpret_cast<const u32x4*>(Kl + (k_at ^ (i << 5)));
+      sc = Elem<T>::mfma32(kf, qf[i], i == 0 ? (f32x16)(0.0f) : sc);
     }
     if constexpr (MODE == 1) {
       if (a.cap2 != 0.0f) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) sc[e >> 4][e & 15] = capped(sc[e >> 4][e & 15] * a.scale, a.two_over_cap, a.cap2);
+        for (int e = 0; e < 16; ++e) sc[e] = capped(sc[e] * a.scale, a.two_over_cap, a.cap2);
       } else {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) sc[e >> 4][e & 15] *= a.scale;
+        for (int e = 0; e < 16; ++e) sc[e] *= a.scale;
       }
       if (a.slopes) {
         const float far = (float)(seen.p - key0 - 4 * half);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) sc[e >> 4][e & 15] = fmaf(-slope, fabsf(far - (float)(32 * (e >> 4) + key_of(e & 15))), sc[e >> 4][e & 15]);
+        for (int e = 0; e < 16; ++e) sc[e] = fmaf(-slope, fabsf(far - (float)key_of(e)), sc[e]);
       }
     }
     if (key0 < lo_w || key0 + kKeys - 1 > hi_w) {
+      asm volatile("");  // (a branch, not 32 comparisons in every step)
       const uint32_t from = (uint32_t)(seen.lo - key0 - 4 * half), width = (uint32_t)(seen.hi - seen.lo);
 #pragma unroll
-      for (int e = 0; e < 32; ++e)
-        if (!some || (uint32_t)(32 * (e >> 4) + key_of(e & 15)) - from > width) sc[e >> 4][e & 15] = kNone;
+      for (int e = 0; e < 16; ++e)
+        if (!some | ((uint32_t)key_of(e) - from > width)) sc[e] = kNone;
     }
     const float f1 = MODE == 1 ? 1.0f : a.scale;
-    float top = sc[0][0];
+    float top = sc[0];
 #pragma unroll
-    for (int e = 1; e < 32; ++e) top = fmaxf(top, sc[e >> 4][e & 15]);
+    for (int e = 1; e < 16; ++e) top = fmaxf(top, sc[e]);
     top *= f1;
     if (__any(top > m + 6.0f)) {
       top = fmaxf(top, __shfl_xor(top, 32));
@@ -286,24 +290,24 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
       for (int i = 0; i < MB; ++i) o[i] *= f;
     }
     const float ref = (m == kNone ? 0.0f : m) - SHIFT;
-    u32x4 pf[2][2];
+    u32x4 pf[2];
     float z0 = 0.0f, z1 = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-      const float p0 = exp2_(fmaf(sc[e >> 4][e & 15], f1, -ref)), p1 = exp2_(fmaf(sc[e >> 4][(e & 15) + 1], f1, -ref));
+    for (int e = 0; e < 16; e += 2) {
+      const float p0 = exp2_(fmaf(sc[e], f1, -ref)), p1 = exp2_(fmaf(sc[e + 1], f1, -ref));
       z0 += p0;
       z1 += p1;
-      pf[e >> 4][(e >> 3) & 1][(e >> 1) & 3] = pack2<T>(p0, p1);
+      pf[e >> 3][(e >> 1) & 3] = pack2<T>(p0, p1);
     }
     z += z0 + z1;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
+    for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) {
         const char* const at = Vl + (v_at ^ (mb << 6)) + 16 * ks * ROW;
         const u32x2 x = read_columns(at), y = read_columns(at + 8 * ROW);
         const u32x4 vf = {x[0], x[1], y[0], y[1]};
-        o[mb] = Elem<T>::mfma32(vf, pf[ks >> 1][ks & 1], o[mb]);
+        o[mb] = Elem<T>::mfma32(vf, pf[ks], o[mb]);
       }
     }
     if (!cut) return;
@@ -312,12 +316,12 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
     for (int w = 0; w < 4; ++w) {
 #pragma unroll 1
       for (uint32_t bad = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_bad[buf][w]); bad != 0; bad &= bad - 1) {
-        const int k = 16 * w + __builtin_ctz(bad), kr = k & 31, word = 8 * (k >> 5) + 2 * (kr >> 3) + ((kr & 3) >> 1);
+        const int k = OWN * w + __builtin_ctz(bad), word = 2 * (k >> 3) + ((k & 3) >> 1);
         uint32_t u = 0;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) u = x == word ? pf[x >> 3][(x >> 2) & 1][x & 3] : u;
-        u = (uint32_t)__shfl((int)u, col + 32 * ((kr >> 2) & 1));
-        const float p = (kr & 1) ? unpack<T>(u, 1) : unpack<T>(u, 0);
+        for (int x = 0; x < 8; ++x) u = x == word ? pf[x >> 2][x & 3] : u;
+        u = (uint32_t)__shfl((int)u, col + 32 * ((k >> 2) & 1));
+        const float p = (k & 1) ? unpack<T>(u, 1) : unpack<T>(u, 0);
         const bool sees = some && key0 + k >= seen.lo && key0 + k <= seen.hi;
         const char* const from = Vb + (int64_t)min(key0 + k, n - 1) * stride + 8 * half;
 #pragma unroll
@@ -372,28 +376,44 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(const PrefillArgs a) {
   if (a.lse && half == 0) a.lse[out_row] = none ? kNone : (m - SHIFT + log2_(z)) * kLn2;
 }
 
-// The ranges' results in order: d / 4 threads per query row.
-template <typename T, int D>
+// The ranges' results of a query row, d / 4 x SHARES threads each: the shares take every SHARES-th range, in order, and are added
+// at the end.
+template <typename T, int D, int SHARES>
 __global__ __launch_bounds__(256) void prefill_join_kernel(const PrefillArgs a) {
-  constexpr int LANES = D / 4;
+  constexpr int LANES = D / 4, ROWS = 256 / LANES / SHARES;
   constexpr float SHIFT = __is_same(T, _Float16) ? 8.0f : 0.0f;
-  const int64_t rows = (int64_t)a.T * a.G, at = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  const int d4 = threadIdx.x % LANES;
-  if (at >= rows * a.B * a.Hkv) return;
-  const int unit = (int)(at / rows);
-  const int64_t row = at - unit * rows;
-  const int b = unit / a.Hkv, g = unit % a.Hkv, t = (int)(row / a.G), h = g * a.G + (int)(row % a.G);
+  __shared__ float lds_sum[SHARES > 1 ? 256 / LANES : 1];
+  __shared__ f32x4 lds_o[SHARES > 1 ? 256 : 1];
+  const int d4 = threadIdx.x % LANES, share = threadIdx.x / LANES % SHARES;
+  const int64_t rows = (int64_t)a.T * a.G, all = rows * a.B * a.Hkv;
+  const int64_t mine = (int64_t)blockIdx.x * ROWS + threadIdx.x / (LANES * SHARES), at = min(mine, all - 1);
   const float* mz = a.part_mz + at * a.S * 2;
   float top = kNone;
   for (int i = 0; i < a.S; ++i) top = fmaxf(top, mz[2 * i]);
   const float ref = top == kNone ? 0.0f : top;
   float sum = 0.0f;
   f32x4 acc = (f32x4)(0.0f);
-  for (int i = 0; i < a.S; ++i) {
+  const float* po = a.part_o + at * a.S * D + 4 * d4;
+#pragma unroll 4
+  for (int i = share; i < a.S; i += SHARES) {
     const float f = exp2_(mz[2 * i] - ref);
     sum += f * mz[2 * i + 1];
-    if (f != 0.0f) acc += f * *reinterpret_cast<const f32x4*>(a.part_o + (at * a.S + i) * D + 4 * d4);
+    acc += f * *reinterpret_cast<const f32x4*>(po + (int64_t)i * D);
   }
+  if constexpr (SHARES > 1) {
+    lds_o[threadIdx.x] = acc;
+    if (d4 == 0) lds_sum[threadIdx.x / LANES] = sum;  // (the same in all threads of a share)
+    __syncthreads();
+    if (share > 0) return;
+    for (int i = 1; i < SHARES; ++i) {
+      acc += lds_o[threadIdx.x + i * LANES];
+      sum += lds_sum[threadIdx.x / LANES + i];
+    }
+  }
+  if (mine >= all) return;
+  const int unit = (int)(at / rows);
+  const int64_t row = at - unit * rows;
+  const int b = unit / a.Hkv, g = unit % a.Hkv, t = (int)(row / a.G), h = g * a.G + (int)(row % a.G);
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   u32x2 w;
   w[0] = pack2<T>(acc[0] * inv, acc[1] * inv);
@@ -411,22 +431,38 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((prefill_kernel<T, D, 0>), grid, block, 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.S == 1) return e;
-  const int64_t rows = (int64_t)a.T * a.G * a.B * a.Hkv, per = 256 / (D / 4);
-  hipLaunchKernelGGL((prefill_join_kernel<T, D>), dim3((unsigned)((rows + per - 1) / per)), block, 0, s, a);
+  const int64_t rows = (int64_t)a.T * a.G * a.B * a.Hkv;
+  constexpr int PER = 256 / (D / 4);  // rows of a workgroup with one share
+  if (a.S <= 4)
+    hipLaunchKernelGGL((prefill_join_kernel<T, D, 1>), dim3((unsigned)((rows + PER - 1) / PER)), block, 0, s, a);
+  else
+    hipLaunchKernelGGL((prefill_join_kernel<T, D, 8>), dim3((unsigned)((rows + PER / 8 - 1) / (PER / 8))), block, 0, s, a);
   return hipGetLastError();
 }
 
 int64_t row_tiles(const pkv_prefill_desc& d) { return ((int64_t)d.T * (d.Hq / d.Hkv) + kRows - 1) / kRows; }
 
-// Ranges of keys per tile of rows: one where the tiles alone give every compute unit its two workgroups, otherwise as many as
-// do, but none below 512 keys.
+// Ranges of keys per tile of rows.  The device holds 768 workgroups at a time (1024 with d = 64): one range where the tiles alone
+// are as many, otherwise the fewest that fill (nearly) the largest share of one or two turns (300 rows of 50k keys, 28 heads:
+// 309 us in 11 ranges, 346 in 8, 361 in 12; 2048 rows of 64k keys, 512 tiles: 2.10 ms in 3, 2.20 undivided).  A range's result is
+// written and read again, 64 KB for 128 rows, so that none has fewer than 768 keys (4 x 64 rows of 3000 keys, 32 heads: 36 us with
+// 1000 keys a range, 48 with 256).
 int parts(const pkv_prefill_desc& d) {
-  const int64_t wgs = row_tiles(d) * d.B * d.Hkv;
-  int64_t S = wgs >= 384 ? 1 : (512 + wgs - 1) / wgs;
-  const int64_t most = ((int64_t)d.N + 511) / 512;
-  if (S > most) S = most;
-  if (S > kMaxParts) S = kMaxParts;
-  return (int)(S < 1 ? 1 : S);
+  const int64_t wgs = row_tiles(d) * d.B * d.Hkv, slots = d.d == 64 ? 1024 : 768;
+  if (wgs >= slots) return 1;
+  int64_t most = d.N / 768;
+  if (most > kMaxParts) most = kMaxParts;
+  if (most > 2 * slots / wgs) most = 2 * slots / wgs;
+  int best = 1;
+  double share = 0.0;
+  for (int64_t S = 1; S <= most; ++S) {
+    const double full = (double)(wgs * S) / (double)((wgs * S + slots - 1) / slots * slots);
+    if (full > 1.03 * share) {
+      best = (int)S;
+      share = full;
+    }
+  }
+  return best;
 }
 
 bool aligned(const void* p, int n) { return ((uintptr_t)p & (n - 1)) == 0; }
