@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import torch
@@ -118,15 +119,15 @@ def load() -> ctypes.CDLL:
         dbl = ctypes.c_double
         lib.pkv_rotary_frequencies.argtypes = [i32, i32, dbl, dbl, dbl, dbl, dbl, vp, vp]
         lib.pkv_rotary_frequencies.restype = ctypes.c_int
-        lib.pkv_rotary_append.argtypes = [ctypes.POINTER(RotaryDesc)] + [vp] * 14
+        lib.pkv_rotary_append.argtypes = [vp] * 15  # (descriptors: a structure's address, or its bytes)
         lib.pkv_rotary_append.restype = ctypes.c_int
-        lib.pkv_prefill_attention.argtypes = [ctypes.POINTER(PrefillDesc)] + [vp] * 11 + [ctypes.c_size_t, vp]
+        lib.pkv_prefill_attention.argtypes = [vp] * 12 + [ctypes.c_size_t, vp]
         lib.pkv_prefill_attention.restype = ctypes.c_int
-        lib.pkv_prefill_workspace_bytes.argtypes = [ctypes.POINTER(PrefillDesc)]
+        lib.pkv_prefill_workspace_bytes.argtypes = [vp]
         lib.pkv_prefill_workspace_bytes.restype = ctypes.c_size_t
-        lib.pkv_decode_attention_long.argtypes = [ctypes.POINTER(DecodeLongDesc)] + [vp] * 11 + [ctypes.c_size_t, vp]
+        lib.pkv_decode_attention_long.argtypes = [vp] * 12 + [ctypes.c_size_t, vp]
         lib.pkv_decode_attention_long.restype = ctypes.c_int
-        lib.pkv_decode_long_workspace_bytes.argtypes = [ctypes.POINTER(DecodeLongDesc)]
+        lib.pkv_decode_long_workspace_bytes.argtypes = [vp]
         lib.pkv_decode_long_workspace_bytes.restype = ctypes.c_size_t
         lib.pkv_status_string.argtypes = [ctypes.c_int]
         lib.pkv_status_string.restype = ctypes.c_char_p
@@ -446,64 +447,82 @@ def compress_layers_paged(Q_win, K, V, k_ls, pool, pool_w, K_pages, V_pages, blo
 
 
 # ---- rotary positions, prompt attention, attention over long caches ----
+#
+# A decoder makes these calls for every layer and token, and the small ones take the device less time than their checks take
+# the host: descriptors are packed as bytes, and what is asked of a tensor are the accessors that cost least.
 
 DTYPES = {torch.bfloat16: 0, torch.float16: 1}            # pkv_dtype
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}            # pkv_rotary_layout
 ROTARY_SCALINGS = {"plain": 0, "linear": 1, "bands": 2, "ramp": 3}
 
+# RotaryDesc, PrefillDesc and DecodeLongDesc as bytes
+_pack_rotary = struct.Struct("12ifi17q").pack
+_pack_prefill = struct.Struct("8i2f9q").pack
+_pack_decode_long = struct.Struct("10i2f7q").pack
 
-def _on_device(device, function, *args):
-    """function(*args) with `device` current: a stream takes launches only while its device is the current one."""
-    if device.index is None or device.index == torch.cuda.current_device():
-        return function(*args)
-    with torch.cuda.device(device):
-        return function(*args)
-
-
-def _need(t: Optional[torch.Tensor], name: str, dtype, shape, device, contiguous: bool = True):
-    """Raise unless t is None or a tensor of this type, shape and device (contiguous, or with contiguous rows)."""
-    if t is None:
-        return
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: need {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the first argument on {device}")
-    if (not t.is_contiguous()) if contiguous else (t.stride(-1) != 1 and t.shape[-1] > 1):
-        raise ValueError(f"{name}: need a contiguous {'tensor' if contiguous else 'last dimension'}")
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _gpu(t: torch.Tensor, name: str, dims: int) -> int:
-    """The type code of a GPU tensor with `dims` dimensions, the last one contiguous."""
+def _call(where: str, function, index: int, *args):
+    """function(*args) with GPU `index` current (a stream takes launches only while its device is the current one)."""
+    if index == _get_device():
+        rc = function(*args)
+    else:
+        with torch.cuda.device(index):
+            rc = function(*args)
+    if rc != OK:
+        raise PkvError(rc, where)
+
+
+def _need(t: torch.Tensor, name: str, dtype, shape, index: int, contiguous: bool = True) -> int:
+    """The address of a tensor of this type, shape and device (contiguous, or with contiguous rows); raise otherwise."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index and \
+            (t.is_contiguous() if contiguous else t.stride(-1) == 1 or shape[-1] == 1):
+        return t.data_ptr()
+    raise ValueError(f"{name}: need a {'contiguous tensor' if contiguous else 'tensor with a contiguous last dimension'} of "
+                     f"{dtype} {tuple(shape)} on GPU {index}, got {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
+
+
+def _gpu(t: torch.Tensor, name: str, dims: int):
+    """(type code, GPU index) of a tensor with `dims` dimensions, the last one contiguous."""
     code = DTYPES.get(t.dtype)
     if code is None or t.dim() != dims or t.stride(-1) != 1:
         raise ValueError(f"{name}: need a {dims}-d bf16 or fp16 tensor with a contiguous last dimension")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name}: need a GPU tensor")
-    return code
+    return code, t.get_device()
 
 
-def _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, device):
-    """(k_cap, page_size, num_pages, max_pages, c_sb, c_sh, c_st) of a compact cache or of page pools."""
+def _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, index):
+    """(k_cap, page_size, num_pages, max_pages, c_sb, c_sh, c_st), and the addresses of K, V and the table, of a compact cache
+    or of page pools."""
+    shape = K_cache.shape
+    if len(shape) != 4:
+        raise ValueError("K_cache: need four dimensions")
     if block_table is None:
         if k_cap is None:
-            k_cap = K_cache.shape[2]
-        if K_cache.dim() != 4 or k_cap > K_cache.shape[2]:
-            raise ValueError("K_cache: need [B, Hkv, k_cap, d]")
-        shape = (B, Hkv, K_cache.shape[2], d)
-        _need(K_cache, "K_cache", dtype, shape, device, False)
-        _need(V_cache, "V_cache", dtype, shape, device, False)
-        if K_cache.stride() != V_cache.stride():
+            k_cap = shape[2]
+        elif k_cap > shape[2]:
+            raise ValueError("k_cap: more rows than the cache has")
+        want = (B, Hkv, shape[2], d)
+        K, V = _need(K_cache, "K_cache", dtype, want, index, False), _need(V_cache, "V_cache", dtype, want, index, False)
+        st = K_cache.stride()
+        if st != V_cache.stride():
             raise ValueError("K_cache and V_cache must have the same strides")
-        return (k_cap, 0, 0, 0) + K_cache.stride()[:3]
-    if K_cache.dim() != 4 or block_table.dim() != 2:
-        raise ValueError("need pools [num_pages, Hkv, page_size, d] and a block table [B, max_pages]")
-    shape = (K_cache.shape[0], Hkv, K_cache.shape[2], d)
-    _need(K_cache, "K_cache", dtype, shape, device)
-    _need(V_cache, "V_cache", dtype, shape, device)
-    _need(block_table, "block_table", torch.int32, (B, block_table.shape[1]), device)
-    if k_cap is None:
-        k_cap = block_table.shape[1] * shape[2]
-    return k_cap, shape[2], shape[0], block_table.shape[1], 0, 0, 0
+        return (k_cap, 0, 0, 0, st[0], st[1], st[2]), K, V, None
+    if block_table.dim() != 2:
+        raise ValueError("block_table: need [B, max_pages]")
+    want, pages = (shape[0], Hkv, shape[2], d), block_table.shape[1]
+    K, V = _need(K_cache, "K_cache", dtype, want, index), _need(V_cache, "V_cache", dtype, want, index)
+    table = _need(block_table, "block_table", torch.int32, (B, pages), index)
+    return (pages * shape[2] if k_cap is None else k_cap, shape[2], shape[0], pages, 0, 0, 0), K, V, table
+
+
+def _row_positions(t: torch.Tensor, name: str, B: int, Hkv: int, k_cap: int, index: int):
+    """(address, strides) of int32 positions [B, Hkv, at least k_cap] of a cache's rows."""
+    if t.dim() != 3 or t.shape[2] < k_cap:
+        raise ValueError(f"{name}: need [B, Hkv, k_cap] or more")
+    return _need(t, name, torch.int32, (B, Hkv, t.shape[2]), index, False), t.stride()
 
 
 def rotary_frequencies(rot: int, scaling: str = "plain", base: float = 10000.0, factor: float = 1.0,
@@ -531,41 +550,37 @@ def rotary_append(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optio
     first = q if q is not None else k
     if first is None or (k is None) != (v is None) or (k is None) != (K_cache is None) or (k is None) != (V_cache is None):
         raise ValueError("need q, or k and v with their caches, or both")
-    code, device = _gpu(first, "q" if q is not None else "k", 4), first.device
+    code, index = _gpu(first, "q" if q is not None else "k", 4)
+    dtype = first.dtype
     B, H, T, d = first.shape
     Hkv = H if k is None else k.shape[1]
-    rot = 2 * inv_freq.numel()
-    _need(inv_freq, "inv_freq", torch.float64, (rot // 2,), device)
+    half = inv_freq.numel()
+    f_p = _need(inv_freq, "inv_freq", torch.float64, (half,), index)
     qs = os_ = ks = vs = ps = (0, 0, 0)
     cache = (1, 0, 0, 0, 0, 0, 0)
+    q_p = o_p = k_p = v_p = K_p = V_p = table_p = pc_p = None
     if q is not None:
         if q_out is None:
-            q_out = (torch.empty if new_lens is None else torch.zeros)((B, H, T, d), dtype=q.dtype, device=device)
-        else:
-            _need(q_out, "q_out", q.dtype, q.shape, device, False)
+            q_out = (torch.empty if new_lens is None else torch.zeros)((B, H, T, d), dtype=dtype, device=first.device)
+        q_p, o_p = q.data_ptr(), _need(q_out, "q_out", dtype, (B, H, T, d), index, False)
         qs, os_ = q.stride(), q_out.stride()
     if k is not None:
-        _need(k, "k", first.dtype, (B, Hkv, T, d), device, False)
-        _need(v, "v", first.dtype, (B, Hkv, T, d), device, False)
+        k_p, v_p = _need(k, "k", dtype, (B, Hkv, T, d), index, False), _need(v, "v", dtype, (B, Hkv, T, d), index, False)
         ks, vs = k.stride(), v.stride()
-        cache = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, first.dtype, device)
-    if pos_cache is not None:
-        _need(pos_cache, "pos_cache", torch.int32, (B, Hkv, pos_cache.shape[2]), device, False)
-        if pos_cache.shape[2] < cache[0]:
-            raise ValueError("pos_cache: shorter than the cache")
-        ps = pos_cache.stride()
-    _need(positions, "positions", torch.int32, (B, T), device)
-    _need(new_lens, "new_lens", torch.int32, (B,), device)
-    _need(count, "count", torch.int32, (B,), device)
-    _need(dropped, "dropped", torch.int32, (B,), device)
-    desc = RotaryDesc(B, H if q is not None else Hkv, Hkv, d, T, rot, ROTARY_LAYOUTS[layout], code, cache[0], cache[1], cache[2],
-                      cache[3], magnitude, 0, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-                      os_[0], os_[1], os_[2], cache[4], cache[5], cache[6], ps[0], ps[1])
-    rc = _on_device(device, load().pkv_rotary_append, ctypes.byref(desc), _a(q), _a(k), _a(v), inv_freq.data_ptr(),
-                    _a(positions), _a(new_lens), _a(count), _a(block_table), _a(q_out), _a(K_cache), _a(V_cache),
-                    _a(pos_cache), _a(dropped), _stream_ptr(device))
-    if rc != OK:
-        raise PkvError(rc, "pkv_rotary_append")
+        cache, K_p, V_p, table_p = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, index)
+        if pos_cache is not None:
+            pc_p, ps = _row_positions(pos_cache, "pos_cache", B, Hkv, cache[0], index)
+    elif pos_cache is not None:
+        raise ValueError("pos_cache: needs keys and values")
+    desc = _pack_rotary(B, H if q is not None else Hkv, Hkv, d, T, 2 * half, ROTARY_LAYOUTS[layout], code, cache[0], cache[1],
+                        cache[2], cache[3], magnitude, 0, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                        os_[0], os_[1], os_[2], cache[4], cache[5], cache[6], ps[0], ps[1])
+    _call("pkv_rotary_append", load().pkv_rotary_append, index, desc, q_p, k_p, v_p, f_p,
+          None if positions is None else _need(positions, "positions", torch.int32, (B, T), index),
+          None if new_lens is None else _need(new_lens, "new_lens", torch.int32, (B,), index),
+          None if count is None else _need(count, "count", torch.int32, (B,), index),
+          table_p, o_p, K_p, V_p, pc_p, None if dropped is None else _need(dropped, "dropped", torch.int32, (B,), index),
+          _stream_of(index))
     return q_out
 
 
@@ -578,41 +593,36 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_len
     """pkv_prefill_attention on the current stream.  q [B,Hq,T,d] at positions q_start[b] (0) and on, K and V [B,Hkv,N,d]
     of the same strides; seq_lens, q_start int32 [B]; doc_start, prefix_end int32 [B,N]; slopes fp32 [Hq].
     Returns (out [B,Hq,T,d] of q's type, lse fp32 [B,Hq,T] or None)."""
-    code, device = _gpu(q, "q", 4), q.device
+    code, index = _gpu(q, "q", 4)
+    dtype = q.dtype
     B, Hq, T, d = q.shape
     if K.dim() != 4:
         raise ValueError("K: need four dimensions")
-    Hkv, N = K.shape[1], K.shape[2]
-    _need(K, "K", q.dtype, (B, Hkv, N, d), device, False)
-    _need(V, "V", q.dtype, (B, Hkv, N, d), device, False)
-    if K.stride() != V.stride():
+    _, Hkv, N, _ = K.shape
+    K_p, V_p = _need(K, "K", dtype, (B, Hkv, N, d), index, False), _need(V, "V", dtype, (B, Hkv, N, d), index, False)
+    ks = K.stride()
+    if ks != V.stride():
         raise ValueError("K and V must have the same strides")
-    _need(seq_lens, "seq_lens", torch.int32, (B,), device)
-    _need(q_start, "q_start", torch.int32, (B,), device)
-    _need(doc_start, "doc_start", torch.int32, (B, N), device)
-    _need(prefix_end, "prefix_end", torch.int32, (B, N), device)
-    _need(slopes, "slopes", torch.float32, (Hq,), device)
     if out is None:
-        out = torch.empty((B, Hq, T, d), dtype=q.dtype, device=device)
-    else:
-        _need(out, "out", q.dtype, q.shape, device, False)
+        out = torch.empty((B, Hq, T, d), dtype=dtype, device=q.device)
+    out_p, qs, os_ = _need(out, "out", dtype, (B, Hq, T, d), index, False), q.stride(), out.stride()
     if want_lse and lse is None:
-        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=device)
-    _need(lse, "lse", torch.float32, (B, Hq, T), device)
-    qs, ks, os_ = q.stride(), K.stride(), out.stride()
-    desc = PrefillDesc(B, Hq, Hkv, d, T, N, code, window, _scale(scale), cap, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
-                       os_[0], os_[1], os_[2])
-    ref = ctypes.byref(desc)
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device)
+    desc = _pack_prefill(B, Hq, Hkv, d, T, N, code, window, _scale(scale), cap, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
+                         os_[0], os_[1], os_[2])
     lib = load()
     if workspace is None:  # (a workspace that is handed over is checked by the call)
-        need = lib.pkv_prefill_workspace_bytes(ref)
+        need = lib.pkv_prefill_workspace_bytes(desc)
         if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    rc = _on_device(device, lib.pkv_prefill_attention, ref, q.data_ptr(), K.data_ptr(), V.data_ptr(), _a(seq_lens), _a(q_start),
-                    _a(doc_start), _a(prefix_end), _a(slopes), out.data_ptr(), _a(lse), _a(workspace),
-                    0 if workspace is None else workspace.numel(), _stream_ptr(device))
-    if rc != OK:
-        raise PkvError(rc, "pkv_prefill_attention")
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _call("pkv_prefill_attention", lib.pkv_prefill_attention, index, desc, q.data_ptr(), K_p, V_p,
+          None if seq_lens is None else _need(seq_lens, "seq_lens", torch.int32, (B,), index),
+          None if q_start is None else _need(q_start, "q_start", torch.int32, (B,), index),
+          None if doc_start is None else _need(doc_start, "doc_start", torch.int32, (B, N), index),
+          None if prefix_end is None else _need(prefix_end, "prefix_end", torch.int32, (B, N), index),
+          None if slopes is None else _need(slopes, "slopes", torch.float32, (Hq,), index),
+          out_p, None if lse is None else _need(lse, "lse", torch.float32, (B, Hq, T), index),
+          None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream_of(index))
     return out, lse
 
 
@@ -626,41 +636,32 @@ def decode_attention_long(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch
     pools [num_pages,Hkv,page_size,d] with block_table int32 [B,max_pages]; count int32 [B]; positions int32
     [B,Hkv,>= k_cap] of the cache's rows and q_pos int32 [B]; slopes fp32 [Hq].
     Returns (out [B,Hq,d] of q's type, lse fp32 [B,Hq] or None)."""
-    code, device = _gpu(q, "q", 3), q.device
+    code, index = _gpu(q, "q", 3)
+    dtype = q.dtype
     B, Hq, d = q.shape
     if K_cache.dim() != 4:
         raise ValueError("K_cache: need four dimensions")
     Hkv = K_cache.shape[1]
-    cache = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, q.dtype, device)
-    _need(count, "count", torch.int32, (B,), device)
-    _need(q_pos, "q_pos", torch.int32, (B,), device)
-    _need(slopes, "slopes", torch.float32, (Hq,), device)
-    ps = (0, 0)
-    if positions is not None:
-        _need(positions, "positions", torch.int32, (B, Hkv, positions.shape[2]), device, False)
-        if positions.shape[2] < cache[0]:
-            raise ValueError("positions: shorter than the cache")
-        ps = positions.stride()
+    cache, K_p, V_p, table_p = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, index)
+    pos_p, ps = (None, (0, 0)) if positions is None else _row_positions(positions, "positions", B, Hkv, cache[0], index)
     if out is None:
-        out = torch.empty((B, Hq, d), dtype=q.dtype, device=device)
-    else:
-        _need(out, "out", q.dtype, (B, Hq, d), device)
+        out = torch.empty((B, Hq, d), dtype=dtype, device=q.device)
     if want_lse and lse is None:
-        lse = torch.empty((B, Hq), dtype=torch.float32, device=device)
-    _need(lse, "lse", torch.float32, (B, Hq), device)
-    desc = DecodeLongDesc(B, Hq, Hkv, d, cache[0], cache[1], cache[2], cache[3], code, window, _scale(scale), cap,
-                          q.stride(0), q.stride(1), cache[4], cache[5], cache[6], ps[0], ps[1])
-    ref = ctypes.byref(desc)
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+    qs = q.stride()
+    desc = _pack_decode_long(B, Hq, Hkv, d, cache[0], cache[1], cache[2], cache[3], code, window, _scale(scale), cap,
+                             qs[0], qs[1], cache[4], cache[5], cache[6], ps[0], ps[1])
     lib = load()
     if workspace is None:  # (a workspace that is handed over is checked by the call)
-        need = lib.pkv_decode_long_workspace_bytes(ref)
+        need = lib.pkv_decode_long_workspace_bytes(desc)
         if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    rc = _on_device(device, lib.pkv_decode_attention_long, ref, q.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(),
-                    _a(block_table), count.data_ptr(), _a(positions), _a(q_pos), _a(slopes), out.data_ptr(), _a(lse),
-                    _a(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(device))
-    if rc != OK:
-        raise PkvError(rc, "pkv_decode_attention_long")
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _call("pkv_decode_attention_long", lib.pkv_decode_attention_long, index, desc, q.data_ptr(), K_p, V_p, table_p,
+          _need(count, "count", torch.int32, (B,), index), pos_p,
+          None if q_pos is None else _need(q_pos, "q_pos", torch.int32, (B,), index),
+          None if slopes is None else _need(slopes, "slopes", torch.float32, (Hq,), index),
+          _need(out, "out", dtype, (B, Hq, d), index), None if lse is None else _need(lse, "lse", torch.float32, (B, Hq), index),
+          None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream_of(index))
     return out, lse
 
 
@@ -673,8 +674,8 @@ def _scale(scale: Optional[float]) -> float:
     return float(scale)
 
 
-def _a(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
+def _stream_of(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream if _raw_stream is None else _raw_stream(index)
 
 
 def probe_read(buf: torch.Tensor, sink: torch.Tensor) -> None:
