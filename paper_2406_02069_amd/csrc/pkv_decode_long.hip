@@ -1,11 +1,14 @@
 // Attention of one new token per sequence over a cache of any length (include/pkv.h: pkv_decode_attention_long).
 //
 // HBM-bound: every seen row of K and V is read once (2 d bytes each), for all query heads of its KV head.
-// Work split: (sequence, KV head, up to 64 of its query heads) x S ranges of keys, a workgroup of four waves each; a wave takes
+// Work split: (sequence, KV head, up to 64 of its query heads) x ranges of keys, a workgroup of four waves each; a wave takes
 // 16 query heads, so that with up to 16, 32 and 64 heads four, two and one of the waves share the range's 32-key tiles.  Every
 // wave works on its own, K tile -> scores -> running softmax -> V tile, the rows of its next tile requested as soon as this
-// tile's are used up, and the waves meet once at the end.  With S > 1 the ranges leave un-normalised results in a workspace and
-// a second kernel joins them in order.
+// tile's are used up, and the waves meet once at the end.  Where a sequence has several ranges, they leave un-normalised results
+// in a workspace, and a second kernel joins them in order.
+// Ranges: as long as fill the device once (512 workgroups), by the sequences' lengths as they are on the device, so that ragged
+// batches have ranges of one length too; every wave works out its place among them from all counts (2 to 64 sequences; beyond
+// that there are workgroups enough to even out what equal numbers of ranges leave uneven).
 //   scores  S^T = K Q^T in v_mfma_f32_16x16x32: 16 keys are the rows of A, loaded straight into operand layout, 16 heads the
 //           columns of B.  Lane (l16, quad) ends with keys 4 quad .. + 3 of head l16, all it needs for its weights.
 //   softmax a reference exponent per head and wave, moved only when a score exceeds it by a factor of 2^8.
@@ -25,7 +28,10 @@ namespace {
 
 constexpr int kTile = 32;          // keys per step of a wave
 constexpr int kWaves = 4;          // per workgroup
-constexpr int kMaxRanges = 512;    // per (sequence, KV head)
+constexpr int kWorkgroups = 512;   // at a time on the device: two per compute unit
+constexpr int kFlatBatch = 64;     // sequences, at most, whose ranges go by their lengths
+constexpr int kLeastTiles = 8;     // of a range
+constexpr int kMaxRanges = 1024;   // of a sequence and KV head
 
 struct LongArgs {
   const uint16_t *q, *K, *V;
@@ -33,9 +39,11 @@ struct LongArgs {
   const float* slopes;
   uint16_t* out;
   float* lse;
-  float* part_o;   // [B * Hq][S][d]
-  float* part_mz;  // [B * Hq][S][2] reference exponent (log2) and sum
-  int32_t B, Hq, Hkv, G, k_cap, page_size, num_pages, max_pages, window, S;
+  float* part_o;   // [workgroup][head of its group][d]
+  float* part_mz;  // [workgroup][head of its group][2] reference exponent (log2) and sum
+  int32_t B, Hq, Hkv, G, k_cap, page_size, num_pages, max_pages, window;
+  int32_t ranges;       // 0: every sequence whole; with 2 .. kFlatBatch sequences workgroups to share out; otherwise ranges of each
+  int32_t units;        // of a sequence: Hkv * head_groups
   int32_t head_groups;  // workgroups that share a KV head's rows: ceil(G / 64)
   int32_t wave_groups;  // 16-head groups in a workgroup: 1, 2 or 4
   uint32_t page_magic;  // floor(2^32 / page_size)
@@ -44,12 +52,67 @@ struct LongArgs {
   float cap2, two_over_cap;  // cap in log2 units (0: none); 2 log2(e) / cap
 };
 
-// A row of a tile as its lane knows it: number in the cache (rows of one stride), position, and whether it is seen.
-struct Row {
-  uint32_t at;
-  int32_t pos;
-  bool seen;
+// A wave's reads and writes of its own part of LDS keep their order.
+__device__ __forceinline__ void own_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
+// The tiles of sequence b that can hold a seen row: all, or with positions of their own numbers those of the window.
+struct Tiles {
+  int n, q_pos, first, count;
 };
+__device__ __forceinline__ Tiles tiles_of(const LongArgs& a, int b) {
+  Tiles r;
+  r.n = min(max(a.count[b], 0), a.k_cap);
+  r.q_pos = a.q_pos ? a.q_pos[b] : r.n - 1;
+  int first = 0, end = r.n;
+  if (!a.positions) {
+    end = (int)min((int64_t)r.n, (int64_t)r.q_pos + 1);
+    if (a.window) first = (int)min((int64_t)r.n, max((int64_t)0, (int64_t)r.q_pos - a.window + 1));
+  }
+  r.first = first / kTile;
+  r.count = end > first ? (end + kTile - 1) / kTile - r.first : 0;
+  return r;
+}
+
+// Sum over the wave, up to and including the own lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_from(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int sum_upto(int x) {
+  x = add_from<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8: within rows of 16
+  x = add_from<0x112, 0xF>(x);
+  x = add_from<0x114, 0xF>(x);
+  x = add_from<0x118, 0xF>(x);
+  x = add_from<0x142, 0xA>(x);  // the rows' sums: row_bcast 15 into rows 1 and 3, row_bcast 31 into rows 2 and 3
+  return add_from<0x143, 0xC>(x);
+}
+
+// How a sequence is cut: its ranges, the tiles of each, and the first of its workgroups.
+struct Cut {
+  int ranges, per, base;
+};
+// For 2 .. kFlatBatch sequences lane b works out sequence b.  Ranges as long as make `ranges` workgroups of all tiles, then longer
+// (a few tries) until the last, shorter ones of the sequences fit among them too; never more than ranges + B * units.
+__device__ __forceinline__ Cut flat_cut(const LongArgs& a, int tiles, int lane) {
+  Cut c;
+  const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(sum_upto(tiles), 63) * (uint32_t)a.units;
+  const int shares = kWaves / a.wave_groups, shift = a.ranges == kWorkgroups ? 9 : 10;
+  c.per = max((int)((all + a.ranges - 1) >> shift), kLeastTiles);
+  c.per = (c.per + shares - 1) / shares * shares;
+  int upto;
+  for (int tries = 0;; ++tries) {
+    c.ranges = lane < a.B ? max(1, (int)((uint32_t)(tiles + c.per - 1) / (uint32_t)c.per)) : 0;
+    upto = sum_upto(c.ranges * a.units);
+    if (shift != 9 || tries == 6 || __builtin_amdgcn_readlane(upto, 63) <= kWorkgroups) break;
+    c.per += max(shares, c.per / 16 / shares * shares);
+  }
+  c.base = upto - c.ranges * a.units;
+  return c;
+}
 
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
@@ -57,24 +120,41 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
   __shared__ __align__(16) char lds_v[kWaves][kTile * D * 2];
   __shared__ float lds_mz[kWaves][16][2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, quad = lane >> 4;
-  const int s = blockIdx.x, g = blockIdx.y / a.head_groups, hg = blockIdx.y % a.head_groups, b = blockIdx.z;
+  int b, s, ranges, unit;
+  Tiles tl;
+  int per;
+  if (a.ranges == 0 || a.B == 1 || a.B > kFlatBatch) {
+    ranges = max(a.ranges, 1);
+    s = blockIdx.x % ranges;
+    b = blockIdx.x / ranges / a.units;
+    unit = blockIdx.x / ranges % a.units;
+    tl = tiles_of(a, b);
+    per = (tl.count + ranges - 1) / ranges;
+  } else {
+    tl = tiles_of(a, min(lane, a.B - 1));
+    const Cut c = flat_cut(a, lane < a.B ? tl.count : 0, lane);
+    const uint64_t mine = __ballot(lane < a.B && (int)blockIdx.x >= c.base && (int)blockIdx.x < c.base + c.ranges * a.units);
+    if (mine == 0) return;  // (no work left for this workgroup)
+    b = __builtin_ctzll(mine);
+    ranges = __builtin_amdgcn_readlane(c.ranges, b);
+    const int at = blockIdx.x - __builtin_amdgcn_readlane(c.base, b);
+    unit = at / ranges;
+    s = at % ranges;
+    per = c.per;
+    tl.n = __builtin_amdgcn_readlane(tl.n, b);
+    tl.q_pos = __builtin_amdgcn_readlane(tl.q_pos, b);
+    tl.first = __builtin_amdgcn_readlane(tl.first, b);
+    tl.count = __builtin_amdgcn_readlane(tl.count, b);
+  }
+  const int g = unit / a.head_groups, hg = unit % a.head_groups;
   const int wg = wave & (a.wave_groups - 1), share = wave / a.wave_groups, shares = kWaves / a.wave_groups;
   const int h_in = 64 * hg + 16 * wg + l16;  // query head within the group of this KV head
   const bool head = h_in < a.G;
   const int h = g * a.G + (head ? h_in : 0);
 
-  const int n = min(max(a.count[b], 0), a.k_cap);
-  const int q_pos = a.q_pos ? a.q_pos[b] : n - 1;
-  // Rows that can be seen: all, or with positions of their own numbers those of the window.
-  int first = 0, end = n;
-  if (!a.positions) {
-    end = (int)min((int64_t)n, (int64_t)q_pos + 1);
-    if (a.window) first = (int)min((int64_t)n, max((int64_t)0, (int64_t)q_pos - a.window + 1));
-  }
-  const int tile0 = first / kTile, tiles = end > first ? (end + kTile - 1) / kTile - tile0 : 0;
-  const int per = (tiles + a.S - 1) / a.S;
-  int t = tile0 + s * per + share;
-  const int t_end = min(tile0 + (s + 1) * per, tile0 + tiles);
+  const int n = tl.n, q_pos = tl.q_pos;
+  int t = tl.first + s * per + share;
+  const int t_end = tl.first + min((s + 1) * per, tl.count);
 
   u32x4 qf[STEPS];
   {
@@ -83,55 +163,58 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
     for (int i = 0; i < STEPS; ++i) qf[i] = head ? *reinterpret_cast<const u32x4*>(qp + 32 * i + 8 * quad) : (u32x4)(0);
   }
   const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
-  const int64_t row_bytes = (a.page_size ? (int64_t)D : a.c_st) * 2;
+  const uint32_t row_bytes = (uint32_t)(a.page_size ? D : a.c_st) * 2;
   const int64_t base = a.page_size ? 0 : (b * a.c_sb + g * a.c_sh) * 2;
-  const char* const Kb = reinterpret_cast<const char*>(a.K) + base + 16 * quad;
+  const char* const Kb = reinterpret_cast<const char*>(a.K) + base + 16 * (lane % LANES);
   const char* const Vb = reinterpret_cast<const char*>(a.V) + base + 16 * (lane % LANES);
   const int32_t* const table = a.table + (int64_t)b * a.max_pages;
   const int32_t* const pos_b = a.positions + b * a.p_sb + g * a.p_sh;
+  const int least = a.window ? max((int)max((int64_t)q_pos - a.window + 1, (int64_t)0), 0) : 0;  // of the seen positions
+  if (q_pos < least) t = t_end;
 
-  // What has to be loaded to know a tile's rows (lane l: row l % 32); rows behind the last one are taken as the last.
-  auto look = [&](int tile, int32_t& page, int32_t& pos) {
+  // What has to be loaded to know a tile's rows: lane l looks after row l % 32.
+  int32_t page = 0, slot = 0, pos_next = 0;
+  auto look = [&](int tile) {
     const int j = min(tile * kTile + (lane & 31), n - 1);
-    page = 0;
+    slot = j;
     if (a.page_size) {
       uint32_t p = __umulhi((uint32_t)j, a.page_magic);
       if ((uint32_t)j - p * a.page_size >= (uint32_t)a.page_size) ++p;
+      slot = j - p * a.page_size;
       page = table[p];
     }
-    pos = a.positions ? pos_b[j] : j;
+    pos_next = a.positions ? pos_b[j] : j;
   };
-  auto row_of = [&](int tile, int32_t page, int32_t pos) {
-    Row r;
-    const int j0 = tile * kTile + (lane & 31), j = min(j0, n - 1);
-    r.at = (uint32_t)j;
-    r.pos = pos;
-    r.seen = j0 < n && pos >= 0 && pos <= q_pos && (a.window == 0 || (int64_t)pos > (int64_t)q_pos - a.window);
+  // The rows that are seen, one bit each, their positions, and where the rows lie (in rows of one stride).  Where a row is not
+  // seen, the cache's first is loaded: nothing that is far, or not there.
+  uint32_t seen = 0, at = 0;
+  int32_t pos = 0;
+  auto resolve = [&](int tile) {
+    pos = pos_next;
+    bool is = tile < t_end && tile * kTile + (lane & 31) < n && (uint32_t)(pos - least) <= (uint32_t)(q_pos - least);
+    at = slot;
     if (a.page_size) {
-      uint32_t p = __umulhi((uint32_t)j, a.page_magic);
-      if ((uint32_t)j - p * a.page_size >= (uint32_t)a.page_size) ++p;
-      const bool there = page >= 0 && page < a.num_pages;
-      r.seen = r.seen && there;
-      r.at = ((uint32_t)(there ? page : 0) * a.Hkv + g) * a.page_size + ((uint32_t)j - p * a.page_size);
+      is = is && (uint32_t)page < (uint32_t)a.num_pages;
+      at = ((uint32_t)page * a.Hkv + g) * a.page_size + slot;
     }
-    return r;
+    at = is ? at : 0;
+    seen = (uint32_t)__ballot(is);
   };
 
-  u32x4 kf[2][STEPS], vr[VLOADS];
-  auto load_k = [&](const Row& r) {
+  // Rows of a tile, 1 KB of neighbouring rows at a time: load i holds rows i 64 / LANES .. of the tile.
+  u32x4 kr[VLOADS], vr[VLOADS];
+  uint32_t at_row[VLOADS];
+  auto load = [&](const char* from, u32x4 (&to)[VLOADS]) {
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const char* p = Kb + (int64_t)(uint32_t)__shfl((int)r.at, 16 * kt + l16) * row_bytes;
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) kf[kt][i] = *reinterpret_cast<const u32x4*>(p + 64 * i);
-    }
+    for (int i = 0; i < VLOADS; ++i) to[i] = *reinterpret_cast<const u32x4*>(from + (uint64_t)at_row[i] * row_bytes);
   };
-  auto load_v = [&](const Row& r) {
+  auto place = [&]() {
 #pragma unroll
-    for (int i = 0; i < VLOADS; ++i)
-      vr[i] = *reinterpret_cast<const u32x4*>(Vb + (int64_t)(uint32_t)__shfl((int)r.at, i * (64 / LANES) + lane / LANES) * row_bytes);
+    for (int i = 0; i < VLOADS; ++i) at_row[i] = (uint32_t)__shfl((int)at, i * (64 / LANES) + lane / LANES);
   };
-  // 16-byte piece c of a row of the copy lies at c ^ swizzle(row): 16 rows' pieces of one column block go to all banks.
+  // 16-byte piece c of a row of the copies lies at c ^ swizzle(row): 16 rows' pieces of one column block go to all banks, whether
+  // whole pieces of K or column blocks of V are read.
+  auto swizzle_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
   auto swizzle = [](int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };
   char* const copy = lds_v[wave];
 
@@ -141,47 +224,55 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
   for (int i = 0; i < MT; ++i) o[i] = (f32x4)(0.0f);
 
   if (t < t_end) {
-    int32_t page, pos, page1, pos1;
-    look(t, page, pos);
-    Row row = row_of(t, page, pos);
-    load_k(row);
-    load_v(row);
-    look(min(t + shares, t_end - 1), page1, pos1);
+    look(t);
+    resolve(t);
+    place();
+    look(min(t + shares, t_end - 1));
+    load(Kb, kr);
+    load(Vb, vr);
     for (; t < t_end; t += shares) {
-      const bool more = t + shares < t_end;
-      const uint32_t seen = (uint32_t)__ballot(row.seen);
+      const uint32_t now = seen;
+      const int32_t pos_now = pos;
+#pragma unroll
+      for (int i = 0; i < VLOADS; ++i) {
+        const int r = i * (64 / LANES) + lane / LANES;
+        *reinterpret_cast<u32x4*>(copy + r * (D * 2) + (((lane % LANES) ^ swizzle_k(r)) << 4)) = kr[i];
+      }
+      resolve(t + shares);
+      place();
+      look(min(t + 2 * shares, t_end - 1));
+      load(Kb, kr);
+      own_lds_order();
       f32x4 sc[2];
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
         sc[kt] = (f32x4)(0.0f);
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) sc[kt] = Elem<T>::mfma16(kf[kt][i], qf[i], sc[kt]);
+        for (int i = 0; i < STEPS; ++i) {
+          const int r = 16 * kt + l16;
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(copy + r * (D * 2) + (((4 * i + quad) ^ swizzle_k(r)) << 4));
+          sc[kt] = Elem<T>::mfma16(kf, qf[i], sc[kt]);
+        }
       }
-      Row next = row;
-      if (more) {
-        next = row_of(t + shares, page1, pos1);
-        load_k(next);
-        look(min(t + 2 * shares, t_end - 1), page1, pos1);
-      }
+      own_lds_order();
       // scores in units of log2
-      if (a.cap2 != 0.0f) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = capped(sc[e >> 2][e & 3] * a.scale, a.two_over_cap, a.cap2);
-      } else {
+      for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] *= a.scale;
+      if (__builtin_expect(a.cap2 != 0.0f, 0)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] *= a.scale;
+        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = capped(sc[e >> 2][e & 3], a.two_over_cap, a.cap2);
       }
-      if (a.slopes) {
+      if (__builtin_expect(a.slopes != nullptr, 0)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int kp = __shfl(row.pos, 16 * (e >> 2) + 4 * quad + (e & 3));
+          const int kp = __shfl(pos_now, 16 * (e >> 2) + 4 * quad + (e & 3));
           sc[e >> 2][e & 3] -= slope * (float)(int)((uint32_t)q_pos - (uint32_t)kp);
         }
       }
-      if (seen != 0xFFFFFFFFu) {
+      if (__builtin_expect(now != 0xFFFFFFFFu, 0)) {
+        const uint32_t mine = now >> (4 * quad);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (!((seen >> (16 * (e >> 2) + 4 * quad + (e & 3))) & 1)) sc[e >> 2][e & 3] = kNone;
+        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = mine & (1u << (16 * (e >> 2) + (e & 3))) ? sc[e >> 2][e & 3] : kNone;
       }
       float top = sc[0][0];
 #pragma unroll
@@ -210,14 +301,17 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
 #pragma unroll
       for (int i = 0; i < VLOADS; ++i) {
         const int r = i * (64 / LANES) + lane / LANES;
-        u32x4 v = vr[i];
-        if (seen != 0xFFFFFFFFu && !((seen >> r) & 1)) v = (u32x4)(0);
-        *reinterpret_cast<u32x4*>(copy + r * (D * 2) + (((lane % LANES) ^ swizzle(r)) << 4)) = v;
+        *reinterpret_cast<u32x4*>(copy + r * (D * 2) + (((lane % LANES) ^ swizzle(r)) << 4)) = vr[i];
       }
-      if (more) load_v(next);
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+      load(Vb, vr);
+      if (__builtin_expect(now != 0xFFFFFFFFu, 0)) {
+        own_lds_order();
+        if (!((now >> (lane & 31)) & 1)) {  // two lanes a row
+#pragma unroll 1
+          for (int c = lane >> 5; c < LANES; c += 2) *reinterpret_cast<u32x4*>(copy + (lane & 31) * (D * 2) + (c << 4)) = (u32x4)(0);
+        }
+      }
+      own_lds_order();
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         u32x4 vf;
@@ -231,12 +325,10 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
         o[mt] = Elem<T>::mfma16(vf, hi, o[mt]);
         o[mt] = Elem<T>::mfma16(vf, lo, o[mt]);
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-      row = next;
+      own_lds_order();
     }
   }
+
   z += __shfl_xor(z, 16);
   z += __shfl_xor(z, 32);
 
@@ -265,11 +357,12 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
       acc += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds_v[w]) + hl * D + ((d4 ^ (hl & 7)) << 2));
     }
     const int64_t row = (int64_t)b * a.Hq + g * a.G + 64 * hg + hh;
-    if (a.S > 1) {
-      *reinterpret_cast<f32x4*>(a.part_o + (row * a.S + s) * D + 4 * d4) = acc;
+    if (ranges > 1) {
+      const int64_t at = (int64_t)blockIdx.x * (16 * a.wave_groups) + hh;
+      *reinterpret_cast<f32x4*>(a.part_o + at * D + 4 * d4) = acc;
       if (d4 == 0) {
-        a.part_mz[(row * a.S + s) * 2] = top;
-        a.part_mz[(row * a.S + s) * 2 + 1] = sum;
+        a.part_mz[at * 2] = top;
+        a.part_mz[at * 2 + 1] = sum;
       }
     } else {
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -282,7 +375,7 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
   }
 }
 
-// One workgroup per (sequence, query head): the ranges' results in order, 8 threads' shares of them added at the end.
+// One workgroup per (sequence, query head): the ranges' results, every PARTS-th of them by one part of the threads, in order.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void decode_long_join_kernel(const LongArgs a) {
   constexpr int PARTS = 256 / (D / 4);
@@ -290,19 +383,30 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const LongArgs a)
   __shared__ float lds_red[8];
   __shared__ f32x4 lds_o[PARTS][D / 4];
   const int64_t row = blockIdx.x;
-  const float* mz = a.part_mz + row * a.S * 2;
+  const int b = (int)(row / a.Hq), h = (int)(row % a.Hq), g = h / a.G, h_in = h % a.G, unit = g * a.head_groups + h_in / 64;
+  int ranges = a.ranges, base = b * a.units * a.ranges;
+  if (a.B > 1 && a.B <= kFlatBatch) {
+    const int lane = threadIdx.x & 63;
+    const Tiles tl = tiles_of(a, min(lane, a.B - 1));
+    const Cut c = flat_cut(a, lane < a.B ? tl.count : 0, lane);
+    ranges = __builtin_amdgcn_readlane(c.ranges, b);
+    base = __builtin_amdgcn_readlane(c.base, b);
+  }
+  if (ranges == 1) return;  // (written already)
+  const int64_t heads = 16 * a.wave_groups, at = ((int64_t)base + unit * ranges) * heads + h_in % 64;
+  const float* const mz = a.part_mz + at * 2;
   float top = kNone;
-  for (int i = threadIdx.x; i < a.S; i += 256) top = fmaxf(top, mz[2 * i]);
+  for (int i = threadIdx.x; i < ranges; i += 256) top = fmaxf(top, mz[2 * heads * i]);
   for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
   if ((threadIdx.x & 63) == 0) lds_red[threadIdx.x >> 6] = top;
   __syncthreads();
   top = fmaxf(fmaxf(lds_red[0], lds_red[1]), fmaxf(lds_red[2], lds_red[3]));
   const float ref = top == kNone ? 0.0f : top;
   float sum = 0.0f;
-  for (int i = threadIdx.x; i < a.S; i += 256) {
-    const float f = exp2_(mz[2 * i] - ref);
+  for (int i = threadIdx.x; i < ranges; i += 256) {
+    const float f = exp2_(mz[2 * heads * i] - ref);
     lds_w[i] = f;
-    sum += f * mz[2 * i + 1];
+    sum += f * mz[2 * heads * i + 1];
   }
   for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
   if ((threadIdx.x & 63) == 0) lds_red[4 + (threadIdx.x >> 6)] = sum;
@@ -310,10 +414,8 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const LongArgs a)
   sum = (lds_red[4] + lds_red[5]) + (lds_red[6] + lds_red[7]);
   const int d4 = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
   f32x4 acc = (f32x4)(0.0f);
-  for (int i = part; i < a.S; i += PARTS) {
-    const float f = lds_w[i];
-    if (f != 0.0f) acc += f * *reinterpret_cast<const f32x4*>(a.part_o + (row * a.S + i) * D + 4 * d4);
-  }
+#pragma unroll 8
+  for (int i = part; i < ranges; i += PARTS) acc += lds_w[i] * *reinterpret_cast<const f32x4*>(a.part_o + (at + heads * i) * D + 4 * d4);
   lds_o[part][d4] = acc;
   __syncthreads();
   if (part == 0) {
@@ -327,25 +429,34 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const LongArgs a)
   }
 }
 
-template <typename T, int D>
-hipError_t launch(const LongArgs& a, hipStream_t s) {
-  const dim3 grid(a.S, a.Hkv * a.head_groups, a.B), block(256);
-  hipLaunchKernelGGL((decode_long_kernel<T, D>), grid, block, 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.S == 1) return e;
-  hipLaunchKernelGGL((decode_long_join_kernel<T, D>), dim3((unsigned)(a.B * a.Hq)), block, 0, s, a);
-  return hipGetLastError();
+// Query heads that a workgroup's results have room for.
+int heads_of(int G) { return G <= 16 ? 16 : G <= 32 ? 32 : 64; }
+
+// Workgroups of a call, and what LongArgs::ranges is for it.
+struct Grid {
+  int64_t workgroups;
+  int32_t ranges;
+};
+Grid grid_of(const pkv_decode_long_desc& d) {
+  const int64_t units = (int64_t)d.Hkv * ((d.Hq / d.Hkv + 63) / 64), all = d.B * units;
+  if (d.k_cap <= kLeastTiles * kTile) return {all, 0};
+  if (d.B > 1 && d.B <= kFlatBatch) {
+    const int64_t share = all <= kWorkgroups / 2 ? kWorkgroups : 2 * kWorkgroups;
+    return all >= 2 * kWorkgroups ? Grid{all, 0} : Grid{share + all, (int32_t)share};
+  }
+  int64_t S = kWorkgroups / all;
+  const int64_t most = ((int64_t)d.k_cap + kLeastTiles * kTile - 1) / (kLeastTiles * kTile);
+  if (S > most) S = most;
+  return S <= 1 ? Grid{all, 0} : Grid{all * S, (int32_t)S};
 }
 
-// Ranges per (sequence, KV head): as many as give 1024 workgroups (two per compute unit at a time, so that a range that starts
-// late costs half a turn at most), but none below 256 keys.
-int ranges(const pkv_decode_long_desc& d) {
-  const int64_t units = (int64_t)d.B * d.Hkv * ((d.Hq / d.Hkv + 63) / 64);
-  int64_t S = (1024 + units - 1) / units;
-  const int64_t most = ((int64_t)d.k_cap + 255) / 256;
-  if (S > most) S = most;
-  if (S > kMaxRanges) S = kMaxRanges;
-  return (int)(S < 1 ? 1 : S);
+template <typename T, int D>
+hipError_t launch(const LongArgs& a, int64_t workgroups, hipStream_t s) {
+  hipLaunchKernelGGL((decode_long_kernel<T, D>), dim3((unsigned)workgroups), dim3(256), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.ranges == 0) return e;
+  hipLaunchKernelGGL((decode_long_join_kernel<T, D>), dim3((unsigned)(a.B * a.Hq)), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 bool aligned(const void* p, int n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -367,7 +478,7 @@ int check_long_desc(const pkv_decode_long_desc* desc) {
   if (d.p_sb < 0 || d.p_sh < 0) return PKV_ERR_INVALID_ARG;
   if (d.d != 64 && d.d != 128) return PKV_ERR_UNSUPPORTED;
   const int64_t G = d.Hq / d.Hkv;
-  if (G > 128 || d.B > 65535 || d.k_cap > (1 << 30) || d.Hkv * ((G + 63) / 64) > 65535 || (int64_t)d.B * d.Hq > 0x7FFFFFFF) return PKV_ERR_UNSUPPORTED;
+  if (G > 128 || d.B > 65535 || d.k_cap > (1 << 30) || d.Hkv > 65535 || (int64_t)d.B * d.Hq > 0x3FFFFFFF) return PKV_ERR_UNSUPPORTED;
   // rows of a pool are counted in 32 bits
   if (d.page_size > 0 && (double)d.num_pages * d.Hkv * d.page_size > 4294967295.0) return PKV_ERR_UNSUPPORTED;
   return PKV_OK;
@@ -382,8 +493,8 @@ extern "C" {
 
 size_t pkv_decode_long_workspace_bytes(const pkv_decode_long_desc* desc) {
   if (check_long_desc(desc) != PKV_OK) return 0;
-  const int S = ranges(*desc);
-  return S == 1 ? 0 : (size_t)desc->B * desc->Hq * S * (desc->d + 2) * sizeof(float);
+  const Grid g = grid_of(*desc);
+  return g.ranges == 0 ? 0 : (size_t)g.workgroups * heads_of(desc->Hq / desc->Hkv) * (desc->d + 2) * sizeof(float);
 }
 
 int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q, const void* K_cache, const void* V_cache,
@@ -407,13 +518,15 @@ int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q, c
   a.table = block_table; a.count = count; a.positions = positions; a.q_pos = q_pos; a.slopes = slopes;
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse_out;
-  a.S = ranges(d);
+  const Grid grid = grid_of(d);
+  a.ranges = grid.ranges;
   a.part_o = static_cast<float*>(workspace);
-  a.part_mz = a.part_o ? a.part_o + (size_t)d.B * d.Hq * a.S * d.d : nullptr;
+  a.part_mz = a.part_o ? a.part_o + (size_t)grid.workgroups * heads_of(d.Hq / d.Hkv) * d.d : nullptr;
   a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.k_cap = d.k_cap;
   a.page_size = d.page_size; a.num_pages = d.num_pages; a.max_pages = d.max_pages; a.window = d.window;
   a.head_groups = (a.G + 63) / 64;
-  a.wave_groups = a.G <= 16 ? 1 : a.G <= 32 ? 2 : 4;
+  a.units = a.Hkv * a.head_groups;
+  a.wave_groups = heads_of(a.G) / 16;
   a.page_magic = d.page_size > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint32_t)d.page_size) : 0xFFFFFFFFu;
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.c_sb = d.c_sb; a.c_sh = d.c_sh; a.c_st = d.c_st; a.p_sb = d.p_sb; a.p_sh = d.p_sh;
   const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d);
@@ -423,9 +536,9 @@ int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q, c
   const hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (d.dtype == PKV_BF16)
-    e = d.d == 128 ? launch<__bf16, 128>(a, st) : launch<__bf16, 64>(a, st);
+    e = d.d == 128 ? launch<__bf16, 128>(a, grid.workgroups, st) : launch<__bf16, 64>(a, grid.workgroups, st);
   else
-    e = d.d == 128 ? launch<_Float16, 128>(a, st) : launch<_Float16, 64>(a, st);
+    e = d.d == 128 ? launch<_Float16, 128>(a, grid.workgroups, st) : launch<_Float16, 64>(a, grid.workgroups, st);
   return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
 }
 
