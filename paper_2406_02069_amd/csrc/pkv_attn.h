@@ -66,10 +66,10 @@ __device__ __forceinline__ u32x2 read_columns(const char* lds) {
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 
-// cap * tanh(x / cap) as cap - 2 cap / (1 + e^(2x / cap)): two transcendental instructions, absolute error about 2^-23 cap, right
-// at both ends (e^... = inf or 0).  two_over_cap carries log2(e).
-__device__ __forceinline__ float capped(float x, float two_over_cap, float cap) {
-  return fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + exp2_(x * two_over_cap)), cap);
+// cap * tanh(s / cap) as cap - 2 cap / (1 + e^(2s / cap)): two transcendental instructions, absolute error about 2^-23 cap, right
+// at both ends (e^... = inf or 0).  x * to_exponent is the exponent to base 2, 2 log2(e) s / cap.
+__device__ __forceinline__ float capped(float x, float to_exponent, float cap) {
+  return fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + exp2_(x * to_exponent)), cap);
 }
 
 }  // namespace

@@ -48,8 +48,8 @@ struct LongArgs {
   int32_t wave_groups;  // 16-head groups in a workgroup: 1, 2 or 4
   uint32_t page_magic;  // floor(2^32 / page_size)
   int64_t q_sb, q_sh, c_sb, c_sh, c_st, p_sb, p_sh;
-  float scale;          // of the products; with a cap: natural units, without: log2
-  float cap2, two_over_cap;  // cap in log2 units (0: none); 2 log2(e) / cap
+  float scale;          // of the products, to log2 units; with a cap 2 log2(e) scale / cap
+  float cap2;           // cap in log2 units (0: none)
 };
 
 // A wave's reads and writes of its own part of LDS keep their order.
@@ -255,12 +255,12 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
         }
       }
       own_lds_order();
-      // scores in units of log2
+      // scores in units of log2 (with a cap: in the exponent's of its tanh)
 #pragma unroll
       for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] *= a.scale;
       if (__builtin_expect(a.cap2 != 0.0f, 0)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = capped(sc[e >> 2][e & 3], a.two_over_cap, a.cap2);
+        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = capped(sc[e >> 2][e & 3], 1.0f, a.cap2);
       }
       if (__builtin_expect(a.slopes != nullptr, 0)) {
 #pragma unroll
@@ -530,9 +530,8 @@ int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q, c
   a.page_magic = d.page_size > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint32_t)d.page_size) : 0xFFFFFFFFu;
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.c_sb = d.c_sb; a.c_sh = d.c_sh; a.c_st = d.c_st; a.p_sb = d.p_sb; a.p_sh = d.p_sh;
   const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d);
-  a.scale = (float)(d.cap > 0.0f ? scale : scale * 1.4426950408889634);
+  a.scale = (float)(scale * 1.4426950408889634 * (d.cap > 0.0f ? 2.0 / d.cap : 1.0));
   a.cap2 = d.cap * kLog2e;
-  a.two_over_cap = d.cap > 0.0f ? 2.0f * kLog2e / d.cap : 0.0f;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (d.dtype == PKV_BF16)

@@ -45,8 +45,8 @@ struct PrefillArgs {
   float* part_mz;  // [B * Hkv][T * G][S][2]
   int32_t B, Hq, Hkv, G, T, N, window, S, tiles;
   int64_t q_sb, q_sh, q_st, kv_sb, kv_sh, kv_st, o_sb, o_sh, o_st;
-  float scale;               // of the products; with a cap: natural units, without: log2
-  float cap2, two_over_cap;  // cap in log2 units (0: none); 2 log2(e) / cap
+  float scale;               // of the products, to log2 units (without a cap)
+  float cap2, two_over_cap;  // cap in log2 units (0: none); 2 log2(e) scale / cap
 };
 
 // What the masks leave a query row: keys lo .. hi (none: lo > hi).
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
     if constexpr (MODE == 1) {
       if (a.cap2 != 0.0f) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] = capped(sc[e] * a.scale, a.two_over_cap, a.cap2);
+        for (int e = 0; e < 16; ++e) sc[e] = capped(sc[e], a.two_over_cap, a.cap2);
       } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[e] *= a.scale;
@@ -529,10 +529,9 @@ int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q, const voi
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.q_st = d.q_st; a.kv_sb = d.kv_sb; a.kv_sh = d.kv_sh; a.kv_st = d.kv_st;
   a.o_sb = d.o_sb; a.o_sh = d.o_sh; a.o_st = d.o_st;
   const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d);
-  // without a cap the scores are taken to log2 units at once (with slopes before these are subtracted)
-  a.scale = (float)(d.cap > 0.0f ? scale : scale * 1.4426950408889634);
+  a.scale = (float)(scale * 1.4426950408889634);
   a.cap2 = d.cap * kLog2e;
-  a.two_over_cap = d.cap > 0.0f ? 2.0f * kLog2e / d.cap : 0.0f;
+  a.two_over_cap = d.cap > 0.0f ? (float)(2.0 * 1.4426950408889634 * scale / d.cap) : 0.0f;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (d.dtype == PKV_BF16)
