@@ -536,8 +536,8 @@ typedef struct {
 } pkv_rotary_desc;
 
 /*
- * desc        HOST.  Strides are >= 0 and multiples of 8 (p_*: any); those of
- *             tensors that are not given are not looked at.
+ * desc        HOST.  Strides are >= 0 and multiples of 8 (p_*: any >= 0);
+ *             those of tensors that are not given are not looked at.
  * q, q_out    DEVICE, 16-byte aligned, both or neither NULL.  q_out may be q
  *             with the same strides, and overlaps it in no other way.  Rows
  *             t >= new_b are neither read nor written.
@@ -559,7 +559,7 @@ typedef struct {
  * dropped_out DEVICE int32 [B] or NULL, written: tokens of b that were dropped.
  * Asynchronous on `stream`, needs no workspace, never allocates.
  * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, rot not a
- * multiple of 8, more than 2^31 - 1 tokens or workgroups), PKV_ERR_HIP.
+ * multiple of 8, B or B * T / 16 > 2^24 - 1, Hq + 2 Hkv > 65535), PKV_ERR_HIP.
  */
 int pkv_rotary_append(const pkv_rotary_desc* desc, const void* q,
                       const void* k, const void* v, const double* inv_freq,
@@ -626,9 +626,10 @@ size_t pkv_prefill_workspace_bytes(const pkv_prefill_desc* desc);
  *            bytes (may be NULL when that is 0); contents irrelevant on
  *            entry, undefined on exit; concurrent calls need distinct ones.
  * Asynchronous on `stream`, never allocates.
- * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv >
- * 128, B > 65535, N or T > 2^30, T * Hq/Hkv > 2^31 - 256, too many workgroups),
- * PKV_ERR_WORKSPACE, PKV_ERR_HIP.
+ * Errors: PKV_ERR_INVALID_ARG (also a scale or cap whose quotient is not a
+ * finite fp32), PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv > 128, B > 65535, N
+ * or T > 2^30, T * Hq/Hkv > 2^31 - 256, kv_st > 2^23, more than 2^24 - 1
+ * workgroups of 128 rows), PKV_ERR_WORKSPACE, PKV_ERR_HIP.
  */
 int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q,
                           const void* K, const void* V,
@@ -675,7 +676,7 @@ typedef struct {
 size_t pkv_decode_long_workspace_bytes(const pkv_decode_long_desc* desc);
 
 /*
- * desc        HOST.  Strides are >= 0 and multiples of 8 (p_*: any).
+ * desc        HOST.  Strides are >= 0 and multiples of 8 (p_*: any >= 0).
  * q           DEVICE, of the descriptor's type, 16-byte aligned.
  * K_cache, V_cache
  *             DEVICE, 16-byte aligned: compact with strides c_*, or pools
@@ -691,9 +692,10 @@ size_t pkv_decode_long_workspace_bytes(const pkv_decode_long_desc* desc);
  *             seen).
  * workspace   as pkv_decode_attention's, pkv_decode_long_workspace_bytes.
  * Asynchronous on `stream`, never allocates.
- * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv >
- * 128, B > 65535, k_cap > 2^30, too many workgroups), PKV_ERR_WORKSPACE,
- * PKV_ERR_HIP.
+ * Errors: PKV_ERR_INVALID_ARG (also a scale or cap whose quotient is not a
+ * finite fp32), PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv > 128, B or Hkv >
+ * 65535, B * Hq > 2^24 - 1, k_cap or c_st > 2^30, a pool of more than 2^32 - 1
+ * rows), PKV_ERR_WORKSPACE, PKV_ERR_HIP.
  */
 int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q,
                               const void* K_cache, const void* V_cache,

@@ -506,16 +506,38 @@ def _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, index)
             raise ValueError("k_cap: more rows than the cache has")
         want = (B, Hkv, shape[2], d)
         K, V = _need(K_cache, "K_cache", dtype, want, index, False), _need(V_cache, "V_cache", dtype, want, index, False)
-        st = K_cache.stride()
-        if st != V_cache.stride():
-            raise ValueError("K_cache and V_cache must have the same strides")
-        return (k_cap, 0, 0, 0, st[0], st[1], st[2]), K, V, None
+        if K_cache.stride() != V_cache.stride():
+            _same_strides(K_cache, V_cache, "K_cache and V_cache")
+        st = _strides(K_cache)
+        return (k_cap, 0, 0, 0, st[0], st[1], st[2] if shape[2] > 1 else d), K, V, None
     if block_table.dim() != 2:
         raise ValueError("block_table: need [B, max_pages]")
     want, pages = (shape[0], Hkv, shape[2], d), block_table.shape[1]
     K, V = _need(K_cache, "K_cache", dtype, want, index), _need(V_cache, "V_cache", dtype, want, index)
     table = _need(block_table, "block_table", torch.int32, (B, pages), index)
     return (pages * shape[2] if k_cap is None else k_cap, shape[2], shape[0], pages, 0, 0, 0), K, V, table
+
+
+def _strides(t: torch.Tensor):
+    """The strides of a 4-d tensor; where they keep no alignment, 0 for dimensions of one element (torch leaves anything there)."""
+    st = t.stride()
+    if (st[0] | st[1] | st[2]) & 7:
+        return [x if n > 1 else 0 for n, x in zip(t.shape, st)]
+    return st
+
+
+def _same_strides(a: torch.Tensor, b: torch.Tensor, names: str):
+    if any(n > 1 and x != y for n, x, y in zip(a.shape, a.stride(), b.stride())):
+        raise ValueError(f"{names} must have the same strides")
+
+
+def _workspace(t: Optional[torch.Tensor], index: int):
+    """(address, bytes) of a workspace; its size is checked by the call."""
+    if t is None:
+        return None, 0
+    if t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"workspace: need a contiguous tensor on GPU {index}")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _row_positions(t: torch.Tensor, name: str, B: int, Hkv: int, k_cap: int, index: int):
@@ -529,7 +551,7 @@ def rotary_frequencies(rot: int, scaling: str = "plain", base: float = 10000.0, 
                        trained: float = 0.0, low: float = 0.0, high: float = 0.0, device=None):
     """pkv_rotary_frequencies: (radians per position of each pair, fp64 [rot / 2] on `device`; magnitude)."""
     out, magnitude = (ctypes.c_double * max(rot // 2, 1))(), ctypes.c_float()
-    rc = load().pkv_rotary_frequencies(rot, ROTARY_SCALINGS[scaling], base, factor, trained, low, high, out,
+    rc = load().pkv_rotary_frequencies(rot, ROTARY_SCALINGS.get(scaling, -1), base, factor, trained, low, high, out,
                                        ctypes.byref(magnitude))
     if rc != OK:
         raise PkvError(rc, "pkv_rotary_frequencies")
@@ -563,16 +585,16 @@ def rotary_append(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optio
         if q_out is None:
             q_out = (torch.empty if new_lens is None else torch.zeros)((B, H, T, d), dtype=dtype, device=first.device)
         q_p, o_p = q.data_ptr(), _need(q_out, "q_out", dtype, (B, H, T, d), index, False)
-        qs, os_ = q.stride(), q_out.stride()
+        qs, os_ = _strides(q), _strides(q_out)
     if k is not None:
         k_p, v_p = _need(k, "k", dtype, (B, Hkv, T, d), index, False), _need(v, "v", dtype, (B, Hkv, T, d), index, False)
-        ks, vs = k.stride(), v.stride()
+        ks, vs = _strides(k), _strides(v)
         cache, K_p, V_p, table_p = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, index)
         if pos_cache is not None:
             pc_p, ps = _row_positions(pos_cache, "pos_cache", B, Hkv, cache[0], index)
     elif pos_cache is not None:
         raise ValueError("pos_cache: needs keys and values")
-    desc = _pack_rotary(B, H if q is not None else Hkv, Hkv, d, T, 2 * half, ROTARY_LAYOUTS[layout], code, cache[0], cache[1],
+    desc = _pack_rotary(B, H if q is not None else Hkv, Hkv, d, T, 2 * half, ROTARY_LAYOUTS.get(layout, -1), code, cache[0], cache[1],
                         cache[2], cache[3], magnitude, 0, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
                         os_[0], os_[1], os_[2], cache[4], cache[5], cache[6], ps[0], ps[1])
     _call("pkv_rotary_append", load().pkv_rotary_append, index, desc, q_p, k_p, v_p, f_p,
@@ -600,12 +622,12 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_len
         raise ValueError("K: need four dimensions")
     _, Hkv, N, _ = K.shape
     K_p, V_p = _need(K, "K", dtype, (B, Hkv, N, d), index, False), _need(V, "V", dtype, (B, Hkv, N, d), index, False)
-    ks = K.stride()
-    if ks != V.stride():
-        raise ValueError("K and V must have the same strides")
+    if K.stride() != V.stride():
+        _same_strides(K, V, "K and V")
+    ks = _strides(K)
     if out is None:
         out = torch.empty((B, Hq, T, d), dtype=dtype, device=q.device)
-    out_p, qs, os_ = _need(out, "out", dtype, (B, Hq, T, d), index, False), q.stride(), out.stride()
+    out_p, qs, os_ = _need(out, "out", dtype, (B, Hq, T, d), index, False), _strides(q), _strides(out)
     if want_lse and lse is None:
         lse = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device)
     desc = _pack_prefill(B, Hq, Hkv, d, T, N, code, window, _scale(scale), cap, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
@@ -622,7 +644,7 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_len
           None if prefix_end is None else _need(prefix_end, "prefix_end", torch.int32, (B, N), index),
           None if slopes is None else _need(slopes, "slopes", torch.float32, (Hq,), index),
           out_p, None if lse is None else _need(lse, "lse", torch.float32, (B, Hq, T), index),
-          None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream_of(index))
+          *_workspace(workspace, index), _stream_of(index))
     return out, lse
 
 
@@ -649,6 +671,8 @@ def decode_attention_long(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch
     if want_lse and lse is None:
         lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
     qs = q.stride()
+    if (qs[0] | qs[1]) & 7:
+        qs = [x if n > 1 else 0 for n, x in zip(q.shape, qs)]
     desc = _pack_decode_long(B, Hq, Hkv, d, cache[0], cache[1], cache[2], cache[3], code, window, _scale(scale), cap,
                              qs[0], qs[1], cache[4], cache[5], cache[6], ps[0], ps[1])
     lib = load()
@@ -661,7 +685,7 @@ def decode_attention_long(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch
           None if q_pos is None else _need(q_pos, "q_pos", torch.int32, (B,), index),
           None if slopes is None else _need(slopes, "slopes", torch.float32, (Hq,), index),
           _need(out, "out", dtype, (B, Hq, d), index), None if lse is None else _need(lse, "lse", torch.float32, (B, Hq), index),
-          None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream_of(index))
+          *_workspace(workspace, index), _stream_of(index))
     return out, lse
 
 

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "pkv_internal.h"
+#include "pkv_hostcheck.h"
 
 namespace pkv {
 namespace {

@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
   const char* const Vb = reinterpret_cast<const char*>(a.V) + base + 16 * (lane % LANES);
   const int32_t* const table = a.table + (int64_t)b * a.max_pages;
   const int32_t* const pos_b = a.positions + b * a.p_sb + g * a.p_sh;
-  const int least = a.window ? max((int)max((int64_t)q_pos - a.window + 1, (int64_t)0), 0) : 0;  // of the seen positions
+  const int least = a.window ? (int)max((int64_t)q_pos - a.window + 1, (int64_t)0) : 0;  // of the seen positions
   if (q_pos < least) t = t_end;
 
   // What has to be loaded to know a tile's rows: lane l looks after row l % 32.
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
   int32_t pos = 0;
   auto resolve = [&](int tile) {
     pos = pos_next;
-    bool is = tile < t_end && tile * kTile + (lane & 31) < n && (uint32_t)(pos - least) <= (uint32_t)(q_pos - least);
+    bool is = tile < t_end && tile * kTile + (lane & 31) < n && (uint32_t)pos - (uint32_t)least <= (uint32_t)q_pos - (uint32_t)least;
     at = slot;
     if (a.page_size) {
       is = is && (uint32_t)page < (uint32_t)a.num_pages;
@@ -459,7 +459,11 @@ hipError_t launch(const LongArgs& a, int64_t workgroups, hipStream_t s) {
   return hipGetLastError();
 }
 
-bool aligned(const void* p, int n) { return ((uintptr_t)p & (n - 1)) == 0; }
+// What a product is multiplied by: see LongArgs::scale.
+float scale_of(const pkv_decode_long_desc& d) {
+  const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d);
+  return (float)(scale * 1.4426950408889634 * (d.cap > 0.0f ? 2.0 / d.cap : 1.0));
+}
 
 int check_long_desc(const pkv_decode_long_desc* desc) {
   if (!desc) return PKV_ERR_INVALID_ARG;
@@ -467,18 +471,18 @@ int check_long_desc(const pkv_decode_long_desc* desc) {
   if (d.B < 1 || d.Hq < 1 || d.Hkv < 1 || d.Hq % d.Hkv != 0 || d.k_cap < 1 || d.page_size < 0 || d.window < 0) return PKV_ERR_INVALID_ARG;
   if (d.dtype != PKV_BF16 && d.dtype != PKV_FP16) return PKV_ERR_INVALID_ARG;
   if (!(d.scale >= 0.0f) || !(d.cap >= 0.0f) || !isfinite(d.scale) || !isfinite(d.cap)) return PKV_ERR_INVALID_ARG;
-  if (d.q_sb < 0 || d.q_sb % 8 != 0 || d.q_sh < 0 || d.q_sh % 8 != 0) return PKV_ERR_INVALID_ARG;
+  if (!good_strides(d.q_sb, d.q_sh, 0)) return PKV_ERR_INVALID_ARG;
   if (d.page_size > 0) {
     if (d.num_pages < 1 || d.max_pages < ((int64_t)d.k_cap + d.page_size - 1) / d.page_size) return PKV_ERR_INVALID_ARG;
   } else {
-    const int64_t st[3] = {d.c_sb, d.c_sh, d.c_st};
-    for (int i = 0; i < 3; ++i)
-      if (st[i] < 0 || st[i] % 8 != 0) return PKV_ERR_INVALID_ARG;
+    if (!good_strides(d.c_sb, d.c_sh, d.c_st)) return PKV_ERR_INVALID_ARG;
   }
   if (d.p_sb < 0 || d.p_sh < 0) return PKV_ERR_INVALID_ARG;
   if (d.d != 64 && d.d != 128) return PKV_ERR_UNSUPPORTED;
+  if (!isfinite(scale_of(d)) || !isfinite(d.cap * kLog2e)) return PKV_ERR_INVALID_ARG;
   const int64_t G = d.Hq / d.Hkv;
-  if (G > 128 || d.B > 65535 || d.k_cap > (1 << 30) || d.Hkv > 65535 || (int64_t)d.B * d.Hq > 0x3FFFFFFF) return PKV_ERR_UNSUPPORTED;
+  if (G > 128 || d.B > 65535 || d.k_cap > (1 << 30) || d.Hkv > 65535 || (int64_t)d.B * d.Hq > kMaxGrid) return PKV_ERR_UNSUPPORTED;
+  if (d.page_size == 0 && d.c_st > (1 << 30)) return PKV_ERR_UNSUPPORTED;  // (a row's bytes: 32 bits)
   // rows of a pool are counted in 32 bits
   if (d.page_size > 0 && (double)d.num_pages * d.Hkv * d.page_size > 4294967295.0) return PKV_ERR_UNSUPPORTED;
   return PKV_OK;
@@ -529,8 +533,7 @@ int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q, c
   a.wave_groups = heads_of(a.G) / 16;
   a.page_magic = d.page_size > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint32_t)d.page_size) : 0xFFFFFFFFu;
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.c_sb = d.c_sb; a.c_sh = d.c_sh; a.c_st = d.c_st; a.p_sb = d.p_sb; a.p_sh = d.p_sh;
-  const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d);
-  a.scale = (float)(scale * 1.4426950408889634 * (d.cap > 0.0f ? 2.0 / d.cap : 1.0));
+  a.scale = scale_of(d);
   a.cap2 = d.cap * kLog2e;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;

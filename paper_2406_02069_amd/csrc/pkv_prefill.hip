@@ -465,10 +465,9 @@ int parts(const pkv_prefill_desc& d) {
   return best;
 }
 
-bool aligned(const void* p, int n) { return ((uintptr_t)p & (n - 1)) == 0; }
-bool good_strides(int64_t sb, int64_t sh, int64_t st) {
-  return sb >= 0 && sh >= 0 && st >= 0 && sb % 8 == 0 && sh % 8 == 0 && st % 8 == 0;
-}
+double scale_of(const pkv_prefill_desc& d) { return d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d); }
+// Of a product, in the exponent's of the cap's tanh.
+float cap_factor(const pkv_prefill_desc& d) { return d.cap > 0.0f ? (float)(2.0 * 1.4426950408889634 * scale_of(d) / d.cap) : 0.0f; }
 
 int check_prefill_desc(const pkv_prefill_desc* desc) {
   if (!desc) return PKV_ERR_INVALID_ARG;
@@ -479,12 +478,11 @@ int check_prefill_desc(const pkv_prefill_desc* desc) {
   if (!good_strides(d.q_sb, d.q_sh, d.q_st) || !good_strides(d.kv_sb, d.kv_sh, d.kv_st) || !good_strides(d.o_sb, d.o_sh, d.o_st))
     return PKV_ERR_INVALID_ARG;
   if (d.d != 64 && d.d != 128) return PKV_ERR_UNSUPPORTED;
+  if (!isfinite(cap_factor(d)) || !isfinite((float)(scale_of(d) * kLog2e)) || !isfinite(d.cap * kLog2e)) return PKV_ERR_INVALID_ARG;
   if (d.Hq / d.Hkv > 128 || d.B > 65535 || d.N > (1 << 30) || d.T > (1 << 30)) return PKV_ERR_UNSUPPORTED;
   if ((int64_t)d.T * (d.Hq / d.Hkv) > 0x7FFFFF00ll) return PKV_ERR_UNSUPPORTED;
-  if (d.kv_st > (1 << 23)) return PKV_ERR_UNSUPPORTED;  // (offsets inside a step of 64 keys: 32 bits)
-  // (a product of at most 2^24 * 2^16 * 2^31 does not fit 64 bits: the head count is bounded first)
-  if ((int64_t)d.B * d.Hkv > 0x7FFFFFFF || row_tiles(d) * parts(d) > 0x7FFFFFFFll / ((int64_t)d.B * d.Hkv)) return PKV_ERR_UNSUPPORTED;
-  if ((double)d.T * d.Hq * d.B > 8e9) return PKV_ERR_UNSUPPORTED;  // (workgroups of the joining kernel)
+  if (d.kv_st > (1 << 23)) return PKV_ERR_UNSUPPORTED;  // (offsets inside a step: 32 bits)
+  if ((int64_t)d.B * d.Hkv > kMaxGrid || row_tiles(d) > kMaxGrid / ((int64_t)d.B * d.Hkv)) return PKV_ERR_UNSUPPORTED;
   return PKV_OK;
 }
 
@@ -528,10 +526,9 @@ int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q, const voi
   a.part_mz = a.part_o ? a.part_o + (size_t)d.B * d.Hq * d.T * a.S * d.d : nullptr;
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.q_st = d.q_st; a.kv_sb = d.kv_sb; a.kv_sh = d.kv_sh; a.kv_st = d.kv_st;
   a.o_sb = d.o_sb; a.o_sh = d.o_sh; a.o_st = d.o_st;
-  const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d);
-  a.scale = (float)(scale * 1.4426950408889634);
+  a.scale = (float)(scale_of(d) * 1.4426950408889634);
   a.cap2 = d.cap * kLog2e;
-  a.two_over_cap = d.cap > 0.0f ? (float)(2.0 * 1.4426950408889634 * scale / d.cap) : 0.0f;
+  a.two_over_cap = cap_factor(d);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (d.dtype == PKV_BF16)

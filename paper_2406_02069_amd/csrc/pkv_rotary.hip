@@ -7,6 +7,7 @@
 // grid until there are enough workgroups.
 #include <math.h>
 
+#include "pkv_hostcheck.h"
 #include "pkv_internal.h"
 
 namespace pkv {
@@ -190,11 +191,6 @@ hipError_t launch_layout(RotaryArgs& a, int layout, hipStream_t s) {
   return layout == PKV_ROTARY_INTERLEAVED ? launch<T, D, true>(a, s) : launch<T, D, false>(a, s);
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
-bool good_strides(int64_t sb, int64_t sh, int64_t st) {
-  return sb >= 0 && sh >= 0 && st >= 0 && sb % 8 == 0 && sh % 8 == 0 && st % 8 == 0;
-}
 
 }  // namespace
 }  // namespace pkv
@@ -242,9 +238,9 @@ int pkv_rotary_append(const pkv_rotary_desc* desc, const void* q, const void* k,
   if (d.dtype != PKV_BF16 && d.dtype != PKV_FP16) return PKV_ERR_INVALID_ARG;
   const bool has_q = q || q_out, has_kv = k || v || K_cache || V_cache;
   if ((!has_q && !has_kv) || (has_q && (!q || !q_out)) || (has_kv && (!k || !v || !K_cache || !V_cache))) return PKV_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(q_out) || !aligned16(k) || !aligned16(v) || !aligned16(K_cache) || !aligned16(V_cache) ||
-      ((uintptr_t)inv_freq & 7) || !aligned4(positions) || !aligned4(new_lens) || !aligned4(count) || !aligned4(block_table) ||
-      !aligned4(pos_cache) || !aligned4(dropped_out))
+  if (!aligned(q, 16) || !aligned(q_out, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(K_cache, 16) || !aligned(V_cache, 16) ||
+      !aligned(inv_freq, 8) || !aligned(positions, 4) || !aligned(new_lens, 4) || !aligned(count, 4) || !aligned(block_table, 4) ||
+      !aligned(pos_cache, 4) || !aligned(dropped_out, 4))
     return PKV_ERR_INVALID_ARG;
   if (has_q && (!good_strides(d.q_sb, d.q_sh, d.q_st) || !good_strides(d.o_sb, d.o_sh, d.o_st))) return PKV_ERR_INVALID_ARG;
   if (has_kv) {
@@ -261,7 +257,7 @@ int pkv_rotary_append(const pkv_rotary_desc* desc, const void* q, const void* k,
   }
   if (d.rot < 2 || d.rot > d.d || d.rot % 2 != 0) return PKV_ERR_INVALID_ARG;
   if ((d.d != 64 && d.d != 128) || d.rot % 8 != 0) return PKV_ERR_UNSUPPORTED;
-  if ((int64_t)d.B * d.T > 0x7FFFFFFF || (int64_t)d.Hq + 2 * (int64_t)d.Hkv > 65535) return PKV_ERR_UNSUPPORTED;
+  if ((int64_t)d.B * d.T > 16 * kMaxGrid || d.B > kMaxGrid || (int64_t)d.Hq + 2 * (int64_t)d.Hkv > 65535) return PKV_ERR_UNSUPPORTED;
   RotaryArgs a;
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);

@@ -62,3 +62,17 @@ def test_binding_refuses_tensors_that_do_not_fit():
         binding.decode_attention_long(q.float(), K, K, torch.zeros(1, dtype=torch.int32))
     with pytest.raises(ValueError):
         binding._scale(0.0)
+
+
+def test_factors_that_are_not_finite_and_wide_rows():
+    assert _call(_desc(cap=1e-44)) == I                        # the quotient of scale and cap
+    assert _call(_desc(cap=3e38)) == I                         # the cap in units of log2
+    assert _call(_desc(scale=3e38)) == I
+    assert _call(_desc(c_st=2 ** 30 + 8)) == U
+    assert _call(_desc(B=65535, Hq=512, Hkv=512)) == U
+
+
+def test_binding_refuses_a_workspace_elsewhere():
+    with pytest.raises(ValueError):
+        binding._workspace(torch.zeros(8, dtype=torch.uint8), 0)
+    assert binding._workspace(None, 0) == (None, 0)

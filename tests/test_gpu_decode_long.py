@@ -175,3 +175,32 @@ def test_agrees_with_the_attention_over_compressed_caches():
     # the other call's values are within 1e-4 of the exact ones, ours within half a step and 2^-13 of the values' size
     assert bool(((out.float() - ref).abs() <= 2.0 ** -8 * ref.abs() + 5e-4).all())
     torch.testing.assert_close(lse, ref_lse, rtol=1e-5, atol=1e-4)
+
+
+@pytest.mark.parametrize("B,Hkv,G,d,k_cap,page,window", [(64, 1, 3, 64, 3000, 0, 0), (65, 2, 2, 64, 1200, 16, 0), (300, 1, 1, 64, 700, 0, 0),
+                                                       (7, 8, 4, 128, 6000, 16, 1000), (40, 8, 1, 64, 900, 0, 0), (2, 1, 70, 128, 9000, 0, 0)])
+def test_ragged_batches_of_all_sizes(B, Hkv, G, d, k_cap, page, window):
+    # ranges by the sequences' lengths, equal numbers of ranges, and none: sequences of all lengths, empty ones among them
+    print("ragged", B, Hkv, G, d, k_cap, page, window, flush=True)
+    q, K, V, Kc, Vc, table = _make(B, Hkv * G, Hkv, d, k_cap, torch.bfloat16, page, B)
+    g = torch.Generator().manual_seed(B)
+    count = torch.randint(0, k_cap + 1, (B,), generator=g).to(torch.int32)
+    count[::5] = torch.randint(0, 40, (len(count[::5]),), generator=g).to(torch.int32)
+    count[B // 2] = k_cap
+    count = count.to(DEV)
+    out, lse = binding.decode_attention_long(q, Kc, Vc, count, block_table=table, k_cap=k_cap, window=window, want_lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, q, K, V, count, torch.bfloat16, window=window)
+
+
+def test_dimensions_of_one_element_may_have_any_stride():
+    g = torch.Generator(device=DEV).manual_seed(12)
+    x = torch.randn(3 * 64 + 5, generator=g, device=DEV).to(torch.bfloat16)
+    q = x.as_strided((1, 1, 64), (7, 3, 1))
+    K, V = x[64:].as_strided((1, 1, 1, 64), (1, 5, 9, 1)), x[128:].as_strided((1, 1, 1, 64), (11, 5, 2, 1))
+    out, lse = binding.decode_attention_long(q, K, V, torch.ones(1, dtype=torch.int32, device=DEV), want_lse=True)
+    torch.cuda.synchronize()
+    assert torch.equal(out, V[:, :, 0])                      # one row: its value, whatever the score
+    out4, _ = binding.prefill_attention(q[:, :, None], K, V)
+    torch.cuda.synchronize()
+    assert torch.equal(out4[:, :, 0], V[:, :, 0])

@@ -59,3 +59,8 @@ def test_binding_refuses_tensors_that_do_not_fit():
     for args in ((q, K, K), (q.float(), K, K), (q[0], K, K), (q.transpose(2, 3), K, K)):
         with pytest.raises(ValueError):
             binding.prefill_attention(*args)
+
+
+def test_factors_that_are_not_finite():
+    for kw in (dict(cap=1e-44), dict(cap=3e38), dict(scale=3e38)):
+        assert _call(_desc(**kw)) == I
