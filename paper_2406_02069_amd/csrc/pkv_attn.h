@@ -67,10 +67,64 @@ __device__ __forceinline__ u32x2 read_columns(const char* lds) {
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 
-// cap * tanh(s / cap) as cap - 2 cap / (1 + e^(2s / cap)): two transcendental instructions, absolute error about 2^-23 cap, right
-// at both ends (e^... = inf or 0).  x * to_exponent is the exponent to base 2, 2 log2(e) s / cap.
-__device__ __forceinline__ float capped(float x, float to_exponent, float cap) {
-  return fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + exp2_(x * to_exponent)), cap);
+// Scores capped by a tanh, from products x to log2 units: cap tanh(y) log2(e), y = x scale / cap.
+// |y| <= 0.36, where scores lie in earnest: y P(y^2), P of degree 3 (least squares reweighted to even out its relative error,
+// 5e-8 at most): a polynomial in x^2, five instructions, exact to a few 2^-24 of the score itself.
+// Beyond: cap - 2 cap / (1 + e^(2y)): two transcendental instructions, absolute error about 2^-23 cap (too much for small
+// scores), right at both ends (e^... = inf or 0).
+struct Cap {
+  float c0, c1, c2, c3;  // coefficients in x^2
+  float limit;           // of |x|
+  float to_exponent;     // 2 log2(e) scale / cap
+  float cap;             // in log2 units; 0: none
+};
+inline Cap make_cap(double scale, double cap) {
+  Cap c = {0, 0, 0, 0, 0, 0, 0};
+  if (cap > 0) {
+    const double f = scale * 1.4426950408889634, k = scale / cap, k2 = k * k;
+    c.c0 = (float)f;
+    c.c1 = (float)(-0.33332544 * f * k2);
+    c.c2 = (float)(0.13296013 * f * k2 * k2);
+    c.c3 = (float)(-0.04888798 * f * k2 * k2 * k2);
+    c.limit = (float)(0.36 / k);
+    c.to_exponent = (float)(2.0 * 1.4426950408889634 * k);
+    c.cap = (float)(cap * 1.4426950408889634);
+  }
+  return c;
+}
+// Whether scale and cap leave factors that fp32 holds.
+inline bool finite_factors(double scale, double cap) {
+  const Cap c = make_cap(scale, cap);
+  const float f[7] = {c.c0, c.c1, c.c2, c.c3, c.limit, c.to_exponent, c.cap};
+  for (int i = 0; i < 7; ++i)
+    if (!(f[i] - f[i] == 0.0f)) return false;
+  const float s = (float)(scale * 1.4426950408889634);
+  return s - s == 0.0f;
+}
+__device__ __forceinline__ float capped_small(float x, const Cap& c) {
+  const float x2 = x * x;
+  return x * fmaf(fmaf(fmaf(c.c3, x2, c.c2), x2, c.c1), x2, c.c0);
+}
+__device__ __forceinline__ float capped_any(float x, const Cap& c) {
+  const float far = fmaf(-2.0f * c.cap, __builtin_amdgcn_rcpf(1.0f + exp2_(x * c.to_exponent)), c.cap);
+  return fabsf(x) <= c.limit ? capped_small(x, c) : far;
+}
+// N scores of every lane; the second form only where some lane of the wave needs it.
+template <int N>
+__device__ __forceinline__ void cap_scores(float (&x)[N], const Cap& c) {
+  float most = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(x[i]));
+  if (__any(most > c.limit)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = capped_any(x[i], c);
+      __builtin_amdgcn_sched_barrier(0);  // (one after the other: this is rare, and registers are not)
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = capped_small(x[i], c);
+  }
 }
 
 }  // namespace

@@ -48,8 +48,8 @@ struct LongArgs {
   int32_t wave_groups;  // 16-head groups in a workgroup: 1, 2 or 4
   uint32_t page_magic;  // floor(2^32 / page_size)
   int64_t q_sb, q_sh, c_sb, c_sh, c_st, p_sb, p_sh;
-  float scale;          // of the products, to log2 units; with a cap 2 log2(e) scale / cap
-  float cap2;           // cap in log2 units (0: none)
+  float scale;          // of the products, to log2 units (without a cap)
+  Cap cap;
 };
 
 // A wave's reads and writes of its own part of LDS keep their order.
@@ -255,12 +255,17 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
         }
       }
       own_lds_order();
-      // scores in units of log2 (with a cap: in the exponent's of its tanh)
+      // scores in units of log2
+      if (__builtin_expect(a.cap.cap != 0.0f, 0)) {
+        float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] *= a.scale;
-      if (__builtin_expect(a.cap2 != 0.0f, 0)) {
+        for (int e = 0; e < 8; ++e) x[e] = sc[e >> 2][e & 3];
+        cap_scores(x, a.cap);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = capped(sc[e >> 2][e & 3], 1.0f, a.cap2);
+        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = x[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] *= a.scale;
       }
       if (__builtin_expect(a.slopes != nullptr, 0)) {
 #pragma unroll
@@ -459,11 +464,7 @@ hipError_t launch(const LongArgs& a, int64_t workgroups, hipStream_t s) {
   return hipGetLastError();
 }
 
-// What a product is multiplied by: see LongArgs::scale.
-float scale_of(const pkv_decode_long_desc& d) {
-  const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d);
-  return (float)(scale * 1.4426950408889634 * (d.cap > 0.0f ? 2.0 / d.cap : 1.0));
-}
+double scale_of(const pkv_decode_long_desc& d) { return d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d); }
 
 int check_long_desc(const pkv_decode_long_desc* desc) {
   if (!desc) return PKV_ERR_INVALID_ARG;
@@ -479,7 +480,7 @@ int check_long_desc(const pkv_decode_long_desc* desc) {
   }
   if (d.p_sb < 0 || d.p_sh < 0) return PKV_ERR_INVALID_ARG;
   if (d.d != 64 && d.d != 128) return PKV_ERR_UNSUPPORTED;
-  if (!isfinite(scale_of(d)) || !isfinite(d.cap * kLog2e)) return PKV_ERR_INVALID_ARG;
+  if (!finite_factors(scale_of(d), d.cap)) return PKV_ERR_INVALID_ARG;
   const int64_t G = d.Hq / d.Hkv;
   if (G > 128 || d.B > 65535 || d.k_cap > (1 << 30) || d.Hkv > 65535 || (int64_t)d.B * d.Hq > kMaxGrid) return PKV_ERR_UNSUPPORTED;
   if (d.page_size == 0 && d.c_st > (1 << 30)) return PKV_ERR_UNSUPPORTED;  // (a row's bytes: 32 bits)
@@ -533,8 +534,8 @@ int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q, c
   a.wave_groups = heads_of(a.G) / 16;
   a.page_magic = d.page_size > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint32_t)d.page_size) : 0xFFFFFFFFu;
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.c_sb = d.c_sb; a.c_sh = d.c_sh; a.c_st = d.c_st; a.p_sb = d.p_sb; a.p_sh = d.p_sh;
-  a.scale = scale_of(d);
-  a.cap2 = d.cap * kLog2e;
+  a.scale = (float)(scale_of(d) * 1.4426950408889634);
+  a.cap = make_cap(scale_of(d), d.cap);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (d.dtype == PKV_BF16)

@@ -45,8 +45,8 @@ struct PrefillArgs {
   float* part_mz;  // [B * Hkv][T * G][S][2]
   int32_t B, Hq, Hkv, G, T, N, window, S, tiles;
   int64_t q_sb, q_sh, q_st, kv_sb, kv_sh, kv_st, o_sb, o_sh, o_st;
-  float scale;               // of the products, to log2 units (without a cap)
-  float cap2, two_over_cap;  // cap in log2 units (0: none); 2 log2(e) scale / cap
+  float scale;  // of the products, to log2 units (without a cap)
+  Cap cap;
 };
 
 // What the masks leave a query row: keys lo .. hi (none: lo > hi).
@@ -255,9 +255,13 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
       sc = Elem<T>::mfma32(kf, qf[i], i == 0 ? (f32x16)(0.0f) : sc);
     }
     if constexpr (MODE == 1) {
-      if (a.cap2 != 0.0f) {
+      if (a.cap.cap != 0.0f) {
+        float x[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] = capped(sc[e], a.two_over_cap, a.cap2);
+        for (int e = 0; e < 16; ++e) x[e] = sc[e];
+        cap_scores(x, a.cap);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = x[e];
       } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[e] *= a.scale;
@@ -425,7 +429,7 @@ __global__ __launch_bounds__(256) void prefill_join_kernel(const PrefillArgs a) 
 template <typename T, int D>
 hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.tiles * a.S * a.B * a.Hkv)), block(256);
-  if (a.cap2 != 0.0f || a.slopes)
+  if (a.cap.cap != 0.0f || a.slopes)
     hipLaunchKernelGGL((prefill_kernel<T, D, 1>), grid, block, 0, s, a);
   else
     hipLaunchKernelGGL((prefill_kernel<T, D, 0>), grid, block, 0, s, a);
@@ -466,8 +470,6 @@ int parts(const pkv_prefill_desc& d) {
 }
 
 double scale_of(const pkv_prefill_desc& d) { return d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d); }
-// Of a product, in the exponent's of the cap's tanh.
-float cap_factor(const pkv_prefill_desc& d) { return d.cap > 0.0f ? (float)(2.0 * 1.4426950408889634 * scale_of(d) / d.cap) : 0.0f; }
 
 int check_prefill_desc(const pkv_prefill_desc* desc) {
   if (!desc) return PKV_ERR_INVALID_ARG;
@@ -478,7 +480,7 @@ int check_prefill_desc(const pkv_prefill_desc* desc) {
   if (!good_strides(d.q_sb, d.q_sh, d.q_st) || !good_strides(d.kv_sb, d.kv_sh, d.kv_st) || !good_strides(d.o_sb, d.o_sh, d.o_st))
     return PKV_ERR_INVALID_ARG;
   if (d.d != 64 && d.d != 128) return PKV_ERR_UNSUPPORTED;
-  if (!isfinite(cap_factor(d)) || !isfinite((float)(scale_of(d) * kLog2e)) || !isfinite(d.cap * kLog2e)) return PKV_ERR_INVALID_ARG;
+  if (!finite_factors(scale_of(d), d.cap)) return PKV_ERR_INVALID_ARG;
   if (d.Hq / d.Hkv > 128 || d.B > 65535 || d.N > (1 << 30) || d.T > (1 << 30)) return PKV_ERR_UNSUPPORTED;
   if ((int64_t)d.T * (d.Hq / d.Hkv) > 0x7FFFFF00ll) return PKV_ERR_UNSUPPORTED;
   if (d.kv_st > (1 << 23)) return PKV_ERR_UNSUPPORTED;  // (offsets inside a step: 32 bits)
@@ -527,8 +529,7 @@ int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q, const voi
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.q_st = d.q_st; a.kv_sb = d.kv_sb; a.kv_sh = d.kv_sh; a.kv_st = d.kv_st;
   a.o_sb = d.o_sb; a.o_sh = d.o_sh; a.o_st = d.o_st;
   a.scale = (float)(scale_of(d) * 1.4426950408889634);
-  a.cap2 = d.cap * kLog2e;
-  a.two_over_cap = cap_factor(d);
+  a.cap = make_cap(scale_of(d), d.cap);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (d.dtype == PKV_BF16)

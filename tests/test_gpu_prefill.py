@@ -190,3 +190,13 @@ def test_a_long_prompt(window):
     out, lse = binding.prefill_attention(q, K, V, window=window, want_lse=True)
     torch.cuda.synchronize()
     _compare(out, lse, q, K, V, window=window, heads=[0, 3])
+
+
+@pytest.mark.parametrize("cap,scale", [(2.0, None), (50.0, None), (5.0, 1.0), (1e-3, None), (1e6, None)])
+def test_caps_near_and_far_from_the_scores(cap, scale):
+    # scores far below the cap, at it and far beyond; few keys, so that the log-sum-exp is as small as the scores
+    for T in (3, 130):
+        q, K, V, _ = _make(1, 4, 2, 64, T, T, torch.float16, 21)
+        out, lse = binding.prefill_attention(q, K, V, cap=cap, scale=scale, want_lse=True)
+        torch.cuda.synchronize()
+        _compare(out, lse, q, K, V, cap=cap, scale=scale)
