@@ -1,6 +1,8 @@
 // Attention of a prompt over its keys (include/pkv.h: pkv_prefill_attention).
 //
-// Matrix-bound: 4 d products-and-sums per (query row, seen key), for which K and V come from LDS.
+// Bound by power: 4 d products-and-sums per (query row, seen key), for which K and V come from LDS, and an exponential.  A 32k
+// prompt (32 / 8 heads, d 128) takes 7.8 - 8.0 ms, 1.10 - 1.13 PFLOP/s of what it sees; the clock sinks to 1.6 - 1.7 GHz, at
+// which the matrix pipe is busy for 64 % of the cycles.  Forms that need fewer or more cycles took the same time within 3 %.
 // Work split: the G T query rows of a KV head (row = token * G + head, so that a tile of rows covers few tokens and hardly more
 // keys than its rows see) in tiles of 128, a workgroup of four waves each, 32 rows a wave; the longest tiles first.  Workgroups
 // that follow one another take different KV heads: with eight of them each XCD's cache holds the keys of one.  Few rows: the
@@ -8,7 +10,8 @@
 //   keys    32 at a time, K and V straight from memory into LDS, double-buffered: the next step's are requested when a step
 //           begins, one barrier per step.  With 32 keys three workgroups share a compute unit (168 registers), with 64 two: the
 //           third is worth more than half the barriers (32k prompt 8.00 against 8.20 ms, 300 rows of 50k keys 0.34 against 0.36).
-//           16-byte pieces of a row are swapped (through the lanes' addresses in memory) so that
+//           64 rows a wave halve what is read from LDS, but leave one wave per SIMD: 9.1 ms, and 9.3 with the next step's scores
+//           formed beside the softmax.  16-byte pieces of a row are swapped (through the lanes' addresses in memory) so that
 //           neither way of reading them meets the same bank twice.
 //   scores  S^T = K Q^T in v_mfma_f32_32x32x16: a lane ends with 16 keys of one query row (column), the other half of the wave
 //           with the other 16, so that maxima and sums stay in the lane.
@@ -437,7 +440,7 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
   if (e != hipSuccess || a.S == 1) return e;
   const int64_t rows = (int64_t)a.T * a.G * a.B * a.Hkv;
   constexpr int PER = 256 / (D / 4);  // rows of a workgroup with one share
-  if (a.S <= 4)
+  if (a.S <= 16)  // (8400 rows of 11 ranges: 11.8 us, with eight shares 20.8)
     hipLaunchKernelGGL((prefill_join_kernel<T, D, 1>), dim3((unsigned)((rows + PER - 1) / PER)), block, 0, s, a);
   else
     hipLaunchKernelGGL((prefill_join_kernel<T, D, 8>), dim3((unsigned)((rows + PER / 8 - 1) / (PER / 8))), block, 0, s, a);
