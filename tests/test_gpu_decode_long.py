@@ -204,3 +204,25 @@ def test_dimensions_of_one_element_may_have_any_stride():
     out4, _ = binding.prefill_attention(q[:, :, None], K, V)
     torch.cuda.synchronize()
     assert torch.equal(out4[:, :, 0], V[:, :, 0])
+
+
+def test_two_calls_at_once_and_shared_pages():
+    # two calls on two streams, each with its own workspace; sequences whose tables name the same pages (a shared beginning)
+    B, Hq, Hkv, d, k_cap, page = 4, 32, 8, 128, 5000, 16
+    q, K, V, Kc, Vc, table = _make(B, Hq, Hkv, d, k_cap, torch.bfloat16, page, 31)
+    shared = 2000 // page
+    table[1:, :shared] = table[0, :shared]
+    K[1:, :, :shared * page], V[1:, :, :shared * page] = K[0, :, :shared * page], V[0, :, :shared * page]
+    count = torch.tensor([5000, 4000, 2001, 1999], dtype=torch.int32, device=DEV)
+    ws = [torch.empty(1 << 25, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for rep in range(8):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i] = binding.decode_attention_long(q, Kc, Vc, count, block_table=table, k_cap=k_cap, workspace=ws[i], want_lse=True,
+                                                       window=300 * i)
+    torch.cuda.synchronize()
+    _compare(*got[0], q, K, V, count, torch.bfloat16)
+    _compare(*got[1], q, K, V, count, torch.bfloat16, window=300)

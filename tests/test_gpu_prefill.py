@@ -200,3 +200,38 @@ def test_caps_near_and_far_from_the_scores(cap, scale):
         out, lse = binding.prefill_attention(q, K, V, cap=cap, scale=scale, want_lse=True)
         torch.cuda.synchronize()
         _compare(out, lse, q, K, V, cap=cap, scale=scale)
+
+
+def test_more_query_rows_than_keys_and_two_calls_at_once():
+    B, Hq, Hkv, d, T, N = 2, 4, 2, 64, 300, 70
+    q, K, V, _ = _make(B, Hq, Hkv, d, T, N, torch.bfloat16, 17)
+    lens, start = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in ([70, 33], [-100, 0]))
+    out, lse = binding.prefill_attention(q, K, V, seq_lens=lens, q_start=start, want_lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, q, K, V, lens, start)
+    q, K, V, _ = _make(1, 8, 2, 128, 60, 9000, torch.float16, 18)
+    start = torch.tensor([8900], dtype=torch.int32, device=DEV)
+    ws = [torch.empty(1 << 25, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for rep in range(6):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i] = binding.prefill_attention(q, K, V, q_start=start, window=1000 * i, want_lse=True, workspace=ws[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        _compare(*got[i], q, K, V, start=start, window=1000 * i)
+
+
+def test_values_of_every_size_and_masked_rows_of_the_lowest_value():
+    # scores over the whole range of the type, some keys at its lowest value: rows whose scores are all far below zero
+    T, d = 96, 64
+    q, K, V, g = _make(1, 2, 1, d, T, T, torch.float16, 19)
+    q[0, 0] *= 30
+    K[0, 0, 40:60] = torch.finfo(torch.float16).min
+    q[0, 1] = q[0, 1].abs()                                   # its scores with those keys: about -4e5 each
+    V[0, 0, ::7] *= 1000
+    out, lse = binding.prefill_attention(q, K, V, want_lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, q, K, V)
