@@ -32,7 +32,6 @@ constexpr int kWaves = 4;          // per workgroup
 constexpr int kWorkgroups = 512;   // at a time on the device: two per compute unit
 constexpr int kFlatBatch = 64;     // sequences, at most, whose ranges go by their lengths
 constexpr int kLeastTiles = 8;     // of a range
-constexpr int kMaxRanges = 1024;   // of a sequence and KV head
 
 struct LongArgs {
   const uint16_t *q, *K, *V;
@@ -381,12 +380,12 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
   }
 }
 
-// One workgroup per (sequence, query head): the ranges' results, every PARTS-th of them by one part of the threads, in order.
+// One workgroup per (sequence, query head): the ranges' results, every PARTS-th of them by one part of the threads, in order, each
+// with a running maximum of its own (so that a range's exponent and its values are requested together), then the parts.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void decode_long_join_kernel(const LongArgs a) {
   constexpr int PARTS = 256 / (D / 4);
-  __shared__ float lds_w[kMaxRanges];
-  __shared__ float lds_red[8];
+  __shared__ float lds_m[PARTS], lds_z[PARTS];
   __shared__ f32x4 lds_o[PARTS][D / 4];
   const int64_t row = blockIdx.x;
   const int b = (int)(row / a.Hq), h = (int)(row % a.Hq), g = h / a.G, h_in = h % a.G, unit = g * a.head_groups + h_in / 64;
@@ -400,39 +399,36 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const LongArgs a)
   }
   if (ranges == 1) return;  // (written already)
   const int64_t heads = 16 * a.wave_groups, at = ((int64_t)base + unit * ranges) * heads + h_in % 64;
-  const float* const mz = a.part_mz + at * 2;
-  float top = kNone;
-  for (int i = threadIdx.x; i < ranges; i += 256) top = fmaxf(top, mz[2 * heads * i]);
-  for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-  if ((threadIdx.x & 63) == 0) lds_red[threadIdx.x >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(lds_red[0], lds_red[1]), fmaxf(lds_red[2], lds_red[3]));
-  const float ref = top == kNone ? 0.0f : top;
-  float sum = 0.0f;
-  for (int i = threadIdx.x; i < ranges; i += 256) {
-    const float f = exp2_(mz[2 * heads * i] - ref);
-    lds_w[i] = f;
-    sum += f * mz[2 * heads * i + 1];
-  }
-  for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
-  if ((threadIdx.x & 63) == 0) lds_red[4 + (threadIdx.x >> 6)] = sum;
-  __syncthreads();
-  sum = (lds_red[4] + lds_red[5]) + (lds_red[6] + lds_red[7]);
   const int d4 = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
+  float m = kNone, z = 0.0f;
   f32x4 acc = (f32x4)(0.0f);
-#pragma unroll 8
-  for (int i = part; i < ranges; i += PARTS) acc += lds_w[i] * *reinterpret_cast<const f32x4*>(a.part_o + (at + heads * i) * D + 4 * d4);
-  lds_o[part][d4] = acc;
-  __syncthreads();
-  if (part == 0) {
-    for (int i = 1; i < PARTS; ++i) acc += lds_o[i][d4];
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    u32x2 w;
-    w[0] = pack2<T>(acc[0] * inv, acc[1] * inv);
-    w[1] = pack2<T>(acc[2] * inv, acc[3] * inv);
-    *reinterpret_cast<u32x2*>(a.out + row * D + 4 * d4) = w;
-    if (d4 == 0 && a.lse) a.lse[row] = sum == 0.0f ? kNone : (top + log2_(sum)) * kLn2;
+  auto join = [&](float m1, float z1, f32x4 v) {
+    const float top = fmaxf(m, m1), ref = top == kNone ? 0.0f : top;
+    const float f0 = exp2_(m - ref), f1 = exp2_(m1 - ref);
+    m = top;
+    z = z * f0 + z1 * f1;
+    acc = acc * f0 + v * f1;
+  };
+#pragma unroll 4
+  for (int i = part; i < ranges; i += PARTS) {
+    const float* const mz = a.part_mz + (at + heads * i) * 2;
+    join(mz[0], mz[1], *reinterpret_cast<const f32x4*>(a.part_o + (at + heads * i) * D + 4 * d4));
   }
+  lds_o[part][d4] = acc;
+  if (d4 == 0) {
+    lds_m[part] = m;
+    lds_z[part] = z;
+  }
+  __syncthreads();
+  if (part != 0) return;
+#pragma unroll
+  for (int i = 1; i < PARTS; ++i) join(lds_m[i], lds_z[i], lds_o[i][d4]);
+  const float inv = z == 0.0f ? 0.0f : 1.0f / z;
+  u32x2 w;
+  w[0] = pack2<T>(acc[0] * inv, acc[1] * inv);
+  w[1] = pack2<T>(acc[2] * inv, acc[3] * inv);
+  *reinterpret_cast<u32x2*>(a.out + row * D + 4 * d4) = w;
+  if (d4 == 0 && a.lse) a.lse[row] = z == 0.0f ? kNone : (m + log2_(z)) * kLn2;
 }
 
 // Query heads that a workgroup's results have room for.
