@@ -224,6 +224,7 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
   for (int i = 0; i < MT; ++i) o[i] = (f32x4)(0.0f);
 
   if (t < t_end) {
+    const int t_first = t;
     look(t);
     resolve(t);
     place();
@@ -331,6 +332,39 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
         o[mt] = Elem<T>::mfma16(vf, lo, o[mt]);
       }
       own_lds_order();
+    }
+    // A value that is not finite in a seen row: its column is what the sum of those is (every weight is positive), and not what
+    // 0 or less, where a weight's second part is that, makes of an infinity.
+    bool odd = false;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd = odd || !(fabsf(o[mt][e]) < __builtin_inff());
+    if (__builtin_expect(__any(odd), 0)) {
+      f32x4 extra[MT];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) extra[mt] = (f32x4)(0.0f);
+      const char* const Vq = reinterpret_cast<const char*>(a.V) + base + 8 * quad;
+      for (t = t_first; t < t_end; t += shares) {
+        look(t);
+        resolve(t);
+        for (uint32_t left = seen; left != 0; left &= left - 1) {
+          const char* const row = Vq + (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, __builtin_ctz(left)) * row_bytes;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            const u32x2 v = *reinterpret_cast<const u32x2*>(row + 32 * mt);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float x = unpack<T>(v[e >> 1], e & 1);
+              extra[mt][e] += fabsf(x) < __builtin_inff() ? 0.0f : x;
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[mt][e] = extra[mt][e] == 0.0f ? o[mt][e] : extra[mt][e];
     }
   }
 

@@ -226,3 +226,31 @@ def test_two_calls_at_once_and_shared_pages():
     torch.cuda.synchronize()
     _compare(*got[0], q, K, V, count, torch.bfloat16)
     _compare(*got[1], q, K, V, count, torch.bfloat16, window=300)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("B,Hq,Hkv,d,k_cap,page", [(1, 8, 2, 128, 40, 0), (2, 6, 1, 64, 2000, 16), (1, 33, 1, 128, 1500, 0)])
+def test_values_that_are_not_finite_in_seen_rows(B, Hq, Hkv, d, k_cap, page, dtype):
+    # their columns are as a sum with positive weights has them, the others untouched
+    print("not finite", B, Hq, Hkv, d, k_cap, page, dtype, flush=True)
+    q, K, V, _, _, _ = _make(B, Hq, Hkv, d, k_cap, dtype, 0, 17)
+    j = [k_cap - 1, k_cap // 2, 3, 20]
+    V[0, 0, j[0], 0], V[0, 0, j[1], d - 1], V[0, 0, j[2], 9] = math.inf, -math.inf, math.nan
+    V[0, 0, j[2], 33], V[0, 0, j[3], 33] = math.inf, -math.inf
+    V[-1, -1, j[3], 40] = V[-1, -1, j[1], 40] = math.inf
+    Kc, Vc, table = K, V, None
+    if page:
+        per = -(-k_cap // page)
+        table = torch.arange(B * per, dtype=torch.int32, device=DEV).flip(0).view(B, per).contiguous()
+        Kc, Vc = (torch.zeros(B * per, Hkv, page, d, dtype=dtype, device=DEV) for _ in range(2))
+        rows = torch.arange(k_cap, device=DEV)
+        for b in range(B):
+            at = table[b].long()[rows // page]
+            Kc[at, :, rows % page], Vc[at, :, rows % page] = K[b].transpose(0, 1), V[b].transpose(0, 1)
+    count = torch.full((B,), k_cap, dtype=torch.int32, device=DEV)
+    out, lse = binding.decode_attention_long(q, Kc, Vc, count, block_table=table, k_cap=k_cap, want_lse=True)
+    torch.cuda.synchronize()
+    odd = (~torch.isfinite(V)).any(2).repeat_interleave(Hq // Hkv, 1)                     # [B, Hq, d]
+    want = V.double().masked_fill(torch.isfinite(V), 0).sum(2).repeat_interleave(Hq // Hkv, 1)
+    assert torch.equal(out.double()[odd].nan_to_num(7, 8, 9), want[odd].nan_to_num(7, 8, 9))
+    _compare(out.masked_fill(odd, 0), lse, q, K, V.masked_fill((~torch.isfinite(V)).any(2, keepdim=True), 0), count, dtype)
