@@ -254,3 +254,37 @@ def test_values_that_are_not_finite_in_seen_rows(B, Hq, Hkv, d, k_cap, page, dty
     want = V.double().masked_fill(torch.isfinite(V), 0).sum(2).repeat_interleave(Hq // Hkv, 1)
     assert torch.equal(out.double()[odd].nan_to_num(7, 8, 9), want[odd].nan_to_num(7, 8, 9))
     _compare(out.masked_fill(odd, 0), lse, q, K, V.masked_fill((~torch.isfinite(V)).any(2, keepdim=True), 0), count, dtype)
+
+
+@pytest.mark.parametrize("B,Hkv,G,d,k_cap,page,longest", [(130, 8, 1, 64, 9000, 16, 9000), (256, 1, 4, 64, 6000, 0, 5999), (66, 1, 2, 128, 20000, 48, 20000),
+                                                        (64, 32, 1, 64, 5000, 16, 5000), (34, 32, 2, 64, 4097, 0, 4097), (257, 2, 1, 64, 3000, 16, 3000)])
+def test_one_long_sequence_among_many_short_ones(B, Hkv, G, d, k_cap, page, longest):
+    print("one long", B, Hkv, G, d, k_cap, page, longest, flush=True)
+    g = torch.Generator().manual_seed(B)
+    count = torch.randint(0, 90, (B,), generator=g).to(torch.int32)
+    count[[1, B // 2, B - 1]] = torch.tensor([700, longest, 33], dtype=torch.int32)
+    count[::7] = 0
+    count[B // 2] = longest
+    gd = torch.Generator(device=DEV).manual_seed(B)
+    q = torch.randn(B, Hkv * G, d, generator=gd, device=DEV).to(torch.bfloat16)
+    rows = int(count.sum()) + B * max(page, 1)
+    step = max(page, 1)
+    K, V = (torch.randn(rows // step + 1, Hkv, step, d, generator=gd, device=DEV).to(torch.bfloat16) for _ in range(2))
+    if page:
+        need = -(-count // page)
+        table = torch.full((B, -(-k_cap // page)), -1, dtype=torch.int32)
+        at = 0
+        for b in range(B):
+            table[b, :int(need[b])] = torch.arange(at, at + int(need[b]), dtype=torch.int32)
+            at += int(need[b])
+        table = table.to(DEV)
+        out, lse = binding.decode_attention_long(q, K, V, count.to(DEV), block_table=table, k_cap=k_cap, want_lse=True)
+        per = lambda x, b: x[table[b, :max(1, int(need[b]))].clamp(0).long()].transpose(0, 1).reshape(Hkv, -1, d)
+    else:
+        Kc, Vc = (torch.randn(1, Hkv, k_cap, d, generator=gd, device=DEV).to(torch.bfloat16).expand(B, Hkv, k_cap, d) for _ in range(2))
+        out, lse = binding.decode_attention_long(q, Kc, Vc, count.to(DEV), want_lse=True)
+        per = lambda x, b: x[b]
+        K, V = Kc, Vc
+    torch.cuda.synchronize()
+    for b in list(range(0, B, 5)) + [1, B // 2, B - 1]:
+        _compare(out[b:b + 1], lse[b:b + 1], q[b:b + 1], per(K, b)[None], per(V, b)[None], count[b:b + 1], torch.bfloat16)
