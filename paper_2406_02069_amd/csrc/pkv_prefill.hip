@@ -127,9 +127,13 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int units = a.B * a.Hkv;
-  const int unit = blockIdx.x % units, rest = blockIdx.x / units;
+  const int rest = blockIdx.x / units;
   const int part = rest % a.S, tile = a.tiles - 1 - rest / a.S;
-  const int b = unit / a.Hkv, g = unit % a.Hkv;
+  // Sequences take turns: where a few are long, workgroups at a fixed distance would be, which go to the same part of a die (2048
+  // rows of 60k keys beside three short sequences 5.1 ms, with turns 2.3).
+  const unsigned turn = rest + (rest >> 1) + (rest >> 2) + (rest >> 3);
+  const int b = (int)((blockIdx.x % units / a.Hkv + turn) % (unsigned)a.B), g = blockIdx.x % a.Hkv;
+  const int unit = b * a.Hkv + g;
   const int n = a.seq_lens ? min(max(a.seq_lens[b], 0), a.N) : a.N;
 
   const int64_t rows = (int64_t)a.T * a.G;
