@@ -602,8 +602,8 @@ typedef struct {
 
 /*
  * Bytes of DEVICE workspace pkv_prefill_attention needs for this shape (0
- * where the query rows alone fill the device; 0 as well if the descriptor is
- * invalid).  HOST only, pure.
+ * where one sequence's query rows fill the device, and for short ones; 0 as
+ * well if the descriptor is invalid).  HOST only, pure.
  */
 size_t pkv_prefill_workspace_bytes(const pkv_prefill_desc* desc);
 

@@ -64,6 +64,20 @@ __device__ __forceinline__ u32x2 read_columns(const char* lds) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds)));
 }
 
+// Sum over the wave, up to and including the own lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_from(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int sum_upto(int x) {
+  x = add_from<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8: within rows of 16
+  x = add_from<0x112, 0xF>(x);
+  x = add_from<0x114, 0xF>(x);
+  x = add_from<0x118, 0xF>(x);
+  x = add_from<0x142, 0xA>(x);  // the rows' sums: row_bcast 15 into rows 1 and 3, row_bcast 31 into rows 2 and 3
+  return add_from<0x143, 0xC>(x);
+}
+
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 

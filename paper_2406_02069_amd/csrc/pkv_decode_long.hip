@@ -78,20 +78,6 @@ __device__ __forceinline__ Tiles tiles_of(const LongArgs& a, int b) {
   return r;
 }
 
-// Sum over the wave, up to and including the own lane.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int add_from(int x) {
-  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
-}
-__device__ __forceinline__ int sum_upto(int x) {
-  x = add_from<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8: within rows of 16
-  x = add_from<0x112, 0xF>(x);
-  x = add_from<0x114, 0xF>(x);
-  x = add_from<0x118, 0xF>(x);
-  x = add_from<0x142, 0xA>(x);  // the rows' sums: row_bcast 15 into rows 1 and 3, row_bcast 31 into rows 2 and 3
-  return add_from<0x143, 0xC>(x);
-}
-
 // How the sequences are cut, for 2 .. 64 E of them: lane i looks after sequences i E .. i E + E - 1, whose numbers of ranges and
 // first workgroup it works out; all ranges but a sequence's last have `per` tiles.  Ranges as long as make `ranges` workgroups of
 // all tiles, then, of one turn of the device, longer (a few tries) until the last, shorter ones of the sequences fit among them

@@ -6,7 +6,8 @@
 // Work split: the G T query rows of a KV head (row = token * G + head, so that a tile of rows covers few tokens and hardly more
 // keys than its rows see) in tiles of 128, a workgroup of four waves each, 32 rows a wave; the longest tiles first.  Workgroups
 // that follow one another take different KV heads: with eight of them each XCD's cache holds the keys of one.  Few rows: the
-// keys of a tile are cut into S ranges, whose un-normalised results a second kernel joins in order.
+// keys of a tile are cut into S ranges, whose un-normalised results a second kernel joins in order; with ragged sequences S and a
+// workgroup's place go by their lengths, worked out by every wave from all of them.
 //   keys    32 at a time, K and V straight from memory into LDS, double-buffered: the next step's are requested when a step
 //           begins, one barrier per step.  With 32 keys three workgroups share a compute unit (168 registers), with 64 two: the
 //           third is worth more than half the barriers (32k prompt 8.00 against 8.20 ms, 300 rows of 50k keys 0.34 against 0.36).
@@ -37,6 +38,7 @@ namespace {
 constexpr int kRows = 128;   // query rows of a workgroup
 constexpr int kKeys = 32;    // keys per step
 constexpr int kMaxParts = 64;  // ranges of keys
+constexpr int kLeastKeys = 768;  // of a range, about
 
 struct PrefillArgs {
   const uint16_t *q, *K, *V;
@@ -44,9 +46,11 @@ struct PrefillArgs {
   const float* slopes;
   uint16_t* out;
   float* lse;
-  float* part_o;   // [B * Hkv][T * G][S][d]
-  float* part_mz;  // [B * Hkv][T * G][S][2]
+  float* part_o;   // [B * Hkv][T * G][S][d]; by length: [slot][128][d], a slot for each workgroup of a tile in several ranges
+  float* part_mz;  // the same with 2 instead of d: reference exponent (log2) and sum
   int32_t B, Hq, Hkv, G, T, N, window, S, tiles;
+  int32_t by_length;  // 2 .. 64 ragged sequences: ranges and places by their lengths, in up to so many workgroups
+  int32_t most_parts, most_slots, turn;  // then: ranges of a tile, slots, workgroups that the device holds at a time
   int64_t q_sb, q_sh, q_st, kv_sb, kv_sh, kv_st, o_sb, o_sh, o_st;
   float scale;  // of the products, to log2 units (without a cap)
   Cap cap;
@@ -78,6 +82,58 @@ __device__ __forceinline__ Seen seen_keys(const PrefillArgs& a, int b, int t, in
 __device__ __forceinline__ int wave_max(int x) {
   for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
   return __builtin_amdgcn_readfirstlane(x);
+}
+
+// The sequences' shares of a call by their lengths, lane b's for sequence b: its tiles first .. first + act - 1 have rows that are
+// there, each in S ranges of keys; its workgroups, slots and tiles in several ranges go before `end`, `slots` and `cut`.
+// Ranges are as long as make one turn of the device of all work where the tiles alone are half of one at most, else two turns.
+struct Shares {
+  int first, act, S;
+  int all, slots, cut;     // own numbers
+  int all_upto, slots_upto, cut_upto;
+};
+__device__ __forceinline__ int last_of(int upto) { return __builtin_amdgcn_readlane(upto, 63); }
+__device__ __forceinline__ Shares shares_of(const PrefillArgs& a, int lane) {
+#pragma clang fp contract(off)  // (the join has to come to the same numbers)
+  Shares s = {0, 0, 1, 0, 0, 0, 0, 0, 0};
+  const int b = min(lane, a.B - 1);
+  const int n = a.seq_lens ? min(max(a.seq_lens[b], 0), a.N) : a.N;
+  const int64_t start = a.q_start ? a.q_start[b] : 0;
+  const int t0 = (int)min(max(-start, (int64_t)0), (int64_t)a.T), t1 = (int)min(max(n - start, (int64_t)t0), (int64_t)a.T);
+  float steps = 0.0f;  // of a tile, in the mean (an estimate: documents are not looked at)
+  int most = 1;
+  if (t1 > t0 && lane < a.B) {
+    s.first = t0 * a.G / kRows;
+    s.act = (t1 * a.G + kRows - 1) / kRows - s.first;
+    int lo = (int)(start + t0) + 1, hi = (int)(start + t1);
+    if (a.prefix_end) lo = hi = n;
+    else if (a.window) {
+      const int span = a.window < a.N ? a.window + kRows / a.G : a.N;
+      lo = min(lo, span);
+      hi = min(hi, span);
+    }
+    steps = (float)(((int64_t)lo + hi) / 2 / kKeys + 1);
+    most = max(1, min(a.most_parts, hi / kLeastKeys));
+  }
+  float work = (float)s.act * steps;
+  for (int o = 32; o > 0; o >>= 1) work += __shfl_xor(work, o);
+  const int active = last_of(sum_upto(s.act * a.Hkv));
+  const bool fit = active <= a.turn / 2;
+  float per = fmaxf(work * (float)a.Hkv / (float)(fit ? a.turn : 2 * a.turn), 1.0f);
+  for (int tries = 0;; ++tries) {
+    s.S = min(most, (int)ceilf(steps / per));
+    s.S = max(s.S, 1);
+    s.all = lane < a.B ? (a.tiles + s.act * (s.S - 1)) * a.Hkv : 0;
+    s.cut = s.S > 1 ? s.act * a.Hkv : 0;
+    s.slots = s.cut * s.S;
+    s.all_upto = sum_upto(s.all);
+    s.slots_upto = sum_upto(s.slots);
+    const bool room = last_of(s.all_upto) <= a.by_length && last_of(s.slots_upto) <= a.most_slots;  // (S = 1 has room)
+    if (room && (!fit || tries >= 6 || last_of(sum_upto(s.act * s.S * a.Hkv)) <= a.turn)) break;
+    per *= room ? 1.0625f : 1.5f;
+  }
+  s.cut_upto = sum_upto(s.cut);
+  return s;
 }
 
 // 16 bytes per lane from base + at into LDS, lane after lane from byte `to` on.  Asynchronous: wait_loads.  (Written out because
@@ -122,24 +178,50 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
   constexpr int ROW = D * 2, BUF = kKeys * ROW;
   constexpr float SHIFT = sizeof(T) == 2 && __is_same(T, _Float16) ? 8.0f : 0.0f;  // fp16 weights: away from its subnormals
   __shared__ __align__(1024) char lds[4 * BUF];  // [buffer][K, V]
-  __shared__ int lds_range[4][4];
+  __shared__ int lds_range[4][4], lds_place[kRows][2];
   __shared__ uint32_t lds_bad[2][4];             // [buffer][wave]: rows of V (eight per wave) that hold a value that is not finite
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int units = a.B * a.Hkv;
-  const int rest = blockIdx.x / units;
-  const int part = rest % a.S, tile = a.tiles - 1 - rest / a.S;
-  // Sequences take turns: where a few are long, workgroups at a fixed distance would be, which go to the same part of a die (2048
-  // rows of 60k keys beside three short sequences 5.1 ms, with turns 2.3).
-  const unsigned turn = rest + (rest >> 1) + (rest >> 2) + (rest >> 3);
-  const int b = (int)((blockIdx.x % units / a.Hkv + turn) % (unsigned)a.B), g = blockIdx.x % a.Hkv;
-  const int unit = b * a.Hkv + g;
+  int b, g, tile, part, S, slot = 0;
+  if (a.by_length) {
+    const Shares sh = shares_of(a, lane);
+    const int at = (int)blockIdx.x;
+    const uint64_t mine = __ballot(at < sh.all_upto && at >= sh.all_upto - sh.all);
+    if (mine == 0) return;  // (no work left for this workgroup)
+    b = __builtin_ctzll(mine);
+    const int k = at - __builtin_amdgcn_readlane(sh.all_upto - sh.all, b), r = k / a.Hkv;
+    const int first = __builtin_amdgcn_readlane(sh.first, b), act = __builtin_amdgcn_readlane(sh.act, b);
+    g = k % a.Hkv;
+    S = __builtin_amdgcn_readlane(sh.S, b);
+    part = r % S;
+    tile = first + act - 1 - r / S;
+    if (r >= act * S) {  // the tiles behind and before those with rows
+      part = 0;
+      S = 1;
+      tile = first + act + (r - act * __builtin_amdgcn_readlane(sh.S, b));
+      if (tile >= a.tiles) tile -= a.tiles;
+    }
+    if (S > 1) slot = __builtin_amdgcn_readlane(sh.slots_upto - sh.slots, b) + k;
+  } else {
+    const int units = a.B * a.Hkv;
+    const int rest = blockIdx.x / units;
+    S = a.S;
+    part = rest % S;
+    tile = a.tiles - 1 - rest / S;
+    // Sequences take turns: where a few are long, workgroups at a fixed distance would be, which go to the same part of a die (2048
+    // rows of 60k keys beside three short sequences 5.1 ms, with turns 2.3).
+    const unsigned turn = rest + (rest >> 1) + (rest >> 2) + (rest >> 3);
+    b = (int)((blockIdx.x % units / a.Hkv + turn) % (unsigned)a.B);
+    g = blockIdx.x % a.Hkv;
+  }
   const int n = a.seq_lens ? min(max(a.seq_lens[b], 0), a.N) : a.N;
 
   const int64_t rows = (int64_t)a.T * a.G;
   const int64_t row = (int64_t)tile * kRows + 32 * wave + col;
   const bool there = row < rows;
   const int t = there ? (int)(row / a.G) : 0, h = g * a.G + (there ? (int)(row % a.G) : 0);
+  lds_place[32 * wave + col][0] = t;  // (both halves of the wave the same)
+  lds_place[32 * wave + col][1] = h;
   Seen seen = {1, 0, 0};
   if (there) seen = seen_keys(a, b, t, n);
   const bool some = seen.lo <= seen.hi;
@@ -167,8 +249,8 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
     step = first / kKeys;
     step_end = last / kKeys + 1;
   }
-  if (a.S > 1) {
-    const int per = (step_end - step + a.S - 1) / a.S;
+  if (S > 1) {
+    const int per = (step_end - step + S - 1) / S;
     const int s0 = step + part * per;
     step_end = min(step_end, s0 + per);
     step = min(s0, step_end);
@@ -355,11 +437,17 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
   }
 
   z += __shfl_xor(z, 32);
-  if (!there) return;
-  const int64_t out_row = ((int64_t)b * a.Hq + h) * a.T + t;
-  if (a.S > 1) {
-    const int64_t at = ((int64_t)unit * rows + row) * a.S + part;
-    float* po = a.part_o + at * D + 4 * half;
+  // (a row's place is not kept in registers, which are short in the loop)
+  int id = threadIdx.x;
+  asm("" : "+v"(id));
+  const int local = 32 * (id >> 6) + (id & 31), end_half = (id >> 5) & 1;
+  const uint32_t end_row = (uint32_t)tile * kRows + local;
+  if (end_row >= (uint32_t)rows) return;
+  const int t_out = lds_place[local][0], h_out = lds_place[local][1];
+  const int64_t out_row = ((int64_t)b * a.Hq + h_out) * a.T + t_out;
+  if (S > 1) {
+    const int64_t at = a.by_length ? (int64_t)slot * kRows + local : ((int64_t)(b * a.Hkv + g) * rows + end_row) * S + part;
+    float* po = a.part_o + at * D + 4 * end_half;
     if (!some) m = kNone, z = 0.0f;
 #pragma unroll
     for (int x = 0; x < MB * 4; ++x) {
@@ -368,7 +456,7 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
       for (int y = 0; y < 4; ++y) v[y] = some ? o[x >> 2][4 * (x & 3) + y] : 0.0f;
       *reinterpret_cast<f32x4*>(po + 8 * x) = v;
     }
-    if (half == 0) {
+    if (end_half == 0) {
       a.part_mz[at * 2] = m;
       a.part_mz[at * 2 + 1] = z;
     }
@@ -376,7 +464,7 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
   }
   const bool none = !some || z == 0.0f;
   const float inv = none ? 0.0f : 1.0f / z;
-  uint16_t* op = a.out + b * a.o_sb + h * a.o_sh + t * a.o_st + 4 * half;
+  uint16_t* op = a.out + b * a.o_sb + h_out * a.o_sh + t_out * a.o_st + 4 * end_half;
 #pragma unroll
   for (int x = 0; x < MB * 4; ++x) {
     u32x2 w;
@@ -384,7 +472,7 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
     w[1] = none ? 0 : pack2<T>(o[x >> 2][4 * (x & 3) + 2] * inv, o[x >> 2][4 * (x & 3) + 3] * inv);
     *reinterpret_cast<u32x2*>(op + 8 * x) = w;
   }
-  if (a.lse && half == 0) a.lse[out_row] = none ? kNone : (m - SHIFT + log2_(z)) * kLn2;
+  if (a.lse && end_half == 0) a.lse[out_row] = none ? kNone : (m - SHIFT + log2_(z)) * kLn2;
 }
 
 // The ranges' results of a query row, d / 4 x SHARES threads each: the shares take every SHARES-th range, in order, and are added
@@ -433,15 +521,73 @@ __global__ __launch_bounds__(256) void prefill_join_kernel(const PrefillArgs a) 
   if (d4 == 0 && a.lse) a.lse[((int64_t)b * a.Hq + h) * a.T + t] = sum == 0.0f ? kNone : (top - SHIFT + log2_(sum)) * kLn2;
 }
 
+// The same by length: a quarter of a tile in several ranges, four rows at a time for d / 4 threads, running maxima.
+constexpr int kJoinRows = 32;
+template <typename T, int D>
+__global__ __launch_bounds__(256) void prefill_join_by_length_kernel(const PrefillArgs a) {
+  constexpr int LANES = D / 4, GROUPS = 256 / LANES, R = kJoinRows / GROUPS;
+  constexpr float SHIFT = __is_same(T, _Float16) ? 8.0f : 0.0f;
+  const int at = (int)blockIdx.x / (kRows / kJoinRows);
+  const Shares sh = shares_of(a, threadIdx.x & 63);
+  const uint64_t mine = __ballot(at < sh.cut_upto && at >= sh.cut_upto - sh.cut);
+  if (mine == 0) return;
+  const int b = __builtin_ctzll(mine), S = __builtin_amdgcn_readlane(sh.S, b);
+  const int k = at - __builtin_amdgcn_readlane(sh.cut_upto - sh.cut, b), g = k % a.Hkv;
+  const int tile = __builtin_amdgcn_readlane(sh.first + sh.act, b) - 1 - k / a.Hkv;
+  const int slot = __builtin_amdgcn_readlane(sh.slots_upto - sh.slots, b) + k / a.Hkv * S * a.Hkv + g;
+  const int d4 = threadIdx.x % LANES, first = (int)(blockIdx.x % (kRows / kJoinRows)) * kJoinRows + threadIdx.x / LANES;
+  const int64_t rows = (int64_t)a.T * a.G, row0 = (int64_t)tile * kRows + first;
+  if (row0 >= rows) return;
+  float m[R], z[R];
+  f32x4 acc[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    m[i] = kNone;
+    z[i] = 0.0f;
+    acc[i] = (f32x4)(0.0f);
+  }
+#pragma unroll 2
+  for (int j = 0; j < S; ++j) {
+    const int64_t from = (int64_t)(slot + j * a.Hkv) * kRows + first;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int64_t r = row0 + i * GROUPS < rows ? from + i * GROUPS : from;  // (rows that are not there leave nothing)
+      const float m1 = a.part_mz[2 * r], z1 = a.part_mz[2 * r + 1];
+      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + r * D + 4 * d4);
+      const float top = fmaxf(m[i], m1), ref = top == kNone ? 0.0f : top;
+      const float f0 = exp2_(m[i] - ref), f1 = exp2_(m1 - ref);
+      m[i] = top;
+      z[i] = z[i] * f0 + z1 * f1;
+      acc[i] = acc[i] * f0 + v * f1;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int64_t row = row0 + i * GROUPS;
+    if (row >= rows) break;
+    const int t = (int)(row / a.G), h = g * a.G + (int)(row % a.G);
+    const float inv = z[i] == 0.0f ? 0.0f : 1.0f / z[i];
+    u32x2 w;
+    w[0] = pack2<T>(acc[i][0] * inv, acc[i][1] * inv);
+    w[1] = pack2<T>(acc[i][2] * inv, acc[i][3] * inv);
+    *reinterpret_cast<u32x2*>(a.out + b * a.o_sb + h * a.o_sh + t * a.o_st + 4 * d4) = w;
+    if (d4 == 0 && a.lse) a.lse[((int64_t)b * a.Hq + h) * a.T + t] = z[i] == 0.0f ? kNone : (m[i] - SHIFT + log2_(z[i])) * kLn2;
+  }
+}
+
 template <typename T, int D>
 hipError_t launch(const PrefillArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.tiles * a.S * a.B * a.Hkv)), block(256);
+  const dim3 grid((unsigned)(a.by_length ? a.by_length : (int64_t)a.tiles * a.S * a.B * a.Hkv)), block(256);
   if (a.cap.cap != 0.0f || a.slopes)
     hipLaunchKernelGGL((prefill_kernel<T, D, 1>), grid, block, 0, s, a);
   else
     hipLaunchKernelGGL((prefill_kernel<T, D, 0>), grid, block, 0, s, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.S == 1) return e;
+  if (e != hipSuccess || (!a.by_length && a.S == 1)) return e;
+  if (a.by_length) {  // (a tile in several ranges has two slots at least)
+    hipLaunchKernelGGL((prefill_join_by_length_kernel<T, D>), dim3((unsigned)(a.most_slots / 2 * (kRows / kJoinRows))), block, 0, s, a);
+    return hipGetLastError();
+  }
   const int64_t rows = (int64_t)a.T * a.G * a.B * a.Hkv;
   constexpr int PER = 256 / (D / 4);  // rows of a workgroup with one share
   if (a.S <= 16)  // (8400 rows of 11 ranges: 11.8 us, with eight shares 20.8)
@@ -453,15 +599,17 @@ hipError_t launch(const PrefillArgs& a, hipStream_t s) {
 
 int64_t row_tiles(const pkv_prefill_desc& d) { return ((int64_t)d.T * (d.Hq / d.Hkv) + kRows - 1) / kRows; }
 
-// Ranges of keys per tile of rows.  The device holds 768 workgroups at a time (1024 with d = 64): one range where the tiles alone
+int turn_of(const pkv_prefill_desc& d) { return d.d == 64 ? 1024 : 768; }  // workgroups that the device holds at a time
+
+// Ranges of keys per tile of rows, where all sequences are as long.  The device holds 768 workgroups at a time (1024 with d = 64): one range where the tiles alone
 // are as many, otherwise the fewest that fill (nearly) the largest share of one or two turns (300 rows of 50k keys, 28 heads:
 // 309 us in 11 ranges, 346 in 8, 361 in 12; 2048 rows of 64k keys, 512 tiles: 2.10 ms in 3, 2.20 undivided).  A range's result is
 // written and read again, 64 KB for 128 rows, so that none has fewer than 768 keys (4 x 64 rows of 3000 keys, 32 heads: 36 us with
 // 1000 keys a range, 48 with 256).
 int parts(const pkv_prefill_desc& d) {
-  const int64_t wgs = row_tiles(d) * d.B * d.Hkv, slots = d.d == 64 ? 1024 : 768;
+  const int64_t wgs = row_tiles(d) * d.B * d.Hkv, slots = turn_of(d);
   if (wgs >= slots) return 1;
-  int64_t most = d.N / 768;
+  int64_t most = d.N / kLeastKeys;
   if (most > kMaxParts) most = kMaxParts;
   if (most > 2 * slots / wgs) most = 2 * slots / wgs;
   int best = 1;
@@ -474,6 +622,22 @@ int parts(const pkv_prefill_desc& d) {
     }
   }
   return best;
+}
+
+// Ragged sequences: PrefillArgs' numbers for shares by length; workgroups 0 where there are none: where a sequence's rows alone
+// fill the device (eight prompts of 200 - 4096 tokens 293 us, by length 313), and for few keys, where it is not worth the second
+// kernel.  32 / 8 heads, d 128, us without and with: 24 x 96 rows of 400 - 8000 keys 229 and 146, of 800 - 16 000 452 and 310, all
+// of 8000 370 and 368; 4 x 1024 rows of 400 - 8000 keys 270 and 232, all of 8000 483 and 502, all of 4000 232 and 263; 8 x 256
+// rows, one sequence of 60 000 keys and seven of 1000, 741 and 351.
+constexpr int kLeastRagged = 8 * kLeastKeys;
+struct ByLength {
+  int32_t workgroups, parts, slots;
+};
+ByLength by_length(const pkv_prefill_desc& d) {
+  const int64_t unit = row_tiles(d) * d.Hkv, wgs = unit * d.B, turn = turn_of(d);
+  if (d.B < 2 || d.B > 64 || d.N < kLeastRagged || unit >= turn) return {0, 1, 0};
+  const int64_t extra = wgs <= turn / 2 ? turn : 2 * turn, most = d.N / kLeastKeys < kMaxParts ? d.N / kLeastKeys : kMaxParts;
+  return {(int32_t)(wgs + extra), (int32_t)most, (int32_t)(wgs * most < 2 * extra ? wgs * most : 2 * extra)};
 }
 
 double scale_of(const pkv_prefill_desc& d) { return d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d); }
@@ -504,8 +668,11 @@ extern "C" {
 
 size_t pkv_prefill_workspace_bytes(const pkv_prefill_desc* desc) {
   if (check_prefill_desc(desc) != PKV_OK) return 0;
+  // (which of the two a call takes depends on its arguments)
   const int S = parts(*desc);
-  return S == 1 ? 0 : (size_t)desc->B * desc->Hq * desc->T * S * (desc->d + 2) * sizeof(float);
+  const size_t row = (desc->d + 2) * sizeof(float), even = S == 1 ? 0 : (size_t)desc->B * desc->Hq * desc->T * S * row;
+  const size_t ragged = (size_t)by_length(*desc).slots * kRows * row;
+  return even > ragged ? even : ragged;
 }
 
 int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q, const void* K, const void* V, const int32_t* seq_lens,
@@ -531,8 +698,17 @@ int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q, const voi
   a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.T = d.T; a.N = d.N; a.window = d.window;
   a.S = parts(d);
   a.tiles = (int32_t)row_tiles(d);
+  a.turn = turn_of(d);
   a.part_o = static_cast<float*>(workspace);
-  a.part_mz = a.part_o ? a.part_o + (size_t)d.B * d.Hq * d.T * a.S * d.d : nullptr;
+  const ByLength ragged = by_length(d);
+  if ((seq_lens || q_start) && ragged.workgroups > 0) {
+    a.by_length = ragged.workgroups;
+    a.most_parts = ragged.parts;
+    a.most_slots = ragged.slots;
+    a.part_mz = a.part_o ? a.part_o + (size_t)ragged.slots * kRows * d.d : nullptr;
+  } else {
+    a.part_mz = a.part_o ? a.part_o + (size_t)d.B * d.Hq * d.T * a.S * d.d : nullptr;
+  }
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.q_st = d.q_st; a.kv_sb = d.kv_sb; a.kv_sh = d.kv_sh; a.kv_st = d.kv_st;
   a.o_sb = d.o_sb; a.o_sh = d.o_sh; a.o_st = d.o_st;
   a.scale = (float)(scale_of(d) * 1.4426950408889634);

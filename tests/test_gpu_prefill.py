@@ -235,3 +235,29 @@ def test_values_of_every_size_and_masked_rows_of_the_lowest_value():
     out, lse = binding.prefill_attention(q, K, V, want_lse=True)
     torch.cuda.synchronize()
     _compare(out, lse, q, K, V)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("B,T,N,Hq,Hkv,d,window,prefix,cap,lens,start", [
+    (3, 40, 9000, 8, 2, 128, 0, False, 0.0, [9000, 1600, 0], None),                        # one long, one short, one empty
+    (5, 300, 7000, 12, 4, 64, 900, False, 30.0, [7000, 6999, 77, 300, 1], None),
+    (2, 129, 6200, 2, 1, 64, 0, True, 0.0, [6200, 5000], None), (2, 129, 3000, 2, 1, 64, 0, True, 0.0, [3000, 2000], None),
+    (4, 70, 6500, 8, 8, 128, 0, False, 0.0, [6500, 2000, 1800, 6400], [-30, 1990, 1800, -70]),   # rows before, behind, none at all
+    (3, 1500, 7001, 4, 2, 128, 0, False, 0.0, [7001, 900, 4000], [5501, -700, 3900]),
+    (64, 2, 6400, 4, 1, 64, 0, False, 0.0, None, None), (65, 2, 6400, 4, 1, 64, 0, False, 0.0, None, None)])
+def test_ragged_sequences_in_ranges(B, T, N, Hq, Hkv, d, window, prefix, cap, lens, start, dtype):
+    print("ragged", B, T, N, Hq, Hkv, d, window, prefix, cap, dtype, flush=True)
+    q, K, V, g = _make(B, Hq, Hkv, d, T, N, dtype, N + T)
+    if lens is None:
+        lens = torch.randint(0, N + 1, (B,), generator=torch.Generator().manual_seed(B)).tolist()
+    lens_t = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    start_t = torch.tensor([n - T for n in lens] if start is None else start, dtype=torch.int32, device=DEV)
+    pre = None
+    if prefix:
+        pre = torch.zeros(B, N, dtype=torch.int32, device=DEV)
+        pre[:, ::3] = N - 5
+    for b in range(B):
+        K[b, :, lens[b]:], V[b, :, lens[b]:] = math.nan, math.inf
+    out, lse = binding.prefill_attention(q, K, V, seq_lens=lens_t, q_start=start_t, prefix_end=pre, window=window, cap=cap, want_lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, q, K, V, lens_t, start_t, pre=pre, window=window, cap=cap)
