@@ -208,9 +208,9 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
     S = a.S;
     part = rest % S;
     tile = a.tiles - 1 - rest / S;
-    // Sequences take turns: where a few are long, workgroups at a fixed distance would be, which go to the same part of a die (2048
-    // rows of 60k keys beside three short sequences 5.1 ms, with turns 2.3).
-    const unsigned turn = rest + (rest >> 1) + (rest >> 2) + (rest >> 3);
+    // Ragged sequences take turns: where a few are long, workgroups at a fixed distance would be, which go to the same part of a die
+    // (eight prompts, one of 8192 tokens and seven of 1000, 1525 us, with turns 658).
+    const unsigned turn = a.seq_lens || a.q_start ? rest + (rest >> 1) + (rest >> 2) + (rest >> 3) : 0;
     b = (int)((blockIdx.x % units / a.Hkv + turn) % (unsigned)a.B);
     g = blockIdx.x % a.Hkv;
   }
