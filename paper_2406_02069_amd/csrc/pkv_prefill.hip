@@ -1,7 +1,7 @@
 // Attention of a prompt over its keys (include/pkv.h: pkv_prefill_attention).
 //
 // Bound by power: 4 d products-and-sums per (query row, seen key), for which K and V come from LDS, and an exponential.  A 32k
-// prompt (32 / 8 heads, d 128) takes 7.8 - 8.0 ms, 1.10 - 1.13 PFLOP/s of what it sees; the clock sinks to 1.6 - 1.7 GHz, at
+// prompt (32 / 8 heads, d 128) takes 7.6 - 8.3 ms by card, 1.06 - 1.17 PFLOP/s of what it sees; the clock sinks to 1.6 - 1.8 GHz, at
 // which the matrix pipe is busy for 64 % of the cycles.  Forms that need fewer or more cycles took the same time within 3 %.
 // Work split: the G T query rows of a KV head (row = token * G + head, so that a tile of rows covers few tokens and hardly more
 // keys than its rows see) in tiles of 128, a workgroup of four waves each, 32 rows a wave; the longest tiles first.  Workgroups
