@@ -509,7 +509,9 @@ int pkv_rotary_frequencies(int32_t rot, int32_t scaling, double base,
  * and position p = positions[b][t], or r if positions is NULL.  Its rotated
  * keys and its values go to row r of K_cache and V_cache.  A row outside
  * [0, k_cap), or one whose page number is out of range, is never written: it
- * is dropped and counted.  Nothing else of the caches is written.
+ * is dropped and counted.  Nothing else of the caches is written.  A row that
+ * two tokens are given (by a page that two sequences name) holds one of them
+ * afterwards, not necessarily the same for every head.
  */
 typedef struct {
   int32_t B, Hq, Hkv; /* sequences, query heads, key/value heads, >= 1       */
@@ -611,7 +613,7 @@ size_t pkv_prefill_workspace_bytes(const pkv_prefill_desc* desc);
  * desc       HOST.  Strides are >= 0 and multiples of 8.
  * q, K, V, out
  *            DEVICE, of the descriptor's type, 16-byte aligned; out overlaps
- *            nothing.
+ *            nothing, and its rows not one another.
  * seq_lens   DEVICE int32 [B]: n_b, clamped to 0..N; NULL: N.
  * q_start    DEVICE int32 [B] or NULL (0).  Any value.
  * doc_start  DEVICE int32 [B,N] contiguous or NULL: where the document of

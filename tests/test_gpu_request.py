@@ -87,3 +87,42 @@ def test_request(page, window, slopes):
                               d ** -0.5, 0.0, None if sl is None else float(sl[h]))
                 check(out[b, h][None], lse[b, h][None], *want, torch.bfloat16)
         at += 1
+
+
+def test_ragged_batches_captured_and_replayed_with_other_lengths():
+    # ranges and places go by lengths that are read on the device: a captured call follows them
+    g = torch.Generator(device=DEV).manual_seed(5)
+    def some(*shape):
+        return torch.randn(*shape, generator=g, device=DEV).to(torch.bfloat16)
+    B, T, N, Hq, Hkv, d = 3, 50, 7000, 8, 2, 128
+    q, K, V = some(B, Hq, T, d), some(B, Hkv, N, d), some(B, Hkv, N, d)
+    lens, start = torch.tensor([7000, 60, 900], dtype=torch.int32, device=DEV), torch.tensor([6950, 10, 850], dtype=torch.int32, device=DEV)
+    B2, k_cap = 70, 5000
+    q2, K2, V2 = some(B2, 4, 64), some(1, 2, k_cap, 64).expand(B2, 2, k_cap, 64), some(1, 2, k_cap, 64).expand(B2, 2, k_cap, 64)
+    count = torch.randint(0, 60, (B2,), generator=g, device=DEV).to(torch.int32)
+    ws = [torch.empty(1 << 26, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    outs = [torch.empty_like(q), torch.empty(B, Hq, T, device=DEV), torch.empty_like(q2), torch.empty(B2, 4, device=DEV)]
+    def both(outs, ws):
+        binding.prefill_attention(q, K, V, seq_lens=lens, q_start=start, out=outs[0], lse=outs[1], workspace=ws[0])
+        binding.decode_attention_long(q2, K2, V2, count, out=outs[2], lse=outs[3], workspace=ws[1])
+    both(outs, ws)
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        both(outs, ws)
+    for step in range(4):
+        lens.copy_(torch.tensor([[7000, 60, 900], [10, 7000, 6500], [0, 0, 6999], [7000, 7000, 7000]][step], dtype=torch.int32))
+        start.copy_(lens - T)
+        count.copy_(torch.randint(0, 60, (B2,), generator=g, device=DEV))
+        count[7 * step + 3] = k_cap - step
+        for w in ws:
+            w.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        again = [torch.full_like(x, 7) for x in outs]
+        both(again, [torch.zeros_like(w) for w in ws])
+        torch.cuda.synchronize()
+        for x, y in zip(outs, again):
+            assert torch.equal(x, y), step
+        fine = [bool(torch.isfinite(x).all()) for x in (outs[0], outs[2])]
+        assert all(fine)
