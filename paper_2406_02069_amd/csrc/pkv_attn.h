@@ -45,6 +45,11 @@ struct Elem<_Float16> {
   }
 };
 
+// Softmax weights in fp16 are 2^(score - reference + kFp16Shift), and the reference moves once a score exceeds it by more than
+// kFp16Slack: 2^15 at most.  The type's steps end at 2^-24, so that weights far below the largest lose their bits and then vanish,
+// while their sum in fp32 keeps them; this way the last step is 2^-37 of the reference.  (bf16 has fp32's exponents.)
+constexpr float kFp16Shift = 13.0f, kFp16Slack = 2.0f;
+
 // Two floats rounded to the type (to nearest, ties to even), the first one in the low half.
 template <typename T>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {

@@ -11,11 +11,13 @@
 // Ranges: as long as fill the device once (512 workgroups), by the sequences' lengths as they are on the device, so that ragged
 // batches have ranges of one length too; every wave works out its place among them from all counts (2 to 256 sequences).
 //   loads   whole rows, 1 KB at a time, into registers; from there to the wave's own tile in LDS, K first, then V in its place.
-//   scores  S^T = K Q^T in v_mfma_f32_16x16x32: 16 keys are the rows of A, 16 heads the columns of B.  Lane (l16, quad) ends with keys 4 quad .. + 3 of head l16, all it needs for its weights.
-//   softmax a reference exponent per head and wave, moved only when a score exceeds it by a factor of 2^8.
+//   scores  S^T = K Q^T in v_mfma_f32_16x16x32: 16 keys are the rows of A, 16 heads the columns of B.  Lane (l16, quad) ends with
+//           keys 4 quad .. + 3 of head l16, all it needs for its weights.
+//   softmax a reference exponent per head and wave, moved only when a score exceeds it by a factor of 2^8 (fp16: 2^2).
 //   values  O^T += V^T P^T: the weights are in B's layout already if the 32 keys of a step are taken in the order in which the
-//           lanes hold them (4 quad .. + 3 of either half), and V^T is read column-wise.  The weights are given as two numbers of the type, their rounding and what it left (16 bits for bf16, 22 for
-//           fp16): the matrix pipe has time for both products.
+//           lanes hold them (4 quad .. + 3 of either half), and V^T is read column-wise.  The weights are given as two numbers of
+//           the type, their rounding and what it left (16 bits for bf16; 22 for fp16, down to steps of 2^-37 of the reference):
+//           the matrix pipe has time for both products.
 // Rows that are not seen (behind the count, outside the window, on a page that does not exist) have weight 0, and their copy of
 // V is zero.
 #include <math.h>
@@ -51,6 +53,14 @@ struct LongArgs {
   int64_t q_sb, q_sh, c_sb, c_sh, c_st, p_sb, p_sh;
   float scale;          // of the products, to log2 units (without a cap)
   Cap cap;
+};
+
+// The factor of the softmax weights, and how far a score may exceed the reference (log2).
+template <typename T>
+struct Weight {
+  static constexpr bool HALF = __is_same(T, _Float16);
+  static constexpr float SHIFT = HALF ? kFp16Shift : 0.0f, SLACK = HALF ? kFp16Slack : 8.0f;
+  static constexpr float UNIT = HALF ? 1.0f / (1 << (int)kFp16Shift) : 1.0f;  // 2^-SHIFT
 };
 
 // A wave's reads and writes of its own part of LDS keep their order.
@@ -320,7 +330,7 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
       float top = sc[0][0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e >> 2][e & 3]);
-      if (__any(top > m + 8.0f)) {
+      if (__any(top > m + Weight<T>::SLACK)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float m1 = fmaxf(m, top);
@@ -330,7 +340,7 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) o[i] *= f;
       }
-      const float ref = m == kNone ? 0.0f : m;
+      const float ref = (m == kNone ? 0.0f : m) - Weight<T>::SHIFT;
       u32x4 hi, lo;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
@@ -446,7 +456,7 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
       w[0] = pack2<T>(acc[0] * inv, acc[1] * inv);
       w[1] = pack2<T>(acc[2] * inv, acc[3] * inv);
       *reinterpret_cast<u32x2*>(a.out + row * D + 4 * d4) = w;
-      if (d4 == 0 && a.lse) a.lse[row] = sum == 0.0f ? kNone : (top + log2_(sum)) * kLn2;
+      if (d4 == 0 && a.lse) a.lse[row] = sum == 0.0f ? kNone : (top + log2_(sum * Weight<T>::UNIT)) * kLn2;
     }
   }
 }
@@ -507,7 +517,7 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const LongArgs a)
       w[0] = pack2<T>(acc[0] * inv, acc[1] * inv);
       w[1] = pack2<T>(acc[2] * inv, acc[3] * inv);
       *reinterpret_cast<u32x2*>(a.out + row * D + 4 * d4) = w;
-      if (d4 == 0 && a.lse) a.lse[row] = z == 0.0f ? kNone : (m + log2_(z)) * kLn2;
+      if (d4 == 0 && a.lse) a.lse[row] = z == 0.0f ? kNone : (m + log2_(z * Weight<T>::UNIT)) * kLn2;
     }
   }
 }

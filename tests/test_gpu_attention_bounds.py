@@ -12,6 +12,8 @@ DEV = "cuda:0"
 # first leaves is 2^-8 or 2^-11 of it, and is rounded by as much).
 PROMPT = HALF_STEP
 TOKEN = {t: h * h for t, h in HALF_STEP.items()}
+# Half the type's last step, in units of the largest weight.
+TOKEN_SMALL = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -38}
 
 
 @pytest.mark.parametrize("dtype,Hq,Hkv,d,T,cap,scale,slope,wide,window", [
@@ -69,8 +71,7 @@ def test_one_token(dtype, Hq, Hkv, d, n, cap, scale, slope, window):
     torch.cuda.synchronize()
     dist = (n - 1 - torch.arange(n, device=DEV))[None]
     seen = dist < (window or n)
-    small = 2.0 ** -25 if dtype == torch.float16 else 0.0
     for h in range(Hq):
         kv = h * Hkv // Hq
         check(out[0, h][None], lse[0, h][None], *attend(q[0, h][None], K[0, kv], V[0, kv], seen, dist, scale or d ** -0.5, dtype, cap, slope,
-                                                        TOKEN[dtype], small))
+                                                        TOKEN[dtype], TOKEN_SMALL[dtype]))
