@@ -584,7 +584,8 @@ int pkv_rotary_append(const pkv_rotary_desc* desc, const void* q,
  *   out[b][h][t] = sum_j softmax_j(s) V_j,  lse[b][h][t] = ln sum_j exp(s_j)
  * Rows that are not there, or see no key: zero and -inf.
  * fp32 scores, sums and accumulation; the softmax weights are rounded to the
- * input's type for the product with V.  Rows >= n_b of K and V are never
+ * input's type for the product with V (fp16: those below 2^-22 of the row's
+ * largest are off by up to 2^-33 of it).  Rows >= n_b of K and V are never
  * read.  A key that a query does not see has no influence on its row,
  * whatever it holds (NaN and infinities included).
  */

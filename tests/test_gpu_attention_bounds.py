@@ -13,6 +13,7 @@ DEV = "cuda:0"
 PROMPT = HALF_STEP
 TOKEN = {t: h * h for t, h in HALF_STEP.items()}
 # Half the type's last step, in units of the largest weight.
+PROMPT_SMALL = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -33}
 TOKEN_SMALL = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -38}
 
 
@@ -34,10 +35,9 @@ def test_prompt(dtype, Hq, Hkv, d, T, cap, scale, slope, wide, window):
     torch.cuda.synchronize()
     dist = torch.arange(T, device=DEV)[:, None] - torch.arange(T, device=DEV)
     seen = (dist >= 0) & (dist < (window or T))
-    small = 2.0 ** -33 if dtype == torch.float16 else 0.0
     for h in range(Hq):
         check(out[0, h], lse[0, h], *attend(q[0, h], K[0, h * Hkv // Hq], V[0, h * Hkv // Hq], seen, dist, scale or d ** -0.5, dtype, cap,
-                                            slope, PROMPT[dtype], small))
+                                            slope, PROMPT[dtype], PROMPT_SMALL[dtype]))
 
 
 @pytest.mark.parametrize("T,N,window,dtype", [(70, 9000, 0, torch.bfloat16), (33, 5000, 1500, torch.float16)])
@@ -50,9 +50,8 @@ def test_chunk_in_ranges(T, N, window, dtype):
     torch.cuda.synchronize()
     dist = N - T + torch.arange(T, device=DEV)[:, None] - torch.arange(N, device=DEV)
     seen = (dist >= 0) & (dist < (window or N))
-    small = 2.0 ** -33 if dtype == torch.float16 else 0.0
     for h in range(Hq):
-        check(out[0, h], lse[0, h], *attend(q[0, h], K[0, h // 2], V[0, h // 2], seen, dist, d ** -0.5, dtype, 0.0, None, PROMPT[dtype], small))
+        check(out[0, h], lse[0, h], *attend(q[0, h], K[0, h // 2], V[0, h // 2], seen, dist, d ** -0.5, dtype, 0.0, None, PROMPT[dtype], PROMPT_SMALL[dtype]))
 
 
 @pytest.mark.parametrize("dtype,Hq,Hkv,d,n,cap,scale,slope,window", [

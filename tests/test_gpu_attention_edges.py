@@ -39,3 +39,19 @@ def test_one_token_weights_far_below_the_largest(B, Hq, Hkv, d, n, gap, size, dt
         for b in {0, B - 1}:
             for h in range(kv * Hq // Hkv, (kv + 1) * Hq // Hkv):
                 check(out[b, h][None], lse[b, h][None], *want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("d,T,n", [(64, 4, 300), (128, 40, 2000), (64, 9, 9001)])
+@pytest.mark.parametrize("gap,size", [(9, 1.0), (12, 1.0), (15, 1.0), (18, 1.0), (18, 1000.0), (20, 1000.0)])
+def test_prompt_weights_far_below_the_largest(d, T, n, gap, size, dtype):
+    # a weight has one rounding of the type, 2^-25 at least in units of 2^-8 of the reference
+    q, K, V = _sink(1, 2, 1, d, n, gap, size, dtype, 5)
+    out, lse = binding.prefill_attention(q[:, :, None].expand(1, 2, T, d), K, V, q_start=torch.tensor([n - T], dtype=torch.int32, device=DEV),
+                                         want_lse=True)
+    torch.cuda.synchronize()
+    dist = n - T + torch.arange(T, device=DEV)[:, None] - torch.arange(n, device=DEV)
+    small = 2.0 ** -33 if dtype == torch.float16 else 0.0
+    want = attend(q[0, :1].expand(T, d), K[0, 0], V[0, 0], dist >= 0, dist, d ** -0.5, dtype, weights=HALF_STEP[dtype], small=small)
+    for h in range(2):
+        check(out[0, h], lse[0, h], *want)
