@@ -587,7 +587,9 @@ int pkv_rotary_append(const pkv_rotary_desc* desc, const void* q,
  * input's type for the product with V (fp16: those below 2^-22 of the row's
  * largest are off by up to 2^-33 of it).  Rows >= n_b of K and V are never
  * read.  A key that a query does not see has no influence on its row,
- * whatever it holds (NaN and infinities included).
+ * whatever it holds (NaN and infinities included).  Where a query sees values
+ * of V that are not finite, that element of out is their sum: every weight is
+ * positive, however small.
  */
 typedef struct {
   int32_t B, Hq, Hkv; /* Hq % Hkv == 0                                       */

@@ -86,6 +86,17 @@ __device__ __forceinline__ int sum_upto(int x) {
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 
+// a f + b g, of results with positive factors, which may be too small for fp32: what is not finite is added as it is.
+__device__ __forceinline__ f32x4 weighed(f32x4 a, float f, f32x4 b, float g) {
+  f32x4 r = a * f + b * g;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool fa = fabsf(a[i]) < __builtin_inff(), fb = fabsf(b[i]) < __builtin_inff();
+    if (!(fa && fb)) r[i] = (fa ? 0.0f : a[i]) + (fb ? 0.0f : b[i]);
+  }
+  return r;
+}
+
 // Scores capped by a tanh, from products x to log2 units: cap tanh(y) log2(e), y = x scale / cap.
 // |y| <= 0.36, where scores lie in earnest: y P(y^2), P of degree 3 (least squares reweighted to even out its relative error,
 // 5e-8 at most): a polynomial in x^2, five instructions, exact to a few 2^-24 of the score itself.

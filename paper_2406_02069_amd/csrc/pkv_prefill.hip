@@ -23,8 +23,9 @@
 //           lanes hold them; V^T is read column-wise.
 // Masks leave each row an interval of keys.  Steps that no row of a wave sees are skipped, those that all of its rows see whole
 // take no comparisons.  In the others hidden keys have the weight 0; a value that is not finite would still spoil their product,
-// so the waves look over the rows that they fetched for such a step, put zeros in LDS for such values, and add them afterwards for
-// the rows that see them.
+// so the waves look over the rows that they fetched for such a step and put zeros in LDS for such values.  Where that happened, or
+// a result is not finite, the rows of V are looked over once more at the end: every weight is positive, so that an element for which
+// a row sees values that are not finite is the sum of those, however small their weights are held.
 #include <math.h>
 #include <string.h>
 
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
   constexpr float SHIFT = sizeof(T) == 2 && __is_same(T, _Float16) ? 8.0f : 0.0f;  // fp16 weights: away from its subnormals
   __shared__ __align__(1024) char lds[4 * BUF];  // [buffer][K, V]
   __shared__ int lds_range[4][4], lds_place[kRows][2];
-  __shared__ uint32_t lds_bad[2][4];             // [buffer][wave]: rows of V (eight per wave) that hold a value that is not finite
+  __shared__ int lds_zeroed;  // whether a value of V that is not finite was put to zero
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   int b, g, tile, part, S, slot = 0;
@@ -235,6 +236,7 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
     lds_range[wave][1] = last_w;
     lds_range[wave][2] = lo_w;
     lds_range[wave][3] = hi_w;
+    if (wave == 0) lds_zeroed = 0;
   }
   __syncthreads();
   int first = 0x7FFFFFFF, last = -1, lo_g = 0, hi_g = 0x7FFFFFFF;
@@ -256,6 +258,7 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
     step_end = min(step_end, s0 + per);
     step = min(s0, step_end);
   }
+  const int step_begin = step;
 
   // Fetching a step: wave w rows 8 w .. 8 w + 7 of K and of V, a row's pieces swapped.
   const char* const Kb = reinterpret_cast<const char*>(a.K + b * a.kv_sb + g * a.kv_sh);
@@ -312,7 +315,6 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
     const bool cut = key0 < lo_g || key0 + kKeys - 1 > hi_g;  // some row of the workgroup does not see all of the step
     wait_loads();
     if (cut) {  // the rows of V that this wave fetched
-      uint32_t bad = 0;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         u32x4* const at = reinterpret_cast<u32x4*>(Vl + (OWN * wave + i * ROWS_PER_LOAD) * ROW + 16 * lane);
@@ -326,14 +328,9 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
         }
         if (any) {
           *at = v;
-          bad |= 1u << (i * ROWS_PER_LOAD + lane / PIECES);
+          lds_zeroed = 1;
         }
       }
-      uint32_t all = 0;
-      if (__any(bad != 0)) {
-        for (int i = 0; i < OWN; ++i) all |= __any((bad >> i) & 1) ? 1u << i : 0u;
-      }
-      if (lane == 0) lds_bad[buf][wave] = all;
     }
     lds_barrier();
     if (step + 1 < step_end) fetch(step + 1, buf ^ 1);
@@ -404,37 +401,57 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
         o[mb] = Elem<T>::mfma32(vf, pf[ks], o[mb]);
       }
     }
-    if (!cut) return;
-    // Values that are not finite, key by key, for the rows that see it (from memory: the copy in LDS holds zeros there).
-#pragma unroll 1
-    for (int w = 0; w < 4; ++w) {
-#pragma unroll 1
-      for (uint32_t bad = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_bad[buf][w]); bad != 0; bad &= bad - 1) {
-        const int k = OWN * w + __builtin_ctz(bad), word = 2 * (k >> 3) + ((k & 3) >> 1);
-        uint32_t u = 0;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) u = x == word ? pf[x >> 2][x & 3] : u;
-        u = (uint32_t)__shfl((int)u, col + 32 * ((k >> 2) & 1));
-        const float p = (k & 1) ? unpack<T>(u, 1) : unpack<T>(u, 0);
-        const bool sees = some && key0 + k >= seen.lo && key0 + k <= seen.hi;
-        const char* const from = Vb + (int64_t)min(key0 + k, n - 1) * stride + 8 * half;
-#pragma unroll
-        for (int x = 0; x < MB * 4; ++x) {
-          const u32x2 v = *reinterpret_cast<const u32x2*>(from + 16 * x);
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const uint32_t nf = not_finite<T>(v[y >> 1]) & ((y & 1) ? 0x80000000u : 0x8000u);
-            if (sees && nf) o[x >> 2][4 * (x & 3) + y] += p * unpack<T>(v[y >> 1], y & 1);
-          }
-        }
-      }
-    }
   };
   while (step < step_end) {
     one_step(std::integral_constant<int, 0>());
     if (++step >= step_end) break;
     one_step(std::integral_constant<int, 1>());
     ++step;
+  }
+
+  bool odd = lds_zeroed != 0;
+#pragma unroll
+  for (int x = 0; x < MB * 16; ++x) odd = odd || !(fabsf(o[x >> 4][x & 15]) < __builtin_inff());
+  if (__builtin_expect(__any(odd), 0)) {
+    f32x16 extra[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) extra[i] = (f32x16)(0.0f);
+    const int k_end = min(last_w + 1, step_end * kKeys);
+#pragma unroll 1
+    for (int k0 = max(first_w, step_begin * kKeys); k0 < k_end; k0 += 4 * ROWS_PER_LOAD) {
+      u32x4 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = min(k0 + i * ROWS_PER_LOAD + lane / PIECES, k_end - 1);
+        v[i] = *reinterpret_cast<const u32x4*>(Vb + (int64_t)r * stride + 16 * (lane % PIECES));
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint64_t left = __ballot((not_finite<T>(v[i][0]) | not_finite<T>(v[i][1]) | not_finite<T>(v[i][2]) | not_finite<T>(v[i][3])) != 0);
+#pragma unroll 1
+        while (left != 0) {
+          const int in = __builtin_ctzll(left) / PIECES, k = k0 + i * ROWS_PER_LOAD + in;
+          left &= ~(((1ull << PIECES) - 1) << (in * PIECES));
+          if (k >= k_end) break;  // (the last row once more)
+          const bool sees = some && k >= seen.lo && k <= seen.hi;
+          const char* const from = Vb + (int64_t)k * stride + 8 * half;
+#pragma unroll
+          for (int x = 0; x < MB * 4; ++x) {
+            const u32x2 u = *reinterpret_cast<const u32x2*>(from + 16 * x);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const float value = unpack<T>(u[y >> 1], y & 1);
+              extra[x >> 2][4 * (x & 3) + y] += sees && !(fabsf(value) < __builtin_inff()) ? value : 0.0f;
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < MB * 16; ++x) {
+      const float e = extra[x >> 4][x & 15];
+      o[x >> 4][x & 15] = e == 0.0f ? o[x >> 4][x & 15] : e;
+    }
   }
 
   z += __shfl_xor(z, 32);
@@ -498,7 +515,7 @@ __global__ __launch_bounds__(256) void prefill_join_kernel(const PrefillArgs a) 
   for (int i = share; i < a.S; i += SHARES) {
     const float f = exp2_(mz[2 * i] - ref);
     sum += f * mz[2 * i + 1];
-    acc += f * *reinterpret_cast<const f32x4*>(po + (int64_t)i * D);
+    acc = weighed(acc, 1.0f, *reinterpret_cast<const f32x4*>(po + (int64_t)i * D), f);
   }
   if constexpr (SHARES > 1) {
     lds_o[threadIdx.x] = acc;
@@ -559,7 +576,7 @@ __global__ __launch_bounds__(256) void prefill_join_by_length_kernel(const Prefi
       const float f0 = exp2_(m[i] - ref), f1 = exp2_(m1 - ref);
       m[i] = top;
       z[i] = z[i] * f0 + z1 * f1;
-      acc[i] = acc[i] * f0 + v * f1;
+      acc[i] = weighed(acc[i], f0, v, f1);
     }
   }
 #pragma unroll

@@ -10,7 +10,9 @@ A score's error e_j, in nats, is the relative error of its weight w_j (the softm
 Then, with spread = sum w |V|:
   out        sum w e (|V| + |out|), since what all weights share divides out; `weights` spread for weights that are rounded;
              `small` sum |V| where they have a least step (`small` in units of the largest weight: a row's sum is 1 at least);
-             n / 8 + 64 additions and rescalings of 2^-23 in the sums of n keys; half a step of the result's type
+             n / 8 + 64 additions and rescalings of 2^-23 in the sums of n keys; half a step of the result's type;
+             2^-126 (sum |V| + 1): fp32 and bf16 have no normal numbers below that, and a weight or a result that is
+             smaller may be taken as 0 (e^-120, a key 120 nats below the largest, is 2^-173, which fp32 does not hold at all)
   lse        sum w e, the same additions, 2^-22 of itself and of ln n
 First-order terms are multiplied by 1.01 for the products of errors."""
 import math
@@ -48,7 +50,8 @@ def attend(q, K, V, seen, dist, scale, dtype, cap=0.0, slope=None, weights=0.0, 
     chain = (n / 8 + 64) * 2.0 ** -23
     room = we @ size + we.sum(-1, keepdim=True) * out.abs() + weights * spread + small * (seen.double() @ size) + \
         chain * (spread + out.abs())
-    room = 1.01 * room * (1 + HALF_STEP[dtype]) + HALF_STEP[dtype] * out.abs() + (2.0 ** -25 if dtype == torch.float16 else 0.0)
+    room = 1.01 * room * (1 + HALF_STEP[dtype]) + HALF_STEP[dtype] * out.abs() + (2.0 ** -25 if dtype == torch.float16 else 0.0) + \
+        2.0 ** -126 * (seen.double() @ size + 1)
     lse_room = 1.01 * (we.sum(-1) + chain + 2.0 ** -22 * (lse.masked_fill(none, 0).abs() + math.log(n) + 1))
     return out, lse, room, lse_room
 

@@ -55,3 +55,49 @@ def test_prompt_weights_far_below_the_largest(d, T, n, gap, size, dtype):
     want = attend(q[0, :1].expand(T, d), K[0, 0], V[0, 0], dist >= 0, dist, d ** -0.5, dtype, weights=HALF_STEP[dtype], small=small)
     for h in range(2):
         check(out[0, h], lse[0, h], *want)
+
+
+def _infinite(V, where):
+    """V with an infinity, a negative one, a NaN and two infinities of both signs, each in a column of its own, at `where`."""
+    V = V.clone()
+    V[..., where, 5], V[..., where, 17], V[..., where, 40] = math.inf, -math.inf, math.nan
+    V[..., where, 33], V[..., where + 1, 33] = math.inf, -math.inf
+    return V
+
+
+def _check_infinite(out, V, seen, want):
+    """out [m, d]: where a row sees values that are not finite their sum, elsewhere within `want` of the finite ones."""
+    odd = seen.double() @ (~torch.isfinite(V)).double() > 0
+    for t in range(out.shape[0]):
+        total = V[seen[t]].double().masked_fill(torch.isfinite(V[seen[t]]), 0).sum(0)
+        assert torch.equal(out[t].double()[odd[t]].nan_to_num(7, 8, 9), total[odd[t]].nan_to_num(7, 8, 9)), t
+    check(torch.where(odd, want[0].to(out.dtype), out), None, *want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,n,where,window", [(4, 70, 3, 0), (5, 70, 67, 0), (70, 70, 31, 0), (90, 90, 40, 20), (3, 1000, 500, 0), (6, 9001, 8000, 0),
+                                              (6, 9001, 9, 0), (40, 7000, 6990, 2000), (300, 1100, 900, 0)])
+@pytest.mark.parametrize("gap", [2, 25, 120])
+def test_prompt_values_that_are_not_finite(gap, T, n, where, window, dtype):
+    # keys of any weight, in steps that all rows see and in others, before and behind the largest score, in its range of keys or not
+    d, at = 64, [0, n // 2, n - T]
+    dist = n - T + torch.arange(T, device=DEV)[:, None] - torch.arange(n, device=DEV)
+    seen = (dist >= 0) & (dist < (window or n))
+    start = torch.tensor([n - T, n - T], dtype=torch.int32, device=DEV)
+    lens = torch.tensor([n, n], dtype=torch.int32, device=DEV)
+    for sink in at:
+        q, K, V = _sink(1, 2, 1, d, n, gap, 1.0, dtype, sink)
+        V = torch.randn(V.shape, generator=torch.Generator(device=DEV).manual_seed(n), device=DEV).to(dtype)
+        Vi = _infinite(V, where)
+        clean = V[0, 0].masked_fill(~torch.isfinite(Vi[0, 0]), 0)
+        want = attend(q[0, :1].expand(T, d), K[0, 0], clean, seen, dist, d ** -0.5, dtype, weights=HALF_STEP[dtype],
+                      small=2.0 ** -33 if dtype == torch.float16 else 0.0)
+        qs = q[:, :, None].expand(1, 2, T, d)
+        out, lse = binding.prefill_attention(qs, K, Vi, q_start=start[:1], window=window, want_lse=True)
+        two, _ = binding.prefill_attention(qs.expand(2, 2, T, d), K.expand(2, 1, n, d), Vi.expand(2, 1, n, d), seq_lens=lens, q_start=start,
+                                           window=window)                                 # (ranges by lengths)
+        torch.cuda.synchronize()
+        for h in range(2):
+            check(want[0].to(dtype), lse[0, h], *want)
+            _check_infinite(out[0, h], Vi[0, 0], seen, want)
+            _check_infinite(two[1, h], Vi[0, 0], seen, want)
