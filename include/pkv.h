@@ -651,9 +651,10 @@ int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q,
  * kept rows of a compression call: its idx_out), or j if positions is NULL;
  * the query's position is q_pos_b, or count_b - 1 if q_pos is NULL.  A row is
  * seen if 0 <= position <= q's and, with a window, position > q's - window.
- * Scores, softmax and lse as pkv_prefill_attention's; the softmax weights keep
- * 16 bits and more (fp16: those below 2^-22 of the row's largest are off by up
- * to 2^-38 of it).  A page number out of range makes its rows count as absent.
+ * Scores, softmax, lse and values that are not finite as
+ * pkv_prefill_attention has them; the softmax weights keep 16 bits and more
+ * (fp16: those below 2^-22 of the row's largest are off by up to 2^-38 of it).
+ * A page number out of range makes its rows count as absent.
  */
 typedef struct {
   int32_t B, Hq, Hkv; /* Hq % Hkv == 0                                       */

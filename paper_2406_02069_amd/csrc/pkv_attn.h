@@ -97,6 +97,10 @@ __device__ __forceinline__ f32x4 weighed(f32x4 a, float f, f32x4 b, float g) {
   return r;
 }
 
+__device__ __forceinline__ bool finite(f32x4 v) {
+  return fabsf(v[0]) < __builtin_inff() && fabsf(v[1]) < __builtin_inff() && fabsf(v[2]) < __builtin_inff() && fabsf(v[3]) < __builtin_inff();
+}
+
 // Scores capped by a tanh, from products x to log2 units: cap tanh(y) log2(e), y = x scale / cap.
 // |y| <= 0.36, where scores lie in earnest: y P(y^2), P of degree 3 (least squares reweighted to even out its relative error,
 // 5e-8 at most): a polynomial in x^2, five instructions, exact to a few 2^-24 of the score itself.

@@ -437,10 +437,16 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
     const float ref = top == kNone ? 0.0f : top;
     float sum = 0.0f;
     f32x4 acc = (f32x4)(0.0f);
+    auto outputs = [&](int w) { return *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds_v[w]) + hl * D + ((d4 ^ (hl & 7)) << 2)); };
     for (int w = w0; w < kWaves; w += a.wave_groups) {
       const float f = exp2_(lds_mz[w][hl][0] - ref);
       sum += f * lds_mz[w][hl][1];
-      acc += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds_v[w]) + hl * D + ((d4 ^ (hl & 7)) << 2));
+      acc += f * outputs(w);
+    }
+    if (__builtin_expect(!finite(acc), 0)) {
+      acc = (f32x4)(0.0f);
+#pragma unroll 1
+      for (int w = w0; w < kWaves; w += a.wave_groups) acc = weighed(acc, 1.0f, outputs(w), exp2_(lds_mz[w][hl][0] - ref));
     }
     const int64_t row = (int64_t)b * a.Hq + g * a.G + 64 * hg + hh;
     if (ranges > 1) {
@@ -482,25 +488,39 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const LongArgs a)
   const int d4 = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
   float m, z;
   f32x4 acc;
-  auto join = [&](float m1, float z1, f32x4 v) {
+  auto join = [&](float m1, float z1, f32x4 v, bool careful = false) {
     const float top = fmaxf(m, m1), ref = top == kNone ? 0.0f : top;
     const float f0 = exp2_(m - ref), f1 = exp2_(m1 - ref);
     m = top;
     z = z * f0 + z1 * f1;
-    acc = acc * f0 + v * f1;
+    if (careful)
+      acc = weighed(acc, f0, v, f1);
+    else
+      acc = __builtin_elementwise_fma(acc, (f32x4)(f0), v * f1);
+  };
+  auto nothing = [&]() {
+    m = kNone;
+    z = 0.0f;
+    acc = (f32x4)(0.0f);
   };
 #pragma unroll 1
   for (int k = 0; k < HEADS; ++k) {
     const int64_t row = (int64_t)blockIdx.x * HEADS + k;
     const int h = (int)(row % a.Hq), h_in = h % a.G, unit = h / a.G * a.head_groups + h_in / 64;
     const int64_t at = ((int64_t)base + unit * ranges) * heads + h_in % 64;
-    m = kNone;
-    z = 0.0f;
-    acc = (f32x4)(0.0f);
+    nothing();
 #pragma unroll 4
     for (int i = part; i < ranges; i += PARTS) {
       const float* const mz = a.part_mz + (at + heads * i) * 2;
       join(mz[0], mz[1], *reinterpret_cast<const f32x4*>(a.part_o + (at + heads * i) * D + 4 * d4));
+    }
+    if (__builtin_expect(!finite(acc), 0)) {  // (0 times an infinity is not what it should be)
+      nothing();
+#pragma unroll 1
+      for (int i = part; i < ranges; i += PARTS) {
+        const float* const mz = a.part_mz + (at + heads * i) * 2;
+        join(mz[0], mz[1], *reinterpret_cast<const f32x4*>(a.part_o + (at + heads * i) * D + 4 * d4), true);
+      }
     }
     if (k > 0) __syncthreads();  // (the last head's parts have been read)
     lds_o[part][d4] = acc;
@@ -512,6 +532,11 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const LongArgs a)
     if (part == 0) {
 #pragma unroll
       for (int i = 1; i < PARTS; ++i) join(lds_m[i], lds_z[i], lds_o[i][d4]);
+      if (__builtin_expect(!finite(acc), 0)) {
+        nothing();
+#pragma unroll 1
+        for (int i = 0; i < PARTS; ++i) join(lds_m[i], lds_z[i], lds_o[i][d4], true);
+      }
       const float inv = z == 0.0f ? 0.0f : 1.0f / z;
       u32x2 w;
       w[0] = pack2<T>(acc[0] * inv, acc[1] * inv);

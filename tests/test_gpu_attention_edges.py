@@ -101,3 +101,26 @@ def test_prompt_values_that_are_not_finite(gap, T, n, where, window, dtype):
             check(want[0].to(dtype), lse[0, h], *want)
             _check_infinite(out[0, h], Vi[0, 0], seen, want)
             _check_infinite(two[1, h], Vi[0, 0], seen, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("Hq,n,where", [(2, 70, 3), (2, 70, 66), (40, 300, 130), (2, 1000, 500), (8, 9001, 8000), (2, 9001, 9)])
+@pytest.mark.parametrize("gap", [2, 25, 120])
+def test_one_token_values_that_are_not_finite(gap, Hq, n, where, dtype):
+    # the value's key and the largest score in one wave, in waves of one range, and in ranges of their own
+    d = 64
+    seen, dist = torch.ones(1, n, dtype=torch.bool, device=DEV), torch.zeros(1, n, device=DEV)
+    for sink in (0, n // 2, n - 3):
+        q, K, V = _sink(2, Hq, 1, d, n, gap, 1.0, dtype, sink)
+        V = torch.randn(V.shape, generator=torch.Generator(device=DEV).manual_seed(n), device=DEV).to(dtype)
+        Vi = _infinite(V, where)
+        clean = V[0, 0].masked_fill(~torch.isfinite(Vi[0, 0]), 0)
+        want = attend(q[0, :1], K[0, 0], clean, seen, dist, d ** -0.5, dtype, weights=HALF_STEP[dtype] ** 2,
+                      small=2.0 ** -38 if dtype == torch.float16 else 0.0)
+        counts = torch.tensor([n, n], dtype=torch.int32, device=DEV)
+        for B in (1, 2):                                    # (equal ranges; ranges by lengths)
+            out, lse = binding.decode_attention_long(q[:B], K.expand(B, 1, n, d), Vi.expand(B, 1, n, d), counts[:B], want_lse=True)
+            torch.cuda.synchronize()
+            for h in (0, Hq - 1):
+                check(want[0].to(dtype), lse[B - 1, h][None], *want)
+                _check_infinite(out[B - 1, h][None], Vi[0, 0], seen, want)
