@@ -409,9 +409,10 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
     ++step;
   }
 
-  bool odd = lds_zeroed != 0;
+  f32x4 naught = (f32x4)(0.0f);  // of what is finite; otherwise NaN
 #pragma unroll
-  for (int x = 0; x < MB * 16; ++x) odd = odd || !(fabsf(o[x >> 4][x & 15]) < __builtin_inff());
+  for (int x = 0; x < MB * 16; ++x) naught[x & 3] = fmaf(o[x >> 4][x & 15], 0.0f, naught[x & 3]);
+  const bool odd = lds_zeroed != 0 || (naught[0] + naught[1]) + (naught[2] + naught[3]) != 0.0f;
   if (__builtin_expect(__any(odd), 0)) {
     f32x16 extra[MB];
 #pragma unroll
@@ -515,7 +516,13 @@ __global__ __launch_bounds__(256) void prefill_join_kernel(const PrefillArgs a) 
   for (int i = share; i < a.S; i += SHARES) {
     const float f = exp2_(mz[2 * i] - ref);
     sum += f * mz[2 * i + 1];
-    acc = weighed(acc, 1.0f, *reinterpret_cast<const f32x4*>(po + (int64_t)i * D), f);
+    acc += f * *reinterpret_cast<const f32x4*>(po + (int64_t)i * D);
+  }
+  if (__builtin_expect(!finite(acc), 0)) {  // (0 times an infinity is not what it should be)
+    acc = (f32x4)(0.0f);
+#pragma unroll 1
+    for (int i = share; i < a.S; i += SHARES)
+      acc = weighed(acc, 1.0f, *reinterpret_cast<const f32x4*>(po + (int64_t)i * D), exp2_(mz[2 * i] - ref));
   }
   if constexpr (SHARES > 1) {
     lds_o[threadIdx.x] = acc;
@@ -558,14 +565,7 @@ __global__ __launch_bounds__(256) void prefill_join_by_length_kernel(const Prefi
   if (row0 >= rows) return;
   float m[R], z[R];
   f32x4 acc[R];
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-    m[i] = kNone;
-    z[i] = 0.0f;
-    acc[i] = (f32x4)(0.0f);
-  }
-#pragma unroll 2
-  for (int j = 0; j < S; ++j) {
+  auto join = [&](int j, auto careful) {
     const int64_t from = (int64_t)(slot + j * a.Hkv) * kRows + first;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -576,8 +576,30 @@ __global__ __launch_bounds__(256) void prefill_join_by_length_kernel(const Prefi
       const float f0 = exp2_(m[i] - ref), f1 = exp2_(m1 - ref);
       m[i] = top;
       z[i] = z[i] * f0 + z1 * f1;
-      acc[i] = weighed(acc[i], f0, v, f1);
+      if constexpr (decltype(careful)::value)
+        acc[i] = weighed(acc[i], f0, v, f1);
+      else
+        acc[i] = __builtin_elementwise_fma(acc[i], (f32x4)(f0), v * f1);
     }
+  };
+  auto nothing = [&]() {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      m[i] = kNone;
+      z[i] = 0.0f;
+      acc[i] = (f32x4)(0.0f);
+    }
+  };
+  nothing();
+#pragma unroll 2
+  for (int j = 0; j < S; ++j) join(j, std::false_type());
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < R; ++i) odd = odd || !finite(acc[i]);
+  if (__builtin_expect(odd, 0)) {  // (0 times an infinity is not what it should be)
+    nothing();
+#pragma unroll 1
+    for (int j = 0; j < S; ++j) join(j, std::true_type());
   }
 #pragma unroll
   for (int i = 0; i < R; ++i) {
