@@ -606,11 +606,15 @@ typedef struct {
 } pkv_prefill_desc;
 
 /*
- * Bytes of DEVICE workspace pkv_prefill_attention needs for this shape (0
- * where one sequence's query rows fill the device, and for short ones; 0 as
- * well if the descriptor is invalid).  HOST only, pure.
+ * Bytes of DEVICE workspace that pkv_prefill_attention needs for this shape
+ * with whatever arguments (up to 204 MB for several long sequences, whose
+ * ranges go by their lengths, up to 102 MB otherwise; 0 where one sequence's
+ * query rows fill the device, and for short ones), and what it needs without
+ * seq_lens and q_start (0 as well where all sequences' rows together fill the
+ * device).  0 if the descriptor is invalid.  HOST only, pure.
  */
 size_t pkv_prefill_workspace_bytes(const pkv_prefill_desc* desc);
+size_t pkv_prefill_even_workspace_bytes(const pkv_prefill_desc* desc);
 
 /*
  * desc       HOST.  Strides are >= 0 and multiples of 8.
@@ -628,8 +632,9 @@ size_t pkv_prefill_workspace_bytes(const pkv_prefill_desc* desc);
  *            neither cap, slopes, window, doc_start nor prefix_end, the rows
  *            of the last alpha tokens are what pkv_compress_layers_lse takes.
  * workspace  DEVICE, 256-byte aligned, >= pkv_prefill_workspace_bytes(desc)
- *            bytes (may be NULL when that is 0); contents irrelevant on
- *            entry, undefined on exit; concurrent calls need distinct ones.
+ *            bytes, or _even_workspace_bytes without seq_lens and q_start (may
+ *            be NULL when that is 0); contents irrelevant on entry, undefined
+ *            on exit; concurrent calls need distinct ones.
  * Asynchronous on `stream`, never allocates.
  * Errors: PKV_ERR_INVALID_ARG (also a scale or cap whose quotient is not a
  * finite fp32), PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv > 128, B > 65535, N

@@ -29,7 +29,8 @@ DESC_FLAGS = 0
 EXPORTS = ["pkv_budgets", "pkv_workspace_bytes", "pkv_compress_layer", "pkv_compress_layer_noalloc", "pkv_compress_layers",
            "pkv_compress_layers_lse", "pkv_compress_layers_paged", "pkv_compress_layers_profiled",
            "pkv_budgets_schedule", "pkv_attention_recall", "pkv_decode_attention", "pkv_decode_workspace_bytes", "pkv_decode_attention_layers",
-           "pkv_decode_layers_workspace_bytes", "pkv_rotary_frequencies", "pkv_rotary_append", "pkv_prefill_attention", "pkv_prefill_workspace_bytes", "pkv_decode_attention_long",
+           "pkv_decode_layers_workspace_bytes", "pkv_rotary_frequencies", "pkv_rotary_append", "pkv_prefill_attention", "pkv_prefill_workspace_bytes",
+           "pkv_prefill_even_workspace_bytes", "pkv_decode_attention_long",
            "pkv_decode_long_workspace_bytes", "pkv_probe_read", "pkv_scoring_route",
            "pkv_scoring_sweeps", "pkv_status_string"]
 
@@ -123,8 +124,9 @@ def load() -> ctypes.CDLL:
         lib.pkv_rotary_append.restype = ctypes.c_int
         lib.pkv_prefill_attention.argtypes = [vp] * 12 + [ctypes.c_size_t, vp]
         lib.pkv_prefill_attention.restype = ctypes.c_int
-        lib.pkv_prefill_workspace_bytes.argtypes = [vp]
-        lib.pkv_prefill_workspace_bytes.restype = ctypes.c_size_t
+        for size in (lib.pkv_prefill_workspace_bytes, lib.pkv_prefill_even_workspace_bytes):
+            size.argtypes = [vp]
+            size.restype = ctypes.c_size_t
         lib.pkv_decode_attention_long.argtypes = [vp] * 12 + [ctypes.c_size_t, vp]
         lib.pkv_decode_attention_long.restype = ctypes.c_int
         lib.pkv_decode_long_workspace_bytes.argtypes = [vp]
@@ -634,7 +636,7 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_len
                          os_[0], os_[1], os_[2])
     lib = load()
     if workspace is None:  # (a workspace that is handed over is checked by the call)
-        need = lib.pkv_prefill_workspace_bytes(desc)
+        need = (lib.pkv_prefill_even_workspace_bytes if seq_lens is None and q_start is None else lib.pkv_prefill_workspace_bytes)(desc)
         if need > 0:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     _call("pkv_prefill_attention", lib.pkv_prefill_attention, index, desc, q.data_ptr(), K_p, V_p,

@@ -680,6 +680,15 @@ ByLength by_length(const pkv_prefill_desc& d) {
   return {(int32_t)(wgs + extra), (int32_t)most, (int32_t)(wgs * most < 2 * extra ? wgs * most : 2 * extra)};
 }
 
+// Bytes of the ranges' results of a call with (ragged) or without lengths or starts.
+size_t workspace_bytes_of(const pkv_prefill_desc& d, bool ragged) {
+  const size_t row = (d.d + 2) * sizeof(float);
+  const ByLength shares = by_length(d);
+  if (ragged && shares.workgroups > 0) return (size_t)shares.slots * kRows * row;
+  const int S = parts(d);
+  return S == 1 ? 0 : (size_t)d.B * d.Hq * d.T * S * row;
+}
+
 double scale_of(const pkv_prefill_desc& d) { return d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.d); }
 
 int check_prefill_desc(const pkv_prefill_desc* desc) {
@@ -706,12 +715,14 @@ using namespace pkv;
 
 extern "C" {
 
+size_t pkv_prefill_even_workspace_bytes(const pkv_prefill_desc* desc) {
+  if (check_prefill_desc(desc) != PKV_OK) return 0;
+  return workspace_bytes_of(*desc, false);
+}
+
 size_t pkv_prefill_workspace_bytes(const pkv_prefill_desc* desc) {
   if (check_prefill_desc(desc) != PKV_OK) return 0;
-  // (which of the two a call takes depends on its arguments)
-  const int S = parts(*desc);
-  const size_t row = (desc->d + 2) * sizeof(float), even = S == 1 ? 0 : (size_t)desc->B * desc->Hq * desc->T * S * row;
-  const size_t ragged = (size_t)by_length(*desc).slots * kRows * row;
+  const size_t even = workspace_bytes_of(*desc, false), ragged = workspace_bytes_of(*desc, true);
   return even > ragged ? even : ragged;
 }
 
@@ -725,7 +736,7 @@ int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q, const voi
   if (!aligned(q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(seq_lens, 4) || !aligned(q_start, 4) ||
       !aligned(doc_start, 4) || !aligned(prefix_end, 4) || !aligned(slopes, 4) || !aligned(lse_out, 4))
     return PKV_ERR_INVALID_ARG;
-  const size_t need = pkv_prefill_workspace_bytes(desc);
+  const size_t need = workspace_bytes_of(d, seq_lens || q_start);
   if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PKV_ERR_WORKSPACE;
   PrefillArgs a;
   memset(&a, 0, sizeof(a));

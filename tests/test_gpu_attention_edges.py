@@ -124,3 +124,25 @@ def test_one_token_values_that_are_not_finite(gap, Hq, n, where, dtype):
             for h in (0, Hq - 1):
                 check(want[0].to(dtype), lse[B - 1, h][None], *want)
                 _check_infinite(out[B - 1, h][None], Vi[0, 0], seen, want)
+
+
+def test_prompts_of_one_length_need_no_workspace():
+    # rows enough for the device: without lengths nothing is cut, and a call takes no memory but its outputs'
+    B, H, T, d = 4, 8, 6200, 64
+    g = torch.Generator(device=DEV).manual_seed(6)
+    q, K, V = (torch.randn(B, H, T, d, generator=g, device=DEV).to(torch.bfloat16) for _ in range(3))
+    out, lse = torch.empty_like(q), torch.empty(B, H, T, device=DEV)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    binding.prefill_attention(q, K, V, out=out, lse=lse)
+    assert torch.cuda.max_memory_allocated() == before
+    binding.prefill_attention(q, K, V, out=out, lse=lse, workspace=torch.empty(0, dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+    ragged, _ = binding.prefill_attention(q, K, V, seq_lens=torch.full((B,), T, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    dist = T - 50 + torch.arange(50, device=DEV)[:, None] - torch.arange(T, device=DEV)
+    for b, h in ((0, 0), (B - 1, H - 1)):
+        want = attend(q[b, h, -50:], K[b, h], V[b, h], dist >= 0, dist, d ** -0.5, torch.bfloat16, weights=HALF_STEP[torch.bfloat16])
+        check(out[b, h, -50:], lse[b, h, -50:], *want)
+        check(ragged[b, h, -50:], None, *want)
