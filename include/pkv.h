@@ -636,8 +636,8 @@ size_t pkv_prefill_even_workspace_bytes(const pkv_prefill_desc* desc);
  *            be NULL when that is 0); contents irrelevant on entry, undefined
  *            on exit; concurrent calls need distinct ones.
  * Asynchronous on `stream`, never allocates.
- * Errors: PKV_ERR_INVALID_ARG (also a scale or cap whose quotient is not a
- * finite fp32), PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv > 128, B > 65535, N
+ * Errors: PKV_ERR_INVALID_ARG (also a scale, a cap, or a quotient of theirs
+ * that is not a finite fp32 in units of log2), PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv > 128, B > 65535, N
  * or T > 2^30, T * Hq/Hkv > 2^31 - 256, kv_st > 2^23, more than 2^24 - 1
  * workgroups of 128 rows), PKV_ERR_WORKSPACE, PKV_ERR_HIP.
  */
@@ -703,8 +703,8 @@ size_t pkv_decode_long_workspace_bytes(const pkv_decode_long_desc* desc);
  *             seen).
  * workspace   as pkv_decode_attention's, pkv_decode_long_workspace_bytes.
  * Asynchronous on `stream`, never allocates.
- * Errors: PKV_ERR_INVALID_ARG (also a scale or cap whose quotient is not a
- * finite fp32), PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv > 128, B or Hkv >
+ * Errors: PKV_ERR_INVALID_ARG (also a scale, a cap, or a quotient of theirs
+ * that is not a finite fp32 in units of log2), PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv > 128, B or Hkv >
  * 65535, B * Hq > 2^24 - 1, k_cap or c_st > 2^30, a pool of more than 2^32 - 1
  * rows), PKV_ERR_WORKSPACE, PKV_ERR_HIP.
  */

@@ -105,7 +105,8 @@ __device__ __forceinline__ bool finite(f32x4 v) {
 // |y| <= 0.36, where scores lie in earnest: y P(y^2), P of degree 3 (least squares reweighted to even out its relative error,
 // 5e-8 at most): a polynomial in x^2, five instructions, exact to a few 2^-24 of the score itself.
 // Beyond: cap - 2 cap / (1 + e^(2y)): two transcendental instructions, absolute error about 2^-23 cap (too much for small
-// scores), right at both ends (e^... = inf or 0).
+// scores), right at both ends (e^... = inf or 0).  This form alone where the polynomial's coefficients leave fp32 (scale / cap above
+// a million): products of any size then give the cap itself.
 struct Cap {
   float c0, c1, c2, c3;  // coefficients in x^2
   float limit;           // of |x|
@@ -123,6 +124,8 @@ inline Cap make_cap(double scale, double cap) {
     c.limit = (float)(0.36 / k);
     c.to_exponent = (float)(2.0 * 1.4426950408889634 * k);
     c.cap = (float)(cap * 1.4426950408889634);
+    if (!(fabsf(c.c1) < __builtin_inff() && fabsf(c.c2) < __builtin_inff() && fabsf(c.c3) < __builtin_inff()))
+      c.c1 = c.c2 = c.c3 = c.limit = 0.0f;
   }
   return c;
 }

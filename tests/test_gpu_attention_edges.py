@@ -146,3 +146,21 @@ def test_prompts_of_one_length_need_no_workspace():
         want = attend(q[b, h, -50:], K[b, h], V[b, h], dist >= 0, dist, d ** -0.5, torch.bfloat16, weights=HALF_STEP[torch.bfloat16])
         check(out[b, h, -50:], lse[b, h, -50:], *want)
         check(ragged[b, h, -50:], None, *want)
+
+
+@pytest.mark.parametrize("cap,scale", [(1e-8, None), (1e-12, None), (1e-30, None), (1e-37, None), (3e-5, 100.0)])
+def test_tiny_caps(cap, scale):
+    # scores are the cap or next to it: the polynomial's coefficients would not be fp32 numbers
+    d, T = 128, 70
+    g = torch.Generator(device=DEV).manual_seed(2)
+    q, K, V = (torch.randn(1, h, T, d, generator=g, device=DEV).to(torch.bfloat16) for h in (2, 1, 1))
+    out, lse = binding.prefill_attention(q, K, V, cap=cap, scale=scale, want_lse=True)
+    one, one_lse = binding.decode_attention_long(q[:, :, -1], K, V, torch.tensor([T], dtype=torch.int32, device=DEV), cap=cap, scale=scale,
+                                                 want_lse=True)
+    torch.cuda.synchronize()
+    dist = torch.arange(T, device=DEV)[:, None] - torch.arange(T, device=DEV)
+    for h in range(2):
+        args = (K[0, 0], V[0, 0], dist >= 0, dist, scale or d ** -0.5, torch.bfloat16, cap, None)
+        check(out[0, h], lse[0, h], *attend(q[0, h], *args, HALF_STEP[torch.bfloat16]))
+        want = attend(q[0, h], *args, HALF_STEP[torch.bfloat16] ** 2)
+        check(one[0, h][None], one_lse[0, h][None], *(x[-1:] for x in want))

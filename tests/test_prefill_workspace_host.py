@@ -42,3 +42,11 @@ def test_what_a_call_asks_for():
 
 def test_invalid_descriptors_have_none():
     assert _even(_desc(B=0)) == _even(_desc(d=96)) == _even(_desc(T=0)) == 0
+
+
+def test_descriptors_with_small_and_large_caps():
+    # what is refused has no workspace: a cap, or a quotient with the scale, that is no fp32 number
+    for cap in (1e-3, 1e-8, 1e-30, 1e-37, 1e6, 1e30):
+        assert _need(_desc(cap=cap)) > 0, cap
+    for cap in (1e-40, 3e38):
+        assert _need(_desc(cap=cap)) == 0, cap
