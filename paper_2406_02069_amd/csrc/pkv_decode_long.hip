@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
       float top = sc[0][0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e >> 2][e & 3]);
-      if (__any(top > m + Weight<T>::SLACK)) {
+      if (__any(top - m > Weight<T>::SLACK)) {  // (top - m, since m + SLACK is rounded where scores are large)
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float m1 = fmaxf(m, top);
@@ -340,11 +340,15 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const LongArgs a) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) o[i] *= f;
       }
-      const float ref = (m == kNone ? 0.0f : m) - Weight<T>::SHIFT;
+      const float ref = m == kNone ? 0.0f : m;
+      auto weight = [&](float x) {
+        const float below = x - ref;
+        return exp2_(Weight<T>::HALF ? below + Weight<T>::SHIFT : below);
+      };
       u32x4 hi, lo;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        const float p0 = exp2_(sc[e >> 2][e & 3] - ref), p1 = exp2_(sc[e >> 2][(e & 3) + 1] - ref);
+        const float p0 = weight(sc[e >> 2][e & 3]), p1 = weight(sc[e >> 2][(e & 3) + 1]);
         z += p0 + p1;
         const uint32_t u = pack2<T>(p0, p1);
         hi[e >> 1] = u;

@@ -164,3 +164,47 @@ def test_tiny_caps(cap, scale):
         check(out[0, h], lse[0, h], *attend(q[0, h], *args, HALF_STEP[torch.bfloat16]))
         want = attend(q[0, h], *args, HALF_STEP[torch.bfloat16] ** 2)
         check(one[0, h][None], one_lse[0, h][None], *(x[-1:] for x in want))
+
+
+LARGE = [(torch.float16, 100.25, 1.0), (torch.float16, 1432.0, 1.0), (torch.float16, 1432.0, 0.7), (torch.float16, 2864.0, 0.125),
+         (torch.float16, 9216.0, 1.0), (torch.bfloat16, 1432.0, 0.7), (torch.bfloat16, 1.39e6, 1.0), (torch.bfloat16, 1.39e9, 0.7)]
+
+
+def _large(n, d, size, dtype):
+    """(q [d], K [n, d], V [n, d], 0 and 1 [n]): scores of two sizes, both far from 0 and from one another."""
+    q, K = torch.full((d,), size, dtype=dtype, device=DEV), torch.full((n, d), size, dtype=dtype, device=DEV)
+    larger = (torch.arange(n, device=DEV) % 7 == 3) & (torch.arange(n, device=DEV) >= n // 2)
+    K[larger] = (K[larger].double() * 1.0625).to(dtype)
+    V = torch.randn(n, d, generator=torch.Generator(device=DEV).manual_seed(n), device=DEV).to(dtype)
+    return q, K, V, larger
+
+
+@pytest.mark.parametrize("dtype,size,scale", LARGE)
+@pytest.mark.parametrize("n", [40, 9001])
+def test_one_token_large_scores(n, dtype, size, scale):
+    # keys of the same score have the same weight, those of the larger one all of it
+    d = 64
+    q, K, V, larger = _large(n, d, size, dtype)
+    out, lse = binding.decode_attention_long(q.expand(1, 2, d), K[None, None], V[None, None], torch.tensor([n], dtype=torch.int32, device=DEV),
+                                             scale=scale, want_lse=True)
+    torch.cuda.synchronize()
+    want = attend(q[None] * 0, K, V, larger[None], torch.zeros(1, n, device=DEV), scale, dtype, weights=HALF_STEP[dtype] ** 2,
+                  small=2.0 ** -38 if dtype == torch.float16 else 0.0)
+    score = float(q.double() @ K[larger][0].double()) * scale
+    for h in range(2):
+        check(out[0, h][None], None, *want)
+        assert abs(float(lse[0, h]) - score - float(want[1])) <= 2.0 ** -20 * score
+
+
+def test_one_token_scores_a_step_apart():
+    # scores of 2^26 whose neighbours are 8 apart: averages of the values, whatever the last place says
+    d, n = 64, 600
+    q, K = torch.zeros(1, 1, d, device=DEV), torch.zeros(1, 1, n, d, device=DEV)
+    q[..., 1:17], K[..., 1:17], q[..., 0] = 2048, 2048, 4
+    K[..., 0] = 2 * (torch.arange(n, device=DEV) // 50 % 5)
+    V = torch.rand(1, 1, n, d, generator=torch.Generator(device=DEV).manual_seed(n), device=DEV) + 1
+    for dtype in (torch.float16, torch.bfloat16):
+        out, lse = binding.decode_attention_long(q.to(dtype), K.to(dtype), V.to(dtype), torch.tensor([n], dtype=torch.int32, device=DEV),
+                                                 scale=1.0, want_lse=True)
+        torch.cuda.synchronize()
+        assert 1 <= float(out.min()) and float(out.max()) <= 2 and abs(float(lse) - 2.0 ** 26 - 32) <= 64
