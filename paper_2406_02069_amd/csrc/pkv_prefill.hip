@@ -41,6 +41,9 @@ constexpr int kRows = 128;   // query rows of a workgroup
 constexpr int kKeys = 32;    // keys per step
 constexpr int kMaxParts = 64;  // ranges of keys
 constexpr int kLeastKeys = 768;  // of a range, about
+// References (log2) beyond which a score is rounded before it is compared with them: what one fma of scale and difference finds
+// left of a rounded product is as large as a step there, and would be a weight's exponent.
+constexpr float kLarge = 0x1p20f;
 
 struct PrefillArgs {
   const uint16_t *q, *K, *V;
@@ -297,6 +300,7 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
   const float slope = MODE == 1 && a.slopes ? a.slopes[h] * kLog2e : 0.0f;
 
   float m = kNone, z = 0.0f;
+  bool large = false;  // some reference is beyond kLarge
   f32x16 o[MB];
 #pragma unroll
   for (int i = 0; i < MB; ++i) o[i] = (f32x16)(0.0f);
@@ -371,7 +375,7 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, sc[e]);
     top *= f1;
-    if (__any(top > m + 6.0f)) {
+    if (__any(top - m > 6.0f)) {
       top = fmaxf(top, __shfl_xor(top, 32));
       const float m1 = fmaxf(m, top);
       const float f = m1 == kNone ? 1.0f : exp2_(m - m1);
@@ -379,13 +383,21 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
       z *= f;
 #pragma unroll
       for (int i = 0; i < MB; ++i) o[i] *= f;
+      large = __any(m != kNone && fabsf(m) > kLarge);
     }
-    const float ref = (m == kNone ? 0.0f : m) - SHIFT;
+    float ref = (m == kNone ? 0.0f : m) - SHIFT, factor = f1;
+    if (__builtin_expect(large, 0)) {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[e] = (sc[e] * f1 - (m == kNone ? 0.0f : m)) + SHIFT;
+      ref = 0.0f;
+      factor = 1.0f;
+    }
     u32x4 pf[2];
     float z0 = 0.0f, z1 = 0.0f;
 #pragma unroll
     for (int e = 0; e < 16; e += 2) {
-      const float p0 = exp2_(fmaf(sc[e], f1, -ref)), p1 = exp2_(fmaf(sc[e + 1], f1, -ref));
+      const float p0 = exp2_(fmaf(sc[e], factor, -ref)), p1 = exp2_(fmaf(sc[e + 1], factor, -ref));
       z0 += p0;
       z1 += p1;
       pf[e >> 3][(e >> 1) & 3] = pack2<T>(p0, p1);

@@ -208,3 +208,37 @@ def test_one_token_scores_a_step_apart():
                                                  scale=1.0, want_lse=True)
         torch.cuda.synchronize()
         assert 1 <= float(out.min()) and float(out.max()) <= 2 and abs(float(lse) - 2.0 ** 26 - 32) <= 64
+
+
+@pytest.mark.parametrize("dtype,size,scale", LARGE)
+@pytest.mark.parametrize("T,n,biased", [(40, 40, False), (300, 300, False), (5, 9001, False), (70, 70, True)])
+def test_prompt_large_scores(T, n, biased, dtype, size, scale):
+    # in rows that see both sizes of score, and in rows before them; with a bias too small to matter (the other form of the kernel)
+    d = 64
+    q, K, V, larger = _large(n, d, size, dtype)
+    sl = torch.full((2,), 2.0 ** -20, device=DEV) if biased else None
+    out, lse = binding.prefill_attention(q.expand(1, 2, T, d), K[None, None], V[None, None], scale=scale, slopes=sl,
+                                         q_start=torch.tensor([n - T], dtype=torch.int32, device=DEV), want_lse=True)
+    torch.cuda.synchronize()
+    seen = torch.arange(n, device=DEV) <= n - T + torch.arange(T, device=DEV)[:, None]
+    seen = torch.where((seen & larger).any(1, keepdim=True), seen & larger, seen)
+    want = attend(q.expand(T, d) * 0, K, V, seen, torch.zeros(T, n, device=DEV), scale, dtype,
+                  weights=HALF_STEP[dtype] + (2.0 ** -13 if biased else 0), small=2.0 ** -33 if dtype == torch.float16 else 0.0)
+    some = torch.where((seen & larger).any(1), K[larger][0].double() @ q.double(), K[0].double() @ q.double()) * scale
+    for h in range(2):
+        check(out[0, h], None, *want)
+        assert bool(((lse[0, h] - some - want[1]).abs() <= 2.0 ** -20 * some).all())
+
+
+def test_prompt_scores_a_step_apart():
+    # as for one token
+    d, n = 64, 600
+    q, K = torch.zeros(1, 1, n, d, device=DEV), torch.zeros(1, 1, n, d, device=DEV)
+    q[..., 1:17], K[..., 1:17], q[..., 0] = 2048, 2048, 4
+    K[..., 0] = 2 * (torch.arange(n, device=DEV) // 50 % 5)
+    V = torch.rand(1, 1, n, d, generator=torch.Generator(device=DEV).manual_seed(n), device=DEV) + 1
+    for dtype in (torch.float16, torch.bfloat16):
+        out, lse = binding.prefill_attention(q.to(dtype), K.to(dtype), V.to(dtype), scale=1.0, want_lse=True)
+        torch.cuda.synchronize()
+        assert 1 - 2.0 ** -6 <= float(out.min()) and float(out.max()) <= 2 + 2.0 ** -6
+        assert bool(((lse - 2.0 ** 26 - 16).abs() <= 64).all())
