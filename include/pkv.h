@@ -586,10 +586,13 @@ int pkv_rotary_append(const pkv_rotary_desc* desc, const void* q,
  * fp32 scores, sums and accumulation; the softmax weights are rounded to the
  * input's type for the product with V (fp16: those below 2^-22 of the row's
  * largest are off by up to 2^-33 of it).  Rows >= n_b of K and V are never
- * read.  A key that a query does not see has no influence on its row,
- * whatever it holds (NaN and infinities included).  Where a query sees values
- * of V that are not finite, that element of out is their sum: every weight is
- * positive, however small.
+ * read.  A key that a query does not see has no influence on its row beyond
+ * rounding, whatever it holds (NaN and infinities included).  Where a query
+ * sees values of V that are not finite, that element of out is their sum:
+ * every weight is positive, however small.
+ * The same call gives the same bits.  What a row is rounded to may depend on
+ * the call's other rows and sequences: ranges of keys go by all lengths, and
+ * rows of a tile are scaled anew together.
  */
 typedef struct {
   int32_t B, Hq, Hkv; /* Hq % Hkv == 0                                       */
@@ -637,9 +640,10 @@ size_t pkv_prefill_even_workspace_bytes(const pkv_prefill_desc* desc);
  *            on exit; concurrent calls need distinct ones.
  * Asynchronous on `stream`, never allocates.
  * Errors: PKV_ERR_INVALID_ARG (also a scale, a cap, or a quotient of theirs
- * that is not a finite fp32 in units of log2), PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv > 128, B > 65535, N
- * or T > 2^30, T * Hq/Hkv > 2^31 - 256, kv_st > 2^23, more than 2^24 - 1
- * workgroups of 128 rows), PKV_ERR_WORKSPACE, PKV_ERR_HIP.
+ * that is not a finite fp32 in units of log2), PKV_ERR_UNSUPPORTED (d not
+ * 64/128, Hq/Hkv > 128, B > 65535, N or T > 2^30, T * Hq/Hkv > 2^31 - 256,
+ * kv_st > 2^23, more than 2^24 - 1 workgroups of 128 rows),
+ * PKV_ERR_WORKSPACE, PKV_ERR_HIP.
  */
 int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q,
                           const void* K, const void* V,
@@ -656,7 +660,7 @@ int pkv_prefill_attention(const pkv_prefill_desc* desc, const void* q,
  * kept rows of a compression call: its idx_out), or j if positions is NULL;
  * the query's position is q_pos_b, or count_b - 1 if q_pos is NULL.  A row is
  * seen if 0 <= position <= q's and, with a window, position > q's - window.
- * Scores, softmax, lse and values that are not finite as
+ * Scores, softmax, lse, rounding and values that are not finite as
  * pkv_prefill_attention has them; the softmax weights keep 16 bits and more
  * (fp16: those below 2^-22 of the row's largest are off by up to 2^-38 of it).
  * A page number out of range makes its rows count as absent.
@@ -704,9 +708,9 @@ size_t pkv_decode_long_workspace_bytes(const pkv_decode_long_desc* desc);
  * workspace   as pkv_decode_attention's, pkv_decode_long_workspace_bytes.
  * Asynchronous on `stream`, never allocates.
  * Errors: PKV_ERR_INVALID_ARG (also a scale, a cap, or a quotient of theirs
- * that is not a finite fp32 in units of log2), PKV_ERR_UNSUPPORTED (d not 64/128, Hq/Hkv > 128, B or Hkv >
- * 65535, B * Hq > 2^24 - 1, k_cap or c_st > 2^30, a pool of more than 2^32 - 1
- * rows), PKV_ERR_WORKSPACE, PKV_ERR_HIP.
+ * that is not a finite fp32 in units of log2), PKV_ERR_UNSUPPORTED (d not
+ * 64/128, Hq/Hkv > 128, B or Hkv > 65535, B * Hq > 2^24 - 1, k_cap or c_st >
+ * 2^30, a pool of more than 2^32 - 1 rows), PKV_ERR_WORKSPACE, PKV_ERR_HIP.
  */
 int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q,
                               const void* K_cache, const void* V_cache,

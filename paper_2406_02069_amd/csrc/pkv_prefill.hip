@@ -653,11 +653,11 @@ int64_t row_tiles(const pkv_prefill_desc& d) { return ((int64_t)d.T * (d.Hq / d.
 
 int turn_of(const pkv_prefill_desc& d) { return d.d == 64 ? 1024 : 768; }  // workgroups that the device holds at a time
 
-// Ranges of keys per tile of rows, where all sequences are as long.  The device holds 768 workgroups at a time (1024 with d = 64): one range where the tiles alone
-// are as many, otherwise the fewest that fill (nearly) the largest share of one or two turns (300 rows of 50k keys, 28 heads:
-// 309 us in 11 ranges, 346 in 8, 361 in 12; 2048 rows of 64k keys, 512 tiles: 2.10 ms in 3, 2.20 undivided).  A range's result is
-// written and read again, 64 KB for 128 rows, so that none has fewer than 768 keys (4 x 64 rows of 3000 keys, 32 heads: 36 us with
-// 1000 keys a range, 48 with 256).
+// Ranges of keys per tile of rows, where all sequences are as long.  The device holds 768 workgroups at a time (1024 with d = 64):
+// one range where the tiles alone are as many, otherwise the fewest that fill (nearly) the largest share of one or two turns (300
+// rows of 50k keys, 28 heads: 309 us in 11 ranges, 346 in 8, 361 in 12; 2048 rows of 64k keys, 512 tiles: 2.10 ms in 3, 2.20
+// undivided).  A range's result is written and read again, 64 KB for 128 rows, so that none has fewer than 768 keys (4 x 64 rows of
+// 3000 keys, 32 heads: 36 us with 1000 keys a range, 48 with 256).  By N, not by what is seen: with a window the ranges are shorter.
 int parts(const pkv_prefill_desc& d) {
   const int64_t wgs = row_tiles(d) * d.B * d.Hkv, slots = turn_of(d);
   if (wgs >= slots) return 1;
