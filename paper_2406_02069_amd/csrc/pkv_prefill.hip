@@ -426,44 +426,61 @@ __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {
   for (int x = 0; x < MB * 16; ++x) naught[x & 3] = fmaf(o[x >> 4][x & 15], 0.0f, naught[x & 3]);
   const bool odd = lds_zeroed != 0 || (naught[0] + naught[1]) + (naught[2] + naught[3]) != 0.0f;
   if (__builtin_expect(__any(odd), 0)) {
-    f32x16 extra[MB];
+    // Sums of what is not finite: first of the steps that all rows see whole, by column, eight columns a lane; then of the others,
+    // which have left nothing in the results, row by row.
+    int id = threadIdx.x;
+    asm("" : "+v"(id));  // (nothing of this is kept in registers during the loop)
+    const int in_load = (id & 63) / PIECES, piece_at = 16 * (id % PIECES), upper_half = (id >> 5) & 1;
+    auto odd_part = [](float value) { return fabsf(value) < __builtin_inff() ? 0.0f : value; };
+    auto rows_of = [&](int k0) { return *reinterpret_cast<const u32x4*>(Vb + (int64_t)min(k0 + in_load, n - 1) * stride + piece_at); };
+    auto any_odd = [](u32x4 v) { return __ballot((not_finite<T>(v[0]) | not_finite<T>(v[1]) | not_finite<T>(v[2]) | not_finite<T>(v[3])) != 0); };
+    auto cut = [&](int st) { return st * kKeys < lo_g || st * kKeys + kKeys - 1 > hi_g; };
+    float all[8];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) extra[i] = (f32x16)(0.0f);
-    const int k_end = min(last_w + 1, step_end * kKeys);
+    for (int x = 0; x < 8; ++x) all[x] = 0.0f;
 #pragma unroll 1
-    for (int k0 = max(first_w, step_begin * kKeys); k0 < k_end; k0 += 4 * ROWS_PER_LOAD) {
+    for (int st = step_begin; st < step_end; ++st) {
+      if (cut(st)) continue;
       u32x4 v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = min(k0 + i * ROWS_PER_LOAD + lane / PIECES, k_end - 1);
-        v[i] = *reinterpret_cast<const u32x4*>(Vb + (int64_t)r * stride + 16 * (lane % PIECES));
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint64_t left = __ballot((not_finite<T>(v[i][0]) | not_finite<T>(v[i][1]) | not_finite<T>(v[i][2]) | not_finite<T>(v[i][3])) != 0);
 #pragma unroll 1
-        while (left != 0) {
-          const int in = __builtin_ctzll(left) / PIECES, k = k0 + i * ROWS_PER_LOAD + in;
-          left &= ~(((1ull << PIECES) - 1) << (in * PIECES));
-          if (k >= k_end) break;  // (the last row once more)
-          const bool sees = some && k >= seen.lo && k <= seen.hi;
-          const char* const from = Vb + (int64_t)k * stride + 8 * half;
+      for (int k0 = st * kKeys; k0 < st * kKeys + kKeys; k0 += 4 * ROWS_PER_LOAD) {
 #pragma unroll
-          for (int x = 0; x < MB * 4; ++x) {
-            const u32x2 u = *reinterpret_cast<const u32x2*>(from + 16 * x);
+        for (int i = 0; i < 4; ++i) v[i] = rows_of(k0 + i * ROWS_PER_LOAD);
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const float value = unpack<T>(u[y >> 1], y & 1);
-              extra[x >> 2][4 * (x & 3) + y] += sees && !(fabsf(value) < __builtin_inff()) ? value : 0.0f;
-            }
-          }
-        }
+        for (int i = 0; i < 4; ++i)
+          if (any_odd(v[i]))
+#pragma unroll
+            for (int x = 0; x < 8; ++x) all[x] += odd_part(unpack<T>(v[i][x >> 1], x & 1));
       }
     }
 #pragma unroll
-    for (int x = 0; x < MB * 16; ++x) {
-      const float e = extra[x >> 4][x & 15];
-      o[x >> 4][x & 15] = e == 0.0f ? o[x >> 4][x & 15] : e;
+    for (int x = 0; x < 8; ++x)
+      for (int across = PIECES; across < 64; across <<= 1) all[x] += __shfl_xor(all[x], across);
+#pragma unroll
+    for (int x = 0; x < MB * 4; ++x)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const float lower = __shfl(all[y], x), upper = __shfl(all[4 + y], x), e = upper_half ? upper : lower;
+        o[x >> 2][4 * (x & 3) + y] = e == 0.0f ? o[x >> 2][4 * (x & 3) + y] : e;
+      }
+#pragma unroll 1
+    for (int k0 = max(first_w, step_begin * kKeys) / ROWS_PER_LOAD * ROWS_PER_LOAD; k0 < min(last_w + 1, step_end * kKeys); k0 += ROWS_PER_LOAD) {
+      if (!cut(k0 / kKeys)) continue;
+      uint64_t left = any_odd(rows_of(k0));
+#pragma unroll 1
+      while (left != 0) {
+        const int in = __builtin_ctzll(left) / PIECES, k = k0 + in;
+        left &= ~(((1ull << PIECES) - 1) << (in * PIECES));
+        if (k >= n) break;  // (the last row once more)
+        const bool sees = some && k >= seen.lo && k <= seen.hi;
+        const char* const from = Vb + (int64_t)k * stride + 8 * upper_half;
+#pragma unroll
+        for (int x = 0; x < MB * 4; ++x) {
+          const u32x2 u = *reinterpret_cast<const u32x2*>(from + 16 * x);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) o[x >> 2][4 * (x & 3) + y] += sees ? odd_part(unpack<T>(u[y >> 1], y & 1)) : 0.0f;
+        }
+      }
     }
   }
 

@@ -242,3 +242,26 @@ def test_prompt_scores_a_step_apart():
         torch.cuda.synchronize()
         assert 1 - 2.0 ** -6 <= float(out.min()) and float(out.max()) <= 2 + 2.0 ** -6
         assert bool(((lse - 2.0 ** 26 - 16).abs() <= 64).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,n,d,window,every", [(300, 300, 128, 0, 3), (260, 700, 64, 150, 2), (33, 9001, 128, 0, 500), (500, 500, 64, 0, 0)])
+def test_prompt_many_values_that_are_not_finite(T, n, d, window, every, dtype):
+    # rows of V by the dozen, in steps that all rows see and at the masks' ends; every 0: all of V
+    g = torch.Generator(device=DEV).manual_seed(n)
+    q, K, V = (torch.randn(1, h, m, d, generator=g, device=DEV).to(dtype) for h, m in ((4, T), (1, n), (1, n)))
+    odd = torch.tensor([math.inf, -math.inf, math.nan], dtype=dtype, device=DEV)
+    which = torch.randint(0, 3, (n, d), generator=g, device=DEV)
+    hit = torch.rand(n, d, generator=g, device=DEV) < (1 if every == 0 else 0.02 / min(every, 3))
+    hit &= (torch.arange(n, device=DEV) % max(every, 1) == 0)[:, None]
+    which[:, :d // 2] = 0                                    # columns of positive infinities alone
+    V[0, 0] = torch.where(hit, odd[which], V[0, 0])
+    out, lse = binding.prefill_attention(q, K, V, q_start=torch.tensor([n - T], dtype=torch.int32, device=DEV), window=window, want_lse=True)
+    torch.cuda.synchronize()
+    dist = n - T + torch.arange(T, device=DEV)[:, None] - torch.arange(n, device=DEV)
+    seen = (dist >= 0) & (dist < (window or n))
+    for h in range(4):
+        want = attend(q[0, h], K[0, 0], V[0, 0].masked_fill(hit, 0), seen, dist, d ** -0.5, dtype, weights=HALF_STEP[dtype],
+                      small=2.0 ** -33 if dtype == torch.float16 else 0.0)
+        check(want[0].to(dtype), lse[0, h], *want)
+        _check_infinite(out[0, h], V[0, 0], seen, want)
