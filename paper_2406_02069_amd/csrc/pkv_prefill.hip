@@ -1,8 +1,9 @@
 // Attention of a prompt over its keys (include/pkv.h: pkv_prefill_attention).
 //
 // Bound by power: 4 d products-and-sums per (query row, seen key), for which K and V come from LDS, and an exponential.  A 32k
-// prompt (32 / 8 heads, d 128) takes 7.6 - 8.3 ms by card, 1.06 - 1.17 PFLOP/s of what it sees; the clock sinks to 1.6 - 1.8 GHz, at
-// which the matrix pipe is busy for 64 % of the cycles.  Forms that need fewer or more cycles took the same time within 3 %.
+// prompt (32 / 8 heads, d 128) takes 7.6 - 8.3 ms by card, 1.06 - 1.17 PFLOP/s of what it sees; the clock sinks to 1.6 GHz, at which
+// the matrix pipe is busy for 67 % of the cycles.  Forms that need fewer or more cycles took the same time within 3 %.  Capped and
+// biased scores and d 64 are bound by vector issue (73 - 82 % of the cycles, 16k prompts).
 // Work split: the G T query rows of a KV head (row = token * G + head, so that a tile of rows covers few tokens and hardly more
 // keys than its rows see) in tiles of 128, a workgroup of four waves each, 32 rows a wave; the longest tiles first.  Workgroups
 // that follow one another take different KV heads: with eight of them each XCD's cache holds the keys of one.  Few rows: the
@@ -17,8 +18,9 @@
 //   scores  S^T = K Q^T in v_mfma_f32_32x32x16: a lane ends with 16 keys of one query row (column), the other half of the wave
 //           with the other 16, so that maxima and sums stay in the lane.
 //   softmax a reference exponent per row, moved only when a score exceeds it by a factor of 2^6.  The weights are rounded to the
-//           type (as the result is), their sum is not.  fp16 weights carry a factor of 2^8, so that the type's last step is 2^-32
-//           of the reference; a factor of 2^13 and moves at 2^2 would make it 2^-37 and cost 1 - 7 % (1k prompt 31.4 -> 33.7 us).
+//           type (as the result is: the error against 64 bits grows by 2 - 17 %, of packed fp16 documents by a third), their sum
+//           is not.  fp16 weights carry a factor of 2^8, so that the type's last step is 2^-32 of the reference; a factor of 2^13
+//           and moves at 2^2 would make it 2^-37 and cost 1 - 7 % (1k prompt 31.4 -> 33.7 us).
 //   values  O^T += V^T P^T: the weights are in B's layout already if the 16 keys of a step are taken in the order in which the
 //           lanes hold them; V^T is read column-wise.
 // Masks leave each row an interval of keys.  Steps that no row of a wave sees are skipped, those that all of its rows see whole
