@@ -720,6 +720,306 @@ int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q,
                               void* out, float* lse_out, void* workspace,
                               size_t workspace_bytes, void* stream);
 
+/*
+ * ---- A cache in use ----
+ *
+ * What a decoder does with a cache besides pkv_decode_attention_long: several
+ * drafted tokens at once, a record of how much attention each row has had with
+ * the eviction of the rows that have had least, and steps that attend over a
+ * part of the rows only.
+ */
+
+/*
+ * Attention of drafted tokens over a cache: each sees the cache's rows and, of
+ * the drafted tokens, those that its bits name (in a tree of guesses: its
+ * ancestors and itself).  The drafted tokens are the last new_b rows of the
+ * cache, where pkv_rotary_append has put them: token t < new_b has row
+ * count_b - new_b + t.  What is verified is appended again behind the past rows
+ * (pkv_rotary_append with the smaller count), which overwrites the rest.
+ *   s_j = q_t . k_j * scale;  cap > 0: s_j = cap tanh(s_j / cap);
+ *   slopes: s_j -= slopes[h] |q_pos_t - position_j|
+ *   out[b][h][t] = sum_j softmax_j(s) V_j,  lse[b][h][t] = ln sum_j exp(s_j)
+ * over the rows 0 <= j < count_b, position_j >= 0, of which token t sees
+ *   of the past (j < count_b - new_b)  those with position_j <= q_pos_t,
+ *   of the drafted tokens u            those with bit u of tree[b][t] set
+ *                                      (tree NULL: u <= t),
+ *   with a window                      of these those with position_j > q_pos_t - window.
+ * Without positions and q_pos a past row's position is its number, a drafted
+ * token's count_b - new_b + the number of drafted tokens that it sees besides
+ * itself.  Rows t >= new_b, and rows that see nothing: zero and -inf.
+ * Scores, softmax and lse as pkv_decode_attention_long has them, the softmax
+ * weights' rounding too, or, where T * Hq/Hkv > 64, as pkv_prefill_attention
+ * has it.  A key that a token does not see has no influence on its row beyond
+ * rounding, whatever it holds; where a token sees values of V that are not
+ * finite, that element of out is their sum.  A page number out of range makes
+ * its rows count as absent.
+ */
+typedef struct {
+  int32_t B, Hq, Hkv; /* Hq % Hkv == 0                                       */
+  int32_t d;          /* 64 or 128                                           */
+  int32_t T;          /* drafted tokens per sequence in q, 1..256            */
+  int32_t k_cap;      /* rows per sequence the cache can hold                */
+  int32_t page_size;  /* 0: compact cache; > 0: paged                        */
+  int32_t num_pages;  /* paged: pages in the pool                            */
+  int32_t max_pages;  /* paged: entries per sequence in the block table,
+                         >= ceil(k_cap / page_size)                          */
+  int32_t dtype;      /* pkv_dtype                                           */
+  int32_t window;     /* 0: none; > 0                                        */
+  int32_t reserved;   /* must be 0                                           */
+  float scale;        /* > 0; 0: 1/sqrt(d)                                   */
+  float cap;          /* 0: none; > 0                                        */
+  int64_t q_sb, q_sh, q_st; /* element strides of q [B,Hq,T,d]               */
+  int64_t c_sb, c_sh, c_st; /* compact: of K_cache and V_cache
+                               [B,Hkv,k_cap,d]                               */
+  int64_t p_sb, p_sh;       /* of positions [B,Hkv,k_cap]                    */
+  int64_t o_sb, o_sh, o_st; /* of out [B,Hq,T,d]                             */
+} pkv_tree_desc;
+
+/*
+ * Bits of a tree of T drafted tokens (1..256) from each one's parent: a token
+ * in front of it, or -1 (it follows the past directly).
+ * parents  HOST int32[T].
+ * bits_out HOST int32[T][ceil(T / 32)], written: bit u % 32 of word u / 32 of
+ *          row t is set for t itself and its ancestors.
+ * HOST only, pure.  Errors: T outside 1..256, a parent outside -1..t-1, NULL
+ * -> PKV_ERR_INVALID_ARG (nothing is written).
+ */
+int pkv_tree_bits(int32_t T, const int32_t* parents, int32_t* bits_out);
+
+/* Bytes of DEVICE workspace that pkv_tree_attention needs for this shape; 0 if
+ * the descriptor is invalid.  HOST only, pure. */
+size_t pkv_tree_workspace_bytes(const pkv_tree_desc* desc);
+
+/*
+ * desc        HOST.  Strides are >= 0 and multiples of 8 (p_*: any >= 0).
+ * q, out      DEVICE, of the descriptor's type, 16-byte aligned; out overlaps
+ *             nothing, and its rows not one another.
+ * K_cache, V_cache
+ *             DEVICE, 16-byte aligned: compact with strides c_*, or pools
+ *             [num_pages,Hkv,page_size,d] contiguous.
+ * block_table DEVICE int32 [B,max_pages] contiguous (paged) or NULL.
+ * count       DEVICE int32 [B]: valid rows, drafted tokens included.
+ * new_lens    DEVICE int32 [B]: new_b, clamped to 0..T; NULL: T.
+ * tree        DEVICE int32 [B,T,ceil(T / 32)] contiguous, or NULL.
+ * positions, q_pos
+ *             DEVICE int32 [B,Hkv,k_cap] and int32 [B,T] contiguous, both or
+ *             neither NULL.  Any value.
+ * slopes      DEVICE fp32 [Hq] or NULL.  Finite.
+ * lse_out     DEVICE fp32 [B,Hq,T] contiguous, or NULL.
+ * workspace   DEVICE, 256-byte aligned, >= pkv_tree_workspace_bytes(desc) bytes
+ *             (may be NULL when that is 0); contents irrelevant on entry,
+ *             undefined on exit; concurrent calls need distinct ones.
+ * Asynchronous on `stream`, never allocates.
+ * Errors: PKV_ERR_INVALID_ARG (also a scale, a cap, or a quotient of theirs
+ * that is not a finite fp32 in units of log2), PKV_ERR_UNSUPPORTED (d not
+ * 64/128, T > 256, Hq/Hkv > 128, B or Hkv > 65535, B * Hq * T > 2^24 - 1,
+ * k_cap or c_st > 2^30, a pool of more than 2^32 - 1 rows), PKV_ERR_WORKSPACE,
+ * PKV_ERR_HIP.
+ */
+int pkv_tree_attention(const pkv_tree_desc* desc, const void* q,
+                       const void* K_cache, const void* V_cache,
+                       const int32_t* block_table, const int32_t* count,
+                       const int32_t* new_lens, const int32_t* tree,
+                       const int32_t* positions, const int32_t* q_pos,
+                       const float* slopes, void* out, float* lse_out,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * pkv_decode_attention_long that also adds each row's softmax weight, summed
+ * over the query heads of its KV head, to a running sum:
+ *   weights[b][g][j] += sum_{h of g} softmax_j(s_h)   for every seen row j.
+ * Nothing else of weights is written.  Same descriptor, results and errors.
+ * weights   DEVICE fp32 [B,Hkv,k_cap], 4-byte aligned, with element strides w_sb
+ *           and w_sh (>= 0; the sums of two heads do not overlap).
+ * workspace DEVICE, 256-byte aligned,
+ *           >= pkv_decode_accumulate_workspace_bytes(desc) bytes; contents
+ *           irrelevant on entry, undefined on exit; concurrent calls need
+ *           distinct ones.
+ * A weight is exact to a few 2^-24 of itself times its score's size, and the
+ * same call gives the same bits.
+ */
+size_t pkv_decode_accumulate_workspace_bytes(const pkv_decode_long_desc* desc);
+
+int pkv_decode_attention_accumulate(
+    const pkv_decode_long_desc* desc, const void* q, const void* K_cache,
+    const void* V_cache, const int32_t* block_table, const int32_t* count,
+    const int32_t* positions, const int32_t* q_pos, const float* slopes,
+    float* weights, int64_t w_sb, int64_t w_sh, void* out, float* lse_out,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction by those sums, in place: of n_b = count_b rows (clamped to
+ * 0..k_cap) of sequence b every KV head keeps min(n_b, budget).
+ * A row is protected if its position is >= 0 and either below `first` or among
+ * the last `recent` ones (> newest - recent, newest: the largest position of
+ * the head's rows).  Protected rows are kept first, then those with the largest
+ * weight; of equal weights (and of protected rows, should they be more than the
+ * budget) the lower row is kept.  A weight that is NaN counts as less than any
+ * other, and a row with a negative position as less than that.
+ * Rows behind the budget that are kept take the places of rows before it that
+ * are not: the i-th of the former moves to the i-th of the latter.  So a step
+ * that drops one row moves one at most, and rows are no longer in the order of
+ * their positions (no call here needs that).
+ */
+typedef struct {
+  int32_t B, Hkv;     /* >= 1                                                */
+  int32_t d;          /* 64 or 128                                           */
+  int32_t k_cap;      /* rows per sequence the cache can hold                */
+  int32_t page_size;  /* 0: compact cache; > 0: paged                        */
+  int32_t num_pages;  /* paged: pages in the pool                            */
+  int32_t max_pages;  /* paged: entries per sequence in the block table,
+                         >= ceil(k_cap / page_size)                          */
+  int32_t budget;     /* rows that stay, >= 1                                */
+  int32_t recent;     /* >= 0                                                */
+  int32_t first;      /* >= 0, first + recent <= budget                      */
+  int64_t c_sb, c_sh, c_st; /* compact: element strides of the caches        */
+  int64_t p_sb, p_sh;       /* of positions [B,Hkv,k_cap]                    */
+  int64_t w_sb, w_sh;       /* of weights                                    */
+  int64_t po_sb, po_sh;     /* of positions_out                              */
+  int64_t wo_sb, wo_sh;     /* of weights_out                                */
+} pkv_evict_desc;
+
+/* Bytes of DEVICE workspace that pkv_cache_evict needs for this shape; 0 if
+ * the descriptor is invalid.  HOST only, pure. */
+size_t pkv_evict_workspace_bytes(const pkv_evict_desc* desc);
+
+/*
+ * desc        HOST.
+ * K_cache, V_cache
+ *             DEVICE, rows of d 16-bit elements, 16-byte aligned, compact or
+ *             pools; rows behind the budget keep their content.  Pages that
+ *             two sequences (or places of a table) name are not for this call.
+ * block_table DEVICE int32 [B,max_pages] contiguous (paged) or NULL.  A page
+ *             number out of range: nothing is read or written through it, and
+ *             the position of a row that would have been moved there, or from
+ *             there, is -1 afterwards.
+ * count       DEVICE int32 [B].
+ * positions   DEVICE int32 [B,Hkv,k_cap].
+ * weights     DEVICE fp32 [B,Hkv,k_cap].
+ * positions_out, weights_out
+ *             DEVICE, as positions and weights, and may be these themselves
+ *             with the same strides: the kept rows' values, and -1 and 0 for
+ *             rows min(n_b, budget) .. n_b - 1.  Rows >= n_b are left as they
+ *             were.
+ * count_out   DEVICE int32 [B] or NULL, written: min(n_b, budget).  Overlaps
+ *             nothing.
+ * workspace   DEVICE, 256-byte aligned, >= pkv_evict_workspace_bytes(desc)
+ *             bytes; contents irrelevant on entry, undefined on exit;
+ *             concurrent calls need distinct ones.
+ * Asynchronous on `stream`, never allocates.
+ * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, B or Hkv >
+ * 65535, B * Hkv > 2^22, k_cap or c_st > 2^30, a pool of more than 2^32 - 1
+ * rows), PKV_ERR_WORKSPACE, PKV_ERR_HIP.
+ */
+int pkv_cache_evict(const pkv_evict_desc* desc, void* K_cache, void* V_cache,
+                    const int32_t* block_table, const int32_t* count,
+                    const int32_t* positions, const float* weights,
+                    int32_t* positions_out, float* weights_out,
+                    int32_t* count_out, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/*
+ * Steps that attend over a part of a whole cache: its rows in blocks, of which
+ * each KV head takes `most` by a bound on their scores.  Three calls: bounds of
+ * new rows, selection, attention over the blocks.
+ */
+typedef struct {
+  int32_t B, Hq, Hkv; /* Hq % Hkv == 0 (pkv_block_bounds: Hq is not used)    */
+  int32_t d;          /* 64 or 128                                           */
+  int32_t k_cap;      /* rows per sequence the cache can hold                */
+  int32_t page_size;  /* 0: compact cache; > 0: paged                        */
+  int32_t num_pages;  /* paged: pages in the pool                            */
+  int32_t max_pages;  /* paged: entries per sequence in the block table,
+                         >= ceil(k_cap / page_size)                          */
+  int32_t dtype;      /* pkv_dtype                                           */
+  int32_t block;      /* rows of a block: 16, 32, 64, 128 or 256             */
+  int32_t most;       /* blocks of a head that are taken, >= 1               */
+  int32_t first;      /* blocks at the beginning that are taken in any case  */
+  int32_t recent;     /* and at the end; both >= 0, together <= most         */
+  int32_t reserved;   /* must be 0                                           */
+  float scale;        /* > 0; 0: 1/sqrt(d)                                   */
+  float cap;          /* 0: none; > 0                                        */
+  int64_t q_sb, q_sh;       /* element strides of q [B,Hq,d]                 */
+  int64_t c_sb, c_sh, c_st; /* compact: of K_cache and V_cache
+                               [B,Hkv,k_cap,d]                               */
+  int64_t b_sb, b_sh;       /* of bounds
+                               [B,Hkv,ceil(k_cap / block),2,d]               */
+} pkv_block_desc;
+
+/*
+ * Least and greatest value of each channel of K over the rows of a block: of
+ * those blocks that hold any of the last new_b rows, from all of their rows <
+ * n_b = count_b (clamped to 0..k_cap).
+ *   bounds[b][g][blk][0][i] = min_j K_ji, bounds[b][g][blk][1][i] = max_j K_ji
+ * exactly.  A channel of a block in which some value is NaN: -inf and +inf.
+ * Rows on pages that are out of range are left out; a block without rows is 0.
+ * Nothing else of bounds is written.
+ * desc        HOST.  B, Hkv, d, k_cap, pages, dtype, block, c_* and b_* are used.
+ * K_cache     DEVICE, 16-byte aligned, compact or pool.
+ * block_table DEVICE int32 [B,max_pages] contiguous (paged) or NULL.
+ * count       DEVICE int32 [B].
+ * new_lens    DEVICE int32 [B]: new_b, clamped to 0..n_b; NULL: n_b (all).
+ * bounds      DEVICE, of the descriptor's type, 16-byte aligned; strides
+ *             multiples of 8, the last three dimensions contiguous.
+ * Asynchronous on `stream`, needs no workspace, never allocates.
+ * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, block none of
+ * the above, B or Hkv > 65535, B * Hkv > 2^22, k_cap or c_st > 2^30, a pool of
+ * more than 2^32 - 1 rows), PKV_ERR_HIP.
+ */
+int pkv_block_bounds(const pkv_block_desc* desc, const void* K_cache,
+                     const int32_t* block_table, const int32_t* count,
+                     const int32_t* new_lens, void* bounds, void* stream);
+
+/*
+ * The blocks a step takes.  The score of block blk of KV head g,
+ *   sum_{h of g} sum_i max(q_hi bounds[..][0][i], q_hi bounds[..][1][i]),
+ * bounds the sum of the heads' products with any of the block's keys from
+ * above.  It is formed in 64 bits and rounded to fp32 once; one that is NaN
+ * counts as +inf.  Of the ceil(n_b / block) blocks the first `first` and the
+ * last `recent` are taken, then those with the largest scores (of equal ones
+ * the lower block) until there are `most`.
+ * desc       HOST.  B, Hq, Hkv, d, k_cap, dtype, block, most, first, recent, q_*
+ *            and b_* are used (cap and scale do not change the order).
+ * q          DEVICE, of the descriptor's type, 16-byte aligned.  Strides are
+ *            multiples of 8.
+ * bounds     DEVICE, as pkv_block_bounds writes them.
+ * count      DEVICE int32 [B].
+ * blocks_out DEVICE int32 [B,Hkv,most] contiguous, written: ascending, -1 behind.
+ * scores_out DEVICE fp32 [B,Hkv,ceil(k_cap / block)] contiguous or NULL: the
+ *            scores; written below ceil(n_b / block).
+ * workspace  DEVICE, 256-byte aligned, >= pkv_block_select_workspace_bytes(desc)
+ *            bytes; contents irrelevant on entry, undefined on exit; concurrent
+ *            calls need distinct ones.
+ * Asynchronous on `stream`, never allocates.
+ * Errors: as pkv_block_bounds, PKV_ERR_UNSUPPORTED also Hq/Hkv > 128,
+ * PKV_ERR_WORKSPACE.
+ */
+size_t pkv_block_select_workspace_bytes(const pkv_block_desc* desc);
+
+int pkv_block_select(const pkv_block_desc* desc, const void* q,
+                     const void* bounds, const int32_t* count,
+                     int32_t* blocks_out, float* scores_out, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/*
+ * pkv_decode_attention_long over the rows of the listed blocks alone, without
+ * positions, window and slopes.  Of a list the first min(most, ceil(n_b /
+ * block)) entries are looked at; one outside 0 .. ceil(n_b / block) - 1 has no
+ * rows, and one that is named twice counts twice.
+ * desc        HOST.  first, recent and b_* are not used.
+ * blocks      DEVICE int32 [B,Hkv,most] contiguous, in any order.
+ * Everything else, and the errors, as pkv_decode_attention_long; most * block >
+ * 2^30 -> PKV_ERR_UNSUPPORTED.
+ */
+size_t pkv_decode_blocks_workspace_bytes(const pkv_block_desc* desc);
+
+int pkv_decode_attention_blocks(const pkv_block_desc* desc, const void* q,
+                                const void* K_cache, const void* V_cache,
+                                const int32_t* block_table,
+                                const int32_t* count, const int32_t* blocks,
+                                void* out, float* lse_out, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
 /* Static, NUL-terminated description of a pkv_status value.  HOST only. */
 const char* pkv_status_string(int status);
 

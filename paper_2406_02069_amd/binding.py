@@ -31,7 +31,10 @@ EXPORTS = ["pkv_budgets", "pkv_workspace_bytes", "pkv_compress_layer", "pkv_comp
            "pkv_budgets_schedule", "pkv_attention_recall", "pkv_decode_attention", "pkv_decode_workspace_bytes", "pkv_decode_attention_layers",
            "pkv_decode_layers_workspace_bytes", "pkv_rotary_frequencies", "pkv_rotary_append", "pkv_prefill_attention", "pkv_prefill_workspace_bytes",
            "pkv_prefill_even_workspace_bytes", "pkv_decode_attention_long",
-           "pkv_decode_long_workspace_bytes", "pkv_probe_read", "pkv_scoring_route",
+           "pkv_decode_long_workspace_bytes", "pkv_tree_bits", "pkv_tree_workspace_bytes", "pkv_tree_attention",
+           "pkv_decode_accumulate_workspace_bytes", "pkv_decode_attention_accumulate", "pkv_evict_workspace_bytes", "pkv_cache_evict",
+           "pkv_block_bounds", "pkv_block_select_workspace_bytes", "pkv_block_select", "pkv_decode_blocks_workspace_bytes",
+           "pkv_decode_attention_blocks", "pkv_probe_read", "pkv_scoring_route",
            "pkv_scoring_sweeps", "pkv_status_string"]
 
 
@@ -73,6 +76,26 @@ class DecodeLongDesc(ctypes.Structure):
                                               "window")] + \
                [("scale", ctypes.c_float), ("cap", ctypes.c_float)] + \
                [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "c_sb", "c_sh", "c_st", "p_sb", "p_sh")]
+
+
+class TreeDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "T", "k_cap", "page_size", "num_pages", "max_pages", "dtype",
+                                              "window", "reserved")] + \
+               [("scale", ctypes.c_float), ("cap", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "q_st", "c_sb", "c_sh", "c_st", "p_sb", "p_sh", "o_sb", "o_sh", "o_st")]
+
+
+class EvictDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hkv", "d", "k_cap", "page_size", "num_pages", "max_pages", "budget", "recent",
+                                              "first")] + \
+               [(n, ctypes.c_int64) for n in ("c_sb", "c_sh", "c_st", "p_sb", "p_sh", "w_sb", "w_sh", "po_sb", "po_sh", "wo_sb", "wo_sh")]
+
+
+class BlockDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "k_cap", "page_size", "num_pages", "max_pages", "dtype", "block",
+                                              "most", "first", "recent", "reserved")] + \
+               [("scale", ctypes.c_float), ("cap", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "c_sb", "c_sh", "c_st", "b_sb", "b_sh")]
 
 
 class PagedDesc(ctypes.Structure):
@@ -131,6 +154,17 @@ def load() -> ctypes.CDLL:
         lib.pkv_decode_attention_long.restype = ctypes.c_int
         lib.pkv_decode_long_workspace_bytes.argtypes = [vp]
         lib.pkv_decode_long_workspace_bytes.restype = ctypes.c_size_t
+        lib.pkv_tree_bits.argtypes = [i32, vp, vp]
+        lib.pkv_tree_attention.argtypes = [vp] * 14 + [ctypes.c_size_t, vp]
+        lib.pkv_decode_attention_accumulate.argtypes = [vp] * 10 + [ctypes.c_int64] * 2 + [vp] * 3 + [ctypes.c_size_t, vp]
+        lib.pkv_cache_evict.argtypes = [vp] * 11 + [ctypes.c_size_t, vp]
+        lib.pkv_block_bounds.argtypes = [vp] * 7
+        lib.pkv_block_select.argtypes = [vp] * 7 + [ctypes.c_size_t, vp]
+        lib.pkv_decode_attention_blocks.argtypes = [vp] * 10 + [ctypes.c_size_t, vp]
+        for size in (lib.pkv_tree_workspace_bytes, lib.pkv_decode_accumulate_workspace_bytes, lib.pkv_evict_workspace_bytes,
+                     lib.pkv_block_select_workspace_bytes, lib.pkv_decode_blocks_workspace_bytes):
+            size.argtypes = [vp]
+            size.restype = ctypes.c_size_t
         lib.pkv_status_string.argtypes = [ctypes.c_int]
         lib.pkv_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -457,10 +491,13 @@ DTYPES = {torch.bfloat16: 0, torch.float16: 1}            # pkv_dtype
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}            # pkv_rotary_layout
 ROTARY_SCALINGS = {"plain": 0, "linear": 1, "bands": 2, "ramp": 3}
 
-# RotaryDesc, PrefillDesc and DecodeLongDesc as bytes
+# The descriptors as bytes
 _pack_rotary = struct.Struct("12ifi17q").pack
 _pack_prefill = struct.Struct("8i2f9q").pack
 _pack_decode_long = struct.Struct("10i2f7q").pack
+_pack_tree = struct.Struct("12i2f11q").pack
+_pack_evict = struct.Struct("10i11q").pack
+_pack_block = struct.Struct("14i2f7q").pack
 
 _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
@@ -544,9 +581,14 @@ def _workspace(t: Optional[torch.Tensor], index: int):
 
 def _row_positions(t: torch.Tensor, name: str, B: int, Hkv: int, k_cap: int, index: int):
     """(address, strides) of int32 positions [B, Hkv, at least k_cap] of a cache's rows."""
+    return _row_values(t, name, torch.int32, B, Hkv, k_cap, index)
+
+
+def _row_values(t: torch.Tensor, name: str, dtype, B: int, Hkv: int, k_cap: int, index: int):
+    """(address, strides) of values [B, Hkv, at least k_cap] of a cache's rows."""
     if t.dim() != 3 or t.shape[2] < k_cap:
         raise ValueError(f"{name}: need [B, Hkv, k_cap] or more")
-    return _need(t, name, torch.int32, (B, Hkv, t.shape[2]), index, False), t.stride()
+    return _need(t, name, dtype, (B, Hkv, t.shape[2]), index, False), t.stride()
 
 
 def rotary_frequencies(rot: int, scaling: str = "plain", base: float = 10000.0, factor: float = 1.0,
@@ -686,6 +728,215 @@ def decode_attention_long(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch
           _need(count, "count", torch.int32, (B,), index), pos_p,
           None if q_pos is None else _need(q_pos, "q_pos", torch.int32, (B,), index),
           None if slopes is None else _need(slopes, "slopes", torch.float32, (Hq,), index),
+          _need(out, "out", dtype, (B, Hq, d), index), None if lse is None else _need(lse, "lse", torch.float32, (B, Hq), index),
+          *_workspace(workspace, index), _stream_of(index))
+    return out, lse
+
+
+def _head_strides(q: torch.Tensor):
+    """The strides of a 3-d tensor; where they keep no alignment, 0 for dimensions of one element."""
+    st = q.stride()
+    return [x if n > 1 else 0 for n, x in zip(q.shape, st)] if (st[0] | st[1]) & 7 else st
+
+
+def _own_workspace(need: int, like: torch.Tensor) -> Optional[torch.Tensor]:
+    """A workspace of `need` bytes on the device of `like`.  (One that is handed over is checked by the call.)"""
+    return torch.empty(need, dtype=torch.uint8, device=like.device) if need > 0 else None
+
+
+def tree_bits(parents: Sequence[int], device=None) -> torch.Tensor:
+    """pkv_tree_bits: int32 [T, ceil(T / 32)] from the drafted tokens' parents (-1: the last token of the past)."""
+    T = len(parents)
+    words = (T + 31) // 32
+    out = (ctypes.c_int32 * max(T * words, 1))()
+    rc = load().pkv_tree_bits(T, (ctypes.c_int32 * max(T, 1))(*parents), out)
+    if rc != OK:
+        raise PkvError(rc, "pkv_tree_bits")
+    return torch.tensor(list(out), dtype=torch.int32, device=device).view(T, words)
+
+
+def tree_attention(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch.Tensor, count: torch.Tensor,
+                   tree: Optional[torch.Tensor] = None, new_lens: Optional[torch.Tensor] = None,
+                   block_table: Optional[torch.Tensor] = None, k_cap: Optional[int] = None,
+                   positions: Optional[torch.Tensor] = None, q_pos: Optional[torch.Tensor] = None,
+                   slopes: Optional[torch.Tensor] = None, cap: float = 0.0, window: int = 0, scale: Optional[float] = None,
+                   want_lse: bool = False, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None):
+    """pkv_tree_attention on the current stream.  q [B,Hq,T,d]: drafted tokens, the last new_lens[b] (T) of the cache's count[b]
+    rows; tree int32 [B,T,ceil(T / 32)]: which of them each sees (None: those up to itself); caches as in decode_attention_long;
+    positions int32 [B,Hkv,>= k_cap] with q_pos int32 [B,T]; slopes fp32 [Hq].
+    Returns (out [B,Hq,T,d] of q's type, lse fp32 [B,Hq,T] or None)."""
+    code, index = _gpu(q, "q", 4)
+    dtype = q.dtype
+    B, Hq, T, d = q.shape
+    if K_cache.dim() != 4:
+        raise ValueError("K_cache: need four dimensions")
+    Hkv = K_cache.shape[1]
+    cache, K_p, V_p, table_p = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, index)
+    pos_p, ps = (None, (0, 0)) if positions is None else _row_positions(positions, "positions", B, Hkv, cache[0], index)
+    if out is None:
+        out = torch.empty((B, Hq, T, d), dtype=dtype, device=q.device)
+    out_p, qs, os_ = _need(out, "out", dtype, (B, Hq, T, d), index, False), _strides(q), _strides(out)
+    if want_lse and lse is None:
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device)
+    desc = _pack_tree(B, Hq, Hkv, d, T, cache[0], cache[1], cache[2], cache[3], code, window, 0, _scale(scale), cap,
+                      qs[0], qs[1], qs[2], cache[4], cache[5], cache[6], ps[0], ps[1], os_[0], os_[1], os_[2])
+    lib = load()
+    if workspace is None:
+        workspace = _own_workspace(lib.pkv_tree_workspace_bytes(desc), q)
+    _call("pkv_tree_attention", lib.pkv_tree_attention, index, desc, q.data_ptr(), K_p, V_p, table_p,
+          _need(count, "count", torch.int32, (B,), index),
+          None if new_lens is None else _need(new_lens, "new_lens", torch.int32, (B,), index),
+          None if tree is None else _need(tree, "tree", torch.int32, (B, T, (T + 31) // 32), index),
+          pos_p, None if q_pos is None else _need(q_pos, "q_pos", torch.int32, (B, T), index),
+          None if slopes is None else _need(slopes, "slopes", torch.float32, (Hq,), index),
+          out_p, None if lse is None else _need(lse, "lse", torch.float32, (B, Hq, T), index),
+          *_workspace(workspace, index), _stream_of(index))
+    return out, lse
+
+
+def decode_attention_accumulate(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch.Tensor, count: torch.Tensor,
+                                weights: torch.Tensor, block_table: Optional[torch.Tensor] = None, k_cap: Optional[int] = None,
+                                positions: Optional[torch.Tensor] = None, q_pos: Optional[torch.Tensor] = None,
+                                slopes: Optional[torch.Tensor] = None, cap: float = 0.0, window: int = 0,
+                                scale: Optional[float] = None, want_lse: bool = False, out: Optional[torch.Tensor] = None,
+                                lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """pkv_decode_attention_accumulate on the current stream: decode_attention_long, and weights fp32 [B,Hkv,>= k_cap] +=
+    each row's softmax weights, summed over the query heads of its KV head.  Returns (out, lse or None)."""
+    code, index = _gpu(q, "q", 3)
+    dtype = q.dtype
+    B, Hq, d = q.shape
+    if K_cache.dim() != 4:
+        raise ValueError("K_cache: need four dimensions")
+    Hkv = K_cache.shape[1]
+    cache, K_p, V_p, table_p = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, index)
+    pos_p, ps = (None, (0, 0)) if positions is None else _row_positions(positions, "positions", B, Hkv, cache[0], index)
+    w_p, ws = _row_values(weights, "weights", torch.float32, B, Hkv, cache[0], index)
+    if out is None:
+        out = torch.empty((B, Hq, d), dtype=dtype, device=q.device)
+    if want_lse and lse is None:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+    qs = _head_strides(q)
+    desc = _pack_decode_long(B, Hq, Hkv, d, cache[0], cache[1], cache[2], cache[3], code, window, _scale(scale), cap,
+                             qs[0], qs[1], cache[4], cache[5], cache[6], ps[0], ps[1])
+    lib = load()
+    if workspace is None:
+        workspace = _own_workspace(lib.pkv_decode_accumulate_workspace_bytes(desc), q)
+    _call("pkv_decode_attention_accumulate", lib.pkv_decode_attention_accumulate, index, desc, q.data_ptr(), K_p, V_p, table_p,
+          _need(count, "count", torch.int32, (B,), index), pos_p,
+          None if q_pos is None else _need(q_pos, "q_pos", torch.int32, (B,), index),
+          None if slopes is None else _need(slopes, "slopes", torch.float32, (Hq,), index), w_p, ws[0], ws[1],
+          _need(out, "out", dtype, (B, Hq, d), index), None if lse is None else _need(lse, "lse", torch.float32, (B, Hq), index),
+          *_workspace(workspace, index), _stream_of(index))
+    return out, lse
+
+
+def cache_evict(K_cache: torch.Tensor, V_cache: torch.Tensor, count: torch.Tensor, positions: torch.Tensor, weights: torch.Tensor,
+                budget: int, recent: int = 0, first: int = 0, block_table: Optional[torch.Tensor] = None,
+                k_cap: Optional[int] = None, positions_out: Optional[torch.Tensor] = None,
+                weights_out: Optional[torch.Tensor] = None, count_out: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """pkv_cache_evict on the current stream: of each head's count[b] rows `budget` stay, by weights fp32 [B,Hkv,>= k_cap], with
+    the positions int32 [B,Hkv,>= k_cap] below `first` and the last `recent` ones.  K_cache, V_cache (bf16 or fp16; compact or
+    pools) change in place; positions_out and weights_out are positions and weights themselves unless given.
+    Returns count_out int32 [B]."""
+    _, index = _gpu(K_cache, "K_cache", 4)
+    B, Hkv, d = count.shape[0] if count.dim() == 1 else -1, K_cache.shape[1], K_cache.shape[3]
+    cache, K_p, V_p, table_p = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, K_cache.dtype, index)
+    p_p, ps = _row_positions(positions, "positions", B, Hkv, cache[0], index)
+    w_p, ws = _row_values(weights, "weights", torch.float32, B, Hkv, cache[0], index)
+    po_p, pos_ = (p_p, ps) if positions_out is None else _row_positions(positions_out, "positions_out", B, Hkv, cache[0], index)
+    wo_p, wos = (w_p, ws) if weights_out is None else _row_values(weights_out, "weights_out", torch.float32, B, Hkv, cache[0], index)
+    if count_out is None:
+        count_out = torch.empty_like(count)
+    desc = _pack_evict(B, Hkv, d, cache[0], cache[1], cache[2], cache[3], budget, recent, first, cache[4], cache[5], cache[6],
+                       ps[0], ps[1], ws[0], ws[1], pos_[0], pos_[1], wos[0], wos[1])
+    lib = load()
+    if workspace is None:
+        workspace = _own_workspace(lib.pkv_evict_workspace_bytes(desc), K_cache)
+    _call("pkv_cache_evict", lib.pkv_cache_evict, index, desc, K_p, V_p, table_p, _need(count, "count", torch.int32, (B,), index),
+          p_p, w_p, po_p, wo_p, _need(count_out, "count_out", torch.int32, (B,), index), *_workspace(workspace, index), _stream_of(index))
+    return count_out
+
+
+def _bounds_of(bounds: torch.Tensor, B: int, Hkv: int, blocks: int, d: int, dtype, index: int):
+    """(address, strides of the first two dimensions) of bounds [B, Hkv, at least `blocks`, 2, d]."""
+    if bounds.dim() != 5 or bounds.shape[2] < blocks or (bounds.numel() and not bounds[0, 0].is_contiguous()):
+        raise ValueError("bounds: need [B, Hkv, ceil(k_cap / block) or more, 2, d] with the last three dimensions contiguous")
+    st = bounds.stride()
+    return _need(bounds, "bounds", dtype, (B, Hkv, bounds.shape[2], 2, d), index, False), (st[0] if B > 1 else 0, st[1] if Hkv > 1 else 0)
+
+
+def block_bounds(K_cache: torch.Tensor, count: torch.Tensor, bounds: torch.Tensor, block: int,
+                 new_lens: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
+                 k_cap: Optional[int] = None) -> torch.Tensor:
+    """pkv_block_bounds on the current stream: bounds [B,Hkv,>= ceil(k_cap / block),2,d] of K's type, of the blocks that hold any of
+    the last new_lens[b] (all) of count[b] rows.  Returns bounds."""
+    code, index = _gpu(K_cache, "K_cache", 4)
+    B, Hkv, d = count.shape[0] if count.dim() == 1 else -1, K_cache.shape[1], K_cache.shape[3]
+    cache, K_p, _, table_p = _cache_layout(K_cache, K_cache, block_table, k_cap, B, Hkv, d, K_cache.dtype, index)
+    b_p, bs = _bounds_of(bounds, B, Hkv, -(-cache[0] // block) if block > 0 else 1, d, K_cache.dtype, index)
+    desc = _pack_block(B, Hkv, Hkv, d, cache[0], cache[1], cache[2], cache[3], code, block, 1, 0, 0, 0, 0.0, 0.0, 0, 0,
+                       cache[4], cache[5], cache[6], bs[0], bs[1])
+    _call("pkv_block_bounds", load().pkv_block_bounds, index, desc, K_p, table_p, _need(count, "count", torch.int32, (B,), index),
+          None if new_lens is None else _need(new_lens, "new_lens", torch.int32, (B,), index), b_p, _stream_of(index))
+    return bounds
+
+
+def block_select(q: torch.Tensor, bounds: torch.Tensor, count: torch.Tensor, block: int, most: int, first: int = 0, recent: int = 0,
+                 k_cap: Optional[int] = None, blocks_out: Optional[torch.Tensor] = None, scores: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """pkv_block_select on the current stream.  q [B,Hq,d]; bounds as block_bounds keeps them; k_cap: rows that the cache can hold
+    (as many as bounds has blocks for); scores fp32 [B,Hkv,ceil(k_cap / block)] are written if given.
+    Returns blocks_out int32 [B,Hkv,most]: ascending, -1 behind."""
+    code, index = _gpu(q, "q", 3)
+    B, Hq, d = q.shape
+    if bounds.dim() != 5:
+        raise ValueError("bounds: need five dimensions")
+    Hkv = bounds.shape[1]
+    if k_cap is None:
+        k_cap = bounds.shape[2] * block
+    blocks = -(-k_cap // block) if block > 0 else 1
+    b_p, bs = _bounds_of(bounds, B, Hkv, blocks, d, q.dtype, index)
+    if blocks_out is None:
+        blocks_out = torch.empty((B, Hkv, most), dtype=torch.int32, device=q.device)
+    qs = _head_strides(q)
+    desc = _pack_block(B, Hq, Hkv, d, k_cap, 0, 0, 0, code, block, most, first, recent, 0, 0.0, 0.0, qs[0], qs[1], 0, 0, 0, bs[0], bs[1])
+    lib = load()
+    if workspace is None:
+        workspace = _own_workspace(lib.pkv_block_select_workspace_bytes(desc), q)
+    _call("pkv_block_select", lib.pkv_block_select, index, desc, q.data_ptr(), b_p, _need(count, "count", torch.int32, (B,), index),
+          _need(blocks_out, "blocks_out", torch.int32, (B, Hkv, most), index),
+          None if scores is None else _need(scores, "scores", torch.float32, (B, Hkv, blocks), index),
+          *_workspace(workspace, index), _stream_of(index))
+    return blocks_out
+
+
+def decode_attention_blocks(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch.Tensor, count: torch.Tensor, blocks: torch.Tensor,
+                            block: int, block_table: Optional[torch.Tensor] = None, k_cap: Optional[int] = None, cap: float = 0.0,
+                            scale: Optional[float] = None, want_lse: bool = False, out: Optional[torch.Tensor] = None,
+                            lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """pkv_decode_attention_blocks on the current stream: decode_attention_long over the rows of blocks int32 [B,Hkv,most] (of
+    `block` rows each).  Returns (out [B,Hq,d] of q's type, lse fp32 [B,Hq] or None)."""
+    code, index = _gpu(q, "q", 3)
+    dtype = q.dtype
+    B, Hq, d = q.shape
+    if K_cache.dim() != 4 or blocks.dim() != 3:
+        raise ValueError("need K_cache with four dimensions and blocks with three")
+    Hkv, most = K_cache.shape[1], blocks.shape[2]
+    cache, K_p, V_p, table_p = _cache_layout(K_cache, V_cache, block_table, k_cap, B, Hkv, d, dtype, index)
+    if out is None:
+        out = torch.empty((B, Hq, d), dtype=dtype, device=q.device)
+    if want_lse and lse is None:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+    qs = _head_strides(q)
+    desc = _pack_block(B, Hq, Hkv, d, cache[0], cache[1], cache[2], cache[3], code, block, most, 0, 0, 0, _scale(scale), cap,
+                       qs[0], qs[1], cache[4], cache[5], cache[6], 0, 0)
+    lib = load()
+    if workspace is None:
+        workspace = _own_workspace(lib.pkv_decode_blocks_workspace_bytes(desc), q)
+    _call("pkv_decode_attention_blocks", lib.pkv_decode_attention_blocks, index, desc, q.data_ptr(), K_p, V_p, table_p,
+          _need(count, "count", torch.int32, (B,), index), _need(blocks, "blocks", torch.int32, (B, Hkv, most), index),
           _need(out, "out", dtype, (B, Hq, d), index), None if lse is None else _need(lse, "lse", torch.float32, (B, Hq), index),
           *_workspace(workspace, index), _stream_of(index))
     return out, lse

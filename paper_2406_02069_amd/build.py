@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libpkv.so")
 SOURCES = ["pkv_api.hip", "pkv_score.hip", "pkv_resident.hip", "pkv_stream.hip", "pkv_lag.hip", "pkv_sift.hip", "pkv_sweep.hip", "pkv_select.hip", "pkv_gather.hip", "pkv_decode.hip",
-           "pkv_rotary.hip", "pkv_decode_long.hip", "pkv_prefill.hip"]
+           "pkv_rotary.hip", "pkv_decode_long.hip", "pkv_prefill.hip", "pkv_tree.hip", "pkv_weigh.hip", "pkv_evict.hip", "pkv_blocks.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

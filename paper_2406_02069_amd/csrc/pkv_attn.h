@@ -1,4 +1,4 @@
-// Pieces shared by the attention kernels over whole caches (pkv_prefill.hip, pkv_decode_long.hip).
+// Pieces shared by the attention kernels over whole caches (pkv_prefill.hip, pkv_long.h).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -67,6 +67,24 @@ __device__ __forceinline__ float unpack(uint32_t u, int i) {
 // lane i gets column i: the elements of rows 0 .. 3.
 __device__ __forceinline__ u32x2 read_columns(const char* lds) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds)));
+}
+
+// Halves of a word whose exponent is all ones (bit 15, bit 31 set).
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t u);
+template <>
+__device__ __forceinline__ uint32_t not_finite<__bf16>(uint32_t u) {
+  return ((u & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+template <>
+__device__ __forceinline__ uint32_t not_finite<_Float16>(uint32_t u) {
+  return ((u & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+}
+
+// (in a scalar register)
+__device__ __forceinline__ int wave_max(int x) {
+  for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
+  return __builtin_amdgcn_readfirstlane(x);
 }
 
 // Sum over the wave, up to and including the own lane.

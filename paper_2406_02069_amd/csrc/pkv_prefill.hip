@@ -86,11 +86,6 @@ __device__ __forceinline__ Seen seen_keys(const PrefillArgs& a, int b, int t, in
   return s;
 }
 
-__device__ __forceinline__ int wave_max(int x) {
-  for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
-  return __builtin_amdgcn_readfirstlane(x);
-}
-
 // The sequences' shares of a call by their lengths, lane b's for sequence b: its tiles first .. first + act - 1 have rows that are
 // there, each in S ranges of keys; its workgroups, slots and tiles in several ranges go before `end`, `slots` and `cut`.
 // Ranges are as long as make one turn of the device of all work where the tiles alone are half of one at most, else two turns.
@@ -155,18 +150,6 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t at, uint3
 __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
   asm volatile("" : : : "memory");
-}
-
-// Halves of a word whose exponent is all ones (bit 15, bit 31 set).
-template <typename T>
-__device__ __forceinline__ uint32_t not_finite(uint32_t u);
-template <>
-__device__ __forceinline__ uint32_t not_finite<__bf16>(uint32_t u) {
-  return ((u & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-}
-template <>
-__device__ __forceinline__ uint32_t not_finite<_Float16>(uint32_t u) {
-  return ((u & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
 }
 
 // The first key of register i of a 32 x 32 product, in the lower half of the wave (the upper half: 4 more).

@@ -1,0 +1,261 @@
+"""Bounds of blocks, their selection and the attention over them (pkv_block_bounds, pkv_block_select, pkv_decode_attention_blocks) against
+plain forms in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from paper_2406_02069_amd import binding
+from tests.cache_ref import block_scores, blocks_taken, bounds_of, check_rows, make_cache, paged
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _same(a, b):
+    assert bool(((a == b) | (torch.isnan(a) & torch.isnan(b))).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("B,Hkv,d,k_cap,block,page,new", [
+    (4, 2, 64, 1, 16, 0, None), (5, 3, 128, 100, 16, 16, None), (5, 2, 64, 333, 32, 7, None), (5, 8, 128, 1000, 64, 48, 1), (5, 1, 64, 700, 128, 1, 200),
+    (2, 8, 128, 5000, 256, 0, None), (70, 1, 64, 90, 16, 0, 17), (3, 4, 128, 20000, 16, 256, 300), (1, 2, 64, 40001, 32, 64, None)])
+def test_bounds(B, Hkv, d, k_cap, block, page, new, dtype):
+    print("bounds", B, Hkv, d, k_cap, block, page, new, dtype, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(k_cap)
+    K, _, Kc, _, table = make_cache(B, Hkv, k_cap, d, dtype, page, g)
+    count = torch.tensor([k_cap, k_cap // 2, 0, 1, k_cap + 9] * 14, dtype=torch.int32, device=DEV)[:B]
+    K[0, 0, k_cap // 3, 3], K[0, 0, k_cap // 2, 5], K[0, -1, 0, 7], K[0, -1, 0, 8] = math.nan, math.inf, -math.inf, -0.0
+    for b in range(B):
+        K[b, :, int(count[b]):] = math.nan                     # behind the count: not looked at
+    if page:
+        Kc = paged(K, page, table, Kc.shape[0])
+    else:
+        Kc = K
+    fresh = None if new is None else torch.tensor([new, 1, new, 5, k_cap + 9] * 14, dtype=torch.int32, device=DEV)[:B]
+    blocks = -(-k_cap // block)
+    bounds = torch.full((B, Hkv, blocks + 1, 2, d), 3.0, dtype=dtype, device=DEV)
+    binding.block_bounds(Kc, count, bounds, block, new_lens=fresh, block_table=table, k_cap=k_cap)
+    torch.cuda.synchronize()
+    for b in range(B):
+        n = min(max(int(count[b]), 0), k_cap)
+        first = 0 if fresh is None else (n - min(max(int(fresh[b]), 0), n)) // block if int(fresh[b]) > 0 else blocks
+        for h in range(Hkv):
+            want = torch.full_like(bounds[b, h], 3.0)
+            have = bounds_of(K[b, h], n, block)
+            want[first:len(have)] = have[first:]
+            _same(bounds[b, h], want)
+
+
+def test_bounds_of_pages_that_do_not_exist_and_strides():
+    B, Hkv, d, k_cap, block, page = 2, 2, 64, 200, 16, 8
+    g = torch.Generator(device=DEV).manual_seed(3)
+    K, _, Kc, _, table = make_cache(B, Hkv, k_cap, d, torch.bfloat16, page, g)
+    table[0, 4], table[0, 6], table[0, 7], table[1, 24] = -1, 10 ** 6, Kc.shape[0], 2 ** 31 - 1
+    absent = torch.zeros(B, k_cap, dtype=torch.bool, device=DEV)
+    absent[0, 32:40] = absent[0, 48:64] = absent[1, 192:] = True
+    buf = torch.full((B, Hkv + 1, 15, 2, d), 3.0, dtype=torch.bfloat16, device=DEV)
+    binding.block_bounds(Kc, torch.tensor([200, 200], dtype=torch.int32, device=DEV), buf[:, 1:], block, block_table=table, k_cap=k_cap)
+    torch.cuda.synchronize()
+    for b in range(B):
+        for h in range(Hkv):
+            assert torch.equal(buf[b, 1 + h, :13], bounds_of(K[b, h], 200, block, absent[b]))
+    assert not buf[0, 1, 3].any() and bool((buf[:, 0] == 3).all()) and bool((buf[:, :, 13:] == 3).all())
+    strided = torch.randn(B, k_cap + 3, Hkv, d + 8, generator=g, device=DEV).to(torch.bfloat16)[:, :k_cap, :, :d].transpose(1, 2)
+    got = binding.block_bounds(strided, torch.tensor([200, 77], dtype=torch.int32, device=DEV), torch.zeros(B, Hkv, 13, 2, d, dtype=torch.bfloat16, device=DEV), block)
+    torch.cuda.synchronize()
+    for b, n in ((0, 200), (1, 77)):
+        for h in range(Hkv):
+            want = bounds_of(strided[b, h], n, block)
+            assert torch.equal(got[b, h, :len(want)], want) and not got[b, h, len(want):].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("B,Hq,Hkv,d,k_cap,block,most,first,recent", [
+    (3, 8, 8, 64, 1, 16, 1, 0, 0), (5, 8, 2, 128, 500, 16, 7, 1, 2), (5, 28, 4, 128, 5000, 16, 64, 1, 2), (2, 64, 1, 64, 3000, 32, 1, 0, 1),
+    (2, 34, 2, 128, 2000, 64, 31, 0, 0), (1, 128, 1, 128, 9000, 16, 562, 4, 4), (2, 16, 16, 64, 40000, 16, 128, 0, 2), (1, 32, 8, 128, 150000, 16, 256, 1, 1),
+    (70, 2, 2, 64, 700, 32, 5, 5, 0), (2, 4, 2, 128, 800, 256, 9, 0, 0)])
+def test_selection(B, Hq, Hkv, d, k_cap, block, most, first, recent, dtype):
+    print("select", B, Hq, Hkv, d, k_cap, block, most, first, recent, dtype, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(k_cap)
+    q = torch.randn(B, Hq, d, generator=g, device=DEV).to(dtype)
+    blocks = -(-k_cap // block)
+    lo = torch.randn(B, Hkv, blocks, d, generator=g, device=DEV)
+    bounds = torch.stack([lo, lo + torch.rand(lo.shape, generator=g, device=DEV) * 3], 3).to(dtype)
+    bounds[:, :, 1::5] = bounds[:, :, 0:1]                                  # equal scores, in many blocks
+    count = torch.tensor([k_cap, k_cap // 2, 0, 1, k_cap + 9] * 14, dtype=torch.int32, device=DEV)[:B]
+    scores = torch.full((B, Hkv, blocks), 9.0, device=DEV)
+    got = binding.block_select(q, bounds, count, block, most, first=first, recent=recent, k_cap=k_cap, scores=scores)
+    torch.cuda.synchronize()
+    same = binding.block_select(q, bounds, count, block, most, first=first, recent=recent, k_cap=k_cap)
+    torch.cuda.synchronize()
+    assert torch.equal(got, same)
+    G = Hq // Hkv
+    for b in range(B):
+        have = -(-min(max(int(count[b]), 0), k_cap) // block)
+        for h in range(Hkv):
+            want = block_scores(q[b, h * G:(h + 1) * G], bounds[b, h, :have])
+            # sums in 64 bits in another order, rounded once: the same, or a neighbour
+            assert bool(((scores[b, h, :have] - want).abs() <= 2.0 ** -23 * want.abs()).all()) and bool((scores[b, h, have:] == 9).all())
+            assert float((scores[b, h, :have] == want).float().mean()) > 0.99 or have < 100
+            assert got[b, h].tolist() == blocks_taken(scores[b, h, :have], most, first, recent)
+
+
+def test_selection_of_odd_bounds():
+    B, Hq, Hkv, d, block, most = 1, 4, 2, 64, 16, 5
+    g = torch.Generator(device=DEV).manual_seed(2)
+    q = torch.randn(B, Hq, d, generator=g, device=DEV).to(torch.bfloat16)
+    q[0, 1, 7] = 0
+    bounds = torch.randn(B, Hkv, 40, 2, d, generator=g, device=DEV).to(torch.bfloat16)
+    bounds[:, :, 5, 0], bounds[:, :, 5, 1] = -math.inf, math.inf            # keys that were NaN: +inf, or NaN with a query's zeros
+    bounds[:, :, 9, 1, 3], bounds[:, :, 11, 0, 3] = -math.inf, math.inf
+    bounds[:, :, 20:] = 0
+    count = torch.tensor([640], dtype=torch.int32, device=DEV)
+    scores = torch.empty(B, Hkv, 40, device=DEV)
+    got = binding.block_select(q, bounds, count, block, most, scores=scores)
+    torch.cuda.synchronize()
+    assert bool((got[0] == 5).any(1).all()) and bool(torch.isposinf(scores[0, :, 5]).all())
+    for h in range(Hkv):
+        assert got[0, h].tolist() == blocks_taken(scores[0, h], most, 0, 0)
+    q[0, 0] = math.nan                                                      # nothing is known: the first blocks, ascending
+    got = binding.block_select(q, bounds, count, block, most, recent=1)
+    torch.cuda.synchronize()
+    assert got[0, 0].tolist() == [0, 1, 2, 3, 39]
+    # strides of q and bounds; zeros of both signs are equal
+    qs = torch.randn(2, 3, Hq, d, generator=g, device=DEV).to(torch.bfloat16)[:, 1]
+    z = torch.zeros(2, Hkv + 1, 40, 2, d, dtype=torch.bfloat16, device=DEV)
+    z[:, :, 1::2] = -0.0
+    got = binding.block_select(qs, z[:, 1:], torch.tensor([640, 33], dtype=torch.int32, device=DEV), block, most)
+    torch.cuda.synchronize()
+    assert got[0].tolist() == [[0, 1, 2, 3, 4]] * 2 and got[1].tolist() == [[0, 1, 2, -1, -1]] * 2
+
+
+def _compare(out, lse, q, K, V, count, blocks, block, cap=0.0, scale=None, absent=None):
+    """(lists without an entry that is named twice)"""
+    B, Hq, d = q.shape
+    Hkv, k_cap = K.shape[1], K.shape[2]
+    G = Hq // Hkv
+    j = torch.arange(k_cap, device=DEV)
+    for b in range(B):
+        n = min(max(int(count[b]), 0), k_cap)
+        have = -(-n // block)
+        for g in range(Hkv):
+            named = [k for k in blocks[b, g, :have].tolist() if 0 <= k < have]
+            seen = (j < n) & torch.isin(j // block, torch.tensor(named, device=DEV))
+            if absent is not None:
+                seen &= ~absent[b]
+            for h in range(g * G, g * G + G):
+                check_rows(out[b, h][None], None if lse is None else lse[b, h][None], q[b, h][None], K[b, g], V[b, g], seen[None], 0 * seen[None],
+                           d ** -0.5 if scale is None else scale, q.dtype, cap)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("B,Hq,Hkv,d,k_cap,block,most,page,cap", [
+    (3, 8, 8, 64, 1, 16, 1, 0, 0.0), (4, 8, 2, 128, 37, 16, 9, 0, 30.0), (4, 28, 4, 128, 500, 16, 7, 16, 0.0), (2, 64, 1, 64, 3000, 32, 50, 48, 50.0),
+    (2, 34, 2, 128, 2000, 64, 31, 7, 0.0), (1, 128, 1, 128, 9000, 128, 20, 1, 0.0), (5, 4, 2, 64, 5000, 256, 4, 100, 0.0), (1, 32, 8, 128, 40001, 16, 128, 16, 0.0),
+    (1, 8, 8, 128, 70000, 32, 900, 256, 0.0), (70, 2, 1, 64, 700, 16, 30, 0, 0.0)])
+def test_listed_blocks(B, Hq, Hkv, d, k_cap, block, most, page, cap, dtype):
+    print("blocks", B, Hq, Hkv, d, k_cap, block, most, page, cap, dtype, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(k_cap)
+    q = (torch.randn(B, Hq, d, generator=g, device=DEV) * 1.5).to(dtype)
+    K, V, Kc, Vc, table = make_cache(B, Hkv, k_cap, d, dtype, page, g)
+    count = torch.tensor([k_cap, k_cap // 2, 0, 1, k_cap + 9] * 14, dtype=torch.int32, device=DEV)[:B]
+    have = -(-k_cap // block)
+    order = torch.rand(B, Hkv, have, generator=g, device=DEV).argsort(2).to(torch.int32)      # in no order
+    blocks = torch.full((B, Hkv, most), -1, dtype=torch.int32, device=DEV)
+    blocks[:, :, :min(most, have)] = order[:, :, :most]
+    if most > 3:
+        blocks[:, 0, 1], blocks[:, 0, 2] = 10 ** 9, -2 ** 31 + 5                              # no blocks
+    out, lse = binding.decode_attention_blocks(q, Kc, Vc, count, blocks, block, block_table=table, k_cap=k_cap, cap=cap, want_lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, q, K, V, count, blocks, block, cap)
+    if B > 2:
+        assert not out[2].any() and bool(torch.isneginf(lse[2]).all())
+
+
+def test_blocks_named_twice_all_blocks_and_what_is_not_seen():
+    B, Hq, Hkv, d, k_cap, block, page = 2, 8, 2, 128, 500, 16, 24
+    g = torch.Generator(device=DEV).manual_seed(9)
+    q = torch.randn(B, Hq, d, generator=g, device=DEV).to(torch.bfloat16)
+    K, V, Kc, Vc, table = make_cache(B, Hkv, k_cap, d, torch.bfloat16, page, g)
+    count = torch.tensor([500, 290], dtype=torch.int32, device=DEV)
+    every = torch.arange(32, dtype=torch.int32, device=DEV).expand(B, Hkv, 32).contiguous()
+    out, lse = binding.decode_attention_blocks(q, Kc, Vc, count, every, block, block_table=table, k_cap=k_cap, want_lse=True, scale=2.0)
+    ref, ref_lse = binding.decode_attention_long(q, Kc, Vc, count, block_table=table, k_cap=k_cap, want_lse=True, scale=2.0)
+    torch.cuda.synchronize()
+    _compare(out, lse, q, K, V, count, every, block, scale=2.0)
+    torch.testing.assert_close(lse, ref_lse, rtol=1e-5, atol=1e-4)
+    # a list that is one block twice is that block, with twice the sum
+    once, twice = (torch.full((B, Hkv, m), 4, dtype=torch.int32, device=DEV) for m in (1, 2))
+    a, la = binding.decode_attention_blocks(q, Kc, Vc, count, once, block, block_table=table, k_cap=k_cap, want_lse=True)
+    b, lb = binding.decode_attention_blocks(q, Kc, Vc, count, twice, block, block_table=table, k_cap=k_cap, want_lse=True)
+    torch.cuda.synchronize()
+    assert bool(((a.float() - b.float()).abs() <= 2.0 ** -7 * a.float().abs() + 2.0 ** -12).all())
+    torch.testing.assert_close(lb, la + math.log(2), rtol=1e-5, atol=1e-5)
+    # NaN and infinities in blocks that are not named, behind the count and on pages that do not exist; infinities in a named one
+    named = torch.tensor([[0, 3, 18, 30, 31], [31, 5, 17, 18, 2]], dtype=torch.int32, device=DEV)[:, None].expand(B, Hkv, 5).contiguous()
+    absent = torch.zeros(B, k_cap, dtype=torch.bool, device=DEV)
+    table[0, 2], table[1, 11] = -1, 10 ** 6
+    absent[0, 48:72] = absent[1, 264:288] = True
+    for b in range(B):
+        keep = torch.isin(torch.arange(k_cap, device=DEV) // block, named[b, 0]) & (torch.arange(k_cap, device=DEV) < int(count[b]))
+        K[b, :, ~keep], V[b, :, ~keep] = math.nan, math.inf
+    V[0, 0, 3, 5], V[0, 0, 290, 6], V[1, 1, 40, 7] = math.inf, -math.inf, math.nan
+    Kc, Vc = paged(K, page, table, Kc.shape[0]), paged(V, page, table, Kc.shape[0])
+    out, lse = binding.decode_attention_blocks(q, Kc, Vc, count, named, block, block_table=table, k_cap=k_cap, want_lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, q, K, V, count, named, block, absent=absent)
+
+
+def test_a_step_from_a_graph_and_on_another_stream():
+    B, Hq, Hkv, d, k_cap, block, most, page = 2, 32, 8, 128, 6000, 16, 40, 16
+    g = torch.Generator(device=DEV).manual_seed(7)
+    q = torch.randn(B, Hq, d, generator=g, device=DEV).to(torch.bfloat16)
+    K, V, Kc, Vc, table = make_cache(B, Hkv, k_cap, d, torch.bfloat16, page, g)
+    count, new = torch.tensor([6000, 2222], dtype=torch.int32, device=DEV), torch.ones(B, dtype=torch.int32, device=DEV)
+    bounds = torch.zeros(B, Hkv, 375, 2, d, dtype=torch.bfloat16, device=DEV)
+    binding.block_bounds(Kc, count, bounds, block, block_table=table, k_cap=k_cap)
+
+    def step(bounds, blocks, out, lse, ws=(None, None)):
+        binding.block_bounds(Kc, count, bounds, block, new_lens=new, block_table=table, k_cap=k_cap)
+        binding.block_select(q, bounds, count, block, most, first=1, recent=2, k_cap=k_cap, blocks_out=blocks, workspace=ws[0])
+        binding.decode_attention_blocks(q, Kc, Vc, count, blocks, block, block_table=table, k_cap=k_cap, out=out, lse=lse, workspace=ws[1])
+        return bounds, blocks, out, lse
+
+    fresh = lambda: (bounds.clone(), torch.zeros(B, Hkv, most, dtype=torch.int32, device=DEV), torch.zeros_like(q), torch.zeros(B, Hq, device=DEV))  # noqa: E731
+    ws = tuple(torch.empty(1 << 25, dtype=torch.uint8, device=DEV) for _ in range(2))
+    step(*fresh())
+    side, graph, held = torch.cuda.Stream(), torch.cuda.CUDAGraph(), fresh()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        step(*held, ws)
+    for i in range(3):
+        q.copy_(torch.randn(q.shape, device=DEV))
+        count.copy_(torch.tensor([6000 - 999 * i, 17 + i], dtype=torch.int32))
+        for w in ws:
+            w.fill_(255)
+        held[0].copy_(bounds)
+        graph.replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            eager = step(*fresh())
+        torch.cuda.synchronize()
+        for a, b in zip(held, eager):
+            assert torch.equal(a, b)
+
+
+def test_longest_offsets():
+    d, Hkv, page, block = 128, 8, 128, 16
+    pages = 2 ** 32 // (Hkv * page * d) + 1
+    K, V = (torch.zeros(pages, Hkv, page, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    g = torch.Generator(device=DEV).manual_seed(6)
+    K[-1], V[-1] = (torch.randn(Hkv, page, d, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(1, 8, d, generator=g, device=DEV).to(torch.bfloat16)
+    table, count = torch.tensor([[pages - 1]], dtype=torch.int32, device=DEV), torch.tensor([120], dtype=torch.int32, device=DEV)
+    bounds = binding.block_bounds(K, count, torch.zeros(1, Hkv, 8, 2, d, dtype=torch.bfloat16, device=DEV), block, block_table=table)
+    blocks = binding.block_select(q, bounds, count, block, 3, recent=1)
+    out, lse = binding.decode_attention_blocks(q, K, V, count, blocks, block, block_table=table, want_lse=True)
+    torch.cuda.synchronize()
+    for h in range(Hkv):
+        assert torch.equal(bounds[0, h], bounds_of(K[-1, h], 120, block))
+    _compare(out, lse, q, K[-1:], V[-1:], count, blocks, block)

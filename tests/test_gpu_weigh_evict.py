@@ -1,0 +1,341 @@
+"""Weights that add up (pkv_decode_attention_accumulate) and eviction by them (pkv_cache_evict) against plain forms in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from paper_2406_02069_amd import binding
+from tests.cache_ref import check_rows, evicted, make_cache, paged, unpaged, weights_of
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+# ---------------------------------------------------------------- weights
+
+def _compare(out, lse, weights, before, q, K, V, count, positions=None, q_pos=None, slopes=None, cap=0.0, window=0, scale=None, absent=None):
+    B, Hq, d = q.shape
+    Hkv, k_cap = K.shape[1], K.shape[2]
+    G = Hq // Hkv
+    j = torch.arange(k_cap, device=DEV)
+    for b in range(B):
+        n = min(max(int(count[b]), 0), k_cap)
+        at = n - 1 if q_pos is None else int(q_pos[b])
+        for g in range(Hkv):
+            pos = j if positions is None else positions[b, g, :k_cap].long()
+            seen = (j < n) & (pos >= 0) & (pos <= at)
+            if window:
+                seen = seen & (pos > at - window)
+            if absent is not None:
+                seen = seen & ~absent[b]
+            dist = (at - pos).abs()
+            hs = slice(g * G, g * G + G)
+            for h in range(g * G, g * G + G):
+                check_rows(out[b, h][None], None if lse is None else lse[b, h][None], q[b, h][None], K[b, g], V[b, g], seen[None], dist[None],
+                           d ** -0.5 if scale is None else scale, q.dtype, cap, None if slopes is None else float(slopes[h]))
+            Kf = K[b, g].clone()
+            Kf[~seen] = 0
+            want, room = weights_of(q[b, hs], Kf, seen, dist, d ** -0.5 if scale is None else scale, cap, None if slopes is None else slopes[hs])
+            got, had = weights[b, g, :k_cap], before[b, g, :k_cap]
+            total = had.double() + want
+            assert bool(((got.double() - total).abs() <= room + 2.0 ** -24 * total).all())
+            assert torch.equal(got[~seen], had[~seen])
+    assert torch.equal(weights[:, :, k_cap:], before[:, :, k_cap:])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("B,Hq,Hkv,d,k_cap,page,cap,slopes,window", [
+    (3, 8, 8, 64, 1, 0, 0.0, False, 0), (4, 8, 2, 128, 31, 0, 30.0, False, 0), (4, 28, 4, 128, 33, 16, 0.0, True, 0),
+    (2, 64, 1, 64, 700, 48, 50.0, True, 100), (2, 34, 2, 128, 1025, 1, 0.0, False, 7), (1, 128, 1, 128, 513, 0, 0.0, False, 0),
+    (5, 6, 2, 128, 5000, 256, 0.0, True, 0), (1, 32, 8, 128, 40001, 16, 0.0, False, 0), (2, 16, 16, 128, 9000, 0, 0.0, False, 2500),
+    (70, 2, 2, 64, 600, 0, 0.0, False, 0)])
+def test_weights(B, Hq, Hkv, d, k_cap, page, cap, slopes, window, dtype):
+    print("weigh", B, Hq, Hkv, d, k_cap, page, cap, slopes, window, dtype, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(k_cap + d)
+    q = (torch.randn(B, Hq, d, generator=g, device=DEV) * 1.5).to(dtype)
+    K, V, Kc, Vc, table = make_cache(B, Hkv, k_cap, d, dtype, page, g)
+    count = torch.tensor([k_cap, k_cap // 2, 0, 1, k_cap + 9] * 14, dtype=torch.int32, device=DEV)[:B]
+    sl = 2.0 ** (-8.0 * torch.arange(1, Hq + 1, device=DEV) / Hq) if slopes else None
+    weights = torch.rand(B, Hkv, k_cap + 3, generator=g, device=DEV)
+    before = weights.clone()
+    out, lse = binding.decode_attention_accumulate(q, Kc, Vc, count, weights, block_table=table, k_cap=k_cap, slopes=sl, cap=cap, window=window,
+                                                   want_lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, weights, before, q, K, V, count, slopes=sl, cap=cap, window=window)
+    same, same_lse = binding.decode_attention_long(q, Kc, Vc, count, block_table=table, k_cap=k_cap, slopes=sl, cap=cap, window=window, want_lse=True)
+    torch.cuda.synchronize()
+    assert torch.equal(out, same) and torch.equal(lse, same_lse)
+    again = before.clone()                                      # without lse, and onto the same sums: the same bits
+    binding.decode_attention_accumulate(q, Kc, Vc, count, again, block_table=table, k_cap=k_cap, slopes=sl, cap=cap, window=window)
+    torch.cuda.synchronize()
+    assert torch.equal(again, weights)
+
+
+@pytest.mark.parametrize("window,slopes,page", [(0, False, 0), (700, True, 16)])
+def test_weights_by_positions_and_of_what_is_not_seen(window, slopes, page):
+    B, Hq, Hkv, d, k_cap = 3, 12, 4, 128, 610
+    g = torch.Generator(device=DEV).manual_seed(8)
+    q = torch.randn(B, Hq, d, generator=g, device=DEV).to(torch.bfloat16)
+    K, V, Kc, Vc, table = make_cache(B, Hkv, k_cap, d, torch.bfloat16, page, g)
+    pos = torch.randint(1, 6, (B, Hkv, k_cap), generator=g, device=DEV).cumsum(2).to(torch.int32) - 1
+    pos[0, :, 17:30] = -1
+    pos[:, 2] = pos[:, 2].flip(1)
+    count, q_pos = torch.tensor([610, 200, 33], dtype=torch.int32, device=DEV), torch.tensor([2500, 500, -1], dtype=torch.int32, device=DEV)
+    absent = torch.zeros(B, k_cap, dtype=torch.bool, device=DEV)
+    if page:
+        table[0, 3] = 10 ** 6
+        absent[0, 48:64] = True
+    bad = (torch.arange(k_cap, device=DEV) >= count[:, None])[:, None] | (pos < 0)
+    K[bad], V[bad] = math.nan, math.inf
+    Kc, Vc = (paged(x, page, table, Kc.shape[0]) for x in (K, V)) if page else (K, V)
+    sl = torch.linspace(0.01, 0.3, Hq, device=DEV) if slopes else None
+    buf = torch.rand(B, Hkv + 2, k_cap + 5, generator=g, device=DEV)
+    weights = buf[:, 1:1 + Hkv, :k_cap]                        # strides of their own
+    before = buf.clone()
+    out, lse = binding.decode_attention_accumulate(q, Kc, Vc, count, weights, block_table=table, k_cap=k_cap, positions=pos, q_pos=q_pos, slopes=sl,
+                                                   window=window, want_lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, weights, before[:, 1:1 + Hkv, :k_cap], q, K, V, count, pos, q_pos, sl, 0.0, window, absent=absent)
+    assert torch.equal(buf[:, 0], before[:, 0]) and torch.equal(buf[:, Hkv + 1], before[:, Hkv + 1]) and torch.equal(buf[:, :, k_cap:], before[:, :, k_cap:])
+
+
+def test_weights_from_a_graph_and_two_calls_at_once():
+    B, Hq, Hkv, d, k_cap = 2, 32, 8, 128, 6000
+    g = torch.Generator(device=DEV).manual_seed(7)
+    q = torch.randn(B, Hq, d, generator=g, device=DEV).to(torch.bfloat16)
+    _, _, Kc, Vc, table = make_cache(B, Hkv, k_cap, d, torch.bfloat16, 16, g)
+    count = torch.tensor([6000, 2222], dtype=torch.int32, device=DEV)
+    weights = torch.zeros(B, Hkv, k_cap, device=DEV)
+    call = lambda w, **kw: binding.decode_attention_accumulate(q, Kc, Vc, count, w, block_table=table, k_cap=k_cap, **kw)  # noqa: E731
+    call(weights.clone())
+    ws = [torch.empty(1 << 26, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    side, graph, o = torch.cuda.Stream(), torch.cuda.CUDAGraph(), torch.empty_like(q)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        call(weights, out=o, workspace=ws[0])
+    eager = weights.clone()
+    for step in range(3):
+        q.copy_(torch.randn(q.shape, device=DEV))
+        count.copy_(torch.tensor([6000 - 999 * step, 17 + step], dtype=torch.int32))
+        ws[0].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        out, _ = call(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(o, out) and torch.equal(eager, weights)
+    torch.testing.assert_close(weights[0].sum(), torch.tensor(3.0 * Hq, device=DEV), rtol=1e-4, atol=0)   # a head's weights sum to 1
+    sums = [torch.zeros_like(weights) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for rep in range(4):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                call(sums[i], workspace=ws[i], window=300 * i)
+    torch.cuda.synchronize()
+    alone = [torch.zeros_like(weights) for _ in range(2)]
+    for rep in range(4):
+        for i in range(2):
+            call(alone[i], window=300 * i)
+    torch.cuda.synchronize()
+    assert torch.equal(sums[0], alone[0]) and torch.equal(sums[1], alone[1])
+
+
+def test_keys_that_are_not_finite_keep_to_their_heads():
+    B, Hq, Hkv, d, k_cap = 1, 4, 2, 64, 300
+    g = torch.Generator(device=DEV).manual_seed(2)
+    q = torch.randn(B, Hq, d, generator=g, device=DEV).to(torch.bfloat16)
+    K, V, _, _, _ = make_cache(B, Hkv, k_cap, d, torch.bfloat16, 0, g)
+    K[0, 0, 40] = math.nan
+    weights = torch.zeros(B, Hkv, k_cap, device=DEV)
+    count = torch.tensor([200], dtype=torch.int32, device=DEV)
+    binding.decode_attention_accumulate(q, K, V, count, weights)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(weights[0, 0, 40])) and bool(torch.isfinite(weights[0, 1]).all()) and not weights[0, :, 200:].any()
+
+
+# ---------------------------------------------------------------- eviction
+
+def _case(B, Hkv, d, k_cap, page, dtype, seed, order="up"):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    K, V, Kc, Vc, table = make_cache(B, Hkv, k_cap, d, dtype, page, g)
+    pos = torch.randint(1, 6, (B, Hkv, k_cap), generator=g, device=DEV).cumsum(2).to(torch.int32) - 1
+    if order == "any":
+        pos = torch.gather(pos, 2, torch.rand(B, Hkv, k_cap, generator=g, device=DEV).argsort(2))
+    w = torch.randn(B, Hkv, k_cap, generator=g, device=DEV).mul_(2).exp_()
+    return K, V, Kc, Vc, table, pos.contiguous(), w, g
+
+
+def _check(K, V, Kc, Vc, table, pos, w, count, budget, recent, first, got, before_out):
+    """got: (positions_out, weights_out, count_out); before_out: what the first two held."""
+    B, Hkv, k_cap = pos.shape
+    po, wo, co = (x.cpu() for x in got)
+    bp, bw = (x.cpu() for x in before_out)
+    Kn, Vn = (x if table is None else unpaged(x, table, K.shape[2]) for x in (Kc, Vc))
+    pos_h, w_h = pos.cpu(), w.cpu()
+    for b in range(B):
+        n = min(max(int(count[b]), 0), k_cap)
+        assert int(co[b]) == min(n, budget)
+        for g in range(Hkv):
+            rows = evicted(pos_h[b, g].tolist(), w_h[b, g].tolist(), n, budget, recent, first)
+            m = len(rows)
+            at = torch.tensor(rows, dtype=torch.long)
+            assert torch.equal(po[b, g, :m], pos_h[b, g, at]) and torch.equal(wo[b, g, :m].view(torch.int32), w_h[b, g, at].view(torch.int32))
+            assert bool((po[b, g, m:n] == -1).all()) and not wo[b, g, m:n].any()
+            assert torch.equal(po[b, g, n:], bp[b, g, n:]) and torch.equal(wo[b, g, n:], bw[b, g, n:])
+            at = at.to(K.device)
+            for new, old in ((Kn, K), (Vn, V)):
+                assert torch.equal(new[b, g, :m].view(torch.int16), old[b, g, at].view(torch.int16))
+                assert torch.equal(new[b, g, m:].view(torch.int16), old[b, g, m:].view(torch.int16))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,Hkv,d,k_cap,budget,recent,first,page,order", [
+    (3, 2, 64, 1, 1, 0, 0, 0, "up"), (5, 2, 128, 33, 32, 4, 2, 0, "up"), (5, 4, 64, 70, 20, 20, 0, 16, "up"), (5, 2, 128, 300, 200, 16, 4, 7, "any"),
+    (2, 8, 128, 2049, 2048, 32, 4, 16, "up"), (5, 3, 64, 1025, 1, 1, 0, 1, "up"), (5, 1, 128, 1500, 1499, 0, 0, 48, "any"),
+    (2, 2, 64, 20000, 700, 64, 1, 0, "up"), (3, 8, 128, 5000, 2500, 100, 4, 256, "any"), (1, 2, 64, 70001, 3001, 32, 4, 0, "any"),
+    (70, 1, 64, 90, 64, 8, 0, 0, "up"), (2, 2, 128, 500, 600, 8, 0, 0, "up"), (2, 2, 64, 40001, 33000, 0, 0, 64, "up")])
+def test_evict(B, Hkv, d, k_cap, budget, recent, first, page, order, in_place):
+    print("evict", B, Hkv, d, k_cap, budget, recent, first, page, order, in_place, flush=True)
+    K, V, Kc, Vc, table, pos, w, g = _case(B, Hkv, d, k_cap, page, torch.bfloat16 if d == 64 else torch.float16, k_cap + budget, order)
+    K, V, Kc, Vc = K.clone(), V.clone(), Kc.clone(), Vc.clone()
+    count = torch.tensor([k_cap, budget + (k_cap - budget) // 2, budget, 0, k_cap + 5] * 14, dtype=torch.int32, device=DEV)[:B]
+    if in_place:
+        po, wo = pos.clone(), w.clone()
+        src = (po, wo)
+        kw = {}
+    else:
+        po, wo = torch.full_like(pos, 77), torch.full_like(w, 5.5)
+        src = (pos, w)
+        kw = dict(positions_out=po, weights_out=wo)
+    before = (po.clone(), wo.clone())
+    co = binding.cache_evict(Kc, Vc, count, *src, budget, recent=recent, first=first, block_table=table, k_cap=k_cap, **kw)
+    torch.cuda.synchronize()
+    _check(K, V, Kc, Vc, table, pos, w, count, budget, recent, first, (po, wo, co), before)
+
+
+@pytest.mark.parametrize("kind", ["equal", "zeros", "steps", "odd", "large", "tiny"])
+@pytest.mark.parametrize("k_cap,budget", [(200, 150), (5000, 1000), (30000, 2048)])
+def test_evict_equal_and_odd_weights(kind, k_cap, budget):
+    # ties go to the lower row, whole plateaus of them; infinities, NaN, negative ones; weights that differ in their last bits
+    K, V, Kc, Vc, table, pos, w, g = _case(2, 2, 64, k_cap, 0, torch.bfloat16, budget)
+    K, V = K.clone(), V.clone()
+    if kind == "equal":
+        w.fill_(0.25)
+    elif kind == "zeros":
+        w.zero_()
+        w[:, :, 1::3] = -0.0
+    elif kind == "steps":
+        w = torch.randint(0, 4, w.shape, generator=g, device=DEV).float()
+    elif kind == "odd":
+        w[:, :, 3::7], w[:, :, 4::11], w[:, :, 5::9], w[:, :, 6::13] = math.nan, math.inf, -math.inf, -1.5
+    elif kind == "large":
+        w = (torch.randint(0, 5000, w.shape, generator=g, device=DEV) + 0x7F000000).to(torch.int32).view(torch.float32)
+    else:
+        w = torch.randint(1, 5000, w.shape, generator=g, device=DEV).to(torch.int32).view(torch.float32)   # below the smallest normal number
+    count = torch.tensor([k_cap, budget + 1], dtype=torch.int32, device=DEV)
+    pos[0, 1, 7:60] = -1                                                   # rows that are not there go first
+    po, wo = torch.zeros_like(pos), torch.zeros_like(w)
+    co = binding.cache_evict(Kc, Vc, count, pos, w, budget, recent=16, first=2, positions_out=po, weights_out=wo)
+    torch.cuda.synchronize()
+    _check(K, V, Kc, Vc, table, pos, w, count, budget, 16, 2, (po, wo, co), (torch.zeros_like(pos), torch.zeros_like(w)))
+
+
+def test_evict_more_protected_rows_than_the_budget():
+    # positions that repeat: the lower rows stay
+    K, V, Kc, Vc, table, pos, w, g = _case(1, 2, 64, 400, 0, torch.bfloat16, 3)
+    K, V = K.clone(), V.clone()
+    pos[:, 0] = 5
+    pos[:, 1, ::2] = 1
+    count = torch.tensor([400], dtype=torch.int32, device=DEV)
+    po, wo = torch.zeros_like(pos), torch.zeros_like(w)
+    co = binding.cache_evict(Kc, Vc, count, pos, w, 50, recent=3, first=4, positions_out=po, weights_out=wo)
+    torch.cuda.synchronize()
+    _check(K, V, Kc, Vc, table, pos, w, count, 50, 3, 4, (po, wo, co), (torch.zeros_like(pos), torch.zeros_like(w)))
+
+
+def test_evict_pages_that_do_not_exist():
+    B, Hkv, d, k_cap, page, budget = 2, 2, 64, 160, 16, 64
+    K, V, Kc, Vc, table, pos, w, g = _case(B, Hkv, d, k_cap, page, torch.bfloat16, 21)
+    table[0, 1], table[0, 8], table[1, 2] = 10 ** 6, -3, Kc.shape[0]        # a destination's page, a source's, one before the budget
+    count = torch.tensor([160, 150], dtype=torch.int32, device=DEV)
+    Kb, Vb = Kc.clone(), Vc.clone()
+    po, wo = torch.full_like(pos, 9), torch.full_like(w, 9)
+    co = binding.cache_evict(Kc, Vc, count, pos, w, budget, recent=4, block_table=table, k_cap=k_cap, positions_out=po, weights_out=wo)
+    torch.cuda.synchronize()
+    assert co.tolist() == [64, 64]
+    touched = torch.zeros(Kc.shape[:3], dtype=torch.bool)
+    lost = 0
+    for b in range(B):
+        page_of = table[b].tolist()
+        for h in range(Hkv):
+            rows = evicted(pos[b, h].tolist(), w[b, h].tolist(), int(count[b]), budget, 4, 0)
+            for r, src in enumerate(rows):
+                p, s = page_of[r // page], page_of[src // page]
+                if r == src:
+                    assert int(po[b, h, r]) == int(pos[b, h, r])
+                elif 0 <= p < Kc.shape[0] and 0 <= s < Kc.shape[0]:
+                    assert int(po[b, h, r]) == int(pos[b, h, src]) and torch.equal(Kc[p, h, r % page], Kb[s, h, src % page])
+                    touched[p, h, r % page] = True
+                else:
+                    assert int(po[b, h, r]) == -1
+                    lost += 1
+    assert lost > 0
+    same = ~touched.to(DEV)
+    assert torch.equal(Kc[same].view(torch.int16), Kb[same].view(torch.int16)) and torch.equal(Vc[same].view(torch.int16), Vb[same].view(torch.int16))
+
+
+def test_evict_strides_and_long_offsets():
+    # rows and heads that lie apart, positions and weights inside larger tensors, a cache of more than 2^32 bytes
+    B, Hkv, d, k_cap, budget = 2, 2, 128, 900, 300
+    g = torch.Generator(device=DEV).manual_seed(4)
+    buf = torch.randn(2, B, k_cap + 5, Hkv, d + 8, generator=g, device=DEV).to(torch.bfloat16)
+    K, V = buf[0, :, :k_cap, :, :d].transpose(1, 2), buf[1, :, :k_cap, :, :d].transpose(1, 2)
+    Kb, Vb, whole = K.clone(), V.clone(), buf.clone()
+    pos = torch.arange(k_cap, device=DEV, dtype=torch.int32).expand(B, Hkv, k_cap)     # one row of positions for all heads
+    wbuf = torch.rand(B, Hkv + 1, k_cap + 9, generator=g, device=DEV)
+    w = wbuf[:, 1:, 3:3 + k_cap]
+    po, wo = torch.zeros(B, Hkv, k_cap, dtype=torch.int32, device=DEV), torch.zeros(B, Hkv, k_cap, device=DEV)
+    count = torch.tensor([900, 301], dtype=torch.int32, device=DEV)
+    co = binding.cache_evict(K, V, count, pos, w, budget, recent=30, first=1, positions_out=po, weights_out=wo)
+    torch.cuda.synchronize()
+    _check(Kb, Vb, K, V, None, pos.contiguous(), w.contiguous(), count, budget, 30, 1, (po, wo, co), (torch.zeros_like(po), torch.zeros_like(wo)))
+    assert torch.equal(buf[:, :, k_cap:].view(torch.int16), whole[:, :, k_cap:].view(torch.int16)) and \
+        torch.equal(buf[..., d:].view(torch.int16), whole[..., d:].view(torch.int16))
+    big = torch.empty(2, 1, 2 ** 24 + 1500, d, dtype=torch.bfloat16, device=DEV)       # 8.6 GB
+    K, V = big[:, :, 2 ** 24:], torch.empty_like(big)[:, :, 2 ** 24:]
+    K.copy_(torch.randn(2, 1, 1500, d, generator=g, device=DEV)), V.copy_(torch.randn(2, 1, 1500, d, generator=g, device=DEV))
+    Kb, Vb = K.clone(), V.clone()
+    pos = torch.arange(1500, device=DEV, dtype=torch.int32).expand(2, 1, 1500).contiguous()
+    w = torch.rand(2, 1, 1500, generator=g, device=DEV)
+    count = torch.tensor([1500, 1500], dtype=torch.int32, device=DEV)
+    po, wo = torch.zeros_like(pos), torch.zeros_like(w)
+    co = binding.cache_evict(K, V, count, pos, w, 600, positions_out=po, weights_out=wo)
+    torch.cuda.synchronize()
+    _check(Kb, Vb, K, V, None, pos, w, count, 600, 0, 0, (po, wo, co), (torch.zeros_like(po), torch.zeros_like(wo)))
+
+
+def test_evict_from_a_graph_and_on_another_stream():
+    B, Hkv, d, k_cap, budget, page = 2, 4, 128, 3000, 1000, 16
+    K, V, Kc, Vc, table, pos, w, g = _case(B, Hkv, d, k_cap, page, torch.bfloat16, 6)
+    count = torch.tensor([3000, 1700], dtype=torch.int32, device=DEV)
+    po, wo, co = torch.zeros_like(pos), torch.zeros_like(w), torch.zeros_like(count)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    Kg, Vg = Kc.clone(), Vc.clone()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        binding.cache_evict(Kg, Vg, count, pos, w, budget, recent=16, first=4, block_table=table, k_cap=k_cap, positions_out=po, weights_out=wo,
+                            count_out=co, workspace=ws)
+    for step in range(3):
+        Kg.copy_(Kc), Vg.copy_(Vc), po.zero_(), wo.zero_()
+        w.copy_(torch.rand(w.shape, device=DEV))
+        count.copy_(torch.tensor([3000 - 700 * step, 900 + 500 * step], dtype=torch.int32))
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        Ke, Ve, pe, we = Kc.clone(), Vc.clone(), torch.zeros_like(pos), torch.zeros_like(w)
+        ce = binding.cache_evict(Ke, Ve, count, pos, w, budget, recent=16, first=4, block_table=table, k_cap=k_cap, positions_out=pe, weights_out=we)
+        torch.cuda.synchronize()
+        for a, b in ((Kg, Ke), (Vg, Ve)):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+        assert torch.equal(po, pe) and torch.equal(wo, we) and torch.equal(co, ce)
