@@ -22,68 +22,90 @@ struct BoundsArgs {
   int64_t c_sb, c_sh, c_st, b_sb, b_sh;
 };
 
+// Pairs of 16-bit numbers as integers in the numbers' order (its own inverse); a NaN lies beyond the infinity of its sign.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ s16x2 as_pair(uint32_t x) { return __builtin_bit_cast(s16x2, x); }
+__device__ __forceinline__ uint32_t as_word(s16x2 x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ s16x2 in_order(s16x2 x) { return x ^ (s16x2)((x >> 15) & (short)0x7FFF); }
+// The least (MAX: the greatest) of both halves' pairs, over the lanes that have the same channels.
+template <bool MAX>
+__device__ __forceinline__ s16x2 better(s16x2 x, s16x2 y) { return MAX ? __builtin_elementwise_max(x, y) : __builtin_elementwise_min(x, y); }
+template <int LANES, bool MAX>
+__device__ __forceinline__ s16x2 over_rows(s16x2 x) {
+  const u32x2 h = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(as_word(x), as_word(x), false, false));
+  x = better<MAX>(as_pair(h[0]), as_pair(h[1]));
+  const u32x2 q = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(as_word(x), as_word(x), false, false));
+  x = better<MAX>(as_pair(q[0]), as_pair(q[1]));
+  if constexpr (LANES == 8)  // row_ror 8
+    x = better<MAX>(x, as_pair((uint32_t)__builtin_amdgcn_update_dpp(0, (int)as_word(x), 0x128, 0xF, 0xF, true)));
+  return x;
+}
+
 // blockIdx: (sequence, KV head) x chunks of four blocks, a wave each, from the first one that is asked for on.
+constexpr int kAtOnce = 4;  // loads of a lane on their way together
 template <typename T, int D>
 __global__ __launch_bounds__(256) void bounds_kernel(const BoundsArgs a, int chunks) {
   constexpr int LANES = D / 8, ROWS = 64 / LANES;
+  constexpr short INF = __is_same(T, __bf16) ? 0x7F80 : 0x7C00, MINUS_INF = ~INF;  // in order
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int unit = blockIdx.x / chunks, b = unit / a.Hkv, g = unit % a.Hkv;
   const int n = min(max(a.count[b], 0), a.k_cap), fresh = a.new_lens ? min(max(a.new_lens[b], 0), n) : n;
   if (fresh == 0) return;
   const int end = (n - 1) >> a.shift;
+  const int32_t* const table = a.table + (int64_t)b * a.max_pages;
   for (int blk = ((n - fresh) >> a.shift) + (int)(blockIdx.x % chunks) * 4 + wave; blk <= end; blk += 4 * chunks) {
-    float lo[8], hi[8];
-    int odd[8];
+    s16x2 lo[4], hi[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      lo[i] = __builtin_inff();
-      hi[i] = -__builtin_inff();
-      odd[i] = 0;
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = (s16x2)(short)0x7FFF;
+      hi[i] = (s16x2)(short)0x8000;
     }
     bool some = false;
     const int last = min(((blk + 1) << a.shift) - 1, n - 1);
-    for (int j = (blk << a.shift) + lane / LANES; j <= last; j += ROWS) {
-      int64_t at = b * a.c_sb + g * a.c_sh + j * a.c_st;
-      if (a.page_size) {
-        uint32_t p = __umulhi((uint32_t)j, a.page_magic);
-        if ((uint32_t)j - p * a.page_size >= (uint32_t)a.page_size) ++p;
-        const int32_t page = a.table[(int64_t)b * a.max_pages + p];
-        if ((uint32_t)page >= (uint32_t)a.num_pages) continue;
-        at = (((int64_t)page * a.Hkv + g) * a.page_size + (j - p * a.page_size)) * D;
-      }
-      const u32x4 v = *reinterpret_cast<const u32x4*>(a.K + at + 8 * (lane % LANES));
-      some = true;
+    for (int j0 = blk << a.shift; j0 <= last; j0 += kAtOnce * ROWS) {
+      int64_t at[kAtOnce];
+      bool is[kAtOnce];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = unpack<T>(v[i >> 1], i & 1);
-        odd[i] |= x != x;
-        lo[i] = fminf(lo[i], x);
-        hi[i] = fmaxf(hi[i], x);
+      for (int k = 0; k < kAtOnce; ++k) {  // (rows behind the last one are taken as the last)
+        const int j = min(j0 + k * ROWS + lane / LANES, last);
+        at[k] = b * a.c_sb + g * a.c_sh + j * a.c_st;
+        is[k] = true;
+        if (a.page_size) {
+          uint32_t p = __umulhi((uint32_t)j, a.page_magic);
+          if ((uint32_t)j - p * a.page_size >= (uint32_t)a.page_size) ++p;
+          const uint32_t page = (uint32_t)table[p];
+          is[k] = page < (uint32_t)a.num_pages;
+          at[k] = is[k] ? (((int64_t)page * a.Hkv + g) * a.page_size + (j - p * a.page_size)) * D : 0;
+        }
       }
-    }
+      u32x4 v[kAtOnce];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+      for (int k = 0; k < kAtOnce; ++k) v[k] = *reinterpret_cast<const u32x4*>(a.K + at[k] + 8 * (lane % LANES));
 #pragma unroll
-      for (int o = LANES; o < 64; o <<= 1) {
-        lo[i] = fminf(lo[i], __shfl_xor(lo[i], o));
-        hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], o));
-        odd[i] |= __shfl_xor(odd[i], o);
-      }
-      if (odd[i]) {
-        lo[i] = -__builtin_inff();
-        hi[i] = __builtin_inff();
+      for (int k = 0; k < kAtOnce; ++k) {
+        some = some || is[k];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const s16x2 x = in_order(as_pair(v[k][i]));
+          lo[i] = is[k] ? better<false>(lo[i], x) : lo[i];
+          hi[i] = is[k] ? better<true>(hi[i], x) : hi[i];
+        }
       }
     }
-    if (!__any(some)) {
+    const bool any = __any(some);
+    u32x4 w;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) lo[i] = hi[i] = 0.0f;
-    }
-    if (lane < 2 * LANES) {  // the first lanes write the least values, the next the greatest
-      u32x4 w;
+    for (int i = 0; i < 4; ++i) {
+      s16x2 l = over_rows<LANES, false>(lo[i]), h = over_rows<LANES, true>(hi[i]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = lane < LANES ? pack2<T>(lo[2 * i], lo[2 * i + 1]) : pack2<T>(hi[2 * i], hi[2 * i + 1]);
-      *reinterpret_cast<u32x4*>(a.bounds + b * a.b_sb + g * a.b_sh + (int64_t)blk * 2 * D + 8 * lane) = w;
+      for (int e = 0; e < 2; ++e) {
+        const bool nan = l[e] < MINUS_INF || h[e] > INF;
+        l[e] = nan ? MINUS_INF : l[e];
+        h[e] = nan ? INF : h[e];
+      }
+      w[i] = any ? as_word(in_order(lane < LANES ? l : h)) : 0;  // the first lanes write the least values, the next the greatest
     }
+    if (lane < 2 * LANES) *reinterpret_cast<u32x4*>(a.bounds + b * a.b_sb + g * a.b_sh + (int64_t)blk * 2 * D + 8 * lane) = w;
   }
 }
 
@@ -96,72 +118,108 @@ struct SelectArgs {
   int64_t q_sb, q_sh, b_sb, b_sh;
 };
 
-// A wave: 64 / (D / 4) blocks at a time, 16 bytes of a block's 2 D numbers a lane.
-constexpr int kScoreBlocks = 64;  // of a workgroup
+// A wave: kLoads times 1 KB of neighbouring blocks' bounds, requested together, 16 bytes of a block's 2 D numbers a lane.  A block's sum
+// is spread over LANES lanes: the first steps of adding up halve the number of sums that a lane looks after.
+constexpr int kLoads = 8;
+template <int D>
+constexpr int blocks_of_wave() { return kLoads * 64 / (D / 4); }
 template <typename T, int D>
 __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, int chunks) {
-  constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
+  constexpr int LANES = D / 4, AT_ONCE = 64 / LANES, OWN = blocks_of_wave<D>();
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = lane % LANES;
   const int unit = blockIdx.x / chunks, b = unit / a.Hkv, g = unit % a.Hkv;
   const int n = min(max(a.count[b], 0), a.k_cap), have = (n + (1 << a.shift) - 1) >> a.shift;
   const bool least = piece < LANES / 2;
-  int c = (int)(blockIdx.x % chunks);
-  if ((int64_t)c * kScoreBlocks >= have) return;
+  int64_t blk0 = (int64_t)(blockIdx.x % chunks * 4 + wave) * OWN;
+  if (blk0 >= have) return;
+  const uint16_t* const from = a.bounds + b * a.b_sb + g * a.b_sh + 8 * piece;
+  u32x4 v[kLoads];
+  auto load = [&](int64_t blk) {
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      v[k] = *reinterpret_cast<const u32x4*>(from + min(blk + k * AT_ONCE + lane / LANES, (int64_t)have - 1) * (2 * D));
+  };
+  load(blk0);
   double f[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = 0.0;
-  for (int h = 0; h < a.G; ++h) {
-    const u32x4 q = *reinterpret_cast<const u32x4*>(a.q + b * a.q_sb + (g * a.G + h) * a.q_sh + 8 * (piece % (LANES / 2)));
+  for (int h0 = 0; h0 < a.G; h0 += 4) {  // four heads' loads at once
+    u32x4 q[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float x = unpack<T>(q[i >> 1], i & 1);
-      f[i] += x != x ? (double)x : (x < 0.0f) == least ? (double)x : 0.0;
-    }
+    for (int k = 0; k < 4; ++k)
+      q[k] = *reinterpret_cast<const u32x4*>(a.q + b * a.q_sb + (g * a.G + min(h0 + k, a.G - 1)) * a.q_sh + 8 * (piece % (LANES / 2)));
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = unpack<T>(q[k][i >> 1], i & 1);
+        f[i] += h0 + k < a.G && (x != x || (x < 0.0f) == least) ? (double)x : 0.0;
+      }
   }
-  const uint16_t* const from = a.bounds + b * a.b_sb + g * a.b_sh + 8 * piece;
-  for (; (int64_t)c * kScoreBlocks < have; c += chunks) {
-    for (int k = AT_ONCE * wave; k < kScoreBlocks; k += 4 * AT_ONCE) {
-      const int blk = c * kScoreBlocks + k + lane / LANES;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(from + (int64_t)min(blk, have - 1) * 2 * D);
-      double s = 0.0;
+  for (;;) {
+    double s[kLoads];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s = __builtin_fma(f[i], (double)unpack<T>(v[i >> 1], i & 1), s);
+    for (int k = 0; k < kLoads; ++k) {
+      s[k] = 0.0;
 #pragma unroll
-      for (int o = 1; o < LANES; o <<= 1) s += __shfl_xor(s, o);
-      if (piece == 0 && blk < have) {
-        const float x = (float)s;
-        a.scores[(int64_t)unit * a.all + blk] = x == x ? x : __builtin_inff();
+      for (int i = 0; i < 8; ++i) s[k] = __builtin_fma(f[i], (double)unpack<T>(v[k][i >> 1], i & 1), s[k]);
+    }
+    const int64_t next = blk0 + (int64_t)chunks * 4 * OWN;
+    if (next < have) load(next);
+#pragma unroll
+    for (int half = kLoads / 2, o = 1; half > 0; half >>= 1, o <<= 1) {
+#pragma unroll
+      for (int k = 0; k < half; ++k) {
+        const double keep = lane & o ? s[k + half] : s[k], give = lane & o ? s[k] : s[k + half];
+        s[k] = keep + __shfl_xor(give, o);
       }
     }
+#pragma unroll
+    for (int o = kLoads; o < LANES; o <<= 1) s[0] += __shfl_xor(s[0], o);
+    // (lane bits 0, 1, 2 chose bits 2, 1, 0 of the load's number)
+    const int64_t blk = blk0 + (((lane & 1) << 2) | (lane & 2) | ((lane >> 2) & 1)) * AT_ONCE + lane / LANES;
+    if (piece < kLoads && blk < have) {
+      const float x = (float)s[0];
+      a.scores[(int64_t)unit * a.all + blk] = x == x ? x : __builtin_inff();
+    }
+    if (next >= have) break;
+    blk0 = next;
   }
 }
 
-constexpr int kThreads = 1024;
+template <int KEPT>
+__device__ __forceinline__ void list_blocks(const SelectArgs& a, int unit, int have, SelectLds& lds) {
+  int32_t* const out = a.blocks + (int64_t)unit * a.most;
+  const float* const score = a.scores + (int64_t)unit * a.all;
+  auto key_at = [&](int k) {
+    const uint32_t key = key_of_float(score[k]);
+    return k < a.first || k >= have - a.recent ? 0xFFFFFFFFu : key;
+  };
+  Keys<KEPT, decltype(key_at)> keys(have, key_at);
+  keys.fill();
+  const Cutoff cut = cutoff_of(keys, a.most, lds);
+  const int equal = equal_before(keys, cut, lds);
+  int mine = 0;
+  each_of_largest(keys, cut, equal, [&](int, bool taken, bool) { mine += __popcll(__ballot(taken)); });
+  Two all;
+  int at = before_wave(mine, 0, all, lds).a;
+  each_of_largest(keys, cut, equal, [&](int k, bool taken, bool) {
+    const uint64_t some = __ballot(taken);
+    if (taken) out[at + below_me(some)] = k;
+    at += __popcll(some);
+  });
+}
+
 __global__ __launch_bounds__(kThreads) void block_list_kernel(const SelectArgs a) {
-  __shared__ uint32_t lds[258];
-  __shared__ int lds_sums[2 * kThreads / 64];
+  __shared__ SelectLds lds;
   const int unit = blockIdx.x, b = unit / a.Hkv;
   const int n = min(max(a.count[b], 0), a.k_cap), have = (n + (1 << a.shift) - 1) >> a.shift;
-  int32_t* const out = a.blocks + (int64_t)unit * a.most;
   if (have <= a.most) {
-    for (int i = threadIdx.x; i < a.most; i += kThreads) out[i] = i < have ? i : -1;
-    return;
-  }
-  const float* const score = a.scores + (int64_t)unit * a.all;
-  auto key_at = [&](int k) { return k < a.first || k >= have - a.recent ? 0xFFFFFFFFu : key_of_float(score[k]); };
-  const Cutoff cut = cutoff_of<kThreads>(have, a.most, key_at, lds);
-  int equal = 0, taken = 0;
-  for (int k0 = 0; k0 < have; k0 += kThreads) {
-    const int k = k0 + threadIdx.x;
-    const uint32_t key = k < have ? key_at(k) : 0;
-    const bool is = k < have && key == cut.key, over = k < have && key > cut.key;
-    Two sums;
-    const Two at = count_before<kThreads>(is, over, sums, lds_sums);
-    // (equal ones are taken while there is room for them)
-    const int mine = min(equal + at.a, cut.equal) + taken + at.b;
-    if (over || (is && equal + at.a < cut.equal)) out[mine] = k;
-    equal += sums.a;
-    taken += sums.b;
+    for (int i = threadIdx.x; i < a.most; i += kThreads) a.blocks[(int64_t)unit * a.most + i] = i < have ? i : -1;
+  } else if (have <= 8 * kThreads) {
+    list_blocks<8>(a, unit, have, lds);
+  } else {
+    list_blocks<0>(a, unit, have, lds);
   }
 }
 
@@ -205,9 +263,12 @@ Grid grid_of(const pkv_block_desc& d) {
   return grid_of(d.B, d.Hkv, d.Hq / d.Hkv, listed < d.k_cap ? listed : d.k_cap);
 }
 
-// Workgroups of `per` blocks each that all blocks of a head can need, as many as a launch holds for all heads.
+// Workgroups of `per` blocks each for every head: as many as a cache's blocks need, but in all no more than the device holds at a time.
+// Most of the blocks of a large cache are not there, or not asked for, and a workgroup that finds nothing to do still has to be started:
+// the bounds of one new row of 4 x 8 heads with room for 128k rows take 31 us in 65536 workgroups.
+constexpr int kAtATime = 2048;
 int chunks_of(int64_t blocks, int per, int64_t units) {
-  const int64_t chunks = (blocks + per - 1) / per, most = kMaxGrid / units;
+  const int64_t chunks = (blocks + per - 1) / per, most = (kAtATime + units - 1) / units;
   return (int)(chunks < most ? chunks : most);
 }
 
@@ -273,7 +334,7 @@ int pkv_block_select(const pkv_block_desc* desc, const void* q, const void* boun
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.b_sb = d.b_sb; a.b_sh = d.b_sh;
   const int64_t units = (int64_t)d.B * d.Hkv;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const int chunks = chunks_of(a.all, kScoreBlocks, units);
+  const int chunks = chunks_of(a.all, 4 * (d.d == 128 ? blocks_of_wave<128>() : blocks_of_wave<64>()), units);
   const dim3 grid((unsigned)(units * chunks)), block(256);
   if (d.dtype == PKV_BF16) {
     if (d.d == 128) hipLaunchKernelGGL((block_score_kernel<__bf16, 128>), grid, block, 0, st, a, chunks);

@@ -5,15 +5,14 @@
 // order, in place.
 #include <string.h>
 
-#include "pkv_attn.h"
 #include "pkv_long.h"
 #include "pkv_topk.h"
 
 namespace pkv {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kPairs = 32;  // of a workgroup of the second launch
+constexpr int kMovedHere = 64;  // rows that the first launch moves by itself
+constexpr int kPairs = 32;      // of a workgroup of the second launch
 
 struct EvictArgs {
   char *K, *V;
@@ -39,75 +38,203 @@ __device__ __forceinline__ int64_t row_at(const EvictArgs& a, int b, int g, int 
   return (((int64_t)page * a.Hkv + g) * a.page_size + (j - p * a.page_size)) * a.d * 2;
 }
 
-__global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs a) {
-  __shared__ uint32_t lds[258];
-  __shared__ int lds_sums[2 * kThreads / 64], lds_newest[kThreads / 64];
-  const int unit = blockIdx.x, b = unit / a.Hkv, g = unit % a.Hkv;
-  const int n = min(max(a.count[b], 0), a.k_cap), kept = min(n, a.budget);
-  const int32_t* const pos = a.positions + b * a.p_sb + g * a.p_sh;
-  const float* const weight = a.weights + b * a.w_sb + g * a.w_sh;
-  int32_t* const pos_out = a.positions_out + b * a.po_sb + g * a.po_sh;
-  float* const weight_out = a.weights_out + b * a.wo_sb + g * a.wo_sh;
-  if (g == 0 && threadIdx.x == 0 && a.count_out) a.count_out[b] = kept;
-  if (n <= a.budget) {
-    for (int r = threadIdx.x; r < n; r += kThreads) {
-      pos_out[r] = pos[r];
-      weight_out[r] = weight[r];
-    }
-    if (threadIdx.x == 0) a.moves[unit] = 0;
-    return;
+// A pair's rows of K and V, a 16-byte piece of each; left out where a page does not exist.
+__device__ __forceinline__ void move_piece(const EvictArgs& a, int b, int g, int to, int from, int piece) {
+  const int64_t dst = row_at(a, b, g, to), src = row_at(a, b, g, from);
+  if (dst < 0 || src < 0) return;
+  const u32x4 k = *reinterpret_cast<const u32x4*>(a.K + src + 16 * piece), v = *reinterpret_cast<const u32x4*>(a.V + src + 16 * piece);
+  *reinterpret_cast<u32x4*>(a.K + dst + 16 * piece) = k;
+  *reinterpret_cast<u32x4*>(a.V + dst + 16 * piece) = v;
+}
+
+// What a workgroup looks after: a sequence and KV head.
+struct Unit {
+  int unit, b, g, n;
+  const int32_t* pos;
+  const float* weight;
+  int32_t* pos_out;
+  float* weight_out;
+};
+
+// Pairs are known: the rows' positions and weights follow, then the rows behind the budget are emptied, and few rows of K and V are
+// moved here.
+__device__ __forceinline__ void finish(const EvictArgs& a, const Unit& u, int late) {
+  const int32_t *const to = a.pairs + (int64_t)u.unit * 2 * a.most, *const from = to + a.most;
+  __threadfence_block();
+  __syncthreads();
+  for (int i = threadIdx.x; i < late; i += kThreads) {
+    const int dst = to[i], src = from[i];
+    const bool there = row_at(a, u.b, u.g, dst) >= 0 && row_at(a, u.b, u.g, src) >= 0;
+    u.pos_out[dst] = there ? u.pos[src] : -1;
+    u.weight_out[dst] = u.weight[src];
   }
-  int newest = -1;
-  for (int r = threadIdx.x; r < n; r += kThreads) newest = max(newest, pos[r]);
+  const bool here = late <= kMovedHere;
+  if (threadIdx.x == 0) a.moves[u.unit] = here ? 0 : late;
+  if (here) {
+    const int lanes = a.d / 8;
+    for (int i = threadIdx.x; i < late * lanes; i += kThreads) move_piece(a, u.b, u.g, to[i / lanes], from[i / lanes], i % lanes);
+  }
+  __syncthreads();
+  for (int r = a.budget + threadIdx.x; r < u.n; r += kThreads) {
+    u.pos_out[r] = -1;
+    u.weight_out[r] = 0.0f;
+  }
+}
+
+// A row's key: rows that are not there 0, weights that are NaN 1, protected rows the greatest.
+__device__ __forceinline__ uint32_t row_key(const EvictArgs& a, int32_t p, float w, int newest) {
+  return p < 0 ? 0u : p < a.first || p > newest - a.recent ? 0xFFFFFFFFu : w == w ? key_of_float(w) : 1u;
+}
+__device__ __forceinline__ int newest_of_all(int newest, SelectLds& lds) {
   newest = wave_max(newest);
-  if ((threadIdx.x & 63) == 0) lds_newest[threadIdx.x >> 6] = newest;
+  if ((threadIdx.x & 63) == 0) lds.sums[threadIdx.x >> 6][0] = newest;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) newest = max(newest, lds_newest[w]);
-  auto key_at = [&](int r) {
-    const int32_t p = pos[r];
-    if (p < 0) return 0u;
-    if (p < a.first || p > newest - a.recent) return 0xFFFFFFFFu;
-    const float w = weight[r];
-    return w == w ? key_of_float(w) : 1u;
-  };
-  const Cutoff cut = cutoff_of<kThreads>(n, a.budget, key_at, lds);
+  for (int w = 0; w < kWavesOf; ++w) newest = max(newest, lds.sums[w][0]);
+  return newest;
+}
 
-  int32_t *const to = a.pairs + (int64_t)unit * 2 * a.most, *const from = to + a.most;
-  int equal = 0, holes = 0, late = 0;
-  for (int r0 = 0; r0 < n; r0 += kThreads) {
-    const int r = r0 + threadIdx.x;
-    const uint32_t key = r < n ? key_at(r) : 0;
-    Two sums;
-    const Two eq = count_before<kThreads>(r < n && key == cut.key, false, sums, lds_sums);
-    const bool stays = r < n && (key > cut.key || (key == cut.key && equal + eq.a < cut.equal));
-    equal += sums.a;
-    const bool hole = r < a.budget && !stays, moves = r >= a.budget && stays;
-    const Two at = count_before<kThreads>(hole, moves, sums, lds_sums);
-    if (hole) to[holes + at.a] = r;
-    if (moves) from[late + at.b] = r;
-    holes += sums.a;
-    late += sums.b;
-    if (r < a.budget && stays) {
-      const int32_t p = pos[r];
-      const float w = weight[r];
-      pos_out[r] = p;
-      weight_out[r] = w;
+template <int KEPT>
+__device__ __forceinline__ void evict_rows(const EvictArgs& a, const Unit& u, SelectLds& lds) {
+  int newest = -1;
+  auto key_at = [&](int r) { return row_key(a, u.pos[r], u.weight[r], newest); };
+  Keys<KEPT, decltype(key_at)> keys(u.n, key_at);
+  if constexpr (KEPT > 0) {
+    int32_t p[KEPT];
+    float w[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) p[i] = u.pos[keys.number(i)];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) w[i] = u.weight[keys.number(i)];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) newest = max(newest, p[i]);
+    newest = newest_of_all(newest, lds);
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) keys.kept[i] = row_key(a, p[i], w[i], newest);
+  } else {
+    for (int i0 = 0; i0 < keys.steps; i0 += kLookups) {
+#pragma unroll
+      for (int i = 0; i < kLookups; ++i) newest = max(newest, u.pos[keys.number(i0 + i)]);
+    }
+    newest = newest_of_all(newest, lds);
+  }
+  const Cutoff cut = cutoff_of(keys, a.budget, lds);
+  const int equal = equal_before(keys, cut, lds);
+  Two mine = {0, 0}, all;
+  each_of_largest(keys, cut, equal, [&](int r, bool stays, bool there) {
+    mine.a += __popcll(__ballot(there && !stays && r < a.budget));
+    mine.b += __popcll(__ballot(stays && r >= a.budget));
+  });
+  Two at = before_wave(mine.a, mine.b, all, lds);
+  int32_t *const to = a.pairs + (int64_t)u.unit * 2 * a.most, *const from = to + a.most;
+  const bool copy = u.pos_out != u.pos || u.weight_out != u.weight;
+  each_of_largest(keys, cut, equal, [&](int r, bool stays, bool there) {
+    const bool hole = there && !stays && r < a.budget, late = stays && r >= a.budget;
+    const uint64_t holes = __ballot(hole), lates = __ballot(late);
+    if (hole) to[at.a + below_me(holes)] = r;
+    if (late) from[at.b + below_me(lates)] = r;
+    at = {at.a + (int)__popcll(holes), at.b + (int)__popcll(lates)};
+    if (copy && stays && r < a.budget) {
+      const int32_t p = u.pos[r];
+      const float w = u.weight[r];
+      u.pos_out[r] = p;
+      u.weight_out[r] = w;
+    }
+  });
+  finish(a, u, all.b);  // (as many holes as late rows)
+}
+
+// One row too many, as in a step of decoding: the row with the least key goes, the last of those that have it.  The last row, which
+// takes its place, is requested before that is known.
+__device__ __forceinline__ void evict_one(const EvictArgs& a, const Unit& u, SelectLds& lds) {
+  const int lanes = a.d / 8, last = u.n - 1;
+  const int64_t src = row_at(a, u.b, u.g, last);
+  u32x4 k = (u32x4)(0), v = (u32x4)(0);
+  if (src >= 0 && (int)threadIdx.x < lanes) {
+    k = *reinterpret_cast<const u32x4*>(a.K + src + 16 * threadIdx.x);
+    v = *reinterpret_cast<const u32x4*>(a.V + src + 16 * threadIdx.x);
+  }
+  const int32_t last_pos = u.pos[last];
+  const float last_weight = u.weight[last];
+  int newest = -1;
+  for (int r0 = threadIdx.x; r0 < u.n; r0 += 4 * kThreads) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) newest = max(newest, u.pos[min(r0 + i * kThreads, last)]);
+  }
+  newest = newest_of_all(newest, lds);
+  uint64_t least = ~(uint64_t)0;  // key and, descending, row
+  const bool copy = u.pos_out != u.pos || u.weight_out != u.weight;
+  for (int r0 = threadIdx.x; r0 < u.n; r0 += 4 * kThreads) {
+    int32_t p[4];
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      p[i] = u.pos[min(r0 + i * kThreads, last)];
+      w[i] = u.weight[min(r0 + i * kThreads, last)];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = min(r0 + i * kThreads, last);
+      least = min(least, (uint64_t)row_key(a, p[i], w[i], newest) << 32 | (uint32_t)~r);
+      if (copy && r < last) {
+        u.pos_out[r] = p[i];
+        u.weight_out[r] = w[i];
+      }
     }
   }
-  __threadfence_block();
-  __syncthreads();  // (holes == late)
-  for (int i = threadIdx.x; i < late; i += kThreads) {
-    const bool there = row_at(a, b, g, to[i]) >= 0 && row_at(a, b, g, from[i]) >= 0;
-    pos_out[to[i]] = there ? pos[from[i]] : -1;
-    weight_out[to[i]] = weight[from[i]];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o));
+  if ((threadIdx.x & 63) == 0) lds.keys[threadIdx.x >> 6] = least;
+  __syncthreads();  // (also: what is copied has been)
+#pragma unroll
+  for (int w = 0; w < kWavesOf; ++w) least = min(least, lds.keys[w]);
+  const int hole = (int)~(uint32_t)least;
+  const int64_t dst = hole < last ? row_at(a, u.b, u.g, hole) : -1;
+  const bool moved = src >= 0 && dst >= 0;
+  if (moved && (int)threadIdx.x < lanes) {
+    *reinterpret_cast<u32x4*>(a.K + dst + 16 * threadIdx.x) = k;
+    *reinterpret_cast<u32x4*>(a.V + dst + 16 * threadIdx.x) = v;
   }
-  __syncthreads();
-  for (int r = a.budget + threadIdx.x; r < n; r += kThreads) {
-    pos_out[r] = -1;
-    weight_out[r] = 0.0f;
+  if (threadIdx.x == 0) {
+    if (hole < last) {
+      u.pos_out[hole] = moved ? last_pos : -1;
+      u.weight_out[hole] = last_weight;
+    }
+    u.pos_out[last] = -1;
+    u.weight_out[last] = 0.0f;
+    a.moves[u.unit] = 0;
   }
-  if (threadIdx.x == 0) a.moves[unit] = late;
+}
+
+__global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs a) {
+  __shared__ SelectLds lds;
+  Unit u;
+  u.unit = blockIdx.x;
+  u.b = u.unit / a.Hkv;
+  u.g = u.unit % a.Hkv;
+  u.n = min(max(a.count[u.b], 0), a.k_cap);
+  u.pos = a.positions + u.b * a.p_sb + u.g * a.p_sh;
+  u.weight = a.weights + u.b * a.w_sb + u.g * a.w_sh;
+  u.pos_out = a.positions_out + u.b * a.po_sb + u.g * a.po_sh;
+  u.weight_out = a.weights_out + u.b * a.wo_sb + u.g * a.wo_sh;
+  if (u.g == 0 && threadIdx.x == 0 && a.count_out) a.count_out[u.b] = min(u.n, a.budget);
+  if (u.n <= a.budget) {
+    if (u.pos_out != u.pos || u.weight_out != u.weight) {
+      for (int r = threadIdx.x; r < u.n; r += kThreads) {
+        u.pos_out[r] = u.pos[r];
+        u.weight_out[r] = u.weight[r];
+      }
+    }
+    if (threadIdx.x == 0) a.moves[u.unit] = 0;
+  } else if (u.n == a.budget + 1) {
+    evict_one(a, u, lds);
+  } else if (u.n <= 4 * kThreads) {
+    evict_rows<4>(a, u, lds);
+  } else if (u.n <= 32 * kThreads) {
+    evict_rows<32>(a, u, lds);
+  } else {
+    evict_rows<0>(a, u, lds);
+  }
 }
 
 // A workgroup: kPairs rows of K and of V, 16 bytes a thread at a time.
@@ -119,12 +246,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a, int 
     for (int i = threadIdx.x; i < kPairs * lanes; i += 256) {
       const int p = (int)(c * kPairs) + i / lanes;
       if (p >= moves) break;
-      const int64_t dst = row_at(a, b, g, to[p]), src = row_at(a, b, g, from[p]);
-      if (dst < 0 || src < 0) continue;
-      const int piece = 16 * (i % lanes);
-      const u32x4 k = *reinterpret_cast<const u32x4*>(a.K + src + piece), v = *reinterpret_cast<const u32x4*>(a.V + src + piece);
-      *reinterpret_cast<u32x4*>(a.K + dst + piece) = k;
-      *reinterpret_cast<u32x4*>(a.V + dst + piece) = v;
+      move_piece(a, b, g, to[p], from[p], i % lanes);
     }
   }
 }
@@ -191,7 +313,7 @@ int pkv_cache_evict(const pkv_evict_desc* desc, void* K_cache, void* V_cache, co
   const hipStream_t st = static_cast<hipStream_t>(stream);
   hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)units), dim3(kThreads), 0, st, a);
   if (hipGetLastError() != hipSuccess) return PKV_ERR_HIP;
-  if (a.most == 0) return PKV_OK;
+  if (a.most <= kMovedHere) return PKV_OK;
   int64_t chunks = (a.most + kPairs - 1) / kPairs;
   if (chunks > kMaxGrid / units) chunks = kMaxGrid / units;
   hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(units * chunks)), dim3(256), 0, st, a, (int)chunks);

@@ -9,76 +9,163 @@
 namespace pkv {
 namespace {
 
+constexpr int kThreads = 1024, kWavesOf = kThreads / 64;  // of a workgroup that selects
+
 // Order of floats as unsigned numbers: -inf 0x007FFFFF .. +inf 0xFF800000; a zero's sign does not count.
 __device__ __forceinline__ uint32_t key_of_float(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// The k-th largest of keys 0 .. n - 1 (1 <= k <= n), and how many of those that equal it are among the k largest: eight bits at a time, by
-// a count of the keys that agree with what is known so far.  Called by all THREADS threads; `lds`: 258 words.
+// A workgroup's n keys: wave w looks after a run of them, 64 neighbours at a time, so that ranks need the waves' counts alone.  Up to
+// KEPT * kThreads keys are kept in registers; KEPT 0: any number, each looked up (key_at) whenever it is needed.  Numbers behind the
+// last one are looked up as the last, so that no load waits for a comparison.
+constexpr int kLookups = 8;  // on their way together
+template <int KEPT, typename KeyAt>
+struct Keys {
+  const KeyAt key_at;
+  const int n, steps, first;  // `first`: the lane's first key
+  uint32_t kept[KEPT > 0 ? KEPT : 1];
+  __device__ __forceinline__ Keys(int n_, KeyAt key_at_)
+      : key_at(key_at_), n(n_), steps((n_ + kThreads - 1) / kThreads),
+        first((int)(threadIdx.x >> 6) * steps * 64 + (int)(threadIdx.x & 63)) {}
+  __device__ __forceinline__ int number(int i) const { return min(first + 64 * i, n - 1); }
+  __device__ __forceinline__ void fill() {
+    if constexpr (KEPT > 0) {
+#pragma unroll
+      for (int i = 0; i < KEPT; ++i) kept[i] = key_at(number(i));
+    }
+  }
+  // f(number, key, whether there is such a key) in ascending order, in all lanes of a wave alike
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    if constexpr (KEPT > 0) {
+#pragma unroll
+      for (int i = 0; i < KEPT; ++i)
+        if (i < steps) f(first + 64 * i, kept[i], first + 64 * i < n);
+    } else {
+      for (int i0 = 0; i0 < steps; i0 += kLookups) {
+        uint32_t key[kLookups];
+#pragma unroll
+        for (int i = 0; i < kLookups; ++i) key[i] = key_at(number(i0 + i));
+#pragma unroll
+        for (int i = 0; i < kLookups; ++i)
+          if (i0 + i < steps) f(first + 64 * (i0 + i), key[i], first + 64 * (i0 + i) < n);
+      }
+    }
+  }
+};
+
+// What a workgroup's selection needs of LDS.
+struct SelectLds {
+  uint32_t bins[2048];
+  int sums[kWavesOf][3];
+  int found[3];
+  uint64_t keys[kWavesOf];
+};
+
+// The k-th largest key (1 <= k <= n), and how many of those that equal it are among the k largest, from the first on (`every`: all).
+// Eleven bits at a time, by a count of the keys that agree with what is known so far: with fewer bits the first count would meet a
+// few exponents' bins only, and additions to one word of LDS wait for one another.  Where all of 64 neighbours meet the same bin,
+// they are added at once.
 struct Cutoff {
   uint32_t key;
   int equal;
+  bool every;
 };
-template <int THREADS, typename KeyAt>
-__device__ __forceinline__ Cutoff cutoff_of(int n, int k, KeyAt key_at, uint32_t* lds) {
+template <typename K>
+__device__ __forceinline__ Cutoff cutoff_of(const K& keys, int k, SelectLds& lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t known = 0, mask = 0;
-  int left = k;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += THREADS) lds[i] = 0;
+  int left = k, met = 0;
+#pragma unroll 1
+  for (int shift = 21; shift >= 0; shift = shift == 10 ? 0 : shift - 11) {
+    const uint32_t wide = shift == 0 ? 1023 : 2047;
+    lds.bins[threadIdx.x] = lds.bins[threadIdx.x + kThreads] = 0;
     __syncthreads();
-    for (int r = threadIdx.x; r < n; r += THREADS) {
-      const uint32_t key = key_at(r);
-      if ((key & mask) == known) atomicAdd(&lds[key >> shift & 255], 1u);
-    }
-    __syncthreads();
-    if (threadIdx.x < 64) {  // lane i: bins 255 - 4 i and the three below
-      const int lane = threadIdx.x;
-      int c[4], sum = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum += c[i] = (int)lds[255 - 4 * lane - i];
-      int before = sum_upto(sum) - sum;
-      if (before < left && before + sum >= left) {
-        int i = 0;
-        while (i < 3 && before + c[i] < left) before += c[i++];
-        lds[256] = 255 - 4 * lane - i;
-        lds[257] = left - before;
+    keys.each([&](int, uint32_t key, bool there) {
+      const bool mine = there && (key & mask) == known;
+      const uint64_t some = __ballot(mine);
+      if (some == 0) return;
+      const uint32_t bin = key >> shift & wide;
+      const int lead = __builtin_ctzll(some);
+      if (__ballot(mine && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, lead)) == some) {
+        if (lane == lead) atomicAdd(&lds.bins[bin], (uint32_t)__popcll(some));
+      } else if (mine) {
+        atomicAdd(&lds.bins[bin], 1u);
       }
+    });
+    __syncthreads();
+    // a thread: two bins, the largest first
+    const int top = 2047 - 2 * (int)threadIdx.x;
+    const int c0 = (int)lds.bins[top], c1 = (int)lds.bins[top - 1], upto = sum_upto(c0 + c1);
+    if (lane == 63) lds.sums[wave][0] = upto;
+    __syncthreads();
+    int before = upto - c0 - c1;
+    for (int w = 0; w < wave; ++w) before += lds.sums[w][0];
+    if (before < left && left <= before + c0 + c1) {
+      const bool second = left > before + c0;
+      lds.found[0] = top - second;
+      lds.found[1] = left - before - (second ? c0 : 0);
+      lds.found[2] = second ? c1 : c0;
     }
     __syncthreads();
-    known |= lds[256] << shift;
-    left = (int)lds[257];
-    mask |= 255u << shift;
-    __syncthreads();
+    known |= (uint32_t)lds.found[0] << shift;
+    left = lds.found[1];
+    met = lds.found[2];
+    mask |= wide << shift;
   }
-  return {known, left};
+  return {known, left, left == met};
 }
 
-// Numbers of the set flags before a thread's own, in the order of the threads, for two flags at once; `sums`: the numbers of all.
-// Called by all THREADS threads; `lds`: 2 * THREADS / 64 words.
+__device__ __forceinline__ int below_me(uint64_t flags) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(flags >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)flags, 0));
+}
+
+// The sums of the earlier waves' numbers a, b, and of all; column `at` and the next of lds.sums.
 struct Two {
   int a, b;
 };
-template <int THREADS>
-__device__ __forceinline__ Two count_before(bool a, bool b, Two& sums, int* lds) {
-  constexpr int WAVES = THREADS / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t wa = __ballot(a), wb = __ballot(b), below = ((uint64_t)1 << lane) - 1;
+__device__ __forceinline__ Two before_wave(int a, int b, Two& all, SelectLds& lds) {
+  const int wave = threadIdx.x >> 6;
   __syncthreads();  // (what was there has been read)
-  if (lane == 0) {
-    lds[2 * wave] = __popcll(wa);
-    lds[2 * wave + 1] = __popcll(wb);
+  if ((threadIdx.x & 63) == 0) {
+    lds.sums[wave][1] = a;
+    lds.sums[wave][2] = b;
   }
   __syncthreads();
-  Two mine = {(int)__popcll(wa & below), (int)__popcll(wb & below)};
-  sums = {0, 0};
+  Two mine = {0, 0};
+  all = {0, 0};
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    if (w == wave) mine = {mine.a + sums.a, mine.b + sums.b};
-    sums = {sums.a + lds[2 * w], sums.b + lds[2 * w + 1]};
+  for (int w = 0; w < kWavesOf; ++w) {
+    if (w == wave) mine = all;
+    all = {all.a + lds.sums[w][1], all.b + lds.sums[w][2]};
   }
   return mine;
+}
+
+// f(number, whether it is one of the k largest, whether there is such a key) in ascending order.
+template <typename K, typename F>
+__device__ __forceinline__ void each_of_largest(const K& keys, const Cutoff& cut, int equal_before, F f) {
+  int equal = equal_before;  // of the keys before
+  keys.each([&](int r, uint32_t key, bool there) {
+    bool in = there && key >= cut.key;
+    if (!cut.every) {
+      const uint64_t same = __ballot(there && key == cut.key);
+      in = in && (key != cut.key || equal + below_me(same) < cut.equal);
+      equal += __popcll(same);
+    }
+    f(r, in, there);
+  });
+}
+// What the waves before have of keys that equal the cutoff (0 where all of those are taken).
+template <typename K>
+__device__ __forceinline__ int equal_before(const K& keys, const Cutoff& cut, SelectLds& lds) {
+  if (cut.every) return 0;
+  int equal = 0;
+  keys.each([&](int, uint32_t key, bool there) { equal += __popcll(__ballot(there && key == cut.key)); });
+  Two all;
+  return before_wave(equal, 0, all, lds).a;
 }
 
 }  // namespace
