@@ -115,6 +115,7 @@ struct SelectArgs {
   int32_t* blocks;
   float* scores;  // [B][Hkv][all]
   int32_t B, Hkv, G, k_cap, shift, all, most, first, recent;
+  int32_t in_lds;  // keys that the launch of block_list_kernel has room for
   int64_t q_sb, q_sh, b_sb, b_sh;
 };
 
@@ -129,34 +130,39 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, in
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = lane % LANES;
   const int unit = blockIdx.x / chunks, b = unit / a.Hkv, g = unit % a.Hkv;
   const int n = min(max(a.count[b], 0), a.k_cap), have = (n + (1 << a.shift) - 1) >> a.shift;
-  const bool least = piece < LANES / 2;
-  int64_t blk0 = (int64_t)(blockIdx.x % chunks * 4 + wave) * OWN;
-  if (blk0 >= have) return;
+  __shared__ __align__(16) double coefficients[2 * D];
+  if ((int64_t)(blockIdx.x % chunks) * 4 * OWN >= have) return;
+  int blk0 = (int)(blockIdx.x % chunks * 4 + wave) * OWN;
   const uint16_t* const from = a.bounds + b * a.b_sb + g * a.b_sh + 8 * piece;
   u32x4 v[kLoads];
-  auto load = [&](int64_t blk) {
+  auto load = [&](int blk) {
 #pragma unroll
     for (int k = 0; k < kLoads; ++k)
-      v[k] = *reinterpret_cast<const u32x4*>(from + min(blk + k * AT_ONCE + lane / LANES, (int64_t)have - 1) * (2 * D));
+      v[k] = *reinterpret_cast<const u32x4*>(from + (int64_t)min(blk + k * AT_ONCE + lane / LANES, have - 1) * (2 * D));
   };
   load(blk0);
+  // the heads' coefficients, a thread each: of the least values first
+  static_assert(2 * D <= 256, "a thread for each coefficient");
+  if (threadIdx.x < 2 * D) {
+    const uint16_t* const qp = a.q + b * a.q_sb + (int64_t)g * a.G * a.q_sh + threadIdx.x % D;
+    double c = 0.0;
+    for (int h0 = 0; h0 < a.G; h0 += 8) {  // eight heads' loads at once
+      uint16_t q[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) q[k] = qp[min(h0 + k, a.G - 1) * a.q_sh];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float x = unpack<T>(q[k], 0);
+        c += h0 + k < a.G && (x != x || (x < 0.0f) == (threadIdx.x < D)) ? (double)x : 0.0;
+      }
+    }
+    coefficients[threadIdx.x] = c;
+  }
+  __syncthreads();
   double f[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = 0.0;
-  for (int h0 = 0; h0 < a.G; h0 += 4) {  // four heads' loads at once
-    u32x4 q[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      q[k] = *reinterpret_cast<const u32x4*>(a.q + b * a.q_sb + (g * a.G + min(h0 + k, a.G - 1)) * a.q_sh + 8 * (piece % (LANES / 2)));
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = unpack<T>(q[k][i >> 1], i & 1);
-        f[i] += h0 + k < a.G && (x != x || (x < 0.0f) == least) ? (double)x : 0.0;
-      }
-  }
-  for (;;) {
+  for (int i = 0; i < 8; ++i) f[i] = coefficients[8 * piece + i];
+  while (blk0 < have) {
     double s[kLoads];
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
@@ -164,7 +170,7 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, in
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[k] = __builtin_fma(f[i], (double)unpack<T>(v[k][i >> 1], i & 1), s[k]);
     }
-    const int64_t next = blk0 + (int64_t)chunks * 4 * OWN;
+    const int next = blk0 + chunks * 4 * OWN;  // (blocks are 2^26 at most, a turn of all chunks 2^17)
     if (next < have) load(next);
 #pragma unroll
     for (int half = kLoads / 2, o = 1; half > 0; half >>= 1, o <<= 1) {
@@ -177,26 +183,19 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, in
 #pragma unroll
     for (int o = kLoads; o < LANES; o <<= 1) s[0] += __shfl_xor(s[0], o);
     // (lane bits 0, 1, 2 chose bits 2, 1, 0 of the load's number)
-    const int64_t blk = blk0 + (((lane & 1) << 2) | (lane & 2) | ((lane >> 2) & 1)) * AT_ONCE + lane / LANES;
+    const int blk = blk0 + (((lane & 1) << 2) | (lane & 2) | ((lane >> 2) & 1)) * AT_ONCE + lane / LANES;
     if (piece < kLoads && blk < have) {
       const float x = (float)s[0];
       a.scores[(int64_t)unit * a.all + blk] = x == x ? x : __builtin_inff();
     }
-    if (next >= have) break;
     blk0 = next;
   }
 }
 
-template <int KEPT>
-__device__ __forceinline__ void list_blocks(const SelectArgs& a, int unit, int have, SelectLds& lds) {
+template <typename KeyAt>
+__device__ __forceinline__ void list_blocks(const SelectArgs& a, int unit, int have, KeyAt key_at, SelectLds& lds) {
   int32_t* const out = a.blocks + (int64_t)unit * a.most;
-  const float* const score = a.scores + (int64_t)unit * a.all;
-  auto key_at = [&](int k) {
-    const uint32_t key = key_of_float(score[k]);
-    return k < a.first || k >= have - a.recent ? 0xFFFFFFFFu : key;
-  };
-  Keys<KEPT, decltype(key_at)> keys(have, key_at);
-  keys.fill();
+  const Keys<KeyAt> keys(have, key_at);
   const Cutoff cut = cutoff_of(keys, a.most, lds);
   const int equal = equal_before(keys, cut, lds);
   int mine = 0;
@@ -212,14 +211,27 @@ __device__ __forceinline__ void list_blocks(const SelectArgs& a, int unit, int h
 
 __global__ __launch_bounds__(kThreads) void block_list_kernel(const SelectArgs a) {
   __shared__ SelectLds lds;
+  extern __shared__ uint32_t kept[];
   const int unit = blockIdx.x, b = unit / a.Hkv;
   const int n = min(max(a.count[b], 0), a.k_cap), have = (n + (1 << a.shift) - 1) >> a.shift;
+  const float* const score = a.scores + (int64_t)unit * a.all;
+  auto key_at = [&](int k) {
+    const uint32_t key = key_of_float(score[k]);
+    return k < a.first || k >= have - a.recent ? 0xFFFFFFFFu : key;
+  };
   if (have <= a.most) {
     for (int i = threadIdx.x; i < a.most; i += kThreads) a.blocks[(int64_t)unit * a.most + i] = i < have ? i : -1;
-  } else if (have <= 8 * kThreads) {
-    list_blocks<8>(a, unit, have, lds);
+  } else if (have <= a.in_lds) {
+    for (int k0 = threadIdx.x; k0 < have; k0 += kLookups * kThreads) {
+      uint32_t key[kLookups];
+#pragma unroll
+      for (int i = 0; i < kLookups; ++i) key[i] = key_at(min(k0 + i * kThreads, have - 1));
+#pragma unroll
+      for (int i = 0; i < kLookups; ++i) kept[min(k0 + i * kThreads, have - 1)] = key[i];
+    }
+    list_blocks(a, unit, have, [&](int k) { return kept[k]; }, lds);  // (its first barrier comes before the first look-up)
   } else {
-    list_blocks<0>(a, unit, have, lds);
+    list_blocks(a, unit, have, key_at, lds);
   }
 }
 
@@ -332,6 +344,9 @@ int pkv_block_select(const pkv_block_desc* desc, const void* q, const void* boun
   a.B = d.B; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.k_cap = d.k_cap; a.shift = shift_of(d.block); a.all = (int32_t)blocks_of(d);
   a.most = d.most; a.first = d.first; a.recent = d.recent;
   a.q_sb = d.q_sb; a.q_sh = d.q_sh; a.b_sb = d.b_sb; a.b_sh = d.b_sh;
+  a.in_lds = keys_in_lds(a.all);
+  static bool granted[kMaxDevices];
+  if (grant_keys(reinterpret_cast<const void*>(block_list_kernel), granted) != hipSuccess) return PKV_ERR_HIP;
   const int64_t units = (int64_t)d.B * d.Hkv;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const int chunks = chunks_of(a.all, 4 * (d.d == 128 ? blocks_of_wave<128>() : blocks_of_wave<64>()), units);
@@ -344,7 +359,7 @@ int pkv_block_select(const pkv_block_desc* desc, const void* q, const void* boun
     else hipLaunchKernelGGL((block_score_kernel<_Float16, 64>), grid, block, 0, st, a, chunks);
   }
   if (hipGetLastError() != hipSuccess) return PKV_ERR_HIP;
-  hipLaunchKernelGGL(block_list_kernel, dim3((unsigned)units), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL(block_list_kernel, dim3((unsigned)units), dim3(kThreads), (size_t)a.in_lds * sizeof(uint32_t), st, a);
   return hipGetLastError() == hipSuccess ? PKV_OK : PKV_ERR_HIP;
 }
 

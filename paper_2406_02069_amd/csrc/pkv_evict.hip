@@ -24,6 +24,7 @@ struct EvictArgs {
   int32_t* moves;  // [unit]
   int32_t* pairs;  // [unit][2][most]: destinations, sources
   int32_t B, Hkv, d, k_cap, page_size, num_pages, max_pages, budget, recent, first, most;
+  int32_t in_lds;  // keys that the launch has room for
   uint32_t page_magic;
   int64_t c_sb, c_sh, c_st, p_sb, p_sh, w_sb, w_sh, po_sb, po_sh, wo_sb, wo_sh;
 };
@@ -94,30 +95,10 @@ __device__ __forceinline__ int newest_of_all(int newest, SelectLds& lds) {
   return newest;
 }
 
-template <int KEPT>
-__device__ __forceinline__ void evict_rows(const EvictArgs& a, const Unit& u, SelectLds& lds) {
-  int newest = -1;
-  auto key_at = [&](int r) { return row_key(a, u.pos[r], u.weight[r], newest); };
-  Keys<KEPT, decltype(key_at)> keys(u.n, key_at);
-  if constexpr (KEPT > 0) {
-    int32_t p[KEPT];
-    float w[KEPT];
-#pragma unroll
-    for (int i = 0; i < KEPT; ++i) p[i] = u.pos[keys.number(i)];
-#pragma unroll
-    for (int i = 0; i < KEPT; ++i) w[i] = u.weight[keys.number(i)];
-#pragma unroll
-    for (int i = 0; i < KEPT; ++i) newest = max(newest, p[i]);
-    newest = newest_of_all(newest, lds);
-#pragma unroll
-    for (int i = 0; i < KEPT; ++i) keys.kept[i] = row_key(a, p[i], w[i], newest);
-  } else {
-    for (int i0 = 0; i0 < keys.steps; i0 += kLookups) {
-#pragma unroll
-      for (int i = 0; i < kLookups; ++i) newest = max(newest, u.pos[keys.number(i0 + i)]);
-    }
-    newest = newest_of_all(newest, lds);
-  }
+// The pairs of a head, by the keys that key_at looks up.
+template <typename KeyAt>
+__device__ __forceinline__ void pair_rows(const EvictArgs& a, const Unit& u, KeyAt key_at, SelectLds& lds) {
+  const Keys<KeyAt> keys(u.n, key_at);
   const Cutoff cut = cutoff_of(keys, a.budget, lds);
   const int equal = equal_before(keys, cut, lds);
   Two mine = {0, 0}, all;
@@ -142,6 +123,48 @@ __device__ __forceinline__ void evict_rows(const EvictArgs& a, const Unit& u, Se
     }
   });
   finish(a, u, all.b);  // (as many holes as late rows)
+}
+
+// Keys in LDS, from rows' positions and weights that are all requested together.
+__device__ __forceinline__ void evict_rows(const EvictArgs& a, const Unit& u, uint32_t* kept, SelectLds& lds) {
+  constexpr int MOST = kKeysInLds / kThreads;
+  int32_t p[MOST];
+  float w[MOST];
+  int newest = -1;
+#pragma unroll
+  for (int i0 = 0; i0 < MOST; i0 += kLookups) {
+    if (i0 * kThreads < u.n) {
+#pragma unroll
+      for (int i = i0; i < i0 + kLookups; ++i) p[i] = u.pos[min((int)threadIdx.x + i * kThreads, u.n - 1)];
+#pragma unroll
+      for (int i = i0; i < i0 + kLookups; ++i) w[i] = u.weight[min((int)threadIdx.x + i * kThreads, u.n - 1)];
+    }
+  }
+#pragma unroll
+  for (int i0 = 0; i0 < MOST; i0 += kLookups) {
+    if (i0 * kThreads < u.n) {
+#pragma unroll
+      for (int i = i0; i < i0 + kLookups; ++i) newest = max(newest, p[i]);
+    }
+  }
+  newest = newest_of_all(newest, lds);
+#pragma unroll
+  for (int i0 = 0; i0 < MOST; i0 += kLookups) {
+    if (i0 * kThreads < u.n) {
+#pragma unroll
+      for (int i = i0; i < i0 + kLookups; ++i) kept[min((int)threadIdx.x + i * kThreads, u.n - 1)] = row_key(a, p[i], w[i], newest);
+    }
+  }
+  pair_rows(a, u, [&](int r) { return kept[r]; }, lds);  // (its first barrier comes before the first look-up)
+}
+__device__ __forceinline__ void evict_rows_of_memory(const EvictArgs& a, const Unit& u, SelectLds& lds) {
+  int newest = -1;
+  for (int r0 = threadIdx.x; r0 < u.n; r0 += kLookups * kThreads) {
+#pragma unroll
+    for (int i = 0; i < kLookups; ++i) newest = max(newest, u.pos[min(r0 + i * kThreads, u.n - 1)]);
+  }
+  newest = newest_of_all(newest, lds);
+  pair_rows(a, u, [&](int r) { return row_key(a, u.pos[r], u.weight[r], newest); }, lds);
 }
 
 // One row too many, as in a step of decoding: the row with the least key goes, the last of those that have it.  The last row, which
@@ -208,6 +231,7 @@ __device__ __forceinline__ void evict_one(const EvictArgs& a, const Unit& u, Sel
 
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs a) {
   __shared__ SelectLds lds;
+  extern __shared__ uint32_t kept[];
   Unit u;
   u.unit = blockIdx.x;
   u.b = u.unit / a.Hkv;
@@ -228,12 +252,10 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs 
     if (threadIdx.x == 0) a.moves[u.unit] = 0;
   } else if (u.n == a.budget + 1) {
     evict_one(a, u, lds);
-  } else if (u.n <= 4 * kThreads) {
-    evict_rows<4>(a, u, lds);
-  } else if (u.n <= 32 * kThreads) {
-    evict_rows<32>(a, u, lds);
+  } else if (u.n <= a.in_lds) {
+    evict_rows(a, u, kept, lds);
   } else {
-    evict_rows<0>(a, u, lds);
+    evict_rows_of_memory(a, u, lds);
   }
 }
 
@@ -311,7 +333,10 @@ int pkv_cache_evict(const pkv_evict_desc* desc, void* K_cache, void* V_cache, co
   a.c_sb = d.c_sb; a.c_sh = d.c_sh; a.c_st = d.c_st; a.p_sb = d.p_sb; a.p_sh = d.p_sh; a.w_sb = d.w_sb; a.w_sh = d.w_sh;
   a.po_sb = d.po_sb; a.po_sh = d.po_sh; a.wo_sb = d.wo_sb; a.wo_sh = d.wo_sh;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)units), dim3(kThreads), 0, st, a);
+  a.in_lds = keys_in_lds(d.k_cap);
+  static bool granted[kMaxDevices];
+  if (grant_keys(reinterpret_cast<const void*>(evict_select_kernel), granted) != hipSuccess) return PKV_ERR_HIP;
+  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)units), dim3(kThreads), (size_t)a.in_lds * sizeof(uint32_t), st, a);
   if (hipGetLastError() != hipSuccess) return PKV_ERR_HIP;
   if (a.most <= kMovedHere) return PKV_OK;
   int64_t chunks = (a.most + kPairs - 1) / kPairs;

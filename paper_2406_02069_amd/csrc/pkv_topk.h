@@ -17,44 +17,43 @@ __device__ __forceinline__ uint32_t key_of_float(float x) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// A workgroup's n keys: wave w looks after a run of them, 64 neighbours at a time, so that ranks need the waves' counts alone.  Up to
-// KEPT * kThreads keys are kept in registers; KEPT 0: any number, each looked up (key_at) whenever it is needed.  Numbers behind the
-// last one are looked up as the last, so that no load waits for a comparison.
+// A workgroup's n keys: wave w looks after a run of them, 64 neighbours at a time, so that ranks need the waves' counts alone.  Numbers
+// behind the last one are looked up as the last, so that no look-up waits for a comparison.
 constexpr int kLookups = 8;  // on their way together
-template <int KEPT, typename KeyAt>
+template <typename KeyAt>
 struct Keys {
   const KeyAt key_at;
   const int n, steps, first;  // `first`: the lane's first key
-  uint32_t kept[KEPT > 0 ? KEPT : 1];
   __device__ __forceinline__ Keys(int n_, KeyAt key_at_)
       : key_at(key_at_), n(n_), steps((n_ + kThreads - 1) / kThreads),
         first((int)(threadIdx.x >> 6) * steps * 64 + (int)(threadIdx.x & 63)) {}
-  __device__ __forceinline__ int number(int i) const { return min(first + 64 * i, n - 1); }
-  __device__ __forceinline__ void fill() {
-    if constexpr (KEPT > 0) {
-#pragma unroll
-      for (int i = 0; i < KEPT; ++i) kept[i] = key_at(number(i));
-    }
-  }
   // f(number, key, whether there is such a key) in ascending order, in all lanes of a wave alike
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    if constexpr (KEPT > 0) {
+    for (int i0 = 0; i0 < steps; i0 += kLookups) {
+      uint32_t key[kLookups];
 #pragma unroll
-      for (int i = 0; i < KEPT; ++i)
-        if (i < steps) f(first + 64 * i, kept[i], first + 64 * i < n);
-    } else {
-      for (int i0 = 0; i0 < steps; i0 += kLookups) {
-        uint32_t key[kLookups];
+      for (int i = 0; i < kLookups; ++i) key[i] = key_at(min(first + 64 * (i0 + i), n - 1));
 #pragma unroll
-        for (int i = 0; i < kLookups; ++i) key[i] = key_at(number(i0 + i));
-#pragma unroll
-        for (int i = 0; i < kLookups; ++i)
-          if (i0 + i < steps) f(first + 64 * (i0 + i), key[i], first + 64 * (i0 + i) < n);
-      }
+      for (int i = 0; i < kLookups; ++i)
+        if (i0 + i < steps) f(first + 64 * (i0 + i), key[i], first + 64 * (i0 + i) < n);
     }
   }
 };
+
+// Keys that wait in LDS between the passes over them: up to so many, as far as a cache can hold that many (kernels take the room as
+// dynamic LDS; a workgroup with all of it has a compute unit to itself).  All others are formed again for each pass.
+constexpr int kKeysInLds = 32 * kThreads;
+// Raises a kernel's dynamic LDS limit to that, once per device (no allocation).
+inline hipError_t grant_keys(const void* kernel, bool* granted) {
+  const int dev = current_device_slot();
+  if (dev < 0) return hipErrorInvalidDevice;
+  if (granted[dev]) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kKeysInLds * (int)sizeof(uint32_t));
+  if (e == hipSuccess) granted[dev] = true;
+  return e;
+}
+inline int keys_in_lds(int64_t most) { return (int)(most < kKeysInLds ? (most + 255) / 256 * 256 : kKeysInLds); }
 
 // What a workgroup's selection needs of LDS.
 struct SelectLds {
