@@ -197,15 +197,27 @@ __device__ __forceinline__ void list_blocks(const SelectArgs& a, int unit, int h
   int32_t* const out = a.blocks + (int64_t)unit * a.most;
   const Keys<KeyAt> keys(have, key_at);
   const Cutoff cut = cutoff_of(keys, a.most, lds);
-  const int equal = equal_before(keys, cut, lds);
-  int mine = 0;
-  each_of_largest(keys, cut, equal, [&](int, bool taken, bool) { mine += __popcll(__ballot(taken)); });
-  Two all;
-  int at = before_wave(mine, 0, all, lds).a;
-  each_of_largest(keys, cut, equal, [&](int k, bool taken, bool) {
-    const uint64_t some = __ballot(taken);
-    if (taken) out[at + below_me(some)] = k;
-    at += __popcll(some);
+  const int equal0 = equal_before(keys, cut, lds);
+  int equal = equal0, taken = 0;
+  keys.each([&](int, const uint32_t(&key)[kBatch]) {
+    bool in[kBatch];
+    among_largest(key, cut, equal, in);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) taken += __popcll(__ballot(in[i]));
+  });
+  lds.sums[this_wave()][2] = taken;
+  __syncthreads();
+  taken = before_wave(lds, 2).mine;
+  equal = equal0;
+  keys.each([&](int k, const uint32_t(&key)[kBatch]) {
+    bool in[kBatch];
+    among_largest(key, cut, equal, in);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const uint64_t some = __ballot(in[i]);
+      if (in[i]) out[taken + below_me(some)] = k + 64 * i;
+      taken += __popcll(some);
+    }
   });
 }
 
@@ -216,18 +228,18 @@ __global__ __launch_bounds__(kThreads) void block_list_kernel(const SelectArgs a
   const int n = min(max(a.count[b], 0), a.k_cap), have = (n + (1 << a.shift) - 1) >> a.shift;
   const float* const score = a.scores + (int64_t)unit * a.all;
   auto key_at = [&](int k) {
-    const uint32_t key = key_of_float(score[k]);
-    return k < a.first || k >= have - a.recent ? 0xFFFFFFFFu : key;
+    const uint32_t key = key_of_float(score[min(k, have - 1)]);
+    return k >= have ? 0u : k < a.first || k >= have - a.recent ? 0xFFFFFFFFu : key;
   };
   if (have <= a.most) {
     for (int i = threadIdx.x; i < a.most; i += kThreads) a.blocks[(int64_t)unit * a.most + i] = i < have ? i : -1;
   } else if (have <= a.in_lds) {
-    for (int k0 = threadIdx.x; k0 < have; k0 += kLookups * kThreads) {
-      uint32_t key[kLookups];
+    for (int k0 = 0; k0 < have; k0 += kRun) {
+      uint32_t key[kBatch];
 #pragma unroll
-      for (int i = 0; i < kLookups; ++i) key[i] = key_at(min(k0 + i * kThreads, have - 1));
+      for (int i = 0; i < kBatch; ++i) key[i] = key_at(k0 + (int)threadIdx.x + i * kThreads);
 #pragma unroll
-      for (int i = 0; i < kLookups; ++i) kept[min(k0 + i * kThreads, have - 1)] = key[i];
+      for (int i = 0; i < kBatch; ++i) kept[k0 + (int)threadIdx.x + i * kThreads] = key[i];
     }
     list_blocks(a, unit, have, [&](int k) { return kept[k]; }, lds);  // (its first barrier comes before the first look-up)
   } else {

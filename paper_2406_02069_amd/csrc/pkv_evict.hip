@@ -82,9 +82,9 @@ __device__ __forceinline__ void finish(const EvictArgs& a, const Unit& u, int la
   }
 }
 
-// A row's key: rows that are not there 0, weights that are NaN 1, protected rows the greatest.
+// A row's key: rows that are not there 1, weights that are NaN 2, protected rows the greatest (0: no row).
 __device__ __forceinline__ uint32_t row_key(const EvictArgs& a, int32_t p, float w, int newest) {
-  return p < 0 ? 0u : p < a.first || p > newest - a.recent ? 0xFFFFFFFFu : w == w ? key_of_float(w) : 1u;
+  return p < 0 ? 1u : p < a.first || p > newest - a.recent ? 0xFFFFFFFFu : w == w ? key_of_float(w) : 2u;
 }
 __device__ __forceinline__ int newest_of_all(int newest, SelectLds& lds) {
   newest = wave_max(newest);
@@ -100,29 +100,61 @@ template <typename KeyAt>
 __device__ __forceinline__ void pair_rows(const EvictArgs& a, const Unit& u, KeyAt key_at, SelectLds& lds) {
   const Keys<KeyAt> keys(u.n, key_at);
   const Cutoff cut = cutoff_of(keys, a.budget, lds);
-  const int equal = equal_before(keys, cut, lds);
-  Two mine = {0, 0}, all;
-  each_of_largest(keys, cut, equal, [&](int r, bool stays, bool there) {
-    mine.a += __popcll(__ballot(there && !stays && r < a.budget));
-    mine.b += __popcll(__ballot(stays && r >= a.budget));
-  });
-  Two at = before_wave(mine.a, mine.b, all, lds);
-  int32_t *const to = a.pairs + (int64_t)u.unit * 2 * a.most, *const from = to + a.most;
-  const bool copy = u.pos_out != u.pos || u.weight_out != u.weight;
-  each_of_largest(keys, cut, equal, [&](int r, bool stays, bool there) {
-    const bool hole = there && !stays && r < a.budget, late = stays && r >= a.budget;
-    const uint64_t holes = __ballot(hole), lates = __ballot(late);
-    if (hole) to[at.a + below_me(holes)] = r;
-    if (late) from[at.b + below_me(lates)] = r;
-    at = {at.a + (int)__popcll(holes), at.b + (int)__popcll(lates)};
-    if (copy && stays && r < a.budget) {
-      const int32_t p = u.pos[r];
-      const float w = u.weight[r];
-      u.pos_out[r] = p;
-      u.weight_out[r] = w;
+  const int equal0 = equal_before(keys, cut, lds);
+  int equal = equal0, holes = 0, late = 0;
+  keys.each([&](int r, const uint32_t(&key)[kBatch]) {
+    bool in[kBatch];
+    among_largest(key, cut, equal, in);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const bool before = r + 64 * i < a.budget;
+      holes += __popcll(__ballot(before && !in[i]));
+      late += __popcll(__ballot(!before && in[i]));
     }
   });
-  finish(a, u, all.b);  // (as many holes as late rows)
+  lds.sums[this_wave()][1] = holes;
+  lds.sums[this_wave()][2] = late;
+  __syncthreads();
+  const Before h = before_wave(lds, 1), l = before_wave(lds, 2);
+  holes = h.mine;
+  late = l.mine;
+  equal = equal0;
+  int32_t *const to = a.pairs + (int64_t)u.unit * 2 * a.most, *const from = to + a.most;
+  const bool copy = u.pos_out != u.pos || u.weight_out != u.weight;
+  keys.each([&](int r, const uint32_t(&key)[kBatch]) {
+    bool in[kBatch];
+    among_largest(key, cut, equal, in);
+    if (__all(r >= a.budget)) {  // behind the budget, where few stay
+      bool some = false;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) some = some || in[i];
+      if (!__any(some)) return;
+    } else if (copy) {
+      int32_t p[kBatch];
+      float w[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        p[i] = u.pos[min(r + 64 * i, u.n - 1)];
+        w[i] = u.weight[min(r + 64 * i, u.n - 1)];
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (in[i] && r + 64 * i < a.budget) {
+          u.pos_out[r + 64 * i] = p[i];
+          u.weight_out[r + 64 * i] = w[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const bool before = r + 64 * i < a.budget;
+      const uint64_t hs = __ballot(before && !in[i]), ls = __ballot(!before && in[i]);
+      if (before && !in[i]) to[holes + below_me(hs)] = r + 64 * i;
+      if (!before && in[i]) from[late + below_me(ls)] = r + 64 * i;
+      holes += __popcll(hs);
+      late += __popcll(ls);
+    }
+  });
+  finish(a, u, l.all);  // (as many holes as late rows)
 }
 
 // Keys in LDS, from rows' positions and weights that are all requested together.
@@ -132,39 +164,46 @@ __device__ __forceinline__ void evict_rows(const EvictArgs& a, const Unit& u, ui
   float w[MOST];
   int newest = -1;
 #pragma unroll
-  for (int i0 = 0; i0 < MOST; i0 += kLookups) {
+  for (int i0 = 0; i0 < MOST; i0 += kBatch) {
     if (i0 * kThreads < u.n) {
 #pragma unroll
-      for (int i = i0; i < i0 + kLookups; ++i) p[i] = u.pos[min((int)threadIdx.x + i * kThreads, u.n - 1)];
+      for (int i = i0; i < i0 + kBatch; ++i) p[i] = u.pos[min((int)threadIdx.x + i * kThreads, u.n - 1)];
 #pragma unroll
-      for (int i = i0; i < i0 + kLookups; ++i) w[i] = u.weight[min((int)threadIdx.x + i * kThreads, u.n - 1)];
+      for (int i = i0; i < i0 + kBatch; ++i) w[i] = u.weight[min((int)threadIdx.x + i * kThreads, u.n - 1)];
     }
   }
 #pragma unroll
-  for (int i0 = 0; i0 < MOST; i0 += kLookups) {
+  for (int i0 = 0; i0 < MOST; i0 += kBatch) {
     if (i0 * kThreads < u.n) {
 #pragma unroll
-      for (int i = i0; i < i0 + kLookups; ++i) newest = max(newest, p[i]);
+      for (int i = i0; i < i0 + kBatch; ++i) newest = max(newest, p[i]);
     }
   }
   newest = newest_of_all(newest, lds);
 #pragma unroll
-  for (int i0 = 0; i0 < MOST; i0 += kLookups) {
+  for (int i0 = 0; i0 < MOST; i0 += kBatch) {
     if (i0 * kThreads < u.n) {
 #pragma unroll
-      for (int i = i0; i < i0 + kLookups; ++i) kept[min((int)threadIdx.x + i * kThreads, u.n - 1)] = row_key(a, p[i], w[i], newest);
+      for (int i = i0; i < i0 + kBatch; ++i) {
+        const int r = (int)threadIdx.x + i * kThreads;
+        kept[r] = r < u.n ? row_key(a, p[i], w[i], newest) : 0u;
+      }
     }
   }
   pair_rows(a, u, [&](int r) { return kept[r]; }, lds);  // (its first barrier comes before the first look-up)
 }
 __device__ __forceinline__ void evict_rows_of_memory(const EvictArgs& a, const Unit& u, SelectLds& lds) {
   int newest = -1;
-  for (int r0 = threadIdx.x; r0 < u.n; r0 += kLookups * kThreads) {
+  for (int r0 = threadIdx.x; r0 < u.n; r0 += kBatch * kThreads) {
 #pragma unroll
-    for (int i = 0; i < kLookups; ++i) newest = max(newest, u.pos[min(r0 + i * kThreads, u.n - 1)]);
+    for (int i = 0; i < kBatch; ++i) newest = max(newest, u.pos[min(r0 + i * kThreads, u.n - 1)]);
   }
   newest = newest_of_all(newest, lds);
-  pair_rows(a, u, [&](int r) { return row_key(a, u.pos[r], u.weight[r], newest); }, lds);
+  const auto key_at = [&](int r) {
+    const uint32_t key = row_key(a, u.pos[min(r, u.n - 1)], u.weight[min(r, u.n - 1)], newest);
+    return r < u.n ? key : 0u;
+  };
+  pair_rows(a, u, key_at, lds);
 }
 
 // One row too many, as in a step of decoding: the row with the least key goes, the last of those that have it.  The last row, which

@@ -17,26 +17,24 @@ __device__ __forceinline__ uint32_t key_of_float(float x) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// A workgroup's n keys: wave w looks after a run of them, 64 neighbours at a time, so that ranks need the waves' counts alone.  Numbers
-// behind the last one are looked up as the last, so that no look-up waits for a comparison.
-constexpr int kLookups = 8;  // on their way together
+// A workgroup's keys: wave w looks after a run of them, kBatch times 64 neighbours at a time, so that ranks need the waves' counts alone.
+// The runs are filled up with keys of 0, which all others are above: no pass has an end to look out for.
+constexpr int kBatch = 8;
+constexpr int kRun = kBatch * kThreads;
 template <typename KeyAt>
 struct Keys {
   const KeyAt key_at;
-  const int n, steps, first;  // `first`: the lane's first key
-  __device__ __forceinline__ Keys(int n_, KeyAt key_at_)
-      : key_at(key_at_), n(n_), steps((n_ + kThreads - 1) / kThreads),
-        first((int)(threadIdx.x >> 6) * steps * 64 + (int)(threadIdx.x & 63)) {}
-  // f(number, key, whether there is such a key) in ascending order, in all lanes of a wave alike
+  const int steps, first;  // batches of a wave; the lane's first key
+  __device__ __forceinline__ Keys(int n, KeyAt key_at_)
+      : key_at(key_at_), steps((n + kRun - 1) / kRun), first((int)(threadIdx.x >> 6) * steps * (64 * kBatch) + (int)(threadIdx.x & 63)) {}
+  // f(number of the first, keys): keys `number`, number + 64, ..
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    for (int i0 = 0; i0 < steps; i0 += kLookups) {
-      uint32_t key[kLookups];
+    for (int i = 0; i < steps; ++i) {
+      uint32_t key[kBatch];
 #pragma unroll
-      for (int i = 0; i < kLookups; ++i) key[i] = key_at(min(first + 64 * (i0 + i), n - 1));
-#pragma unroll
-      for (int i = 0; i < kLookups; ++i)
-        if (i0 + i < steps) f(first + 64 * (i0 + i), key[i], first + 64 * (i0 + i) < n);
+      for (int k = 0; k < kBatch; ++k) key[k] = key_at(first + 64 * (kBatch * i + k));
+      f(first + 64 * kBatch * i, key);
     }
   }
 };
@@ -53,7 +51,7 @@ inline hipError_t grant_keys(const void* kernel, bool* granted) {
   if (e == hipSuccess) granted[dev] = true;
   return e;
 }
-inline int keys_in_lds(int64_t most) { return (int)(most < kKeysInLds ? (most + 255) / 256 * 256 : kKeysInLds); }
+inline int keys_in_lds(int64_t most) { return (int)(most < kKeysInLds ? (most + kRun - 1) / kRun * kRun : kKeysInLds); }
 
 // What a workgroup's selection needs of LDS.
 struct SelectLds {
@@ -63,10 +61,27 @@ struct SelectLds {
   uint64_t keys[kWavesOf];
 };
 
-// The k-th largest key (1 <= k <= n), and how many of those that equal it are among the k largest, from the first on (`every`: all).
-// Eleven bits at a time, by a count of the keys that agree with what is known so far: with fewer bits the first count would meet a
-// few exponents' bins only, and additions to one word of LDS wait for one another.  Where all of 64 neighbours meet the same bin,
-// they are added at once.
+__device__ __forceinline__ int this_wave() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// The sum of the earlier waves' numbers in a column of lds.sums, and of all.
+struct Before {
+  int mine, all;
+};
+__device__ __forceinline__ Before before_wave(const SelectLds& lds, int column) {
+  static_assert(kWavesOf == 16, "a row of lanes");
+  int x = lds.sums[threadIdx.x & 15][column];
+  x = add_from<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8
+  x = add_from<0x112, 0xF>(x);
+  x = add_from<0x114, 0xF>(x);
+  x = add_from<0x118, 0xF>(x);
+  const int wave = this_wave();
+  return {wave > 0 ? __builtin_amdgcn_readlane(x, wave - 1) : 0, __builtin_amdgcn_readlane(x, 15)};
+}
+
+// The k-th largest key (there are k above 0), and how many of those that equal it are among the k largest, from the first on (`every`:
+// all).  Eleven bits at a time, by a count of the keys that agree with what is known so far: with fewer bits the first count would meet
+// a few exponents' bins only, and additions to one word of LDS wait for one another.  Where 64 neighbours all meet the same bin, they
+// are added at once.
 struct Cutoff {
   uint32_t key;
   int equal;
@@ -74,7 +89,7 @@ struct Cutoff {
 };
 template <typename K>
 __device__ __forceinline__ Cutoff cutoff_of(const K& keys, int k, SelectLds& lds) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   uint32_t known = 0, mask = 0;
   int left = k, met = 0;
 #pragma unroll 1
@@ -82,26 +97,29 @@ __device__ __forceinline__ Cutoff cutoff_of(const K& keys, int k, SelectLds& lds
     const uint32_t wide = shift == 0 ? 1023 : 2047;
     lds.bins[threadIdx.x] = lds.bins[threadIdx.x + kThreads] = 0;
     __syncthreads();
-    keys.each([&](int, uint32_t key, bool there) {
-      const bool mine = there && (key & mask) == known;
-      const uint64_t some = __ballot(mine);
-      if (some == 0) return;
-      const uint32_t bin = key >> shift & wide;
-      const int lead = __builtin_ctzll(some);
-      if (__ballot(mine && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, lead)) == some) {
-        if (lane == lead) atomicAdd(&lds.bins[bin], (uint32_t)__popcll(some));
-      } else if (mine) {
-        atomicAdd(&lds.bins[bin], 1u);
+    keys.each([&](int, const uint32_t(&key)[kBatch]) {
+      bool some = false;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) some = some || (key[i] & mask) == known;
+      if (!__any(some)) return;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const bool mine = (key[i] & mask) == known;
+        const uint32_t bin = key[i] >> shift & wide;
+        if (__all(mine && bin == (uint32_t)__builtin_amdgcn_readfirstlane((int)bin))) {
+          if (lane == 0) atomicAdd(&lds.bins[bin], 64u);
+        } else if (mine) {
+          atomicAdd(&lds.bins[bin], 1u);
+        }
       }
     });
     __syncthreads();
     // a thread: two bins, the largest first
     const int top = 2047 - 2 * (int)threadIdx.x;
     const int c0 = (int)lds.bins[top], c1 = (int)lds.bins[top - 1], upto = sum_upto(c0 + c1);
-    if (lane == 63) lds.sums[wave][0] = upto;
+    if (lane == 63) lds.sums[this_wave()][0] = upto;
     __syncthreads();
-    int before = upto - c0 - c1;
-    for (int w = 0; w < wave; ++w) before += lds.sums[w][0];
+    const int before = before_wave(lds, 0).mine + upto - c0 - c1;
     if (before < left && left <= before + c0 + c1) {
       const bool second = left > before + c0;
       lds.found[0] = top - second;
@@ -121,50 +139,31 @@ __device__ __forceinline__ int below_me(uint64_t flags) {
   return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(flags >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)flags, 0));
 }
 
-// The sums of the earlier waves' numbers a, b, and of all; column `at` and the next of lds.sums.
-struct Two {
-  int a, b;
-};
-__device__ __forceinline__ Two before_wave(int a, int b, Two& all, SelectLds& lds) {
-  const int wave = threadIdx.x >> 6;
-  __syncthreads();  // (what was there has been read)
-  if ((threadIdx.x & 63) == 0) {
-    lds.sums[wave][1] = a;
-    lds.sums[wave][2] = b;
-  }
-  __syncthreads();
-  Two mine = {0, 0};
-  all = {0, 0};
+// Which of a batch's keys are among the k largest; `equal`: of the keys that equal the cutoff, those before (moves on).
+__device__ __forceinline__ void among_largest(const uint32_t (&key)[kBatch], const Cutoff& cut, int& equal, bool (&in)[kBatch]) {
 #pragma unroll
-  for (int w = 0; w < kWavesOf; ++w) {
-    if (w == wave) mine = all;
-    all = {all.a + lds.sums[w][1], all.b + lds.sums[w][2]};
-  }
-  return mine;
-}
-
-// f(number, whether it is one of the k largest, whether there is such a key) in ascending order.
-template <typename K, typename F>
-__device__ __forceinline__ void each_of_largest(const K& keys, const Cutoff& cut, int equal_before, F f) {
-  int equal = equal_before;  // of the keys before
-  keys.each([&](int r, uint32_t key, bool there) {
-    bool in = there && key >= cut.key;
-    if (!cut.every) {
-      const uint64_t same = __ballot(there && key == cut.key);
-      in = in && (key != cut.key || equal + below_me(same) < cut.equal);
+  for (int i = 0; i < kBatch; ++i) in[i] = key[i] >= cut.key;
+  if (!cut.every) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const uint64_t same = __ballot(key[i] == cut.key);
+      in[i] = in[i] && (key[i] != cut.key || equal + below_me(same) < cut.equal);
       equal += __popcll(same);
     }
-    f(r, in, there);
-  });
+  }
 }
 // What the waves before have of keys that equal the cutoff (0 where all of those are taken).
 template <typename K>
 __device__ __forceinline__ int equal_before(const K& keys, const Cutoff& cut, SelectLds& lds) {
   if (cut.every) return 0;
   int equal = 0;
-  keys.each([&](int, uint32_t key, bool there) { equal += __popcll(__ballot(there && key == cut.key)); });
-  Two all;
-  return before_wave(equal, 0, all, lds).a;
+  keys.each([&](int, const uint32_t(&key)[kBatch]) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) equal += __popcll(__ballot(key[i] == cut.key));
+  });
+  lds.sums[this_wave()][0] = equal;
+  __syncthreads();
+  return before_wave(lds, 0).mine;
 }
 
 }  // namespace
