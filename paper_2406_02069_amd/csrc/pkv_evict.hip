@@ -57,8 +57,15 @@ struct Unit {
   float* weight_out;
 };
 
-// Pairs are known: the rows' positions and weights follow, then the rows behind the budget are emptied, and few rows of K and V are
-// moved here.
+// What becomes of a row that is not moved into: before the budget it stays (holes are filled later), behind it it is emptied.  Where the
+// outputs are the inputs, the former is there already, and the latter waits until the moved rows have been read.
+__device__ __forceinline__ void keep_row(const EvictArgs& a, const Unit& u, int r, int32_t p, float w) {
+  const bool stays = r < a.budget;
+  if (u.pos_out != u.pos) u.pos_out[r] = stays ? p : -1;
+  if (u.weight_out != u.weight) u.weight_out[r] = stays ? w : 0.0f;
+}
+
+// Pairs are known: the rows' positions and weights follow, and few rows of K and V are moved here.
 __device__ __forceinline__ void finish(const EvictArgs& a, const Unit& u, int late) {
   const int32_t *const to = a.pairs + (int64_t)u.unit * 2 * a.most, *const from = to + a.most;
   __threadfence_block();
@@ -75,10 +82,11 @@ __device__ __forceinline__ void finish(const EvictArgs& a, const Unit& u, int la
     const int lanes = a.d / 8;
     for (int i = threadIdx.x; i < late * lanes; i += kThreads) move_piece(a, u.b, u.g, to[i / lanes], from[i / lanes], i % lanes);
   }
+  if (u.pos_out != u.pos && u.weight_out != u.weight) return;
   __syncthreads();
   for (int r = a.budget + threadIdx.x; r < u.n; r += kThreads) {
-    u.pos_out[r] = -1;
-    u.weight_out[r] = 0.0f;
+    if (u.pos_out == u.pos) u.pos_out[r] = -1;
+    if (u.weight_out == u.weight) u.weight_out[r] = 0.0f;
   }
 }
 
@@ -102,14 +110,17 @@ __device__ __forceinline__ void pair_rows(const EvictArgs& a, const Unit& u, Key
   const Cutoff cut = cutoff_of(keys, a.budget, lds);
   const int equal0 = equal_before(keys, cut, lds);
   int equal = equal0, holes = 0, late = 0;
+  const int lane = threadIdx.x & 63;
   keys.each([&](int r, const uint32_t(&key)[kBatch]) {
     bool in[kBatch];
     among_largest(key, cut, equal, in);
+    const int r0 = __builtin_amdgcn_readfirstlane(r - lane);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const bool before = r + 64 * i < a.budget;
-      holes += __popcll(__ballot(before && !in[i]));
-      late += __popcll(__ballot(!before && in[i]));
+      const int before = min(max(a.budget - r0 - 64 * i, 0), 64);  // of the 64 rows, in front of the budget
+      const uint64_t stay = __ballot(in[i]), front = before == 64 ? ~(uint64_t)0 : ((uint64_t)1 << before) - 1;
+      holes += before - __popcll(stay & front);
+      late += __popcll(stay & ~front);
     }
   });
   lds.sums[this_wave()][1] = holes;
@@ -120,38 +131,23 @@ __device__ __forceinline__ void pair_rows(const EvictArgs& a, const Unit& u, Key
   late = l.mine;
   equal = equal0;
   int32_t *const to = a.pairs + (int64_t)u.unit * 2 * a.most, *const from = to + a.most;
-  const bool copy = u.pos_out != u.pos || u.weight_out != u.weight;
   keys.each([&](int r, const uint32_t(&key)[kBatch]) {
     bool in[kBatch];
     among_largest(key, cut, equal, in);
-    if (__all(r >= a.budget)) {  // behind the budget, where few stay
-      bool some = false;
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) some = some || in[i];
-      if (!__any(some)) return;
-    } else if (copy) {
-      int32_t p[kBatch];
-      float w[kBatch];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        p[i] = u.pos[min(r + 64 * i, u.n - 1)];
-        w[i] = u.weight[min(r + 64 * i, u.n - 1)];
-      }
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-        if (in[i] && r + 64 * i < a.budget) {
-          u.pos_out[r + 64 * i] = p[i];
-          u.weight_out[r + 64 * i] = w[i];
-        }
-    }
+    const int r0 = __builtin_amdgcn_readfirstlane(r - lane);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const bool before = r + 64 * i < a.budget;
-      const uint64_t hs = __ballot(before && !in[i]), ls = __ballot(!before && in[i]);
-      if (before && !in[i]) to[holes + below_me(hs)] = r + 64 * i;
-      if (!before && in[i]) from[late + below_me(ls)] = r + 64 * i;
-      holes += __popcll(hs);
-      late += __popcll(ls);
+      const int before = min(max(a.budget - r0 - 64 * i, 0), 64);
+      const uint64_t stay = __ballot(in[i]), front = before == 64 ? ~(uint64_t)0 : ((uint64_t)1 << before) - 1;
+      const uint64_t hs = ~stay & front, ls = stay & ~front;
+      if (hs != 0) {
+        if (hs >> lane & 1) to[holes + below_me(hs)] = r + 64 * i;
+        holes += __popcll(hs);
+      }
+      if (ls != 0) {
+        if (ls >> lane & 1) from[late + below_me(ls)] = r + 64 * i;
+        late += __popcll(ls);
+      }
     }
   });
   finish(a, u, l.all);  // (as many holes as late rows)
@@ -187,6 +183,7 @@ __device__ __forceinline__ void evict_rows(const EvictArgs& a, const Unit& u, ui
       for (int i = i0; i < i0 + kBatch; ++i) {
         const int r = (int)threadIdx.x + i * kThreads;
         kept[r] = r < u.n ? row_key(a, p[i], w[i], newest) : 0u;
+        if (r < u.n) keep_row(a, u, r, p[i], w[i]);
       }
     }
   }
@@ -203,6 +200,8 @@ __device__ __forceinline__ void evict_rows_of_memory(const EvictArgs& a, const U
     const uint32_t key = row_key(a, u.pos[min(r, u.n - 1)], u.weight[min(r, u.n - 1)], newest);
     return r < u.n ? key : 0u;
   };
+  if (u.pos_out != u.pos || u.weight_out != u.weight)
+    for (int r = threadIdx.x; r < u.n; r += kThreads) keep_row(a, u, r, u.pos[r], u.weight[r]);
   pair_rows(a, u, key_at, lds);
 }
 

@@ -98,16 +98,27 @@ __device__ __forceinline__ Cutoff cutoff_of(const K& keys, int k, SelectLds& lds
     lds.bins[threadIdx.x] = lds.bins[threadIdx.x + kThreads] = 0;
     __syncthreads();
     keys.each([&](int, const uint32_t(&key)[kBatch]) {
-      bool some = false;
+      if (mask == 0) {
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) some = some || (key[i] & mask) == known;
-      if (!__any(some)) return;
+        for (int i = 0; i < kBatch; ++i) {
+          const uint32_t bin = key[i] >> 21;
+          if (__all(bin == (uint32_t)__builtin_amdgcn_readfirstlane((int)bin))) {
+            if (lane == 0) atomicAdd(&lds.bins[bin], 64u);
+          } else {
+            atomicAdd(&lds.bins[bin], 1u);
+          }
+        }
+        return;
+      }
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
         const bool mine = (key[i] & mask) == known;
+        const uint64_t some = __ballot(mine);
+        if (some == 0) continue;
         const uint32_t bin = key[i] >> shift & wide;
-        if (__all(mine && bin == (uint32_t)__builtin_amdgcn_readfirstlane((int)bin))) {
-          if (lane == 0) atomicAdd(&lds.bins[bin], 64u);
+        const int lead = __builtin_ctzll(some);
+        if (__popcll(some) >= 16 && __ballot(mine && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, lead)) == some) {
+          if (lane == lead) atomicAdd(&lds.bins[bin], (uint32_t)__popcll(some));
         } else if (mine) {
           atomicAdd(&lds.bins[bin], 1u);
         }
@@ -131,6 +142,7 @@ __device__ __forceinline__ Cutoff cutoff_of(const K& keys, int k, SelectLds& lds
     left = lds.found[1];
     met = lds.found[2];
     mask |= wide << shift;
+    if (left == met) break;  // (all that agree are taken)
   }
   return {known, left, left == met};
 }
