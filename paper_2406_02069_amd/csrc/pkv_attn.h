@@ -87,6 +87,9 @@ __device__ __forceinline__ int wave_max(int x) {
   return __builtin_amdgcn_readfirstlane(x);
 }
 
+// The wave's number in its workgroup, in a scalar register.
+__device__ __forceinline__ int this_wave() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
 // Sum over the wave, up to and including the own lane.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int add_from(int x) {
@@ -181,6 +184,28 @@ __device__ __forceinline__ void cap_scores(float (&x)[N], const Cap& c) {
     for (int i = 0; i < N; ++i) x[i] = capped_small(x[i], c);
   }
 }
+
+// ---- kernels that form 32 x 32 tiles of scores, keys and values straight from memory in LDS ----
+
+// References (log2) beyond which a score is rounded before it is compared with them: what one fma of scale and difference finds
+// left of a rounded product is as large as a step there, and would be a weight's exponent.
+constexpr float kLarge = 0x1p20f;
+
+// Waits for the asynchronous loads into LDS, but for the last LATER (below 16) of them: loads end in the order of their requests.
+template <int LATER = 0>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(LATER < 16, "the counter's low bits");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | LATER);  // vmcnt
+  asm volatile("" : : : "memory");
+}
+
+// The first key of register i of a 32 x 32 product, in the lower half of the wave (the upper half: 4 more).
+__device__ __forceinline__ constexpr int key_of(int i) { return 8 * (i >> 2) + (i & 3); }
+
+template <int D>
+__device__ __forceinline__ int swizzle_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int swizzle_v(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
 
 }  // namespace
 }  // namespace pkv

@@ -16,10 +16,13 @@ constexpr int kWaves = 4;          // per workgroup
 constexpr int kWorkgroups = 512;   // at a time on the device: two per compute unit
 constexpr int kLaneSequences = 4;  // sequences a lane looks after where ranges go by lengths,
 constexpr int kFlatBatch = 64 * kLaneSequences;  // and so many at most in all
-constexpr int kLeastTiles = 8;     // of a range
+constexpr int kLeastTiles = 8;     // of a range,
+constexpr int kLeastWide = 24;     // of many query rows,
+constexpr int kWideTurn = 768;     // whose workgroups are so many at a time
 
 // What the kernel is built for: one token over all rows; the same, handing its scores on; drafted tokens; listed blocks of rows.
-enum { kOneToken = 0, kWeigh = 1, kTree = 2, kBlocks = 3 };
+// (kTreeWide: drafted tokens whose query rows are many, in pkv_tree.hip's own kernel.)
+enum { kOneToken = 0, kWeigh = 1, kTree = 2, kBlocks = 3, kTreeWide = 4 };
 
 struct LongArgs {
   const uint16_t *q, *K, *V;
@@ -56,6 +59,14 @@ struct TreeArgs : LongArgs {
   int64_t q_st, o_sb, o_sh, o_st;
   static constexpr int MODE = kTree;
 };
+struct TreeWideArgs : TreeArgs {
+  static constexpr int MODE = kTreeWide;
+};
+template <typename A>
+constexpr bool drafted_mode() { return A::MODE == kTree || A::MODE == kTreeWide; }
+// Query rows of a workgroup, and the factor that its sums carry (2^-).
+template <typename A>
+constexpr int group_rows() { return A::MODE == kTreeWide ? 128 : 64; }
 // Listed blocks: place x of the list's rows is row list[x >> shift] << shift | (x & (block - 1)).
 struct BlocksArgs : LongArgs {
   const int32_t* blocks;  // [B][Hkv][most]
@@ -70,6 +81,8 @@ struct Weight {
   static constexpr float SHIFT = HALF ? kFp16Shift : 0.0f, SLACK = HALF ? kFp16Slack : 8.0f;
   static constexpr float UNIT = HALF ? 1.0f / (1 << (int)kFp16Shift) : 1.0f;  // 2^-SHIFT
 };
+
+constexpr int kWideShift = 8;  // kTreeWide, fp16: as pkv_prefill.hip has it
 
 // A wave's reads and writes of its own part of LDS keep their order.
 __device__ __forceinline__ void own_lds_order() {
@@ -94,7 +107,7 @@ __device__ __forceinline__ Tiles tiles_of(const A& a, int b) {
     r.count = ((min(a.most, (r.n + (1 << a.shift) - 1) >> a.shift) << a.shift) + kTile - 1) / kTile;
     return r;
   }
-  if constexpr (A::MODE == kTree) {
+  if constexpr (drafted_mode<A>()) {
     r.q_pos = max(a.count[b], 0) - (a.new_lens ? min(max(a.new_lens[b], 0), a.T) : a.T);
     if (!a.positions && a.window) first = (int)min((int64_t)r.n, max((int64_t)0, (int64_t)r.q_pos - a.window + 1));
     r.first = first / kTile;
@@ -130,8 +143,8 @@ __device__ __forceinline__ Cut<E> flat_cut(const A& a, int lane) {
     sum += lane * E + e < a.B ? c.tl[e].count : 0;
   }
   const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(sum_upto(sum), 63) * (uint32_t)a.units;
-  const int shares = kWaves / a.wave_groups, shift = a.ranges == kWorkgroups ? 9 : 10;
-  c.per = max((int)((all + a.ranges - 1) >> shift), kLeastTiles);
+  const int shares = A::MODE == kTreeWide ? 1 : kWaves / a.wave_groups, shift = a.ranges == kWorkgroups ? 9 : 10;
+  c.per = A::MODE == kTreeWide ? max((int)((all + a.ranges - 1) / (uint32_t)a.ranges), kLeastWide) : max((int)((all + a.ranges - 1) >> shift), kLeastTiles);
   c.per = (c.per + shares - 1) / shares * shares;
   for (int tries = 0;; ++tries) {
     sum = 0;
@@ -141,7 +154,10 @@ __device__ __forceinline__ Cut<E> flat_cut(const A& a, int lane) {
       sum += c.ranges[e] * a.units;
     }
     c.end = sum_upto(sum);
-    if (shift != 9 || tries == 6 || __builtin_amdgcn_readlane(c.end, 63) <= kWorkgroups) break;
+    if constexpr (A::MODE == kTreeWide) {
+      if (a.ranges != kWideTurn || tries == 6 || __builtin_amdgcn_readlane(c.end, 63) <= kWideTurn) break;
+    }
+    if (A::MODE != kTreeWide && (shift != 9 || tries == 6 || __builtin_amdgcn_readlane(c.end, 63) <= kWorkgroups)) break;
     c.per += max(shares, c.per / 16 / shares * shares);
   }
   c.base = c.end - sum;
@@ -226,14 +242,14 @@ __device__ __forceinline__ uint32_t drafted_seen(const TreeArgs& a, int b, int t
 // A row's place in out: row h_in of those that share KV head g.
 template <typename A>
 __device__ __forceinline__ int64_t out_at(const A& a, int b, int g, int h_in, int D) {
-  if constexpr (A::MODE == kTree)
+  if constexpr (drafted_mode<A>())
     return b * a.o_sb + (g * a.heads + h_in % a.heads) * a.o_sh + (h_in / a.heads) * a.o_st;
   else
     return ((int64_t)b * a.Hq + g * a.G + h_in) * D;
 }
 template <typename A>
 __device__ __forceinline__ int64_t lse_at(const A& a, int b, int g, int h_in) {
-  if constexpr (A::MODE == kTree)
+  if constexpr (drafted_mode<A>())
     return ((int64_t)b * (a.Hkv * a.heads) + g * a.heads + h_in % a.heads) * a.T + h_in / a.heads;
   else
     return (int64_t)b * a.Hq + g * a.G + h_in;
@@ -675,7 +691,9 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const A a) {
     base = p.base;
   }
   if (ranges == 1) return;  // (written already)
-  const int64_t heads = 16 * a.wave_groups;
+  constexpr bool WIDE = A::MODE == kTreeWide;
+  constexpr float UNIT = WIDE && Weight<T>::HALF ? 1.0f / (1 << kWideShift) : Weight<T>::UNIT;
+  const int64_t heads = WIDE ? 128 : 16 * a.wave_groups, step = WIDE ? heads * a.units : heads;  // between a row's ranges
   const int d4 = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
   float m, z;
   f32x4 acc;
@@ -697,20 +715,21 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const A a) {
 #pragma unroll 1
   for (int k = 0; k < HEADS; ++k) {
     const int64_t row = (int64_t)blockIdx.x * HEADS + k;
-    const int h = (int)(row % a.Hq), h_in = h % a.G, unit = h / a.G * a.head_groups + h_in / 64;
-    const int64_t at = ((int64_t)base + unit * ranges) * heads + h_in % 64;
+    const int h = (int)(row % a.Hq), h_in = h % a.G, group = h_in / group_rows<A>();
+    const int unit = WIDE ? group * a.Hkv + h / a.G : h / a.G * a.head_groups + group;
+    const int64_t at = ((int64_t)base + (WIDE ? unit : unit * ranges)) * heads + h_in % group_rows<A>();
     nothing();
 #pragma unroll 4
     for (int i = part; i < ranges; i += PARTS) {
-      const float* const mz = a.part_mz + (at + heads * i) * 2;
-      join(mz[0], mz[1], *reinterpret_cast<const f32x4*>(a.part_o + (at + heads * i) * D + 4 * d4));
+      const float* const mz = a.part_mz + (at + step * i) * 2;
+      join(mz[0], mz[1], *reinterpret_cast<const f32x4*>(a.part_o + (at + step * i) * D + 4 * d4));
     }
     if (__builtin_expect(!finite(acc), 0)) {  // (0 times an infinity is not what it should be)
       nothing();
 #pragma unroll 1
       for (int i = part; i < ranges; i += PARTS) {
-        const float* const mz = a.part_mz + (at + heads * i) * 2;
-        join(mz[0], mz[1], *reinterpret_cast<const f32x4*>(a.part_o + (at + heads * i) * D + 4 * d4), true);
+        const float* const mz = a.part_mz + (at + step * i) * 2;
+        join(mz[0], mz[1], *reinterpret_cast<const f32x4*>(a.part_o + (at + step * i) * D + 4 * d4), true);
       }
     }
     if (k > 0) __syncthreads();  // (the last head's parts have been read)
@@ -733,7 +752,7 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const A a) {
       w[0] = pack2<T>(acc[0] * inv, acc[1] * inv);
       w[1] = pack2<T>(acc[2] * inv, acc[3] * inv);
       *reinterpret_cast<u32x2*>(a.out + out_at(a, b, h / a.G, h_in, D) + 4 * d4) = w;
-      if (d4 == 0 && a.lse) a.lse[lse_at(a, b, h / a.G, h_in)] = z == 0.0f ? kNone : (m + log2_(z * Weight<T>::UNIT)) * kLn2;
+      if (d4 == 0 && a.lse) a.lse[lse_at(a, b, h / a.G, h_in)] = z == 0.0f ? kNone : (m + log2_(z * UNIT)) * kLn2;
       if constexpr (A::MODE == kWeigh) {
         if (d4 == 0) keep_mz(a, b, h / a.G, h_in, m == kNone ? 0.0f : m, inv * (1.0f / Weight<T>::UNIT));
       }
@@ -774,16 +793,20 @@ inline size_t parts_bytes(const Grid& g, int rows, int d) {
 }
 
 template <typename T, int D, typename A>
-hipError_t launch_long(const A& a, int64_t workgroups, hipStream_t s) {
-  hipLaunchKernelGGL((decode_long_kernel<T, D, A>), dim3((unsigned)workgroups), dim3(256), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.ranges == 0) return e;
+hipError_t launch_join(const A& a, hipStream_t s) {
   // Many heads: four a workgroup (128 sequences of 32 heads, 100 rows each: 25 us, one by one 30; 64 of 16 are faster one by one).
   if (a.Hq % 4 == 0 && a.B * a.Hq >= 4 * kWorkgroups)
     hipLaunchKernelGGL((decode_long_join_kernel<T, D, 4, A>), dim3((unsigned)(a.B * a.Hq / 4)), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((decode_long_join_kernel<T, D, 1, A>), dim3((unsigned)(a.B * a.Hq)), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+template <typename T, int D, typename A>
+hipError_t launch_long(const A& a, int64_t workgroups, hipStream_t s) {
+  hipLaunchKernelGGL((decode_long_kernel<T, D, A>), dim3((unsigned)workgroups), dim3(256), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.ranges == 0 ? e : launch_join<T, D>(a, s);
 }
 template <typename A>
 hipError_t launch_long(const A& a, int dtype, int d, int64_t workgroups, hipStream_t s) {

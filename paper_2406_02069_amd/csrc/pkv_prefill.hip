@@ -43,9 +43,6 @@ constexpr int kRows = 128;   // query rows of a workgroup
 constexpr int kKeys = 32;    // keys per step
 constexpr int kMaxParts = 64;  // ranges of keys
 constexpr int kLeastKeys = 768;  // of a range, about
-// References (log2) beyond which a score is rounded before it is compared with them: what one fma of scale and difference finds
-// left of a rounded product is as large as a step there, and would be a weight's exponent.
-constexpr float kLarge = 0x1p20f;
 
 struct PrefillArgs {
   const uint16_t *q, *K, *V;
@@ -147,19 +144,6 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t at, uint3
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
 }
 #pragma clang diagnostic pop
-__device__ __forceinline__ void wait_loads() {
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-  asm volatile("" : : : "memory");
-}
-
-// The first key of register i of a 32 x 32 product, in the lower half of the wave (the upper half: 4 more).
-__device__ __forceinline__ constexpr int key_of(int i) { return 8 * (i >> 2) + (i & 3); }
-
-template <int D>
-__device__ __forceinline__ int swizzle_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
-template <int D>
-__device__ __forceinline__ int swizzle_v(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
-
 // MODE 1: scores are capped or biased.
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {

@@ -61,8 +61,6 @@ struct SelectLds {
   uint64_t keys[kWavesOf];
 };
 
-__device__ __forceinline__ int this_wave() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
-
 // The sum of the earlier waves' numbers in a column of lds.sums, and of all.
 struct Before {
   int mine, all;

@@ -2,10 +2,466 @@
 //
 // The T Hq/Hkv query rows of a KV head share its rows of the cache; up to 64 of them are a workgroup of pkv_decode_long.hip's
 // kernel, in which only the tiles that hold drafted tokens look at the tree: 32 of its bits are one word, shifted to the tile.
+#include <type_traits>
+
 #include "pkv_long.h"
+#include "pkv_lds.h"
 
 namespace pkv {
 namespace {
+
+// 16 bytes per lane from a lane's own address into LDS, lane after lane from byte `to` on.  Asynchronous: wait_loads.  (As
+// pkv_prefill.hip's, but rows of a cache in pages lie anywhere; nothing is returned in registers.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is a register that the compiler keeps to itself; nothing else here uses it)
+__device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
+}
+// The same of 4 bytes.
+__device__ __forceinline__ void word_to_lds(const int32_t* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(to), "v"(from) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+constexpr int kBuffers = 3;  // of a step's keys and values
+
+// MODE 1: scores are capped or biased.
+template <typename T, int D, int MODE>
+__global__ __launch_bounds__(256, 3) void tree_wide_kernel(const TreeWideArgs a) {
+  constexpr int STEPS = D / 16, MB = D / 32, PIECES = D / 8, ROWS_PER_LOAD = 64 / PIECES, ROWS = group_rows<TreeWideArgs>();
+  constexpr int OWN = kTile / 4, LOADS = OWN / ROWS_PER_LOAD;  // rows of a step that a wave fetches, loads of K (and of V) for them
+  constexpr int ROW = D * 2, BUF = kTile * ROW;
+  constexpr float SHIFT = Weight<T>::HALF ? kWideShift : 0.0f;
+  __shared__ __align__(1024) char lds[kBuffers * 2 * BUF];  // [buffer][K, V]
+  __shared__ int32_t lds_depth[kMostDrafted];
+  __shared__ __align__(16) int32_t lds_pos[4][kTile];
+  __shared__ int32_t lds_span[4][2];
+  __shared__ int lds_zeroed;  // whether a value of V that is not finite was put to zero
+  __shared__ int32_t lds_look[4][2][2][kTile];  // [wave][step % 2][page, position]: what has to be loaded to know a step's rows
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const uint32_t look_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_look;
+  const int lane = threadIdx.x & 63, wave = this_wave(), col = lane & 31, half = lane >> 5;
+
+  // Workgroups that follow one another take different KV heads, then the tiles of rows that read the same keys.
+  int b, ranges, per, k;
+  Tiles tl;
+  if (!a.by_length) {
+    ranges = max(a.ranges, 1);
+    b = blockIdx.x / (a.units * ranges);
+    k = blockIdx.x % (a.units * ranges);
+    tl = tiles_of(a, b);
+    per = (tl.count + ranges - 1) / ranges;
+  } else {
+    const Place p = a.B <= 64 ? place_of_workgroup<1>(a, blockIdx.x, lane) : place_of_workgroup<kLaneSequences>(a, blockIdx.x, lane);
+    if (p.b < 0) return;
+    b = p.b;
+    ranges = p.ranges;
+    per = p.per;
+    k = (int)blockIdx.x - p.base;
+    tl = p.tl;
+  }
+  const int unit = k % a.units, range = k / a.units, g = unit % a.Hkv, tile = unit / a.Hkv;
+  const int n = tl.n, past = tl.q_pos;
+  int step = tl.first + range * per;
+  const int step_end = tl.first + min((range + 1) * per, tl.count);
+
+  const int row = ROWS * tile + 32 * wave + col;  // of those that share the KV head
+  const int t = row < a.G ? row / a.heads : 0, h = g * a.heads + (row < a.G ? row % a.heads : 0);
+  const int drafted = a.new_lens ? min(max(a.new_lens[b], 0), a.T) : a.T;
+  const bool there = row < a.G && t < drafted, wave_there = __any(there);
+  const bool placed = a.positions || a.window || (MODE == 1 && a.slopes);  // positions matter
+  int32_t p_row = 0;
+  if (placed) {
+    if (!a.q_pos) {
+      for (int i = threadIdx.x; i < a.T; i += 256) lds_depth[i] = ancestors(a, b, i, drafted);
+      __syncthreads();
+    }
+    p_row = a.q_pos ? a.q_pos[(int64_t)b * a.T + t] : past + lds_depth[t];
+  }
+  // the least and the greatest position of the wave's rows, and of the workgroup's
+  const int32_t w_min = ~wave_max(there ? ~p_row : INT32_MIN), w_max = wave_max(there ? p_row : INT32_MIN);
+  if (lane == 0) {
+    lds_span[wave][0] = w_min;
+    lds_span[wave][1] = w_max;
+    if (wave == 0) lds_zeroed = 0;
+  }
+  __syncthreads();
+  const int32_t g_min = min(min(lds_span[0][0], lds_span[1][0]), min(lds_span[2][0], lds_span[3][0]));
+  const int32_t g_max = max(max(lds_span[0][1], lds_span[1][1]), max(lds_span[2][1], lds_span[3][1]));
+  if (ROWS * tile >= drafted * a.heads) step = step_end;  // no row is there
+  const int step_begin = step;
+
+  const uint32_t row_bytes = (uint32_t)(a.page_size ? D : a.c_st) * 2;
+  const int64_t base = a.page_size ? 0 : (b * a.c_sb + g * a.c_sh) * 2;
+  const char* const Kb = reinterpret_cast<const char*>(a.K) + base;
+  const char* const Vb = reinterpret_cast<const char*>(a.V) + base;
+  const int32_t* const table = a.table + (int64_t)b * a.max_pages;
+  const int32_t* const pos_b = a.positions + b * a.p_sb + g * a.p_sh;
+
+  // A step's rows, lane l row l % 32: which of them are there (one bit each), their positions, and where they lie.  Where a row is not
+  // there, the cache's first is taken, with a weight of 0.  Page numbers and positions come through LDS like the rows themselves: were
+  // they loaded into registers, their first use would wait for all that has been requested since.
+  int32_t pos = 0;
+  uint32_t seen = 0, at = 0;
+  auto page_of = [&](int j, int& slot) {
+    uint32_t p = __umulhi((uint32_t)j, a.page_magic);
+    if ((uint32_t)j - p * a.page_size >= (uint32_t)a.page_size) ++p;
+    slot = j - p * a.page_size;
+    return p;
+  };
+  auto look = [&](int st) {
+    const int j = min(st * kTile + col, n - 1);
+    const uint32_t to = look_base + (wave * 4 + (st & 1) * 2) * (kTile * 4);
+    if (half == 0) {
+      int slot;
+      if (a.page_size) word_to_lds(table + page_of(j, slot), to);
+      if (a.positions) word_to_lds(pos_b + j, to + kTile * 4);
+    }
+  };
+  auto resolve = [&](int st) {
+    const int j = min(st * kTile + col, n - 1);
+    int slot = j;
+    pos = j;
+    if (a.positions)
+      pos = lds_look[wave][st & 1][1][col];
+    else if (placed && j >= past)
+      pos = past + lds_depth[min(j - past, a.T - 1)];
+    bool is = st * kTile + col < n && (!a.positions || pos >= 0);
+    at = slot;
+    if (a.page_size) {
+      page_of(j, slot);
+      const uint32_t page = (uint32_t)lds_look[wave][st & 1][0][col];
+      is = is && page < (uint32_t)a.num_pages;
+      at = (page * a.Hkv + g) * a.page_size + slot;
+    }
+    at = is ? at : 0;
+    seen = (uint32_t)__ballot(is);
+  };
+  // Fetching a step: wave w rows 8 w .. 8 w + 7 of K and of V, a row's pieces swapped.
+  auto fetch = [&](int buf) {
+    const uint32_t to = lds_base + buf * 2 * BUF + OWN * wave * ROW;
+    int id = lane;
+    asm("" : "+v"(id));  // (what follows from it is not kept in registers, which are short)
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = OWN * wave + i * ROWS_PER_LOAD + id / PIECES, piece = id % PIECES;
+      const uint64_t from = (uint64_t)(uint32_t)__shfl((int)at, r) * row_bytes;
+      load_to_lds(Kb + from + 16 * (piece ^ swizzle_k<D>(r)), to + i * 1024);
+      load_to_lds(Vb + from + 16 * (piece ^ swizzle_v<D>(r)), to + i * 1024 + BUF);
+    }
+  };
+  // Whether rows whose positions are from least to greatest see all rows of a step that are there.
+  auto whole = [&](int st, uint32_t now, int32_t pos_now, int32_t least, int32_t greatest) {
+    const int off = st * kTile - past;
+    if (off + kTile > 0) return false;
+    if (!a.positions && !a.window) return true;
+    const bool all = pos_now <= least && (!a.window || (int64_t)pos_now > (int64_t)greatest - a.window);
+    return (now & ~(uint32_t)__ballot(all)) == 0;
+  };
+  // Of the rows that are there, those that the own row sees.
+  auto visible = [&](int st, uint32_t now, int32_t pos_now) {
+    const int off = st * kTile - past;
+    uint32_t mine = now;
+    if (off + kTile > 0) mine &= drafted_seen(a, b, t, off);
+    if (a.positions || a.window) {
+      const bool before = off + col < 0;
+      const bool all = (!before || pos_now <= w_min) && (!a.window || (int64_t)pos_now > (int64_t)w_max - a.window);
+      for (uint32_t left = now & ~(uint32_t)__ballot(all); left != 0; left &= left - 1) {
+        const int i = __builtin_ctz(left);
+        const int32_t kp = __builtin_amdgcn_readlane(pos_now, i);
+        if ((off + i < 0 && kp > p_row) || (a.window && (int64_t)kp <= (int64_t)p_row - a.window)) mine &= ~(1u << i);
+      }
+    }
+    return there ? mine : now;
+  };
+
+  // Two steps are on their way while a third is worked on.
+  uint32_t seen_now = 0, seen_next = 0;
+  int32_t pos_now = 0, pos_of_next = 0;
+  if (step < step_end) {
+    look(step);
+    look(step + 1);
+    wait_loads();
+    resolve(step);
+    seen_now = seen;
+    pos_now = pos;
+    fetch(0);
+    resolve(step + 1);
+    look(step + 2);
+    if (step + 1 < step_end) fetch(1);
+    seen_next = seen;
+    pos_of_next = pos;
+  }
+
+  u32x4 qf[STEPS];
+  {
+    const uint16_t* qp = a.q + b * a.q_sb + h * a.q_sh + t * a.q_st + 8 * half;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) qf[i] = there ? *reinterpret_cast<const u32x4*>(qp + 16 * i) : (u32x4)(0);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) asm volatile("" : "+v"(qf[i]));  // (they are waited for here, and not by every step's products)
+  }
+  float slope = MODE == 1 && a.slopes ? a.slopes[h] * kLog2e : 0.0f;
+  asm volatile("" : "+v"(slope));
+
+  float m = kNone, z = 0.0f;
+  bool large = false;  // some reference is beyond kLarge
+  f32x16 o[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) o[i] = (f32x16)(0.0f);
+
+  // Places in a step's rows, as in pkv_prefill.hip.
+  const int k_at = col * ROW + ((half ^ swizzle_k<D>(col)) << 4);
+  const int v_row = 4 * half + ((lane & 15) >> 2), v_piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const int v_at = v_row * ROW + ((v_piece ^ swizzle_v<D>(v_row)) << 4) + 8 * (lane & 1);
+
+  auto one_step = [&](auto buffer) {
+    constexpr int buf = decltype(buffer)::value;
+    const char* const Kl = lds + buf * 2 * BUF;
+    char* const Vl = lds + buf * 2 * BUF + BUF;
+    const uint32_t now = seen_now;
+    if (step + 1 < step_end)
+      wait_loads<2 * LOADS>();  // (those of the next step)
+    else
+      wait_loads();
+    if (now != ~0u || !whole(step, now, pos_now, g_min, g_max)) {
+      // a row that is hidden from some: values of V that are not finite would spoil the product with a weight of 0
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        u32x4* const mine = reinterpret_cast<u32x4*>(Vl + (OWN * wave + i * ROWS_PER_LOAD) * ROW + 16 * lane);
+        u32x4 v = *mine;
+        uint32_t any = 0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t nf = not_finite<T>(v[x]);
+          any |= nf;
+          v[x] &= ~((nf >> 15) * 0xFFFFu);
+        }
+        if (any) {
+          *mine = v;
+          lds_zeroed = 1;
+        }
+      }
+    }
+    lds_barrier();
+    if (step + 2 < step_end) {
+      resolve(step + 2);
+      look(step + 3);
+      fetch((buf + 2) % kBuffers);
+    }
+    if (!wave_there) return;
+    f32x16 sc;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const u32x4 kf = *reinterpret_cast<const u32x4*>(Kl + (k_at ^ (i << 5)));
+      sc = Elem<T>::mfma32(kf, qf[i], i == 0 ? (f32x16)(0.0f) : sc);
+    }
+    if constexpr (MODE == 1) {
+      if (a.cap.cap != 0.0f) {
+        float x[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = sc[e];
+        cap_scores(x, a.cap);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = x[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] *= a.scale;
+      }
+      if (a.slopes) {
+        if (lane < kTile) lds_pos[wave][lane] = pos_now;
+        own_lds_order();
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const u32x4 kp = *reinterpret_cast<const u32x4*>(&lds_pos[wave][8 * x + 4 * half]);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const uint32_t d = (uint32_t)p_row - kp[y];
+            sc[4 * x + y] = fmaf(-slope, (float)((int32_t)kp[y] > p_row ? 0u - d : d), sc[4 * x + y]);
+          }
+        }
+        own_lds_order();
+      }
+    }
+    if (now != ~0u || !whole(step, now, pos_now, w_min, w_max)) {
+      const uint32_t mine = visible(step, now, pos_now) >> (4 * half);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!(mine & (1u << key_of(e)))) sc[e] = kNone;
+    }
+    const float f1 = MODE == 1 ? 1.0f : a.scale;
+    float top = sc[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) top = fmaxf(top, sc[e]);
+    top *= f1;
+    if (__any(top - m > 6.0f)) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m1 = fmaxf(m, top);
+      const float f = m1 == kNone ? 1.0f : exp2_(m - m1);
+      m = m1;
+      z *= f;
+#pragma unroll
+      for (int i = 0; i < MB; ++i) o[i] *= f;
+      large = __any(m != kNone && fabsf(m) > kLarge);
+    }
+    float ref = (m == kNone ? 0.0f : m) - SHIFT, factor = f1;
+    if (__builtin_expect(large, 0)) {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[e] = (sc[e] * f1 - (m == kNone ? 0.0f : m)) + SHIFT;
+      ref = 0.0f;
+      factor = 1.0f;
+    }
+    u32x4 pf[2];
+    float z0 = 0.0f, z1 = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      const float p0 = exp2_(fmaf(sc[e], factor, -ref)), p1 = exp2_(fmaf(sc[e + 1], factor, -ref));
+      z0 += p0;
+      z1 += p1;
+      pf[e >> 3][(e >> 1) & 3] = pack2<T>(p0, p1);
+    }
+    z += z0 + z1;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        const char* const from = Vl + (v_at ^ (mb << 6)) + 16 * ks * ROW;
+        const u32x2 x = read_columns(from), y = read_columns(from + 8 * ROW);
+        const u32x4 vf = {x[0], x[1], y[0], y[1]};
+        o[mb] = Elem<T>::mfma32(vf, pf[ks], o[mb]);
+      }
+    }
+  };
+  auto advance = [&]() {
+    seen_now = seen_next;
+    pos_now = pos_of_next;
+    seen_next = seen;
+    pos_of_next = pos;
+    return ++step < step_end;
+  };
+  while (step < step_end) {
+    one_step(std::integral_constant<int, 0>());
+    if (!advance()) break;
+    one_step(std::integral_constant<int, 1>());
+    if (!advance()) break;
+    one_step(std::integral_constant<int, 2>());
+    advance();
+  }
+
+  if (!there)  // (0 times what is not finite)
+#pragma unroll
+    for (int i = 0; i < MB; ++i) o[i] = (f32x16)(0.0f);
+  f32x4 naught = (f32x4)(0.0f);  // of what is finite; otherwise NaN
+#pragma unroll
+  for (int x = 0; x < MB * 16; ++x) naught[x & 3] = fmaf(o[x >> 4][x & 15], 0.0f, naught[x & 3]);
+  const bool odd = lds_zeroed != 0 || (naught[0] + naught[1]) + (naught[2] + naught[3]) != 0.0f;
+  if (__builtin_expect(__any(odd) && wave_there, 0)) {
+    // Values of V that are not finite: where a row sees some, its element is their sum (every weight is positive).
+    f32x16 extra[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) extra[i] = (f32x16)(0.0f);
+#pragma unroll 1
+    for (int st = step_begin; st < step_end; ++st) {
+      look(st);
+      wait_loads();
+      resolve(st);
+      uint32_t left = 0;  // rows with such values
+#pragma unroll 1
+      for (int r0 = 0; r0 < kTile; r0 += ROWS_PER_LOAD) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(Vb + (uint64_t)(uint32_t)__shfl((int)at, r0 + lane / PIECES) * row_bytes + 16 * (lane % PIECES));
+        const uint64_t some = __ballot((not_finite<T>(v[0]) | not_finite<T>(v[1]) | not_finite<T>(v[2]) | not_finite<T>(v[3])) != 0);
+#pragma unroll
+        for (int r = 0; r < ROWS_PER_LOAD; ++r) left |= (some >> (r * PIECES) & (((uint64_t)1 << PIECES) - 1)) != 0 ? 1u << (r0 + r) : 0u;
+      }
+      left &= seen;
+      if (left == 0) continue;
+      const uint32_t mine = there ? visible(st, seen, pos) : 0u;
+#pragma unroll 1
+      for (; left != 0; left &= left - 1) {
+        const int i = __builtin_ctz(left);
+        const char* const from = Vb + (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, i) * row_bytes + 8 * half;
+        const bool sees = mine >> i & 1;
+#pragma unroll
+        for (int x = 0; x < MB * 4; ++x) {
+          const u32x2 u = *reinterpret_cast<const u32x2*>(from + 16 * x);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const float e = unpack<T>(u[y >> 1], y & 1);
+            extra[x >> 2][4 * (x & 3) + y] += sees && !(fabsf(e) < __builtin_inff()) ? e : 0.0f;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < MB * 16; ++x) o[x >> 4][x & 15] = extra[x >> 4][x & 15] == 0.0f ? o[x >> 4][x & 15] : extra[x >> 4][x & 15];
+  }
+
+  z += __shfl_xor(z, 32);
+  int id = threadIdx.x;
+  asm("" : "+v"(id));
+  const int end_local = 32 * (id >> 6) + (id & 31), end_row = ROWS * tile + end_local, end_half = (id >> 5) & 1;
+  if (end_row >= a.G) return;
+  if (!there) {
+    m = kNone;
+    z = 0.0f;
+  }
+  if (ranges > 1) {
+    const int64_t to = (int64_t)blockIdx.x * ROWS + end_local;
+    float* const po = a.part_o + to * D + 4 * end_half;
+#pragma unroll
+    for (int x = 0; x < MB * 4; ++x) {
+      f32x4 v;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) v[y] = o[x >> 2][4 * (x & 3) + y];
+      *reinterpret_cast<f32x4*>(po + 8 * x) = v;
+    }
+    if (end_half == 0) {
+      a.part_mz[to * 2] = m;
+      a.part_mz[to * 2 + 1] = z;
+    }
+    return;
+  }
+  const float inv = z == 0.0f ? 0.0f : 1.0f / z;
+  uint16_t* const op = a.out + out_at(a, b, g, end_row, D) + 4 * end_half;
+#pragma unroll
+  for (int x = 0; x < MB * 4; ++x) {
+    u32x2 w;
+    w[0] = pack2<T>(o[x >> 2][4 * (x & 3)] * inv, o[x >> 2][4 * (x & 3) + 1] * inv);
+    w[1] = pack2<T>(o[x >> 2][4 * (x & 3) + 2] * inv, o[x >> 2][4 * (x & 3) + 3] * inv);
+    *reinterpret_cast<u32x2*>(op + 8 * x) = w;
+  }
+  if (a.lse && end_half == 0) a.lse[lse_at(a, b, g, end_row)] = z == 0.0f ? kNone : (m - SHIFT + log2_(z)) * kLn2;
+}
+
+template <typename T, int D>
+hipError_t launch_wide(const TreeWideArgs& a, int64_t workgroups, hipStream_t s) {
+  if (a.cap.cap != 0.0f || a.slopes)
+    hipLaunchKernelGGL((tree_wide_kernel<T, D, 1>), dim3((unsigned)workgroups), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((tree_wide_kernel<T, D, 0>), dim3((unsigned)workgroups), dim3(256), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.ranges == 0 ? e : launch_join<T, D>(a, s);
+}
+
+// More than 64 query rows a KV head: the kernel above.
+bool wide(const pkv_tree_desc& d) { return (int64_t)d.T * (d.Hq / d.Hkv) > 64; }
+
+// As grid_of of pkv_long.h, in workgroups of 128 rows, of which the device holds three per compute unit.
+Grid wide_grid(const pkv_tree_desc& d) {
+  constexpr int ROWS = group_rows<TreeWideArgs>();
+  const int64_t units = d.Hkv * (((int64_t)d.T * (d.Hq / d.Hkv) + ROWS - 1) / ROWS), all = d.B * units;
+  if (d.k_cap <= kLeastWide * kTile) return {all, 0, 0};
+  if (d.B > 1 && d.B <= kFlatBatch && (int64_t)d.B * d.k_cap <= (int64_t)1 << 36) {
+    const int64_t share = all <= kWideTurn / 2 ? kWideTurn : 2 * kWideTurn;
+    return all >= 2 * kWideTurn && (d.k_cap <= kWhole || all > kMostUnits) ? Grid{all, 0, 0} : Grid{share + all, (int32_t)share, 1};
+  }
+  int64_t S = kWideTurn / all;
+  const int64_t most = ((int64_t)d.k_cap + kLeastWide * kTile - 1) / (kLeastWide * kTile);
+  if (S > most) S = most;
+  return S <= 1 ? Grid{all, 0, 0} : Grid{all * S, (int32_t)S, 0};
+}
+size_t wide_bytes(const Grid& g, int d) { return g.ranges == 0 ? 0 : (size_t)g.workgroups * group_rows<TreeWideArgs>() * (d + 2) * sizeof(float); }
 
 int check_tree_desc(const pkv_tree_desc* desc) {
   if (!desc) return PKV_ERR_INVALID_ARG;
@@ -46,6 +502,7 @@ int pkv_tree_bits(int32_t T, const int32_t* parents, int32_t* bits_out) {
 
 size_t pkv_tree_workspace_bytes(const pkv_tree_desc* desc) {
   if (check_tree_desc(desc) != PKV_OK) return 0;
+  if (wide(*desc)) return wide_bytes(wide_grid(*desc), desc->d);
   return parts_bytes(grid_of(*desc), desc->T * (desc->Hq / desc->Hkv), desc->d);
 }
 
@@ -64,9 +521,10 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q, const void* K_c
   if ((d.page_size > 0 && !block_table) || !positions != !q_pos) return PKV_ERR_INVALID_ARG;
   const size_t need = pkv_tree_workspace_bytes(desc);
   if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PKV_ERR_WORKSPACE;
-  TreeArgs a;
+  TreeWideArgs a;
   memset(&a, 0, sizeof(a));
-  const Grid grid = grid_of(d);
+  const bool many = wide(d);
+  const Grid grid = many ? wide_grid(d) : grid_of(d);
   fill_long(a, d, grid, d.T * (d.Hq / d.Hkv), q, K_cache, V_cache, out, workspace);
   a.table = block_table; a.count = count; a.positions = positions; a.q_pos = q_pos; a.slopes = slopes;
   a.new_lens = new_lens; a.tree = tree;
@@ -75,7 +533,20 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q, const void* K_c
   a.p_sb = d.p_sb; a.p_sh = d.p_sh;
   a.T = d.T; a.words = (d.T + 31) / 32; a.heads = d.Hq / d.Hkv;
   a.q_st = d.q_st; a.o_sb = d.o_sb; a.o_sh = d.o_sh; a.o_st = d.o_st;
-  const hipError_t e = launch_long(a, d.dtype, d.d, grid.workgroups, static_cast<hipStream_t>(stream));
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  if (!many) {
+    e = launch_long(static_cast<const TreeArgs&>(a), d.dtype, d.d, grid.workgroups, st);
+  } else {
+    constexpr int ROWS = group_rows<TreeWideArgs>();
+    a.head_groups = (a.G + ROWS - 1) / ROWS;
+    a.units = a.Hkv * a.head_groups;
+    a.part_mz = a.part_o ? a.part_o + (size_t)grid.workgroups * ROWS * d.d : nullptr;
+    if (d.dtype == PKV_BF16)
+      e = d.d == 128 ? launch_wide<__bf16, 128>(a, grid.workgroups, st) : launch_wide<__bf16, 64>(a, grid.workgroups, st);
+    else
+      e = d.d == 128 ? launch_wide<_Float16, 128>(a, grid.workgroups, st) : launch_wide<_Float16, 64>(a, grid.workgroups, st);
+  }
   return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
 }
 
