@@ -17,8 +17,7 @@ constexpr int kWorkgroups = 512;   // at a time on the device: two per compute u
 constexpr int kLaneSequences = 4;  // sequences a lane looks after where ranges go by lengths,
 constexpr int kFlatBatch = 64 * kLaneSequences;  // and so many at most in all
 constexpr int kLeastTiles = 8;     // of a range,
-constexpr int kLeastWide = 24;     // of many query rows,
-constexpr int kWideTurn = 768;     // whose workgroups are so many at a time
+constexpr int kLeastWide = 12;     // of many query rows
 
 // What the kernel is built for: one token over all rows; the same, handing its scores on; drafted tokens; listed blocks of rows.
 // (kTreeWide: drafted tokens whose query rows are many, in pkv_tree.hip's own kernel.)
@@ -60,6 +59,7 @@ struct TreeArgs : LongArgs {
   static constexpr int MODE = kTree;
 };
 struct TreeWideArgs : TreeArgs {
+  int32_t turn;  // workgroups that the device holds at a time
   static constexpr int MODE = kTreeWide;
 };
 template <typename A>
@@ -155,7 +155,7 @@ __device__ __forceinline__ Cut<E> flat_cut(const A& a, int lane) {
     }
     c.end = sum_upto(sum);
     if constexpr (A::MODE == kTreeWide) {
-      if (a.ranges != kWideTurn || tries == 6 || __builtin_amdgcn_readlane(c.end, 63) <= kWideTurn) break;
+      if (a.ranges != a.turn || tries == 6 || __builtin_amdgcn_readlane(c.end, 63) <= a.turn) break;
     }
     if (A::MODE != kTreeWide && (shift != 9 || tries == 6 || __builtin_amdgcn_readlane(c.end, 63) <= kWorkgroups)) break;
     c.per += max(shares, c.per / 16 / shares * shares);

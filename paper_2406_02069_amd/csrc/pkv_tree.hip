@@ -26,8 +26,10 @@ __device__ __forceinline__ void word_to_lds(const int32_t* from, uint32_t to) {
 constexpr int kBuffers = 3;  // of a step's keys and values
 
 // MODE 1: scores are capped or biased.
+template <int D, int MODE>
+constexpr int wide_per_unit() { return D == 128 && MODE == 1 ? 2 : 3; }  // workgroups of a compute unit
 template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256, 3) void tree_wide_kernel(const TreeWideArgs a) {
+__global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_kernel(const TreeWideArgs a) {
   constexpr int STEPS = D / 16, MB = D / 32, PIECES = D / 8, ROWS_PER_LOAD = 64 / PIECES, ROWS = group_rows<TreeWideArgs>();
   constexpr int OWN = kTile / 4, LOADS = OWN / ROWS_PER_LOAD;  // rows of a step that a wave fetches, loads of K (and of V) for them
   constexpr int ROW = D * 2, BUF = kTile * ROW;
@@ -244,18 +246,20 @@ __global__ __launch_bounds__(256, 3) void tree_wide_kernel(const TreeWideArgs a)
       }
     }
     lds_barrier();
-    if (step + 2 < step_end) {
+    f32x16 sc;
+    if (wave_there) {
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const u32x4 kf = *reinterpret_cast<const u32x4*>(Kl + (k_at ^ (i << 5)));
+        sc = Elem<T>::mfma32(kf, qf[i], i == 0 ? (f32x16)(0.0f) : sc);
+      }
+    }
+    if (step + 2 < step_end) {  // (beside the products)
       resolve(step + 2);
       look(step + 3);
       fetch((buf + 2) % kBuffers);
     }
     if (!wave_there) return;
-    f32x16 sc;
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-      const u32x4 kf = *reinterpret_cast<const u32x4*>(Kl + (k_at ^ (i << 5)));
-      sc = Elem<T>::mfma32(kf, qf[i], i == 0 ? (f32x16)(0.0f) : sc);
-    }
     if constexpr (MODE == 1) {
       if (a.cap.cap != 0.0f) {
         float x[16];
@@ -448,15 +452,16 @@ hipError_t launch_wide(const TreeWideArgs& a, int64_t workgroups, hipStream_t s)
 bool wide(const pkv_tree_desc& d) { return (int64_t)d.T * (d.Hq / d.Hkv) > 64; }
 
 // As grid_of of pkv_long.h, in workgroups of 128 rows, of which the device holds three per compute unit.
-Grid wide_grid(const pkv_tree_desc& d) {
+int wide_turn(const pkv_tree_desc& d, bool biased) { return 256 * (d.d == 128 && (d.cap > 0.0f || biased) ? 2 : 3); }
+Grid wide_grid(const pkv_tree_desc& d, int turn) {
   constexpr int ROWS = group_rows<TreeWideArgs>();
   const int64_t units = d.Hkv * (((int64_t)d.T * (d.Hq / d.Hkv) + ROWS - 1) / ROWS), all = d.B * units;
   if (d.k_cap <= kLeastWide * kTile) return {all, 0, 0};
   if (d.B > 1 && d.B <= kFlatBatch && (int64_t)d.B * d.k_cap <= (int64_t)1 << 36) {
-    const int64_t share = all <= kWideTurn / 2 ? kWideTurn : 2 * kWideTurn;
-    return all >= 2 * kWideTurn && (d.k_cap <= kWhole || all > kMostUnits) ? Grid{all, 0, 0} : Grid{share + all, (int32_t)share, 1};
+    const int64_t share = all <= turn / 2 ? turn : 2 * turn;
+    return all >= 2 * turn && (d.k_cap <= kWhole || all > kMostUnits) ? Grid{all, 0, 0} : Grid{share + all, (int32_t)share, 1};
   }
-  int64_t S = kWideTurn / all;
+  int64_t S = turn / all;
   const int64_t most = ((int64_t)d.k_cap + kLeastWide * kTile - 1) / (kLeastWide * kTile);
   if (S > most) S = most;
   return S <= 1 ? Grid{all, 0, 0} : Grid{all * S, (int32_t)S, 0};
@@ -502,7 +507,10 @@ int pkv_tree_bits(int32_t T, const int32_t* parents, int32_t* bits_out) {
 
 size_t pkv_tree_workspace_bytes(const pkv_tree_desc* desc) {
   if (check_tree_desc(desc) != PKV_OK) return 0;
-  if (wide(*desc)) return wide_bytes(wide_grid(*desc), desc->d);
+  if (wide(*desc)) {  // (with slopes or without)
+    const size_t plain = wide_bytes(wide_grid(*desc, wide_turn(*desc, false)), desc->d), biased = wide_bytes(wide_grid(*desc, wide_turn(*desc, true)), desc->d);
+    return plain > biased ? plain : biased;
+  }
   return parts_bytes(grid_of(*desc), desc->T * (desc->Hq / desc->Hkv), desc->d);
 }
 
@@ -524,7 +532,7 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q, const void* K_c
   TreeWideArgs a;
   memset(&a, 0, sizeof(a));
   const bool many = wide(d);
-  const Grid grid = many ? wide_grid(d) : grid_of(d);
+  const Grid grid = many ? wide_grid(d, wide_turn(d, slopes)) : grid_of(d);
   fill_long(a, d, grid, d.T * (d.Hq / d.Hkv), q, K_cache, V_cache, out, workspace);
   a.table = block_table; a.count = count; a.positions = positions; a.q_pos = q_pos; a.slopes = slopes;
   a.new_lens = new_lens; a.tree = tree;
@@ -539,6 +547,7 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q, const void* K_c
     e = launch_long(static_cast<const TreeArgs&>(a), d.dtype, d.d, grid.workgroups, st);
   } else {
     constexpr int ROWS = group_rows<TreeWideArgs>();
+    a.turn = wide_turn(d, slopes);
     a.head_groups = (a.G + ROWS - 1) / ROWS;
     a.units = a.Hkv * a.head_groups;
     a.part_mz = a.part_o ? a.part_o + (size_t)grid.workgroups * ROWS * d.d : nullptr;
