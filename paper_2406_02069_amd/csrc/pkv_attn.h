@@ -191,6 +191,16 @@ __device__ __forceinline__ void cap_scores(float (&x)[N], const Cap& c) {
 // left of a rounded product is as large as a step there, and would be a weight's exponent.
 constexpr float kLarge = 0x1p20f;
 
+// 16 bytes per lane from base + at into LDS, lane after lane from byte `to` on.  Asynchronous: wait_loads.  (Written out because
+// the compiler lets every later read of LDS wait for such a load, though it goes to another buffer; nothing is returned in
+// registers.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is a register that the compiler keeps to itself; nothing else here uses it)
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 // Waits for the asynchronous loads into LDS, but for the last LATER (below 16) of them: loads end in the order of their requests.
 template <int LATER = 0>
 __device__ __forceinline__ void wait_loads() {

@@ -135,15 +135,6 @@ __device__ __forceinline__ Shares shares_of(const PrefillArgs& a, int lane) {
   return s;
 }
 
-// 16 bytes per lane from base + at into LDS, lane after lane from byte `to` on.  Asynchronous: wait_loads.  (Written out because
-// the compiler lets every later read of LDS wait for such a load, though it goes to another buffer; nothing is returned in
-// registers.)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is a register that the compiler keeps to itself; nothing else here uses it)
-__device__ __forceinline__ void load_to_lds(const char* base, uint32_t at, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(base) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 // MODE 1: scores are capped or biased.
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(256, 3) void prefill_kernel(const PrefillArgs a) {

@@ -10,10 +10,9 @@
 namespace pkv {
 namespace {
 
-// 16 bytes per lane from a lane's own address into LDS, lane after lane from byte `to` on.  Asynchronous: wait_loads.  (As
-// pkv_prefill.hip's, but rows of a cache in pages lie anywhere; nothing is returned in registers.)
+// load_to_lds from a lane's own address: rows of a cache in pages lie anywhere.
 #pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is a register that the compiler keeps to itself; nothing else here uses it)
+#pragma clang diagnostic ignored "-Winline-asm"  // (as there)
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
 }
@@ -24,6 +23,7 @@ __device__ __forceinline__ void word_to_lds(const int32_t* from, uint32_t to) {
 #pragma clang diagnostic pop
 
 constexpr int kBuffers = 3;  // of a step's keys and values
+constexpr int kSlots = 4;    // of what is known of a step: from three steps before it on
 
 // MODE 1: scores are capped or biased.
 template <int D, int MODE>
@@ -36,12 +36,15 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
   constexpr float SHIFT = Weight<T>::HALF ? kWideShift : 0.0f;
   __shared__ __align__(1024) char lds[kBuffers * 2 * BUF];  // [buffer][K, V]
   __shared__ int32_t lds_depth[kMostDrafted];
-  __shared__ __align__(16) int32_t lds_pos[4][kTile];
+  __shared__ __align__(16) int32_t lds_pos[kSlots][kTile];   // [step % kSlots]: given positions
+  __shared__ __align__(16) int32_t lds_own_pos[4][kTile];    // [wave]: positions that are worked out
+  __shared__ int32_t lds_page[4][2][OWN];                    // [wave][step % 2]: pages of the rows that the wave fetches
+  __shared__ uint32_t lds_seen[kSlots];                      // [step % kSlots]: rows on pages that exist, a byte of each wave
   __shared__ int32_t lds_span[4][2];
   __shared__ int lds_zeroed;  // whether a value of V that is not finite was put to zero
-  __shared__ int32_t lds_look[4][2][2][kTile];  // [wave][step % 2][page, position]: what has to be loaded to know a step's rows
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  const uint32_t look_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_look;
+  const uint32_t pos_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_pos;
+  const uint32_t page_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_page;
   const int lane = threadIdx.x & 63, wave = this_wave(), col = lane & 31, half = lane >> 5;
 
   // Workgroups that follow one another take different KV heads, then the tiles of rows that read the same keys.
@@ -100,57 +103,81 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
   const int32_t* const table = a.table + (int64_t)b * a.max_pages;
   const int32_t* const pos_b = a.positions + b * a.p_sb + g * a.p_sh;
 
-  // A step's rows, lane l row l % 32: which of them are there (one bit each), their positions, and where they lie.  Where a row is not
-  // there, the cache's first is taken, with a weight of 0.  Page numbers and positions come through LDS like the rows themselves: were
-  // they loaded into registers, their first use would wait for all that has been requested since.
-  int32_t pos = 0;
-  uint32_t seen = 0, at = 0;
-  auto page_of = [&](int j, int& slot) {
+  // Fetching a step: wave w rows 8 w .. 8 w + 7 of K and of V, a row's pieces swapped.  Their page numbers, and positions that are given,
+  // come through LDS like the rows themselves, a step before: were they loaded into registers, their first use would wait for all that
+  // has been requested since.  Eight rows in a row of a page, or of a compact cache, have one base; others are looked up one by one.
+  const bool even_rows = (a.page_size == 0 || a.page_size % OWN == 0) && row_bytes <= 1u << 26;
+  uint32_t at_k[LOADS], at_v[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int r = i * ROWS_PER_LOAD + lane / PIECES, piece = lane % PIECES;
+    at_k[i] = r * row_bytes + 16 * (piece ^ swizzle_k<D>(OWN * wave + r));
+    at_v[i] = r * row_bytes + 16 * (piece ^ swizzle_v<D>(OWN * wave + r));
+  }
+  auto page_of = [&](int j) {
     uint32_t p = __umulhi((uint32_t)j, a.page_magic);
     if ((uint32_t)j - p * a.page_size >= (uint32_t)a.page_size) ++p;
-    slot = j - p * a.page_size;
     return p;
   };
   auto look = [&](int st) {
-    const int j = min(st * kTile + col, n - 1);
-    const uint32_t to = look_base + (wave * 4 + (st & 1) * 2) * (kTile * 4);
-    if (half == 0) {
-      int slot;
-      if (a.page_size) word_to_lds(table + page_of(j, slot), to);
-      if (a.positions) word_to_lds(pos_b + j, to + kTile * 4);
+    if ((a.page_size || a.positions) && lane < OWN) {
+      const int j = min(st * kTile + OWN * wave + lane, n - 1);
+      if (a.page_size) word_to_lds(table + page_of(j), page_base + (wave * 2 + (st & 1)) * (OWN * 4));
+      if (a.positions) word_to_lds(pos_b + j, pos_base + ((st % kSlots) * kTile + OWN * wave) * 4);
     }
   };
-  auto resolve = [&](int st) {
-    const int j = min(st * kTile + col, n - 1);
-    int slot = j;
-    pos = j;
-    if (a.positions)
-      pos = lds_look[wave][st & 1][1][col];
-    else if (placed && j >= past)
-      pos = past + lds_depth[min(j - past, a.T - 1)];
-    bool is = st * kTile + col < n && (!a.positions || pos >= 0);
-    at = slot;
-    if (a.page_size) {
-      page_of(j, slot);
-      const uint32_t page = (uint32_t)lds_look[wave][st & 1][0][col];
-      is = is && page < (uint32_t)a.num_pages;
-      at = (page * a.Hkv + g) * a.page_size + slot;
-    }
-    at = is ? at : 0;
-    seen = (uint32_t)__ballot(is);
-  };
-  // Fetching a step: wave w rows 8 w .. 8 w + 7 of K and of V, a row's pieces swapped.
-  auto fetch = [&](int buf) {
+  auto fetch = [&](int st, int buf) {
     const uint32_t to = lds_base + buf * 2 * BUF + OWN * wave * ROW;
-    int id = lane;
-    asm("" : "+v"(id));  // (what follows from it is not kept in registers, which are short)
+    const int j0 = st * kTile + OWN * wave;
+    uint32_t there8 = 0xFF;
+    if (even_rows && j0 + OWN <= n) {
+      uint64_t row0 = (uint64_t)(uint32_t)j0;
+      if (a.page_size) {
+        const uint32_t slot = (uint32_t)j0 - page_of(j0) * a.page_size, page = (uint32_t)__builtin_amdgcn_readfirstlane(lds_page[wave][st & 1][0]);
+        const bool is = page < (uint32_t)a.num_pages;
+        there8 = is ? 0xFF : 0;
+        row0 = is ? (page * a.Hkv + g) * a.page_size + slot : 0;
+      }
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int r = OWN * wave + i * ROWS_PER_LOAD + id / PIECES, piece = id % PIECES;
-      const uint64_t from = (uint64_t)(uint32_t)__shfl((int)at, r) * row_bytes;
-      load_to_lds(Kb + from + 16 * (piece ^ swizzle_k<D>(r)), to + i * 1024);
-      load_to_lds(Vb + from + 16 * (piece ^ swizzle_v<D>(r)), to + i * 1024 + BUF);
+      for (int i = 0; i < LOADS; ++i) {
+        load_to_lds(Kb + row0 * row_bytes, at_k[i], to + i * 1024);
+        load_to_lds(Vb + row0 * row_bytes, at_v[i], to + i * 1024 + BUF);
+      }
+    } else {  // (rows behind the last one are taken as the last, those that are not there as the cache's first)
+      there8 = 0;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int r = i * ROWS_PER_LOAD + lane / PIECES, piece = lane % PIECES, j = min(j0 + r, n - 1);
+        uint32_t at = (uint32_t)j;
+        bool is = true;
+        if (a.page_size) {
+          const uint32_t page = (uint32_t)lds_page[wave][st & 1][r];
+          is = page < (uint32_t)a.num_pages;
+          at = is ? (page * a.Hkv + g) * a.page_size + ((uint32_t)j - page_of(j) * a.page_size) : 0;
+        }
+        const uint64_t is64 = __ballot(is);
+#pragma unroll
+        for (int x = 0; x < ROWS_PER_LOAD; ++x) there8 |= (uint32_t)(is64 >> (x * PIECES) & 1) << (i * ROWS_PER_LOAD + x);
+        load_to_lds(Kb + (uint64_t)at * row_bytes + 16 * (piece ^ swizzle_k<D>(OWN * wave + r)), to + i * 1024);
+        load_to_lds(Vb + (uint64_t)at * row_bytes + 16 * (piece ^ swizzle_v<D>(OWN * wave + r)), to + i * 1024 + BUF);
+      }
     }
+    if (a.page_size && lane == 0) reinterpret_cast<uint8_t*>(&lds_seen[st % kSlots])[wave] = (uint8_t)there8;
+  };
+  // Behind the barrier of the step before (by which all waves have made the step's fetch known): a step's rows that are there, one bit each, and the position of row l % 32.
+  auto rows_there = [&](int st, int32_t& pos) {
+    const int left = n - st * kTile;
+    uint32_t is = left >= kTile ? ~0u : (1u << left) - 1;
+    if (a.page_size) is &= (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_seen[st % kSlots]);
+    const int j = st * kTile + col;
+    pos = j;
+    if (a.positions) {
+      pos = lds_pos[st % kSlots][col];
+      is &= (uint32_t)__ballot(pos >= 0);
+    } else if (placed && st * kTile + kTile > past && j >= past) {
+      pos = past + lds_depth[min(j - past, a.T - 1)];
+    }
+    return is;
   };
   // Whether rows whose positions are from least to greatest see all rows of a step that are there.
   auto whole = [&](int st, uint32_t now, int32_t pos_now, int32_t least, int32_t greatest) {
@@ -178,21 +205,14 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
   };
 
   // Two steps are on their way while a third is worked on.
-  uint32_t seen_now = 0, seen_next = 0;
-  int32_t pos_now = 0, pos_of_next = 0;
   if (step < step_end) {
     look(step);
     look(step + 1);
     wait_loads();
-    resolve(step);
-    seen_now = seen;
-    pos_now = pos;
-    fetch(0);
-    resolve(step + 1);
+    fetch(step, 0);
     look(step + 2);
-    if (step + 1 < step_end) fetch(1);
-    seen_next = seen;
-    pos_of_next = pos;
+    if (step + 1 < step_end) fetch(step + 1, 1);
+    lds_barrier();
   }
 
   u32x4 qf[STEPS];
@@ -221,13 +241,14 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
     constexpr int buf = decltype(buffer)::value;
     const char* const Kl = lds + buf * 2 * BUF;
     char* const Vl = lds + buf * 2 * BUF + BUF;
-    const uint32_t now = seen_now;
     if (step + 1 < step_end)
       wait_loads<2 * LOADS>();  // (those of the next step)
     else
       wait_loads();
-    if (now != ~0u || !whole(step, now, pos_now, g_min, g_max)) {
-      // a row that is hidden from some: values of V that are not finite would spoil the product with a weight of 0
+    int32_t pos_now;
+    const uint32_t now = rows_there(step, pos_now);
+    if (now != ~0u || !whole(step, now, pos_now, g_min, g_max)) {  // some row of the workgroup does not see all of the step
+      // values of V that are not finite would spoil the product with a weight of 0: each wave those that it fetched
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         u32x4* const mine = reinterpret_cast<u32x4*>(Vl + (OWN * wave + i * ROWS_PER_LOAD) * ROW + 16 * lane);
@@ -255,9 +276,8 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
       }
     }
     if (step + 2 < step_end) {  // (beside the products)
-      resolve(step + 2);
       look(step + 3);
-      fetch((buf + 2) % kBuffers);
+      fetch(step + 2, (buf + 2) % kBuffers);
     }
     if (!wave_there) return;
     if constexpr (MODE == 1) {
@@ -273,11 +293,14 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
         for (int e = 0; e < 16; ++e) sc[e] *= a.scale;
       }
       if (a.slopes) {
-        if (lane < kTile) lds_pos[wave][lane] = pos_now;
-        own_lds_order();
+        if (!a.positions) {
+          if (lane < kTile) lds_own_pos[wave][lane] = pos_now;
+          own_lds_order();
+        }
+        const int32_t* const at = a.positions ? lds_pos[step % kSlots] : lds_own_pos[wave];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const u32x4 kp = *reinterpret_cast<const u32x4*>(&lds_pos[wave][8 * x + 4 * half]);
+          const u32x4 kp = *reinterpret_cast<const u32x4*>(&at[8 * x + 4 * half]);
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const uint32_t d = (uint32_t)p_row - kp[y];
@@ -337,20 +360,13 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
       }
     }
   };
-  auto advance = [&]() {
-    seen_now = seen_next;
-    pos_now = pos_of_next;
-    seen_next = seen;
-    pos_of_next = pos;
-    return ++step < step_end;
-  };
   while (step < step_end) {
     one_step(std::integral_constant<int, 0>());
-    if (!advance()) break;
+    if (++step >= step_end) break;
     one_step(std::integral_constant<int, 1>());
-    if (!advance()) break;
+    if (++step >= step_end) break;
     one_step(std::integral_constant<int, 2>());
-    advance();
+    ++step;
   }
 
   if (!there)  // (0 times what is not finite)
@@ -367,10 +383,17 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
     for (int i = 0; i < MB; ++i) extra[i] = (f32x16)(0.0f);
 #pragma unroll 1
     for (int st = step_begin; st < step_end; ++st) {
-      look(st);
-      wait_loads();
-      resolve(st);
-      uint32_t left = 0;  // rows with such values
+      const int j = min(st * kTile + col, n - 1);
+      uint32_t at = (uint32_t)j, left = 0;  // `left`: rows with such values
+      int32_t pos = a.positions ? pos_b[j] : placed && j >= past ? past + lds_depth[min(j - past, a.T - 1)] : j;
+      bool is = st * kTile + col < n && (!a.positions || pos >= 0);
+      if (a.page_size) {
+        const uint32_t p = page_of(j), page = (uint32_t)table[p];
+        is = is && page < (uint32_t)a.num_pages;
+        at = (page * a.Hkv + g) * a.page_size + ((uint32_t)j - p * a.page_size);
+      }
+      at = is ? at : 0;
+      const uint32_t seen = (uint32_t)__ballot(is);
 #pragma unroll 1
       for (int r0 = 0; r0 < kTile; r0 += ROWS_PER_LOAD) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(Vb + (uint64_t)(uint32_t)__shfl((int)at, r0 + lane / PIECES) * row_bytes + 16 * (lane % PIECES));
