@@ -23,7 +23,8 @@ __device__ __forceinline__ void word_to_lds(const int32_t* from, uint32_t to) {
 #pragma clang diagnostic pop
 
 constexpr int kBuffers = 3;  // of a step's keys and values
-constexpr int kSlots = 4;    // of what is known of a step: from three steps before it on
+constexpr int kSlots = 4;    // of what is known of a step: from two steps before it on
+constexpr int kAhead = 8;    // steps whose page numbers and positions are requested at a time
 
 // MODE 1: scores are capped or biased.
 template <int D, int MODE>
@@ -35,15 +36,17 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
   constexpr int ROW = D * 2, BUF = kTile * ROW;
   constexpr float SHIFT = Weight<T>::HALF ? kWideShift : 0.0f;
   __shared__ __align__(1024) char lds[kBuffers * 2 * BUF];  // [buffer][K, V]
-  __shared__ int32_t lds_depth[kMostDrafted];
-  __shared__ __align__(16) int32_t lds_pos[kSlots][kTile];   // [step % kSlots]: given positions
-  __shared__ __align__(16) int32_t lds_own_pos[4][kTile];    // [wave]: positions that are worked out
-  __shared__ int32_t lds_page[4][2][OWN];                    // [wave][step % 2]: pages of the rows that the wave fetches
-  __shared__ uint32_t lds_seen[kSlots];                      // [step % kSlots]: rows on pages that exist, a byte of each wave
+  __shared__ int16_t lds_depth[kMostDrafted];
+  __shared__ __align__(16) int32_t lds_pos[2][4][kAhead][OWN];  // [step / kAhead % 2][rows' wave][step % kAhead]: given positions
+  __shared__ __align__(16) int32_t lds_own_pos[MODE == 1 ? 4 : 1][kTile];  // [wave]: positions that are worked out
+  __shared__ int32_t lds_pages[4][2][kAhead * 4];               // [wave][step / kAhead % 2][step % kAhead, rows' wave]: pages of eight rows
+  __shared__ int32_t lds_page[4][2][OWN];                       // [wave][step % 2]: of each row that the wave fetches
+  __shared__ uint32_t lds_seen[kSlots];                         // [step % kSlots]: rows on pages that exist, a byte of each wave
   __shared__ int32_t lds_span[4][2];
   __shared__ int lds_zeroed;  // whether a value of V that is not finite was put to zero
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const uint32_t pos_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_pos;
+  const uint32_t pages_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_pages;
   const uint32_t page_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_page;
   const int lane = threadIdx.x & 63, wave = this_wave(), col = lane & 31, half = lane >> 5;
 
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
   int32_t p_row = 0;
   if (placed) {
     if (!a.q_pos) {
-      for (int i = threadIdx.x; i < a.T; i += 256) lds_depth[i] = ancestors(a, b, i, drafted);
+      for (int i = threadIdx.x; i < a.T; i += 256) lds_depth[i] = (int16_t)ancestors(a, b, i, drafted);
       __syncthreads();
     }
     p_row = a.q_pos ? a.q_pos[(int64_t)b * a.T + t] : past + lds_depth[t];
@@ -103,76 +106,98 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
   const int32_t* const table = a.table + (int64_t)b * a.max_pages;
   const int32_t* const pos_b = a.positions + b * a.p_sb + g * a.p_sh;
 
-  // Fetching a step: wave w rows 8 w .. 8 w + 7 of K and of V, a row's pieces swapped.  Their page numbers, and positions that are given,
-  // come through LDS like the rows themselves, a step before: were they loaded into registers, their first use would wait for all that
-  // has been requested since.  Eight rows in a row of a page, or of a compact cache, have one base; others are looked up one by one.
-  const bool even_rows = (a.page_size == 0 || a.page_size % OWN == 0) && row_bytes <= 1u << 26;
-  uint32_t at_k[LOADS], at_v[LOADS];
-#pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    const int r = i * ROWS_PER_LOAD + lane / PIECES, piece = lane % PIECES;
-    at_k[i] = r * row_bytes + 16 * (piece ^ swizzle_k<D>(OWN * wave + r));
-    at_v[i] = r * row_bytes + 16 * (piece ^ swizzle_v<D>(OWN * wave + r));
-  }
+  // Fetching a step: wave w rows 8 w .. 8 w + 7 of K and of V, a row's pieces swapped.  Page numbers, and positions that are given, come
+  // through LDS like the rows themselves, for eight steps at a time: were they loaded into registers, their first use would wait for all
+  // that has been requested since.  Eight rows in a row of a page, or of a compact cache, have one base; where pages end inside of eight
+  // rows, each row is looked up, a step at a time.  Rows behind the last one are taken as the last, those on pages that do not exist as
+  // the cache's first.
+  const bool odd_pages = a.page_size % OWN != 0;
   auto page_of = [&](int j) {
     uint32_t p = __umulhi((uint32_t)j, a.page_magic);
     if ((uint32_t)j - p * a.page_size >= (uint32_t)a.page_size) ++p;
     return p;
   };
-  auto look = [&](int st) {
-    if ((a.page_size || a.positions) && lane < OWN) {
-      const int j = min(st * kTile + OWN * wave + lane, n - 1);
-      if (a.page_size) word_to_lds(table + page_of(j), page_base + (wave * 2 + (st & 1)) * (OWN * 4));
-      if (a.positions) word_to_lds(pos_b + j, pos_base + ((st % kSlots) * kTile + OWN * wave) * 4);
+  auto look_ahead = [&](int block) {
+    const uint32_t slot = block & 1;
+    if (a.positions) {
+      const int j = min((block * kAhead + lane / OWN) * kTile + OWN * wave + lane % OWN, n - 1);
+      word_to_lds(pos_b + j, pos_base + (slot * 4 + wave) * (64 * 4));
+    }
+    if (a.page_size && !odd_pages && lane < kAhead * 4) {
+      const int j = min((block * kAhead + lane / 4) * kTile + OWN * (lane % 4), n - 1);
+      word_to_lds(table + page_of(j), pages_base + (wave * 2 + slot) * (kAhead * 4 * 4));
     }
   };
+  auto look = [&](int st) {
+    if (odd_pages && lane < OWN) word_to_lds(table + page_of(min(st * kTile + OWN * wave + lane, n - 1)), page_base + (wave * 2 + (st & 1)) * (OWN * 4));
+  };
+  int32_t pages = 0;       // of the block of steps that is fetched, lane 4 i + w: step i, wave w's rows
+  uint32_t pages_are = 0;  // which of them exist
+  auto take_pages = [&](int block) {
+    if (a.page_size && !odd_pages) {
+      pages = lds_pages[wave][block & 1][lane % (kAhead * 4)];
+      pages_are = (uint32_t)__ballot((uint32_t)pages < (uint32_t)a.num_pages);
+    }
+  };
+  // (returns which of the step's rows are on pages that exist, where pages do not end inside of eight)
   auto fetch = [&](int st, int buf) {
     const uint32_t to = lds_base + buf * 2 * BUF + OWN * wave * ROW;
-    const int j0 = st * kTile + OWN * wave;
-    uint32_t there8 = 0xFF;
-    if (even_rows && j0 + OWN <= n) {
-      uint64_t row0 = (uint64_t)(uint32_t)j0;
+    uint32_t is = ~0u;
+    int id = lane;
+    asm("" : "+v"(id));  // (what follows from it is not kept in registers, which are short)
+    if (!odd_pages) {
+      const int j0 = min(st * kTile + OWN * wave, (n - 1) / OWN * OWN), most = n - 1 - j0;
+      uint64_t row0 = (uint32_t)j0;
       if (a.page_size) {
-        const uint32_t slot = (uint32_t)j0 - page_of(j0) * a.page_size, page = (uint32_t)__builtin_amdgcn_readfirstlane(lds_page[wave][st & 1][0]);
-        const bool is = page < (uint32_t)a.num_pages;
-        there8 = is ? 0xFF : 0;
-        row0 = is ? (page * a.Hkv + g) * a.page_size + slot : 0;
+        const int at = st % kAhead * 4;
+        const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(pages, at + wave), own = pages_are >> at & 15;
+        is = (own & 1) * 0xFF | (own >> 1 & 1) * 0xFF00 | (own >> 2 & 1) * 0xFF0000 | (own >> 3) * 0xFF000000;
+        row0 = own >> wave & 1 ? (page * a.Hkv + g) * a.page_size + ((uint32_t)j0 - page_of(j0) * a.page_size) : 0;
       }
+      const char *const Kr = Kb + row0 * row_bytes, *const Vr = Vb + row0 * row_bytes;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
-        load_to_lds(Kb + row0 * row_bytes, at_k[i], to + i * 1024);
-        load_to_lds(Vb + row0 * row_bytes, at_v[i], to + i * 1024 + BUF);
-      }
-    } else {  // (rows behind the last one are taken as the last, those that are not there as the cache's first)
-      there8 = 0;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int r = i * ROWS_PER_LOAD + lane / PIECES, piece = lane % PIECES, j = min(j0 + r, n - 1);
-        uint32_t at = (uint32_t)j;
-        bool is = true;
-        if (a.page_size) {
-          const uint32_t page = (uint32_t)lds_page[wave][st & 1][r];
-          is = page < (uint32_t)a.num_pages;
-          at = is ? (page * a.Hkv + g) * a.page_size + ((uint32_t)j - page_of(j) * a.page_size) : 0;
+        const int r = i * ROWS_PER_LOAD + id / PIECES, piece = id % PIECES;
+        const uint32_t in_k = 16 * (piece ^ swizzle_k<D>(OWN * wave + r)), in_v = 16 * (piece ^ swizzle_v<D>(OWN * wave + r));
+        if (row_bytes <= 1u << 26) {
+          const uint32_t at = min(r, most) * row_bytes;
+          load_to_lds(Kr, at + in_k, to + i * 1024);
+          load_to_lds(Vr, at + in_v, to + i * 1024 + BUF);
+        } else {
+          const uint64_t at = (uint64_t)min(r, most) * row_bytes;
+          load_to_lds(Kr + at + in_k, to + i * 1024);
+          load_to_lds(Vr + at + in_v, to + i * 1024 + BUF);
         }
-        const uint64_t is64 = __ballot(is);
+      }
+    } else {
+      const int j0 = st * kTile + OWN * wave;
+      uint32_t there8 = 0;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int r = i * ROWS_PER_LOAD + id / PIECES, piece = id % PIECES, j = min(j0 + r, n - 1);
+        const uint32_t page = (uint32_t)lds_page[wave][st & 1][r];
+        const bool exists = page < (uint32_t)a.num_pages;
+        const uint64_t row = exists ? (page * a.Hkv + g) * a.page_size + ((uint32_t)j - page_of(j) * a.page_size) : 0;
+        const uint64_t is64 = __ballot(exists);
 #pragma unroll
         for (int x = 0; x < ROWS_PER_LOAD; ++x) there8 |= (uint32_t)(is64 >> (x * PIECES) & 1) << (i * ROWS_PER_LOAD + x);
-        load_to_lds(Kb + (uint64_t)at * row_bytes + 16 * (piece ^ swizzle_k<D>(OWN * wave + r)), to + i * 1024);
-        load_to_lds(Vb + (uint64_t)at * row_bytes + 16 * (piece ^ swizzle_v<D>(OWN * wave + r)), to + i * 1024 + BUF);
+        load_to_lds(Kb + row * row_bytes + 16 * (piece ^ swizzle_k<D>(OWN * wave + r)), to + i * 1024);
+        load_to_lds(Vb + row * row_bytes + 16 * (piece ^ swizzle_v<D>(OWN * wave + r)), to + i * 1024 + BUF);
       }
+      if (lane == 0) reinterpret_cast<uint8_t*>(&lds_seen[st % kSlots])[wave] = (uint8_t)there8;
     }
-    if (a.page_size && lane == 0) reinterpret_cast<uint8_t*>(&lds_seen[st % kSlots])[wave] = (uint8_t)there8;
+    return is;
   };
-  // Behind the barrier of the step before (by which all waves have made the step's fetch known): a step's rows that are there, one bit each, and the position of row l % 32.
-  auto rows_there = [&](int st, int32_t& pos) {
+  // Behind the barrier of the step before (by which all waves have made the step's fetch known): a step's rows that are there, one bit
+  // each, and the position of row l % 32.  `is`: what fetch returned.
+  auto rows_there = [&](int st, uint32_t is, int32_t& pos) {
     const int left = n - st * kTile;
-    uint32_t is = left >= kTile ? ~0u : (1u << left) - 1;
-    if (a.page_size) is &= (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_seen[st % kSlots]);
+    if (left < kTile) is &= (1u << left) - 1;
+    if (odd_pages) is &= (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_seen[st % kSlots]);
     const int j = st * kTile + col;
     pos = j;
     if (a.positions) {
-      pos = lds_pos[st % kSlots][col];
+      pos = lds_pos[st / kAhead & 1][col / OWN][st % kAhead][col % OWN];
       is &= (uint32_t)__ballot(pos >= 0);
     } else if (placed && st * kTile + kTile > past && j >= past) {
       pos = past + lds_depth[min(j - past, a.T - 1)];
@@ -205,13 +230,20 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
   };
 
   // Two steps are on their way while a third is worked on.
+  uint32_t is_now = 0, is_next = 0, is_then = 0;
   if (step < step_end) {
+    look_ahead(step / kAhead);
+    look_ahead(step / kAhead + 1);
     look(step);
     look(step + 1);
     wait_loads();
-    fetch(step, 0);
+    take_pages(step / kAhead);
+    is_now = fetch(step, 0);
     look(step + 2);
-    if (step + 1 < step_end) fetch(step + 1, 1);
+    if (step + 1 < step_end) {
+      if ((step + 1) % kAhead == 0) take_pages((step + 1) / kAhead);
+      is_next = fetch(step + 1, 1);
+    }
     lds_barrier();
   }
 
@@ -246,7 +278,7 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
     else
       wait_loads();
     int32_t pos_now;
-    const uint32_t now = rows_there(step, pos_now);
+    const uint32_t now = rows_there(step, is_now, pos_now);
     if (now != ~0u || !whole(step, now, pos_now, g_min, g_max)) {  // some row of the workgroup does not see all of the step
       // values of V that are not finite would spoil the product with a weight of 0: each wave those that it fetched
 #pragma unroll
@@ -276,9 +308,13 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
       }
     }
     if (step + 2 < step_end) {  // (beside the products)
+      if (step % kAhead == 0 && step != step_begin) look_ahead(step / kAhead + 1);
       look(step + 3);
-      fetch(step + 2, (buf + 2) % kBuffers);
+      if ((step + 2) % kAhead == 0) take_pages((step + 2) / kAhead);
+      is_then = fetch(step + 2, (buf + 2) % kBuffers);
     }
+    is_now = is_next;
+    is_next = is_then;
     if (!wave_there) return;
     if constexpr (MODE == 1) {
       if (a.cap.cap != 0.0f) {
@@ -297,10 +333,11 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
           if (lane < kTile) lds_own_pos[wave][lane] = pos_now;
           own_lds_order();
         }
-        const int32_t* const at = a.positions ? lds_pos[step % kSlots] : lds_own_pos[wave];
+        const int32_t* const at = a.positions ? lds_pos[step / kAhead & 1][0][step % kAhead] : lds_own_pos[wave];
+        const int next = a.positions ? kAhead * OWN : OWN;  // from one wave's rows to the next one's
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const u32x4 kp = *reinterpret_cast<const u32x4*>(&at[8 * x + 4 * half]);
+          const u32x4 kp = *reinterpret_cast<const u32x4*>(&at[x * next + 4 * half]);
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const uint32_t d = (uint32_t)p_row - kp[y];
