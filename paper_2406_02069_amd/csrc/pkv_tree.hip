@@ -140,12 +140,13 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
     }
   };
   // (returns which of the step's rows are on pages that exist, where pages do not end inside of eight)
-  auto fetch = [&](int st, int buf) {
+  auto fetch = [&](int st, int buf, auto plain) {
+    constexpr bool PLAIN = decltype(plain)::value;  // (known beforehand: neither odd pages nor wide rows)
     const uint32_t to = lds_base + buf * 2 * BUF + OWN * wave * ROW;
     uint32_t is = ~0u;
     int id = lane;
     asm("" : "+v"(id));  // (what follows from it is not kept in registers, which are short)
-    if (!odd_pages) {
+    if (PLAIN || !odd_pages) {
       const int j0 = min(st * kTile + OWN * wave, (n - 1) / OWN * OWN), most = n - 1 - j0;
       uint64_t row0 = (uint32_t)j0;
       if (a.page_size) {
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
       for (int i = 0; i < LOADS; ++i) {
         const int r = i * ROWS_PER_LOAD + id / PIECES, piece = id % PIECES;
         const uint32_t in_k = 16 * (piece ^ swizzle_k<D>(OWN * wave + r)), in_v = 16 * (piece ^ swizzle_v<D>(OWN * wave + r));
-        if (row_bytes <= 1u << 26) {
+        if (PLAIN || row_bytes <= 1u << 26) {
           const uint32_t at = min(r, most) * row_bytes;
           load_to_lds(Kr, at + in_k, to + i * 1024);
           load_to_lds(Vr, at + in_v, to + i * 1024 + BUF);
@@ -238,11 +239,11 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
     look(step + 1);
     wait_loads();
     take_pages(step / kAhead);
-    is_now = fetch(step, 0);
+    is_now = fetch(step, 0, std::false_type());
     look(step + 2);
     if (step + 1 < step_end) {
       if ((step + 1) % kAhead == 0) take_pages((step + 1) / kAhead);
-      is_next = fetch(step + 1, 1);
+      is_next = fetch(step + 1, 1, std::false_type());
     }
     lds_barrier();
   }
@@ -269,17 +270,19 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
   const int v_row = 4 * half + ((lane & 15) >> 2), v_piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
   const int v_at = v_row * ROW + ((v_piece ^ swizzle_v<D>(v_row)) << 4) + 8 * (lane & 1);
 
-  auto one_step = [&](auto buffer) {
+  // `inner`: the step lies in the past, rows are told apart by pages that do not exist at most, and fetch is plain.
+  auto one_step = [&](auto buffer, auto inner) {
     constexpr int buf = decltype(buffer)::value;
+    constexpr bool INNER = decltype(inner)::value;
     const char* const Kl = lds + buf * 2 * BUF;
     char* const Vl = lds + buf * 2 * BUF + BUF;
-    if (step + 1 < step_end)
-      wait_loads<2 * LOADS>();  // (those of the next step)
+    if (INNER || step + 1 < step_end)  // (the last of the inner steps has one behind it)
+      wait_loads<2 * LOADS>();         // (those of the next step)
     else
       wait_loads();
-    int32_t pos_now;
-    const uint32_t now = rows_there(step, is_now, pos_now);
-    if (now != ~0u || !whole(step, now, pos_now, g_min, g_max)) {  // some row of the workgroup does not see all of the step
+    int32_t pos_now = 0;
+    const uint32_t now = INNER ? is_now : rows_there(step, is_now, pos_now);
+    if (now != ~0u || (!INNER && !whole(step, now, pos_now, g_min, g_max))) {  // some row of the workgroup does not see all of the step
       // values of V that are not finite would spoil the product with a weight of 0: each wave those that it fetched
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
@@ -309,9 +312,9 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
     }
     if (step + 2 < step_end) {  // (beside the products)
       if (step % kAhead == 0 && step != step_begin) look_ahead(step / kAhead + 1);
-      look(step + 3);
+      if (!INNER) look(step + 3);
       if ((step + 2) % kAhead == 0) take_pages((step + 2) / kAhead);
-      is_then = fetch(step + 2, (buf + 2) % kBuffers);
+      is_then = fetch(step + 2, (buf + 2) % kBuffers, inner);
     }
     is_now = is_next;
     is_next = is_then;
@@ -328,7 +331,11 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[e] *= a.scale;
       }
-      if (a.slopes) {
+      if (INNER && a.slopes) {
+        const float far = (float)(p_row - step * kTile - 4 * half);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = fmaf(-slope, far - (float)key_of(e), sc[e]);
+      } else if (a.slopes) {
         if (!a.positions) {
           if (lane < kTile) lds_own_pos[wave][lane] = pos_now;
           own_lds_order();
@@ -347,8 +354,8 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
         own_lds_order();
       }
     }
-    if (now != ~0u || !whole(step, now, pos_now, w_min, w_max)) {
-      const uint32_t mine = visible(step, now, pos_now) >> (4 * half);
+    if (now != ~0u || (!INNER && !whole(step, now, pos_now, w_min, w_max))) {
+      const uint32_t mine = (INNER ? now : visible(step, now, pos_now)) >> (4 * half);
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (!(mine & (1u << key_of(e)))) sc[e] = kNone;
@@ -397,12 +404,22 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
       }
     }
   };
+  // The inner steps three at a time, so that the others begin with the first buffer again.
+  const int inner_end = a.positions || a.window || odd_pages || row_bytes > 1u << 26 ? step : min(step_end - 1, past / kTile);
+  while (step + 3 <= inner_end) {
+    one_step(std::integral_constant<int, 0>(), std::true_type());
+    ++step;
+    one_step(std::integral_constant<int, 1>(), std::true_type());
+    ++step;
+    one_step(std::integral_constant<int, 2>(), std::true_type());
+    ++step;
+  }
   while (step < step_end) {
-    one_step(std::integral_constant<int, 0>());
+    one_step(std::integral_constant<int, 0>(), std::false_type());
     if (++step >= step_end) break;
-    one_step(std::integral_constant<int, 1>());
+    one_step(std::integral_constant<int, 1>(), std::false_type());
     if (++step >= step_end) break;
-    one_step(std::integral_constant<int, 2>());
+    one_step(std::integral_constant<int, 2>(), std::false_type());
     ++step;
   }
 
