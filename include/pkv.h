@@ -748,7 +748,7 @@ int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q,
  * token's count_b - new_b + the number of drafted tokens that it sees besides
  * itself.  Rows t >= new_b, and rows that see nothing: zero and -inf.
  * Scores, softmax and lse as pkv_decode_attention_long has them, the softmax
- * weights' rounding too, or, where T * Hq/Hkv > 64, as pkv_prefill_attention
+ * weights' rounding too, or, where T * Hq/Hkv > 32, as pkv_prefill_attention
  * has it.  A key that a token does not see has no influence on its row beyond
  * rounding, whatever it holds; where a token sees values of V that are not
  * finite, that element of out is their sum.  A page number out of range makes

@@ -27,10 +27,10 @@ constexpr int kSlots = 4;    // of what is known of a step: from two steps befor
 constexpr int kAhead = 8;    // steps whose page numbers and positions are requested at a time
 
 // MODE 1: scores are capped or biased.
-template <int D, int MODE>
-constexpr int wide_per_unit() { return D == 128 && MODE == 1 ? 2 : 3; }  // workgroups of a compute unit
+template <int D>
+constexpr int wide_per_unit() { return D == 128 ? 2 : 3; }  // workgroups of a compute unit
 template <typename T, int D, int MODE>
-__global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_kernel(const TreeWideArgs a) {
+__global__ __launch_bounds__(256, (wide_per_unit<D>())) void tree_wide_kernel(const TreeWideArgs a) {
   constexpr int STEPS = D / 16, MB = D / 32, PIECES = D / 8, ROWS_PER_LOAD = 64 / PIECES, ROWS = group_rows<TreeWideArgs>();
   constexpr int OWN = kTile / 4, LOADS = OWN / ROWS_PER_LOAD;  // rows of a step that a wave fetches, loads of K (and of V) for them
   constexpr int ROW = D * 2, BUF = kTile * ROW;
@@ -282,7 +282,8 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
       wait_loads();
     int32_t pos_now = 0;
     const uint32_t now = INNER ? is_now : rows_there(step, is_now, pos_now);
-    if (now != ~0u || (!INNER && !whole(step, now, pos_now, g_min, g_max))) {  // some row of the workgroup does not see all of the step
+    const bool all = now == ~0u && (INNER || whole(step, now, pos_now, g_min, g_max));  // every row of the workgroup sees all of the step
+    if (!all) {
       // values of V that are not finite would spoil the product with a weight of 0: each wave those that it fetched
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
@@ -345,16 +346,21 @@ __global__ __launch_bounds__(256, (wide_per_unit<D, MODE>())) void tree_wide_ker
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const u32x4 kp = *reinterpret_cast<const u32x4*>(&at[x * next + 4 * half]);
+          if (all) {  // (positions up to the row's own)
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const uint32_t d = (uint32_t)p_row - kp[y];
-            sc[4 * x + y] = fmaf(-slope, (float)((int32_t)kp[y] > p_row ? 0u - d : d), sc[4 * x + y]);
+            for (int y = 0; y < 4; ++y) sc[4 * x + y] = fmaf(-slope, (float)((uint32_t)p_row - kp[y]), sc[4 * x + y]);
+          } else {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const uint32_t d = (uint32_t)p_row - kp[y];
+              sc[4 * x + y] = fmaf(-slope, (float)((int32_t)kp[y] > p_row ? 0u - d : d), sc[4 * x + y]);
+            }
           }
         }
         own_lds_order();
       }
     }
-    if (now != ~0u || (!INNER && !whole(step, now, pos_now, w_min, w_max))) {
+    if (!all && (now != ~0u || !whole(step, now, pos_now, w_min, w_max))) {
       const uint32_t mine = (INNER ? now : visible(step, now, pos_now)) >> (4 * half);
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -525,11 +531,12 @@ hipError_t launch_wide(const TreeWideArgs& a, int64_t workgroups, hipStream_t s)
   return e != hipSuccess || a.ranges == 0 ? e : launch_join<T, D>(a, s);
 }
 
-// More than 64 query rows a KV head: the kernel above.
-bool wide(const pkv_tree_desc& d) { return (int64_t)d.T * (d.Hq / d.Hkv) > 64; }
+// More than kFewRows query rows a KV head: the kernel above.
+constexpr int kFewRows = 32;
+bool wide(const pkv_tree_desc& d) { return (int64_t)d.T * (d.Hq / d.Hkv) > kFewRows; }
 
 // As grid_of of pkv_long.h, in workgroups of 128 rows, of which the device holds three per compute unit.
-int wide_turn(const pkv_tree_desc& d, bool biased) { return 256 * (d.d == 128 && (d.cap > 0.0f || biased) ? 2 : 3); }
+int wide_turn(const pkv_tree_desc& d) { return d.d == 128 ? 512 : 768; }
 Grid wide_grid(const pkv_tree_desc& d, int turn) {
   constexpr int ROWS = group_rows<TreeWideArgs>();
   const int64_t units = d.Hkv * (((int64_t)d.T * (d.Hq / d.Hkv) + ROWS - 1) / ROWS), all = d.B * units;
@@ -584,10 +591,7 @@ int pkv_tree_bits(int32_t T, const int32_t* parents, int32_t* bits_out) {
 
 size_t pkv_tree_workspace_bytes(const pkv_tree_desc* desc) {
   if (check_tree_desc(desc) != PKV_OK) return 0;
-  if (wide(*desc)) {  // (with slopes or without)
-    const size_t plain = wide_bytes(wide_grid(*desc, wide_turn(*desc, false)), desc->d), biased = wide_bytes(wide_grid(*desc, wide_turn(*desc, true)), desc->d);
-    return plain > biased ? plain : biased;
-  }
+  if (wide(*desc)) return wide_bytes(wide_grid(*desc, wide_turn(*desc)), desc->d);
   return parts_bytes(grid_of(*desc), desc->T * (desc->Hq / desc->Hkv), desc->d);
 }
 
@@ -609,7 +613,7 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q, const void* K_c
   TreeWideArgs a;
   memset(&a, 0, sizeof(a));
   const bool many = wide(d);
-  const Grid grid = many ? wide_grid(d, wide_turn(d, slopes)) : grid_of(d);
+  const Grid grid = many ? wide_grid(d, wide_turn(d)) : grid_of(d);
   fill_long(a, d, grid, d.T * (d.Hq / d.Hkv), q, K_cache, V_cache, out, workspace);
   a.table = block_table; a.count = count; a.positions = positions; a.q_pos = q_pos; a.slopes = slopes;
   a.new_lens = new_lens; a.tree = tree;
@@ -624,7 +628,7 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q, const void* K_c
     e = launch_long(static_cast<const TreeArgs&>(a), d.dtype, d.d, grid.workgroups, st);
   } else {
     constexpr int ROWS = group_rows<TreeWideArgs>();
-    a.turn = wide_turn(d, slopes);
+    a.turn = wide_turn(d);
     a.head_groups = (a.G + ROWS - 1) / ROWS;
     a.units = a.Hkv * a.head_groups;
     a.part_mz = a.part_o ? a.part_o + (size_t)grid.workgroups * ROWS * d.d : nullptr;

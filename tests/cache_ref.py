@@ -8,7 +8,7 @@ from tests import attention_bounds
 from tests.attention_bounds import HALF_STEP
 
 DEV = "cuda:0"
-# Rounding of a weight for the product with V: to two numbers of the type (up to 64 query rows a KV head), else once.
+# Rounding of a weight for the product with V: to two numbers of the type (up to 32 query rows a KV head), else once.
 TOKEN = {t: h * h for t, h in HALF_STEP.items()}
 TOKEN_SMALL = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -38}
 PROMPT = HALF_STEP
@@ -85,7 +85,7 @@ def check_rows(out, lse, q, K, V, seen, dist, scale, dtype, cap=0.0, slope=None,
     any_seen = seen.any(0)
     Kf, Vf = K.clone(), Vf.clone()
     Kf[~any_seen] = 0
-    token = rows <= 64
+    token = rows <= 32
     want = attention_bounds.attend(q, Kf, Vf, seen, dist, scale, dtype, cap, slope, (TOKEN if token else PROMPT)[dtype],
                                    (TOKEN_SMALL if token else PROMPT_SMALL)[dtype])
     special = odd != 0
