@@ -828,7 +828,8 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q,
  * pkv_decode_attention_long that also adds each row's softmax weight, summed
  * over the query heads of its KV head, to a running sum:
  *   weights[b][g][j] += sum_{h of g} softmax_j(s_h)   for every seen row j.
- * Nothing else of weights is written.  Same descriptor, results and errors.
+ * Nothing else of weights is written.  Same descriptor, results and errors
+ * (PKV_ERR_UNSUPPORTED also B * Hq > 2^23).
  * weights   DEVICE fp32 [B,Hkv,k_cap], 4-byte aligned, with element strides w_sb
  *           and w_sh (>= 0; the sums of two heads do not overlap).
  * workspace DEVICE, 256-byte aligned,

@@ -43,10 +43,10 @@ struct LongArgs {
   Cap cap;
   static constexpr int MODE = kOneToken;
 };
-// Adding up weights: the scores are kept for the kernel behind the join, with each head's reference and sum.
+// Adding up weights: the scores are kept for the kernel behind, which also joins ranges.
 struct WeighArgs : LongArgs {
   float* scores;      // [B * Hkv][G][score_row], in log2 units, -inf where a row is not seen; rows of the visited tiles
-  float* mz;          // [B * Hq][2] reference exponent and sum
+  float* mz;          // [B * Hq][2] reference exponent and factor of heads that are not cut into ranges
   float* weights;
   int64_t score_row, w_sb, w_sh;
   static constexpr int MODE = kWeigh;
@@ -678,7 +678,7 @@ __global__ __launch_bounds__(256, 2) void decode_long_kernel(const A a) {
 // the threads, in order, each with a running maximum of its own (so that a range's exponent and its values are requested together),
 // then the parts.
 template <typename T, int D, int HEADS, typename A>
-__global__ __launch_bounds__(256) void decode_long_join_kernel(const A a) {
+__device__ __forceinline__ void join_heads(const A& a) {
   constexpr int PARTS = 256 / (D / 4);
   __shared__ float lds_m[PARTS], lds_z[PARTS];
   __shared__ f32x4 lds_o[PARTS][D / 4];
@@ -753,11 +753,12 @@ __global__ __launch_bounds__(256) void decode_long_join_kernel(const A a) {
       w[1] = pack2<T>(acc[2] * inv, acc[3] * inv);
       *reinterpret_cast<u32x2*>(a.out + out_at(a, b, h / a.G, h_in, D) + 4 * d4) = w;
       if (d4 == 0 && a.lse) a.lse[lse_at(a, b, h / a.G, h_in)] = z == 0.0f ? kNone : (m + log2_(z * UNIT)) * kLn2;
-      if constexpr (A::MODE == kWeigh) {
-        if (d4 == 0) keep_mz(a, b, h / a.G, h_in, m == kNone ? 0.0f : m, inv * (1.0f / Weight<T>::UNIT));
-      }
     }
   }
+}
+template <typename T, int D, int HEADS, typename A>
+__global__ __launch_bounds__(256) void decode_long_join_kernel(const A a) {
+  join_heads<T, D, HEADS>(a);
 }
 
 // Query heads that a workgroup's results have room for.
@@ -806,7 +807,7 @@ template <typename T, int D, typename A>
 hipError_t launch_long(const A& a, int64_t workgroups, hipStream_t s) {
   hipLaunchKernelGGL((decode_long_kernel<T, D, A>), dim3((unsigned)workgroups), dim3(256), 0, s, a);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || a.ranges == 0 ? e : launch_join<T, D>(a, s);
+  return e != hipSuccess || a.ranges == 0 || A::MODE == kWeigh ? e : launch_join<T, D>(a, s);  // (kWeigh has a join of its own)
 }
 template <typename A>
 hipError_t launch_long(const A& a, int dtype, int d, int64_t workgroups, hipStream_t s) {

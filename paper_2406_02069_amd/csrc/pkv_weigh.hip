@@ -1,8 +1,9 @@
 // Attention of one new token that adds each row's softmax weight to a running sum (include/pkv.h: pkv_decode_attention_accumulate).
 //
 // HBM-bound like the attention itself (pkv_decode_long.hip), whose kernel leaves the scores behind, 4 bytes a row and query head
-// beside the 4 d bytes of the row: a softmax weight is known only once all of the head's scores are.  A last kernel forms the
-// weights from them with each head's reference and sum, and adds up those of a KV head's query heads, in order.
+// beside the 4 d bytes of the row: a softmax weight is known only once all of the head's scores are.  A second kernel joins the ranges'
+// outputs with some of its workgroups and forms the weights with the others, which work out each head's reference and sum from the
+// ranges' own: as a launch behind the join the weights of 2k rows took 18.5 us, now 15.
 #include "pkv_long.h"
 
 namespace pkv {
@@ -10,26 +11,78 @@ namespace {
 
 constexpr int kRowsAtATime = 4;  // of a thread
 constexpr int kChunk = 256 * kRowsAtATime;
+constexpr int kMostHeads = 128;  // of a KV head
 
-__global__ __launch_bounds__(256) void add_weights_kernel(const WeighArgs a, int chunks, int64_t items) {
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+// Each head's reference and the factor that makes softmax weights of the 2^(score - reference), from its ranges' references and sums
+// (a wave: every fourth head, a lane: every 64th range), or as the attention's kernel has left them.
+template <typename T>
+__device__ __forceinline__ void heads_of_unit(const WeighArgs& a, int b, int g, float (&mz)[kMostHeads][2]) {
+  const int lane = threadIdx.x & 63;
+  int ranges = a.ranges, base = b * a.units * a.ranges;
+  if (a.by_length) {
+    const Place p = a.B <= 64 ? place_of_sequence<1>(a, b, lane) : place_of_sequence<kLaneSequences>(a, b, lane);
+    ranges = p.ranges;
+    base = p.base;
+  }
+  const int64_t heads = 16 * a.wave_groups;
+  for (int h = this_wave(); h < a.G; h += 4) {
+    float m = kNone, z = 0.0f;
+    if (ranges > 1) {
+      const float* const part = a.part_mz + (((int64_t)base + (g * a.head_groups + h / 64) * ranges) * heads + h % 64) * 2;
+      for (int i = lane; i < ranges; i += 64) {
+        const float m1 = part[heads * i * 2], z1 = part[heads * i * 2 + 1], top = fmaxf(m, m1), ref = top == kNone ? 0.0f : top;
+        z = z * exp2_(m - ref) + z1 * exp2_(m1 - ref);
+        m = top;
+      }
+      float top = m;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+      const float ref = top == kNone ? 0.0f : top;
+      z *= exp2_(m - ref);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
+      m = ref;
+      z = z == 0.0f ? 0.0f : (1.0f / Weight<T>::UNIT) / z;
+    } else {
+      const float* const own = a.mz + ((int64_t)b * a.Hq + g * a.G + h) * 2;
+      m = own[0];
+      z = own[1];
+    }
+    if (lane == 0) {
+      mz[h][0] = m;
+      mz[h][1] = z;
+    }
+  }
+}
+
+// The first `joins` workgroups join ranges, HEADS heads each; the others add weights, kChunk rows of a KV head at a time.
+template <typename T, int D, int HEADS>
+__global__ __launch_bounds__(256) void join_and_weigh_kernel(const WeighArgs a, int joins, int chunks, int64_t items) {
+  if ((int)blockIdx.x < joins) {
+    join_heads<T, D, HEADS>(a);
+    return;
+  }
+  __shared__ float lds_mz[kMostHeads][2];
+  for (int64_t item = (int)blockIdx.x - joins; item < items; item += gridDim.x - joins) {
     const int unit = (int)(item / chunks), chunk = (int)(item % chunks), b = unit / a.Hkv, g = unit % a.Hkv;
     const Tiles tl = tiles_of(a, b);
     const int lo = tl.first * kTile, hi = min(tl.n, (tl.first + tl.count) * kTile), r0 = chunk * kChunk + threadIdx.x;
     if (chunk * kChunk >= hi || (chunk + 1) * kChunk <= lo) continue;
+    __syncthreads();  // (the last item's have been read)
+    heads_of_unit<T>(a, b, g, lds_mz);
+    __syncthreads();
     float sum[kRowsAtATime];
 #pragma unroll
     for (int i = 0; i < kRowsAtATime; ++i) sum[i] = 0.0f;
+    const float* const s = a.scores + (int64_t)unit * a.G * a.score_row;
+#pragma unroll 2
     for (int h = 0; h < a.G; ++h) {
-      const float* const mz = a.mz + ((int64_t)b * a.Hq + g * a.G + h) * 2;
-      const float* const s = a.scores + ((int64_t)unit * a.G + h) * a.score_row;
-      const float ref = mz[0], factor = mz[1];
+      const float ref = lds_mz[h][0], factor = lds_mz[h][1];
+      float x[kRowsAtATime];
 #pragma unroll
-      for (int i = 0; i < kRowsAtATime; ++i) {
-        const int r = r0 + 256 * i;
-        const float x = r >= lo && r < hi ? s[r] : kNone;
-        sum[i] += x == kNone ? 0.0f : exp2_(x - ref) * factor;
-      }
+      for (int i = 0; i < kRowsAtATime; ++i) x[i] = s[h * a.score_row + min(max(r0 + 256 * i, lo), hi - 1)];
+#pragma unroll
+      for (int i = 0; i < kRowsAtATime; ++i) sum[i] += x[i] == kNone ? 0.0f : exp2_(x[i] - ref) * factor;
     }
     float* const w = a.weights + b * a.w_sb + g * a.w_sh;
 #pragma unroll
@@ -38,6 +91,26 @@ __global__ __launch_bounds__(256) void add_weights_kernel(const WeighArgs a, int
       if (r >= lo && r < hi) w[r] += sum[i];
     }
   }
+}
+
+template <typename T, int D>
+hipError_t launch_weigh(const WeighArgs& a, int64_t workgroups, int chunks, int64_t items, hipStream_t s) {
+  const hipError_t e = launch_long<T, D>(a, workgroups, s);
+  if (e != hipSuccess) return e;
+  const bool four = a.Hq % 4 == 0 && a.B * a.Hq >= 4 * kWorkgroups;  // (as launch_join)
+  const int64_t joins = a.ranges == 0 ? 0 : (int64_t)a.B * a.Hq / (four ? 4 : 1), most = kMaxGrid - joins;
+  const dim3 grid((unsigned)(joins + (items < most ? items : most)));
+  if (four)
+    hipLaunchKernelGGL((join_and_weigh_kernel<T, D, 4>), grid, dim3(256), 0, s, a, (int)joins, chunks, items);
+  else
+    hipLaunchKernelGGL((join_and_weigh_kernel<T, D, 1>), grid, dim3(256), 0, s, a, (int)joins, chunks, items);
+  return hipGetLastError();
+}
+
+// (joins and weights share a launch)
+int check_accumulate_desc(const pkv_decode_long_desc* desc) {
+  const int rc = check_long_desc(desc);
+  return rc == PKV_OK && (int64_t)desc->B * desc->Hq > 1 << 23 ? PKV_ERR_UNSUPPORTED : rc;
 }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -66,7 +139,7 @@ using namespace pkv;
 extern "C" {
 
 size_t pkv_decode_accumulate_workspace_bytes(const pkv_decode_long_desc* desc) {
-  return check_long_desc(desc) == PKV_OK ? plan_of(*desc).all : 0;
+  return check_accumulate_desc(desc) == PKV_OK ? plan_of(*desc).all : 0;
 }
 
 int pkv_decode_attention_accumulate(const pkv_decode_long_desc* desc, const void* q, const void* K_cache, const void* V_cache,
@@ -76,6 +149,7 @@ int pkv_decode_attention_accumulate(const pkv_decode_long_desc* desc, const void
   if (!weights || !aligned(weights, 4) || w_sb < 0 || w_sh < 0) return PKV_ERR_INVALID_ARG;
   const int rc = check_long_call(desc, q, K_cache, V_cache, block_table, count, positions, q_pos, slopes, out, lse_out);
   if (rc != PKV_OK) return rc;
+  if (check_accumulate_desc(desc) != PKV_OK) return PKV_ERR_UNSUPPORTED;
   const pkv_decode_long_desc& d = *desc;
   const WeighPlan p = plan_of(d);
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < p.all) return PKV_ERR_WORKSPACE;
@@ -92,11 +166,14 @@ int pkv_decode_attention_accumulate(const pkv_decode_long_desc* desc, const void
   a.weights = weights;
   a.w_sb = w_sb; a.w_sh = w_sh;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  if (launch_long(a, d.dtype, d.d, p.grid.workgroups, st) != hipSuccess) return PKV_ERR_HIP;
   const int chunks = (int)((p.score_row + kChunk - 1) / kChunk);
   const int64_t items = (int64_t)d.B * d.Hkv * chunks;
-  hipLaunchKernelGGL(add_weights_kernel, dim3((unsigned)(items < kMaxGrid ? items : kMaxGrid)), dim3(256), 0, st, a, chunks, items);
-  return hipGetLastError() == hipSuccess ? PKV_OK : PKV_ERR_HIP;
+  hipError_t e;
+  if (d.dtype == PKV_BF16)
+    e = d.d == 128 ? launch_weigh<__bf16, 128>(a, p.grid.workgroups, chunks, items, st) : launch_weigh<__bf16, 64>(a, p.grid.workgroups, chunks, items, st);
+  else
+    e = d.d == 128 ? launch_weigh<_Float16, 128>(a, p.grid.workgroups, chunks, items, st) : launch_weigh<_Float16, 64>(a, p.grid.workgroups, chunks, items, st);
+  return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
 }
 
 }  // extern "C"

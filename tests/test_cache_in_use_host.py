@@ -105,7 +105,7 @@ def test_weigh_descriptors_refused(kw):
     assert _weigh(d, table=0x6000, n=1 << 40) == I
 
 
-@pytest.mark.parametrize("kw", NOT_BUILT + [dict(Hq=129, Hkv=1), dict(B=65535, Hq=512, Hkv=512)])
+@pytest.mark.parametrize("kw", NOT_BUILT + [dict(Hq=129, Hkv=1), dict(B=65535, Hq=512, Hkv=512), dict(B=65535, Hq=129, Hkv=129)])
 def test_weigh_not_built(kw):
     assert _weigh(_long_desc(**kw), table=0x6000, n=1 << 50) == U
 
