@@ -134,13 +134,19 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, in
   if ((int64_t)(blockIdx.x % chunks) * 4 * OWN >= have) return;
   int blk0 = (int)(blockIdx.x % chunks * 4 + wave) * OWN;
   const uint16_t* const from = a.bounds + b * a.b_sb + g * a.b_sh + 8 * piece;
-  u32x4 v[kLoads];
-  auto load = [&](int blk) {
+  u32x4 v[kLoads], w[kLoads];
+  auto load = [&](int blk, u32x4 (&v)[kLoads]) {
+    if (blk + OWN <= have) {
+      const uint16_t* const first = from + (int64_t)(blk + lane / LANES) * (2 * D);
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) v[k] = *reinterpret_cast<const u32x4*>(first + k * AT_ONCE * 2 * D);
+      return;
+    }
 #pragma unroll
     for (int k = 0; k < kLoads; ++k)
       v[k] = *reinterpret_cast<const u32x4*>(from + (int64_t)min(blk + k * AT_ONCE + lane / LANES, have - 1) * (2 * D));
   };
-  load(blk0);
+  load(min(blk0, have - 1), v);
   // the heads' coefficients, a thread each: of the least values first
   static_assert(2 * D <= 256, "a thread for each coefficient");
   if (threadIdx.x < 2 * D) {
@@ -163,6 +169,8 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, in
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = coefficients[8 * piece + i];
   while (blk0 < have) {
+    const int next = blk0 + chunks * 4 * OWN;  // (blocks are 2^26 at most, a turn of all chunks 2^17)
+    if (next < have) load(next, w);
     double s[kLoads];
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
@@ -170,14 +178,17 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, in
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[k] = __builtin_fma(f[i], (double)unpack<T>(v[k][i >> 1], i & 1), s[k]);
     }
-    const int next = blk0 + chunks * 4 * OWN;  // (blocks are 2^26 at most, a turn of all chunks 2^17)
-    if (next < have) load(next);
+    static_assert(kLoads == 8, "three halvings");
 #pragma unroll
-    for (int half = kLoads / 2, o = 1; half > 0; half >>= 1, o <<= 1) {
+    for (int i = 0; i < 3; ++i) {
 #pragma unroll
-      for (int k = 0; k < half; ++k) {
-        const double keep = lane & o ? s[k + half] : s[k], give = lane & o ? s[k] : s[k + half];
-        s[k] = keep + __shfl_xor(give, o);
+      for (int k = 0; k < kLoads / 2; ++k) {
+        const int half = kLoads >> (i + 1), o = 1 << i;
+        if (k < half) {
+          const bool upper = lane & o;
+          const double x = s[k], y = s[k + half], keep = upper ? y : x, give = upper ? x : y;
+          s[k] = keep + __shfl_xor(give, o);
+        }
       }
     }
 #pragma unroll
@@ -188,6 +199,8 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, in
       const float x = (float)s[0];
       a.scores[(int64_t)unit * a.all + blk] = x == x ? x : __builtin_inff();
     }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) v[k] = w[k];
     blk0 = next;
   }
 }
@@ -290,9 +303,8 @@ Grid grid_of(const pkv_block_desc& d) {
 // Workgroups of `per` blocks each for every head: as many as a cache's blocks need, but in all no more than the device holds at a time.
 // Most of the blocks of a large cache are not there, or not asked for, and a workgroup that finds nothing to do still has to be started:
 // the bounds of one new row of 4 x 8 heads with room for 128k rows take 31 us in 65536 workgroups.
-constexpr int kAtATime = 2048;
-int chunks_of(int64_t blocks, int per, int64_t units) {
-  const int64_t chunks = (blocks + per - 1) / per, most = (kAtATime + units - 1) / units;
+int chunks_of(int64_t blocks, int per, int64_t units, int at_a_time) {
+  const int64_t chunks = (blocks + per - 1) / per, most = (at_a_time + units - 1) / units;
   return (int)(chunks < most ? chunks : most);
 }
 
@@ -322,7 +334,7 @@ int pkv_block_bounds(const pkv_block_desc* desc, const void* K_cache, const int3
   a.page_magic = magic_of(d.page_size);
   a.c_sb = d.c_sb; a.c_sh = d.c_sh; a.c_st = d.c_st; a.b_sb = d.b_sb; a.b_sh = d.b_sh;
   const int64_t units = (int64_t)d.B * d.Hkv;
-  const int chunks = chunks_of(blocks_of(d), 4, units);
+  const int chunks = chunks_of(blocks_of(d), 4, units, 2048);
   const dim3 grid((unsigned)(units * chunks)), block(256);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   if (d.dtype == PKV_BF16) {
@@ -361,7 +373,7 @@ int pkv_block_select(const pkv_block_desc* desc, const void* q, const void* boun
   if (grant_keys(reinterpret_cast<const void*>(block_list_kernel), granted) != hipSuccess) return PKV_ERR_HIP;
   const int64_t units = (int64_t)d.B * d.Hkv;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const int chunks = chunks_of(a.all, 4 * (d.d == 128 ? blocks_of_wave<128>() : blocks_of_wave<64>()), units);
+  const int chunks = chunks_of(a.all, 4 * (d.d == 128 ? blocks_of_wave<128>() : blocks_of_wave<64>()), units, 1024);
   const dim3 grid((unsigned)(units * chunks)), block(256);
   if (d.dtype == PKV_BF16) {
     if (d.d == 128) hipLaunchKernelGGL((block_score_kernel<__bf16, 128>), grid, block, 0, st, a, chunks);
