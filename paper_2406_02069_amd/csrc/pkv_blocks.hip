@@ -206,10 +206,10 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, in
 }
 
 template <typename KeyAt>
-__device__ __forceinline__ void list_blocks(const SelectArgs& a, int unit, int have, KeyAt key_at, SelectLds& lds) {
+__device__ __forceinline__ void list_blocks(const SelectArgs& a, int unit, int have, KeyAt key_at, const Met& met, SelectLds& lds) {
   int32_t* const out = a.blocks + (int64_t)unit * a.most;
   const Keys<KeyAt> keys(have, key_at);
-  const Cutoff cut = cutoff_of(keys, a.most, lds);
+  const Cutoff cut = cutoff_of(keys, met, a.most, lds);
   const int equal0 = equal_before(keys, cut, lds);
   int equal = equal0, taken = 0;
   keys.each([&](int, const uint32_t(&key)[kBatch]) {
@@ -242,8 +242,9 @@ __global__ __launch_bounds__(kThreads) void block_list_kernel(const SelectArgs a
   const float* const score = a.scores + (int64_t)unit * a.all;
   auto key_at = [&](int k) {
     const uint32_t key = key_of_float(score[min(k, have - 1)]);
-    return k >= have ? 0u : k < a.first || k >= have - a.recent ? 0xFFFFFFFFu : key;
+    return k >= have ? 0u : k < a.first || k >= have - a.recent ? kTop : key;
   };
+  Met met;
   if (have <= a.most) {
     for (int i = threadIdx.x; i < a.most; i += kThreads) a.blocks[(int64_t)unit * a.most + i] = i < have ? i : -1;
   } else if (have <= a.in_lds) {
@@ -252,11 +253,18 @@ __global__ __launch_bounds__(kThreads) void block_list_kernel(const SelectArgs a
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) key[i] = key_at(k0 + (int)threadIdx.x + i * kThreads);
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) kept[k0 + (int)threadIdx.x + i * kThreads] = key[i];
+      for (int i = 0; i < kBatch; ++i) {
+        met.meet(key[i]);
+        kept[k0 + (int)threadIdx.x + i * kThreads] = key[i];
+      }
     }
-    list_blocks(a, unit, have, [&](int k) { return kept[k]; }, lds);  // (its first barrier comes before the first look-up)
+    list_blocks(a, unit, have, [&](int k) { return kept[k]; }, met, lds);  // (its first barrier comes before the first look-up)
   } else {
-    list_blocks(a, unit, have, key_at, lds);
+    for (int k0 = 0; k0 < have; k0 += kRun) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) met.meet(key_at(k0 + (int)threadIdx.x + i * kThreads));
+    }
+    list_blocks(a, unit, have, key_at, met, lds);
   }
 }
 

@@ -92,7 +92,7 @@ __device__ __forceinline__ void finish(const EvictArgs& a, const Unit& u, int la
 
 // A row's key: rows that are not there 1, weights that are NaN 2, protected rows the greatest (0: no row).
 __device__ __forceinline__ uint32_t row_key(const EvictArgs& a, int32_t p, float w, int newest) {
-  return p < 0 ? 1u : p < a.first || p > newest - a.recent ? 0xFFFFFFFFu : w == w ? key_of_float(w) : 2u;
+  return p < 0 ? 1u : p < a.first || p > newest - a.recent ? kTop : w == w ? key_of_float(w) : 2u;
 }
 __device__ __forceinline__ int newest_of_all(int newest, SelectLds& lds) {
   newest = wave_max(newest);
@@ -105,9 +105,9 @@ __device__ __forceinline__ int newest_of_all(int newest, SelectLds& lds) {
 
 // The pairs of a head, by the keys that key_at looks up.
 template <typename KeyAt>
-__device__ __forceinline__ void pair_rows(const EvictArgs& a, const Unit& u, KeyAt key_at, SelectLds& lds) {
+__device__ __forceinline__ void pair_rows(const EvictArgs& a, const Unit& u, KeyAt key_at, const Met& met, SelectLds& lds) {
   const Keys<KeyAt> keys(u.n, key_at);
-  const Cutoff cut = cutoff_of(keys, a.budget, lds);
+  const Cutoff cut = cutoff_of(keys, met, a.budget, lds);
   const int equal0 = equal_before(keys, cut, lds);
   int equal = equal0, holes = 0, late = 0;
   const int lane = threadIdx.x & 63;
@@ -176,18 +176,21 @@ __device__ __forceinline__ void evict_rows(const EvictArgs& a, const Unit& u, ui
     }
   }
   newest = newest_of_all(newest, lds);
+  Met met;
 #pragma unroll
   for (int i0 = 0; i0 < MOST; i0 += kBatch) {
     if (i0 * kThreads < u.n) {
 #pragma unroll
       for (int i = i0; i < i0 + kBatch; ++i) {
         const int r = (int)threadIdx.x + i * kThreads;
-        kept[r] = r < u.n ? row_key(a, p[i], w[i], newest) : 0u;
+        const uint32_t key = r < u.n ? row_key(a, p[i], w[i], newest) : 0u;
+        met.meet(key);
+        kept[r] = key;
         if (r < u.n) keep_row(a, u, r, p[i], w[i]);
       }
     }
   }
-  pair_rows(a, u, [&](int r) { return kept[r]; }, lds);  // (its first barrier comes before the first look-up)
+  pair_rows(a, u, [&](int r) { return kept[r]; }, met, lds);  // (its first barrier comes before the first look-up)
 }
 __device__ __forceinline__ void evict_rows_of_memory(const EvictArgs& a, const Unit& u, SelectLds& lds) {
   int newest = -1;
@@ -202,7 +205,12 @@ __device__ __forceinline__ void evict_rows_of_memory(const EvictArgs& a, const U
   };
   if (u.pos_out != u.pos || u.weight_out != u.weight)
     for (int r = threadIdx.x; r < u.n; r += kThreads) keep_row(a, u, r, u.pos[r], u.weight[r]);
-  pair_rows(a, u, key_at, lds);
+  Met met;
+  for (int r0 = threadIdx.x; r0 < u.n; r0 += kBatch * kThreads) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) met.meet(key_at(r0 + i * kThreads));
+  }
+  pair_rows(a, u, key_at, met, lds);
 }
 
 // One row too many, as in a step of decoding: the row with the least key goes, the last of those that have it.  The last row, which

@@ -76,44 +76,64 @@ __device__ __forceinline__ Before before_wave(const SelectLds& lds, int column) 
   return {wave > 0 ? __builtin_amdgcn_readlane(x, wave - 1) : 0, __builtin_amdgcn_readlane(x, 15)};
 }
 
+__device__ __forceinline__ uint32_t min_of_row(uint32_t x) {  // over 16 lanes
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) x = min(x, (uint32_t)__shfl_xor((int)x, o));
+  return x;
+}
+
 // The k-th largest key (there are k above 0), and how many of those that equal it are among the k largest, from the first on (`every`:
-// all).  Eleven bits at a time, by a count of the keys that agree with what is known so far: with fewer bits the first count would meet
-// a few exponents' bins only, and additions to one word of LDS wait for one another.  Where 64 neighbours all meet the same bin, they
-// are added at once.
+// all).  Keys of kTop come first, whatever their number; the others' range is counted in up to 2048 parts, then the part that holds the
+// k-th key in as many, until all keys of a part are taken or they are equal.  (Eleven bits of the keys themselves at a time, without
+// their range, meet a few exponents' parts only where values are alike, and additions to one word of LDS wait for one another: 8192
+// scores 14.4 us.)  Where neighbours all meet the same part, they are added at once.
+constexpr uint32_t kTop = 0xFFFFFFFFu;
 struct Cutoff {
   uint32_t key;
   int equal;
   bool every;
 };
+// What a thread has met: of keys that are neither 0 nor kTop the least, less one, and the greatest, and one; keys of kTop.
+struct Met {
+  uint32_t least = ~0u, most = 0;
+  int tops = 0;
+  __device__ __forceinline__ void meet(uint32_t key) {
+    least = min(least, key - 1);
+    most = max(most, key + 1);
+    tops += key == kTop;
+  }
+};
 template <typename K>
-__device__ __forceinline__ Cutoff cutoff_of(const K& keys, int k, SelectLds& lds) {
+__device__ __forceinline__ Cutoff cutoff_of(const K& keys, const Met& own, int k, SelectLds& lds) {
   const int lane = threadIdx.x & 63;
-  uint32_t known = 0, mask = 0;
-  int left = k, met = 0;
-#pragma unroll 1
-  for (int shift = 21; shift >= 0; shift = shift == 10 ? 0 : shift - 11) {
-    const uint32_t wide = shift == 0 ? 1023 : 2047;
+  uint32_t least = min_of_row(own.least), most = ~min_of_row(~own.most);
+  __syncthreads();  // (keys in LDS are there; lds.sums has been read)
+  least = min(least, min((uint32_t)__builtin_amdgcn_readlane((int)least, 16), min((uint32_t)__builtin_amdgcn_readlane((int)least, 32), (uint32_t)__builtin_amdgcn_readlane((int)least, 48))));
+  most = max(most, max((uint32_t)__builtin_amdgcn_readlane((int)most, 16), max((uint32_t)__builtin_amdgcn_readlane((int)most, 32), (uint32_t)__builtin_amdgcn_readlane((int)most, 48))));
+  int tops = __builtin_amdgcn_readlane(sum_upto(own.tops), 63);
+  if (lane == 0) {
+    lds.sums[this_wave()][0] = tops;
+    lds.sums[this_wave()][1] = (int)least;
+    lds.sums[this_wave()][2] = (int)most;
+  }
+  __syncthreads();
+  tops = before_wave(lds, 0).all;
+  uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)min_of_row((uint32_t)lds.sums[lane & 15][1])) + 1;
+  const uint32_t high = (uint32_t)__builtin_amdgcn_readfirstlane((int)~min_of_row(~(uint32_t)lds.sums[lane & 15][2])) - 1;
+  if (tops >= k) return {kTop, k, tops == k};
+  int left = k - tops, met = 0;
+  uint32_t span = high - low;  // of the part that is looked at, less one
+  for (;;) {
+    const int shift = max(21 - __clz((int)(span | 1)), 0);
     lds.bins[threadIdx.x] = lds.bins[threadIdx.x + kThreads] = 0;
     __syncthreads();
     keys.each([&](int, const uint32_t(&key)[kBatch]) {
-      if (mask == 0) {
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const uint32_t bin = key[i] >> 21;
-          if (__all(bin == (uint32_t)__builtin_amdgcn_readfirstlane((int)bin))) {
-            if (lane == 0) atomicAdd(&lds.bins[bin], 64u);
-          } else {
-            atomicAdd(&lds.bins[bin], 1u);
-          }
-        }
-        return;
-      }
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        const bool mine = (key[i] & mask) == known;
+        const bool mine = key[i] - low <= span;
         const uint64_t some = __ballot(mine);
         if (some == 0) continue;
-        const uint32_t bin = key[i] >> shift & wide;
+        const uint32_t bin = (key[i] - low) >> shift;
         const int lead = __builtin_ctzll(some);
         if (__popcll(some) >= 16 && __ballot(mine && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, lead)) == some) {
           if (lane == lead) atomicAdd(&lds.bins[bin], (uint32_t)__popcll(some));
@@ -123,7 +143,7 @@ __device__ __forceinline__ Cutoff cutoff_of(const K& keys, int k, SelectLds& lds
       }
     });
     __syncthreads();
-    // a thread: two bins, the largest first
+    // a thread: two parts, the highest first
     const int top = 2047 - 2 * (int)threadIdx.x;
     const int c0 = (int)lds.bins[top], c1 = (int)lds.bins[top - 1], upto = sum_upto(c0 + c1);
     if (lane == 63) lds.sums[this_wave()][0] = upto;
@@ -136,13 +156,12 @@ __device__ __forceinline__ Cutoff cutoff_of(const K& keys, int k, SelectLds& lds
       lds.found[2] = second ? c1 : c0;
     }
     __syncthreads();
-    known |= (uint32_t)lds.found[0] << shift;
+    low += (uint32_t)lds.found[0] << shift;
+    span = (1u << shift) - 1;
     left = lds.found[1];
     met = lds.found[2];
-    mask |= wide << shift;
-    if (left == met) break;  // (all that agree are taken)
+    if (shift == 0 || left == met) return {low, left, left == met};  // (all above `low` are taken, or all that equal it alike)
   }
-  return {known, left, left == met};
 }
 
 __device__ __forceinline__ int below_me(uint64_t flags) {
