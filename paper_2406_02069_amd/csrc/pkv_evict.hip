@@ -23,6 +23,8 @@ struct EvictArgs {
   int32_t* count_out;
   int32_t* moves;  // [unit]
   int32_t* pairs;  // [unit][2][most]: destinations, sources
+  uint32_t* keys;  // [unit][key_room], for more rows than LDS holds
+  int64_t key_room;
   int32_t B, Hkv, d, k_cap, page_size, num_pages, max_pages, budget, recent, first, most;
   int32_t in_lds;  // keys that the launch has room for
   uint32_t page_magic;
@@ -192,25 +194,35 @@ __device__ __forceinline__ void evict_rows(const EvictArgs& a, const Unit& u, ui
   }
   pair_rows(a, u, [&](int r) { return kept[r]; }, met, lds);  // (its first barrier comes before the first look-up)
 }
-__device__ __forceinline__ void evict_rows_of_memory(const EvictArgs& a, const Unit& u, SelectLds& lds) {
+// Keys in memory, for more rows than LDS holds: once more than there, each pass goes over them in L2.
+__device__ __forceinline__ void evict_many_rows(const EvictArgs& a, const Unit& u, SelectLds& lds) {
+  uint32_t* const kept = a.keys + (int64_t)u.unit * a.key_room;
   int newest = -1;
-  for (int r0 = threadIdx.x; r0 < u.n; r0 += kBatch * kThreads) {
+  for (int r0 = threadIdx.x; r0 < u.n; r0 += kRun) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) newest = max(newest, u.pos[min(r0 + i * kThreads, u.n - 1)]);
   }
   newest = newest_of_all(newest, lds);
-  const auto key_at = [&](int r) {
-    const uint32_t key = row_key(a, u.pos[min(r, u.n - 1)], u.weight[min(r, u.n - 1)], newest);
-    return r < u.n ? key : 0u;
-  };
-  if (u.pos_out != u.pos || u.weight_out != u.weight)
-    for (int r = threadIdx.x; r < u.n; r += kThreads) keep_row(a, u, r, u.pos[r], u.weight[r]);
   Met met;
-  for (int r0 = threadIdx.x; r0 < u.n; r0 += kBatch * kThreads) {
+  for (int r0 = 0; r0 < u.n; r0 += kRun) {
+    int32_t p[kBatch];
+    float w[kBatch];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) met.meet(key_at(r0 + i * kThreads));
+    for (int i = 0; i < kBatch; ++i) {
+      const int r = min(r0 + (int)threadIdx.x + i * kThreads, u.n - 1);
+      p[i] = u.pos[r];
+      w[i] = u.weight[r];
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int r = r0 + (int)threadIdx.x + i * kThreads;
+      const uint32_t key = r < u.n ? row_key(a, p[i], w[i], newest) : 0u;
+      met.meet(key);
+      kept[r] = key;
+      if (r < u.n) keep_row(a, u, r, p[i], w[i]);
+    }
   }
-  pair_rows(a, u, key_at, met, lds);
+  pair_rows(a, u, [&](int r) { return kept[r]; }, met, lds);  // (its first barrier comes before the first look-up)
 }
 
 // One row too many, as in a step of decoding: the row with the least key goes, the last of those that have it.  The last row, which
@@ -301,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs 
   } else if (u.n <= a.in_lds) {
     evict_rows(a, u, kept, lds);
   } else {
-    evict_rows_of_memory(a, u, lds);
+    evict_many_rows(a, u, lds);
   }
 }
 
@@ -336,6 +348,9 @@ int64_t most_moves(const pkv_evict_desc& d) {
   return behind < 0 ? 0 : behind < d.budget ? behind : d.budget;
 }
 
+// Keys of a head that wait in memory.
+int64_t room_of_keys(const pkv_evict_desc& d) { return d.k_cap <= kKeysInLds ? 0 : ((int64_t)d.k_cap + kRun - 1) / kRun * kRun; }
+
 }  // namespace
 }  // namespace pkv
 
@@ -345,7 +360,7 @@ extern "C" {
 
 size_t pkv_evict_workspace_bytes(const pkv_evict_desc* desc) {
   if (check_evict_desc(desc) != PKV_OK) return 0;
-  return (size_t)desc->B * desc->Hkv * (1 + 2 * (size_t)most_moves(*desc)) * sizeof(int32_t);
+  return (size_t)desc->B * desc->Hkv * (1 + 2 * (size_t)most_moves(*desc) + (size_t)room_of_keys(*desc)) * sizeof(int32_t);
 }
 
 int pkv_cache_evict(const pkv_evict_desc* desc, void* K_cache, void* V_cache, const int32_t* block_table, const int32_t* count,
@@ -375,6 +390,8 @@ int pkv_cache_evict(const pkv_evict_desc* desc, void* K_cache, void* V_cache, co
   a.B = d.B; a.Hkv = d.Hkv; a.d = d.d; a.k_cap = d.k_cap; a.page_size = d.page_size; a.num_pages = d.num_pages;
   a.max_pages = d.max_pages; a.budget = d.budget; a.recent = d.recent; a.first = d.first;
   a.most = (int32_t)most_moves(d);
+  a.key_room = room_of_keys(d);
+  a.keys = reinterpret_cast<uint32_t*>(a.pairs + (size_t)units * 2 * a.most);
   a.page_magic = magic_of(d.page_size);
   a.c_sb = d.c_sb; a.c_sh = d.c_sh; a.c_st = d.c_st; a.p_sb = d.p_sb; a.p_sh = d.p_sh; a.w_sb = d.w_sb; a.w_sh = d.w_sh;
   a.po_sb = d.po_sb; a.po_sh = d.po_sh; a.wo_sb = d.wo_sb; a.wo_sh = d.wo_sh;

@@ -30,10 +30,16 @@ struct Keys {
   // f(number of the first, keys): keys `number`, number + 64, ..
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
+    uint32_t next[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) next[k] = key_at(first + 64 * k);
     for (int i = 0; i < steps; ++i) {
       uint32_t key[kBatch];
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) key[k] = key_at(first + 64 * (kBatch * i + k));
+      for (int k = 0; k < kBatch; ++k) key[k] = next[k];
+      const int ahead = first + 64 * kBatch * min(i + 1, steps - 1);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) next[k] = key_at(ahead + 64 * k);
       f(first + 64 * kBatch * i, key);
     }
   }
