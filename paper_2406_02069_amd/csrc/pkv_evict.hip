@@ -27,6 +27,7 @@ struct EvictArgs {
   int64_t key_room;
   int32_t B, Hkv, d, k_cap, page_size, num_pages, max_pages, budget, recent, first, most;
   int32_t in_lds;  // keys that the launch has room for
+  int32_t second;  // whether there is a second launch
   uint32_t page_magic;
   int64_t c_sb, c_sh, c_st, p_sb, p_sh, w_sb, w_sh, po_sb, po_sh, wo_sb, wo_sh;
 };
@@ -60,9 +61,11 @@ struct Unit {
 };
 
 // What becomes of a row that is not moved into: before the budget it stays (holes are filled later), behind it it is emptied.  Where the
-// outputs are the inputs, the former is there already, and the latter waits until the moved rows have been read.
+// outputs are the inputs, the former is there already, and the latter waits until the moved rows have been read; where there is a second
+// launch, its many workgroups empty the rows (32k rows to 2k: 33.9 + 11 us without, 32.8 + 11 with).
 __device__ __forceinline__ void keep_row(const EvictArgs& a, const Unit& u, int r, int32_t p, float w) {
   const bool stays = r < a.budget;
+  if (!stays && a.second) return;
   if (u.pos_out != u.pos) u.pos_out[r] = stays ? p : -1;
   if (u.weight_out != u.weight) u.weight_out[r] = stays ? w : 0.0f;
 }
@@ -84,7 +87,7 @@ __device__ __forceinline__ void finish(const EvictArgs& a, const Unit& u, int la
     const int lanes = a.d / 8;
     for (int i = threadIdx.x; i < late * lanes; i += kThreads) move_piece(a, u.b, u.g, to[i / lanes], from[i / lanes], i % lanes);
   }
-  if (u.pos_out != u.pos && u.weight_out != u.weight) return;
+  if (a.second || (u.pos_out != u.pos && u.weight_out != u.weight)) return;
   __syncthreads();
   for (int r = a.budget + threadIdx.x; r < u.n; r += kThreads) {
     if (u.pos_out == u.pos) u.pos_out[r] = -1;
@@ -317,10 +320,16 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs 
   }
 }
 
-// A workgroup: kPairs rows of K and of V, 16 bytes a thread at a time.
+// A workgroup: kPairs rows of K and of V, 16 bytes a thread at a time, and its share of the rows that are emptied.
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a, int chunks) {
   const int unit = blockIdx.x / chunks, chunk = blockIdx.x % chunks, b = unit / a.Hkv, g = unit % a.Hkv;
-  const int moves = a.moves[unit], lanes = a.d / 8;
+  const int moves = a.moves[unit], lanes = a.d / 8, n = min(max(a.count[b], 0), a.k_cap);
+  int32_t* const pos_out = a.positions_out + b * a.po_sb + g * a.po_sh;
+  float* const weight_out = a.weights_out + b * a.wo_sb + g * a.wo_sh;
+  for (int64_t r = a.budget + (int64_t)chunk * 256 + threadIdx.x; r < n; r += (int64_t)chunks * 256) {
+    pos_out[r] = -1;
+    weight_out[r] = 0.0f;
+  }
   const int32_t *const to = a.pairs + (int64_t)unit * 2 * a.most, *const from = to + a.most;
   for (int64_t c = chunk; c * kPairs < moves; c += chunks) {
     for (int i = threadIdx.x; i < kPairs * lanes; i += 256) {
@@ -397,11 +406,12 @@ int pkv_cache_evict(const pkv_evict_desc* desc, void* K_cache, void* V_cache, co
   a.po_sb = d.po_sb; a.po_sh = d.po_sh; a.wo_sb = d.wo_sb; a.wo_sh = d.wo_sh;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   a.in_lds = keys_in_lds(d.k_cap);
+  a.second = a.most > kMovedHere;
   static bool granted[kMaxDevices];
   if (grant_keys(reinterpret_cast<const void*>(evict_select_kernel), granted) != hipSuccess) return PKV_ERR_HIP;
   hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)units), dim3(kThreads), (size_t)a.in_lds * sizeof(uint32_t), st, a);
   if (hipGetLastError() != hipSuccess) return PKV_ERR_HIP;
-  if (a.most <= kMovedHere) return PKV_OK;
+  if (!a.second) return PKV_OK;
   int64_t chunks = (a.most + kPairs - 1) / kPairs;
   if (chunks > kMaxGrid / units) chunks = kMaxGrid / units;
   hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(units * chunks)), dim3(256), 0, st, a, (int)chunks);
