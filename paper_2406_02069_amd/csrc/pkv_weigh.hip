@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void join_and_weigh_kernel(const WeighArgs a, 
 #pragma unroll
       for (int i = 0; i < kRowsAtATime; ++i) x[i] = s[h * a.score_row + min(max(r0 + 256 * i, lo), hi - 1)];
 #pragma unroll
-      for (int i = 0; i < kRowsAtATime; ++i) sum[i] += x[i] == kNone ? 0.0f : exp2_(x[i] - ref) * factor;
+      for (int i = 0; i < kRowsAtATime; ++i) sum[i] += x[i] == kNone || factor == 0.0f ? 0.0f : exp2_(x[i] - ref) * factor;
     }
     float* const w = a.weights + b * a.w_sb + g * a.w_sh;
 #pragma unroll

@@ -99,6 +99,28 @@ def test_weights_by_positions_and_of_what_is_not_seen(window, slopes, page):
     assert torch.equal(buf[:, 0], before[:, 0]) and torch.equal(buf[:, Hkv + 1], before[:, Hkv + 1]) and torch.equal(buf[:, :, k_cap:], before[:, :, k_cap:])
 
 
+def test_nothing_of_the_workspace_reaches_the_weights():
+    # a query that sees nothing, an empty cache, rows outside the window, with whatever the workspace holds
+    B, Hq, Hkv, d, k_cap = 4, 8, 2, 64, 900
+    g = torch.Generator(device=DEV).manual_seed(3)
+    q = torch.randn(B, Hq, d, generator=g, device=DEV).to(torch.bfloat16)
+    K, V, _, _, _ = make_cache(B, Hkv, k_cap, d, torch.bfloat16, 0, g)
+    pos = torch.arange(k_cap, dtype=torch.int32, device=DEV).expand(B, Hkv, k_cap).contiguous()
+    count, q_pos = torch.tensor([900, 0, 900, 500], dtype=torch.int32, device=DEV), torch.tensor([-1, 5, 899, 3], dtype=torch.int32, device=DEV)
+    for fill in (255, 127, 0):
+        ws = torch.full((1 << 23,), fill, dtype=torch.uint8, device=DEV)
+        weights = torch.rand(B, Hkv, k_cap, generator=g, device=DEV)
+        before = weights.clone()
+        out, lse = binding.decode_attention_accumulate(q, K, V, count, weights, positions=pos, q_pos=q_pos, window=100, want_lse=True, workspace=ws)
+        torch.cuda.synchronize()
+        _compare(out, lse, weights, before, q, K, V, count, pos, q_pos, window=100)
+        weights = before.clone()
+        ws.fill_(fill)
+        out, lse = binding.decode_attention_accumulate(q, K, V, count, weights, q_pos=q_pos, window=100, want_lse=True, workspace=ws)
+        torch.cuda.synchronize()
+        _compare(out, lse, weights, before, q, K, V, count, None, q_pos, window=100)
+
+
 def test_weights_from_a_graph_and_two_calls_at_once():
     B, Hq, Hkv, d, k_cap = 2, 32, 8, 128, 6000
     g = torch.Generator(device=DEV).manual_seed(7)
