@@ -909,7 +909,7 @@ size_t pkv_evict_workspace_bytes(const pkv_evict_desc* desc);
  *             concurrent calls need distinct ones.
  * Asynchronous on `stream`, never allocates.
  * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, B or Hkv >
- * 65535, B * Hkv > 2^22, k_cap or c_st > 2^30, a pool of more than 2^32 - 1
+ * 65535, B * Hkv > 2^22 - 1, k_cap or c_st > 2^30, a pool of more than 2^32 - 1
  * rows), PKV_ERR_WORKSPACE, PKV_ERR_HIP.
  */
 int pkv_cache_evict(const pkv_evict_desc* desc, void* K_cache, void* V_cache,
@@ -964,8 +964,8 @@ typedef struct {
  *             multiples of 8, the last three dimensions contiguous.
  * Asynchronous on `stream`, needs no workspace, never allocates.
  * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, block none of
- * the above, B or Hkv > 65535, B * Hkv > 2^22, k_cap or c_st > 2^30, a pool of
- * more than 2^32 - 1 rows), PKV_ERR_HIP.
+ * the above, B or Hkv > 65535, B * Hkv > 2^22 - 1, k_cap or c_st > 2^30, a pool
+ * of more than 2^32 - 1 rows), PKV_ERR_HIP.
  */
 int pkv_block_bounds(const pkv_block_desc* desc, const void* K_cache,
                      const int32_t* block_table, const int32_t* count,
@@ -992,8 +992,8 @@ int pkv_block_bounds(const pkv_block_desc* desc, const void* K_cache,
  *            bytes; contents irrelevant on entry, undefined on exit; concurrent
  *            calls need distinct ones.
  * Asynchronous on `stream`, never allocates.
- * Errors: as pkv_block_bounds, PKV_ERR_UNSUPPORTED also Hq/Hkv > 128,
- * PKV_ERR_WORKSPACE.
+ * Errors: as pkv_block_bounds, PKV_ERR_UNSUPPORTED also Hq/Hkv > 128 or most >
+ * 2^30, PKV_ERR_WORKSPACE.
  */
 size_t pkv_block_select_workspace_bytes(const pkv_block_desc* desc);
 

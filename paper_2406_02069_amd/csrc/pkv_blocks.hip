@@ -282,8 +282,8 @@ int check_block_desc(const pkv_block_desc* desc, bool queries, bool cache) {
   if (queries && (check_scores(d) != PKV_OK || d.most < 1)) return PKV_ERR_INVALID_ARG;
   if (cache && check_pages(d) != PKV_OK) return PKV_ERR_INVALID_ARG;
   if (shift_of(d.block) < 0) return PKV_ERR_UNSUPPORTED;
-  if ((int64_t)d.B * d.Hkv > 1 << 22) return PKV_ERR_UNSUPPORTED;
-  if (queries && (d.Hq / d.Hkv > 128 || (int64_t)d.B * d.Hq > kMaxGrid)) return PKV_ERR_UNSUPPORTED;
+  if ((int64_t)d.B * d.Hkv >= 1 << 22) return PKV_ERR_UNSUPPORTED;  // (workgroups of 1024: 2^32 threads)
+  if (queries && (d.most > 1 << 30 || d.Hq / d.Hkv > 128 || (int64_t)d.B * d.Hq > kMaxGrid)) return PKV_ERR_UNSUPPORTED;
   if (cache) return check_cache_limits(d);
   return (d.d != 64 && d.d != 128) || d.B > 65535 || d.Hkv > 65535 || d.k_cap > (1 << 30) ? PKV_ERR_UNSUPPORTED : PKV_OK;
 }

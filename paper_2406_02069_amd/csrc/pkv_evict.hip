@@ -347,7 +347,7 @@ int check_evict_desc(const pkv_evict_desc* desc) {
       check_pages(d) != PKV_OK)
     return PKV_ERR_INVALID_ARG;
   if (d.p_sb < 0 || d.p_sh < 0 || d.w_sb < 0 || d.w_sh < 0 || d.po_sb < 0 || d.po_sh < 0 || d.wo_sb < 0 || d.wo_sh < 0) return PKV_ERR_INVALID_ARG;
-  if ((int64_t)d.B * d.Hkv > 1 << 22) return PKV_ERR_UNSUPPORTED;
+  if ((int64_t)d.B * d.Hkv >= 1 << 22) return PKV_ERR_UNSUPPORTED;  // (workgroups of 1024: 2^32 threads)
   return check_cache_limits(d);
 }
 

@@ -244,6 +244,16 @@ def test_block_pointers_and_workspaces_refused():
     assert _blocks(_block_desc(page_size=16, num_pages=600, max_pages=512)) == I
 
 
+def test_launches_of_too_many_threads_and_lists_past_32_bits_refused():
+    many = dict(B=2048, Hkv=2048)                                       # 2^22 workgroups of 1024
+    assert _evict(_evict_desc(**many), n=1 << 50) == U
+    assert _bounds(_block_desc(**many)) == U
+    assert _select(_block_desc(Hq=2048, **many), n=1 << 50) == U
+    for most in (2 ** 30 + 1, 2 ** 31 - 1):
+        assert _select(_block_desc(most=most), n=1 << 50) == U
+        assert binding.load().pkv_block_select_workspace_bytes(_ref(_block_desc(most=most))) == 0
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     q, K = torch.zeros(1, 8, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 16, 64, dtype=torch.bfloat16)
     n, w, p = torch.zeros(1, dtype=torch.int32), torch.zeros(1, 2, 16), torch.zeros(1, 2, 16, dtype=torch.int32)
