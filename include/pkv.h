@@ -831,7 +831,8 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q,
  * Nothing else of weights is written.  Same descriptor, results and errors
  * (PKV_ERR_UNSUPPORTED also B * Hq > 2^23).
  * weights   DEVICE fp32 [B,Hkv,k_cap], 4-byte aligned, with element strides w_sb
- *           and w_sh (>= 0; the sums of two heads do not overlap).
+ *           and w_sh (>= 0, and >= k_cap where there are several sequences or
+ *           heads: their sums do not overlap).
  * workspace DEVICE, 256-byte aligned,
  *           >= pkv_decode_accumulate_workspace_bytes(desc) bytes; contents
  *           irrelevant on entry, undefined on exit; concurrent calls need
@@ -885,7 +886,9 @@ typedef struct {
 size_t pkv_evict_workspace_bytes(const pkv_evict_desc* desc);
 
 /*
- * desc        HOST.
+ * desc        HOST.  What is written has places of its own: po_* and wo_* are >=
+ *             k_cap and c_* >= d, where there are several sequences, heads or
+ *             rows.
  * K_cache, V_cache
  *             DEVICE, rows of d 16-bit elements, 16-byte aligned, compact or
  *             pools; rows behind the budget keep their content.  Pages that
@@ -961,7 +964,8 @@ typedef struct {
  * count       DEVICE int32 [B].
  * new_lens    DEVICE int32 [B]: new_b, clamped to 0..n_b; NULL: n_b (all).
  * bounds      DEVICE, of the descriptor's type, 16-byte aligned; strides
- *             multiples of 8, the last three dimensions contiguous.
+ *             multiples of 8, the last three dimensions contiguous; those of
+ *             two heads do not overlap.
  * Asynchronous on `stream`, needs no workspace, never allocates.
  * Errors: PKV_ERR_INVALID_ARG, PKV_ERR_UNSUPPORTED (d not 64/128, block none of
  * the above, B or Hkv > 65535, B * Hkv > 2^22 - 1, k_cap or c_st > 2^30, a pool

@@ -873,6 +873,9 @@ inline int check_long_call(const pkv_decode_long_desc* desc, const void* q, cons
   return PKV_OK;
 }
 
+// Whether places of [B, Hkv, n] with these strides, neighbours in the last dimension, are distinct: what a call writes must be.
+inline bool apart(int64_t B, int64_t Hkv, int64_t n, int64_t sb, int64_t sh) { return (B == 1 || sb >= n) && (Hkv == 1 || sh >= n); }
+
 inline uint32_t magic_of(int page_size) { return page_size > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint32_t)page_size) : 0xFFFFFFFFu; }
 
 // The fields that a descriptor gives; rows: query rows that share a KV head.

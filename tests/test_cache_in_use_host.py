@@ -254,6 +254,16 @@ def test_launches_of_too_many_threads_and_lists_past_32_bits_refused():
         assert binding.load().pkv_block_select_workspace_bytes(_ref(_block_desc(most=most))) == 0
 
 
+def test_places_written_twice_refused():
+    for kw in (dict(po_sh=0), dict(wo_sh=8191), dict(B=2, po_sb=0), dict(B=2, wo_sb=8191), dict(c_st=0), dict(c_sh=0), dict(B=2, c_sb=0)):
+        assert _evict(_evict_desc(**kw)) == I, kw
+    for kw in (dict(w_sh=0), dict(w_sh=8191)):
+        assert _weigh(_long_desc(), **kw) == I, kw
+    assert _weigh(_long_desc(B=2), w_sb=0) == I
+    for kw in (dict(b_sh=0), dict(b_sh=512 * 256 - 8), dict(B=2, b_sb=0)):
+        assert _bounds(_block_desc(**kw)) == I, kw
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     q, K = torch.zeros(1, 8, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 16, 64, dtype=torch.bfloat16)
     n, w, p = torch.zeros(1, dtype=torch.int32), torch.zeros(1, 2, 16), torch.zeros(1, 2, 16, dtype=torch.int32)
