@@ -977,7 +977,7 @@ int pkv_block_bounds(const pkv_block_desc* desc, const void* K_cache,
 
 /*
  * The blocks a step takes.  The score of block blk of KV head g,
- *   sum_{h of g} sum_i max(q_hi bounds[..][0][i], q_hi bounds[..][1][i]),
+ *   sum_{h of g} sum_i q_hi bounds[..][q_hi < 0 ? 0 : 1][i],
  * bounds the sum of the heads' products with any of the block's keys from
  * above.  It is formed in 64 bits and rounded to fp32 once; one that is NaN
  * counts as +inf.  Of the ceil(n_b / block) blocks the first `first` and the

@@ -2,8 +2,8 @@
 // pkv_decode_attention_blocks).
 //
 //   bounds  a wave takes a block's rows whole, eight channels a lane, and joins the lanes that have the same channels.
-//   select  sum_h sum_i max(q_hi lo_i, q_hi hi_i) = sum_i P_i hi_i + N_i lo_i with P_i = sum_h max(q_hi, 0), N_i = sum_h min(q_hi, 0):
-//           one product of 2 d numbers a block for all heads of a group, in 64 bits (16-bit numbers' products and their sums are
+//   select  sum_h sum_i q_hi (q_hi < 0 ? lo_i : hi_i) = sum_i P_i hi_i + N_i lo_i with P_i = sum_h max(q_hi, 0), N_i = sum_h min(q_hi, 0)
+//           (where bounds are finite): one product of 2 d numbers a block for all heads of a group, in 64 bits (16-bit numbers' products and their sums are
 //           exact there but for extreme spreads), so that which blocks are taken does not hang on an order of additions.
 //           Then a workgroup per (sequence, KV head) finds the smallest score that is taken and lists the blocks in order.
 //   attention  pkv_decode_long.hip's kernel, which looks its rows up in the list.
@@ -196,7 +196,20 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectArgs a, in
     // (lane bits 0, 1, 2 chose bits 2, 1, 0 of the load's number)
     const int blk = blk0 + (((lane & 1) << 2) | (lane & 2) | ((lane >> 2) & 1)) * AT_ONCE + lane / LANES;
     if (piece < kLoads && blk < have) {
-      const float x = (float)s[0];
+      float x = (float)s[0];
+      if (__builtin_expect(!(fabsf(x) < __builtin_inff()), 0)) {  // a coefficient of 0 times a bound that is not finite: term by term
+        const uint16_t *const qp = a.q + b * a.q_sb + (int64_t)g * a.G * a.q_sh, *const own = a.bounds + b * a.b_sb + g * a.b_sh + (int64_t)blk * (2 * D);
+        double sum = 0.0;
+#pragma unroll 1
+        for (int h = 0; h < a.G; ++h) {
+#pragma unroll 8
+          for (int i = 0; i < D; ++i) {
+            const float y = unpack<T>(qp[h * a.q_sh + i], 0);
+            sum = __builtin_fma((double)y, (double)unpack<T>(own[(y < 0.0f ? 0 : D) + i], 0), sum);
+          }
+        }
+        x = (float)sum;
+      }
       a.scores[(int64_t)unit * a.all + blk] = x == x ? x : __builtin_inff();
     }
 #pragma unroll

@@ -130,6 +130,31 @@ def test_selection_of_odd_bounds():
     assert got[0].tolist() == [[0, 1, 2, 3, 4]] * 2 and got[1].tolist() == [[0, 1, 2, -1, -1]] * 2
 
 
+@pytest.mark.parametrize("G", [1, 4, 9])
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float16, 64)])
+def test_scores_of_infinite_bounds(G, dtype, d):
+    # a bound that no head's sign asks for has no part in the score, whatever it is
+    Hkv, blocks = 2, 70
+    g = torch.Generator(device=DEV).manual_seed(G)
+    bounds = torch.randn(1, Hkv, blocks, 2, d, generator=g, device=DEV).to(dtype)
+    bounds[:, :, 3, 1, 5], bounds[:, :, 7, 0, 5], bounds[:, :, 40, 1, d - 1], bounds[:, :, 69, 0, 0] = math.inf, -math.inf, math.nan, math.nan
+    bounds[:, :, 20, 1], bounds[:, :, 21, 0], bounds[:, :, 22, 0, 9] = math.inf, -math.inf, math.inf
+    count = torch.tensor([blocks * 16], dtype=torch.int32, device=DEV)
+    for signs in (-1, 1, 0):
+        q = torch.randn(1, Hkv * G, d, generator=g, device=DEV).to(dtype)
+        q = signs * q.abs() if signs else q
+        scores = torch.empty(1, Hkv, blocks, device=DEV)
+        got = binding.block_select(q, bounds, count, 16, 6, scores=scores)
+        torch.cuda.synchronize()
+        for h in range(Hkv):
+            want = block_scores(q[0, h * G:(h + 1) * G], bounds[0, h])
+            assert torch.equal(torch.isinf(scores[0, h]), torch.isinf(want))
+            near = torch.isfinite(want)
+            assert torch.equal(scores[0, h][~near], want[~near])
+            assert bool(((scores[0, h] - want)[near].abs() <= 2.0 ** -23 * want[near].abs()).all())
+            assert got[0, h].tolist() == blocks_taken(scores[0, h], 6, 0, 0)
+
+
 def _compare(out, lse, q, K, V, count, blocks, block, cap=0.0, scale=None, absent=None):
     """(lists without an entry that is named twice)"""
     B, Hq, d = q.shape
