@@ -1,11 +1,15 @@
 // Attention over the blocks of a cache that a bound on their scores selects (include/pkv.h: pkv_block_bounds, pkv_block_select,
 // pkv_decode_attention_blocks).
 //
-//   bounds  a wave takes a block's rows whole, eight channels a lane, and joins the lanes that have the same channels.
+//   bounds  a wave takes a block's rows whole, eight channels a lane, and joins the lanes that have the same channels.  HBM-bound: 2 x 8
+//           heads of 32k rows, d 128 (134 MB), 26.6 us, 5 TB/s; a chunk of 300 rows in 8 sequences of 4 heads 7.6.
 //   select  sum_h sum_i q_hi (q_hi < 0 ? lo_i : hi_i) = sum_i P_i hi_i + N_i lo_i with P_i = sum_h max(q_hi, 0), N_i = sum_h min(q_hi, 0)
-//           (where bounds are finite): one product of 2 d numbers a block for all heads of a group, in 64 bits (16-bit numbers' products and their sums are
-//           exact there but for extreme spreads), so that which blocks are taken does not hang on an order of additions.
-//           Then a workgroup per (sequence, KV head) finds the smallest score that is taken and lists the blocks in order.
+//           (where bounds are finite): one product of 2 d numbers a block for all heads of a group, in 64 bits (16-bit numbers'
+//           products and their sums are exact there but for extreme spreads), so that which blocks are taken does not hang on an
+//           order of additions.
+//           HBM-bound, 512 bytes a block at d 128: 164k blocks 17.5 us, 4.8 TB/s.
+//           Then a workgroup per (sequence, KV head) finds the smallest score that is taken (pkv_topk.h) and lists the blocks in
+//           order: 7.5 us of 512 blocks, 9.4 of 8192, launch and barriers for the most part.
 //   attention  pkv_decode_long.hip's kernel, which looks its rows up in the list.
 #include "pkv_long.h"
 #include "pkv_topk.h"

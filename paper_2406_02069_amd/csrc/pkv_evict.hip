@@ -1,8 +1,13 @@
 // Eviction by accumulated weights, in place (include/pkv.h: pkv_cache_evict).
 //
 // Two launches.  The first, a workgroup per (sequence, KV head), finds the smallest weight that stays and pairs the rows behind the
-// budget that stay with the holes before it: sources lie behind all destinations, so that the second can copy the pairs' rows in any
-// order, in place.
+// budget that stay with the holes before it, the i-th with the i-th by counting both (a prefix sum over waves): sources lie behind all
+// destinations, so that the second can copy the pairs' rows in any order, in place, by as many workgroups as the device holds.
+// Up to 64 rows are moved by the first already, which is the only one where there can be no more.
+// What bounds it: the first launch is one compute unit's time for a head, a few passes over 4-byte keys (pkv_topk.h) which stand in LDS
+// for up to 32k rows and in L2, through the workspace, beyond; the second the copy.  d 128, 8 heads: one row too many of 2049 in 8
+// sequences 6.7 us, 4 sequences of up to 32k rows to 2k 33 + 11 (keys formed again in each pass: 121), 131072 to 2048 117 (312 with keys
+// formed again), four times that at once 140, 64 sequences of 4096 to 2048 116 (0.5 GB moved).
 #include <string.h>
 
 #include "pkv_long.h"

@@ -1,4 +1,5 @@
-// What the entry points of pkv_rotary.hip, pkv_prefill.hip and pkv_decode_long.hip ask of their arguments.
+// What the entry points of pkv_rotary.hip, pkv_prefill.hip, pkv_decode_long.hip and, through pkv_long.h, pkv_tree.hip, pkv_weigh.hip,
+// pkv_evict.hip and pkv_blocks.hip ask of their arguments.
 #pragma once
 
 #include <stddef.h>

@@ -17,7 +17,7 @@ constexpr int kWorkgroups = 512;   // at a time on the device: two per compute u
 constexpr int kLaneSequences = 4;  // sequences a lane looks after where ranges go by lengths,
 constexpr int kFlatBatch = 64 * kLaneSequences;  // and so many at most in all
 constexpr int kLeastTiles = 8;     // of a range,
-constexpr int kLeastWide = 12;     // of many query rows
+constexpr int kLeastWide = 12;     // of many query rows (whose results are more to join)
 
 // What the kernel is built for: one token over all rows; the same, handing its scores on; drafted tokens; listed blocks of rows.
 // (kTreeWide: drafted tokens whose query rows are many, in pkv_tree.hip's own kernel.)

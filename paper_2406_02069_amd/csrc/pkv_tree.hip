@@ -1,7 +1,25 @@
 // Attention of drafted tokens over a cache (include/pkv.h: pkv_tree_attention).
 //
-// The T Hq/Hkv query rows of a KV head share its rows of the cache; up to 64 of them are a workgroup of pkv_decode_long.hip's
-// kernel, in which only the tiles that hold drafted tokens look at the tree: 32 of its bits are one word, shifted to the tile.
+//   out_t = sum_j 2^(s_tj - m_t) V_j / sum_j 2^(s_tj - m_t)  over the rows j that token t sees, m_t a running reference.
+// The T Hq/Hkv query rows of a KV head share its rows of the cache: the more of them, the more products for each byte.  Up to 32 rows
+// HBM bounds (decode_long_kernel, which is described in pkv_decode_long.hip: 8 tokens of 32/8 heads, d 128, behind 100k rows 91 us, 4.5
+// TB/s); from there on feeding the matrix pipe does (tree_wide_kernel: 16 tokens 87 us, 64 147, 128 256).  In both only the steps that
+// hold drafted tokens look at the tree: 32 of its bits are one word, shifted to the step.
+//
+// tree_wide_kernel: a workgroup is 128 query rows of a KV head x a range of its cache, a wave 32 of the rows against all keys of the
+// range, 32 at a time.  What a wave of decode_long_kernel reads for 16 rows serves 128 here: 64 tokens took 439 us there, 209 at once
+// with this split.
+//   loads   K and V straight into LDS, 8 rows of a step by each wave, two steps ahead in three buffers; a step waits for its own loads
+//           only and for the other waves once.  Rows of a page have one base where pages are of 8 k rows (page size 1: 177 us for the
+//           64 tokens); page numbers and positions come the same way, for eight steps at a time.
+//   scores  S^T = K Q^T in v_mfma_f32_32x32x16: 32 keys are the rows of A, 32 query rows the columns of B, which stay in registers.
+//           Lane (col, half) ends with 16 keys of row col.
+//   softmax the reference moves when a score exceeds it by 2^6.
+//   values  O^T += V^T P^T, V read column-wise.  The weights are rounded to the type once (decode_long_kernel's second product for
+//           what the rounding left would take the pipe's time here: 24 products a step at d 128 in place of 16).
+// What is left at 64 tokens behind 100k rows: two workgroups a compute unit run at 1.6 GHz under this load, the matrix pipe busy 37 %
+// of it, and 512 ranges' results are 33 MB that are written and read again (13 us in the join).  Capped and biased scores are bound by
+// vector instructions (a batch of 26 tokens with 5000 kept rows each: 47 us + 13).
 #include <type_traits>
 
 #include "pkv_long.h"
@@ -26,9 +44,11 @@ constexpr int kBuffers = 3;  // of a step's keys and values
 constexpr int kSlots = 4;    // of what is known of a step: from two steps before it on
 constexpr int kAhead = 8;    // steps whose page numbers and positions are requested at a time
 
-// MODE 1: scores are capped or biased.
+// Workgroups of a compute unit.  d 128: three would fit LDS, with 168 registers a lane, and 9 - 32 tokens behind 100k rows take 94 - 111
+// us then, 84 - 97 with two (ranges' results are a third fewer); 64 tokens 147 and 150.  d 64: 16 tokens 26.1 with three, 28.0 with two.
 template <int D>
-constexpr int wide_per_unit() { return D == 128 ? 2 : 3; }  // workgroups of a compute unit
+constexpr int wide_per_unit() { return D == 128 ? 2 : 3; }
+// MODE 1: scores are capped or biased.
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(256, (wide_per_unit<D>())) void tree_wide_kernel(const TreeWideArgs a) {
   constexpr int STEPS = D / 16, MB = D / 32, PIECES = D / 8, ROWS_PER_LOAD = 64 / PIECES, ROWS = group_rows<TreeWideArgs>();
@@ -531,11 +551,12 @@ hipError_t launch_wide(const TreeWideArgs& a, int64_t workgroups, hipStream_t s)
   return e != hipSuccess || a.ranges == 0 ? e : launch_join<T, D>(a, s);
 }
 
-// More than kFewRows query rows a KV head: the kernel above.
+// More than kFewRows query rows a KV head: the kernel above.  32/8 heads, d 128, behind 100k rows: 32 rows 91 us in decode_long_kernel,
+// 36 rows 84 here, 64 rows 127 there and 87 here.  Behind 4000 rows the two are 2 us apart.
 constexpr int kFewRows = 32;
 bool wide(const pkv_tree_desc& d) { return (int64_t)d.T * (d.Hq / d.Hkv) > kFewRows; }
 
-// As grid_of of pkv_long.h, in workgroups of 128 rows, of which the device holds three per compute unit.
+// As grid_of of pkv_long.h, in workgroups of 128 rows, of which the device holds wide_per_unit per compute unit.
 int wide_turn(const pkv_tree_desc& d) { return d.d == 128 ? 512 : 768; }
 Grid wide_grid(const pkv_tree_desc& d, int turn) {
   constexpr int ROWS = group_rows<TreeWideArgs>();
