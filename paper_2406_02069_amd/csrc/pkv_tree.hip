@@ -98,26 +98,18 @@ __global__ __launch_bounds__(256, (wide_per_unit<D>())) void tree_wide_kernel(co
   const int drafted = a.new_lens ? min(max(a.new_lens[b], 0), a.T) : a.T;
   const bool there = row < a.G && t < drafted, wave_there = __any(there);
   const bool placed = a.positions || a.window || (MODE == 1 && a.slopes);  // positions matter
-  int32_t p_row = 0;
-  if (placed) {
-    if (!a.q_pos) {
-      for (int i = threadIdx.x; i < a.T; i += 256) lds_depth[i] = (int16_t)ancestors(a, b, i, drafted);
-      __syncthreads();
-    }
-    p_row = a.q_pos ? a.q_pos[(int64_t)b * a.T + t] : past + lds_depth[t];
-  }
-  // the least and the greatest position of the wave's rows, and of the workgroup's
-  const int32_t w_min = ~wave_max(there ? ~p_row : INT32_MIN), w_max = wave_max(there ? p_row : INT32_MIN);
-  if (lane == 0) {
-    lds_span[wave][0] = w_min;
-    lds_span[wave][1] = w_max;
-    if (wave == 0) lds_zeroed = 0;
-  }
-  __syncthreads();
-  const int32_t g_min = min(min(lds_span[0][0], lds_span[1][0]), min(lds_span[2][0], lds_span[3][0]));
-  const int32_t g_max = max(max(lds_span[0][1], lds_span[1][1]), max(lds_span[2][1], lds_span[3][1]));
   if (ROWS * tile >= drafted * a.heads) step = step_end;  // no row is there
   const int step_begin = step;
+
+  // What is known of the query rows is requested here, what the first steps' rows are behind it, and waited for together.
+  u32x4 qf[STEPS];
+  {
+    const uint16_t* qp = a.q + b * a.q_sb + h * a.q_sh + t * a.q_st + 8 * half;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) qf[i] = there ? *reinterpret_cast<const u32x4*>(qp + 16 * i) : (u32x4)(0);
+  }
+  float slope = MODE == 1 && a.slopes ? a.slopes[h] * kLog2e : 0.0f;
+  int32_t p_row = placed && a.q_pos ? a.q_pos[(int64_t)b * a.T + t] : 0;
 
   const uint32_t row_bytes = (uint32_t)(a.page_size ? D : a.c_st) * 2;
   const int64_t base = a.page_size ? 0 : (b * a.c_sb + g * a.c_sh) * 2;
@@ -225,6 +217,42 @@ __global__ __launch_bounds__(256, (wide_per_unit<D>())) void tree_wide_kernel(co
     }
     return is;
   };
+  // Two steps are on their way while a third is worked on.
+  uint32_t is_now = 0, is_next = 0, is_then = 0;
+  if (step < step_end) {
+    look_ahead(step / kAhead);
+    look_ahead(step / kAhead + 1);
+    look(step);
+    look(step + 1);
+  }
+  if (placed && !a.q_pos) {
+    for (int i = threadIdx.x; i < a.T; i += 256) lds_depth[i] = (int16_t)ancestors(a, b, i, drafted);
+    __syncthreads();
+    p_row = past + lds_depth[t];
+  }
+  wait_loads();
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) asm volatile("" : "+v"(qf[i]));  // (they are waited for here, and not by every step's products)
+  asm volatile("" : "+v"(slope), "+v"(p_row));
+  if (step < step_end) {
+    take_pages(step / kAhead);
+    is_now = fetch(step, 0, std::false_type());
+    look(step + 2);
+    if (step + 1 < step_end) {
+      if ((step + 1) % kAhead == 0) take_pages((step + 1) / kAhead);
+      is_next = fetch(step + 1, 1, std::false_type());
+    }
+  }
+  // the least and the greatest position of the wave's rows, and of the workgroup's
+  const int32_t w_min = ~wave_max(there ? ~p_row : INT32_MIN), w_max = wave_max(there ? p_row : INT32_MIN);
+  if (lane == 0) {
+    lds_span[wave][0] = w_min;
+    lds_span[wave][1] = w_max;
+    if (wave == 0) lds_zeroed = 0;
+  }
+  lds_barrier();
+  const int32_t g_min = min(min(lds_span[0][0], lds_span[1][0]), min(lds_span[2][0], lds_span[3][0]));
+  const int32_t g_max = max(max(lds_span[0][1], lds_span[1][1]), max(lds_span[2][1], lds_span[3][1]));
   // Whether rows whose positions are from least to greatest see all rows of a step that are there.
   auto whole = [&](int st, uint32_t now, int32_t pos_now, int32_t least, int32_t greatest) {
     const int off = st * kTile - past;
@@ -249,35 +277,6 @@ __global__ __launch_bounds__(256, (wide_per_unit<D>())) void tree_wide_kernel(co
     }
     return there ? mine : now;
   };
-
-  // Two steps are on their way while a third is worked on.
-  uint32_t is_now = 0, is_next = 0, is_then = 0;
-  if (step < step_end) {
-    look_ahead(step / kAhead);
-    look_ahead(step / kAhead + 1);
-    look(step);
-    look(step + 1);
-    wait_loads();
-    take_pages(step / kAhead);
-    is_now = fetch(step, 0, std::false_type());
-    look(step + 2);
-    if (step + 1 < step_end) {
-      if ((step + 1) % kAhead == 0) take_pages((step + 1) / kAhead);
-      is_next = fetch(step + 1, 1, std::false_type());
-    }
-    lds_barrier();
-  }
-
-  u32x4 qf[STEPS];
-  {
-    const uint16_t* qp = a.q + b * a.q_sb + h * a.q_sh + t * a.q_st + 8 * half;
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) qf[i] = there ? *reinterpret_cast<const u32x4*>(qp + 16 * i) : (u32x4)(0);
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) asm volatile("" : "+v"(qf[i]));  // (they are waited for here, and not by every step's products)
-  }
-  float slope = MODE == 1 && a.slopes ? a.slopes[h] * kLog2e : 0.0f;
-  asm volatile("" : "+v"(slope));
 
   float m = kNone, z = 0.0f;
   bool large = false;  // some reference is beyond kLarge
