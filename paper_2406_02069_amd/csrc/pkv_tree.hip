@@ -540,6 +540,65 @@ __global__ __launch_bounds__(256, (wide_per_unit<D>())) void tree_wide_kernel(co
   if (a.lse && end_half == 0) a.lse[lse_at(a, b, g, end_row)] = z == 0.0f ? kNone : (m - SHIFT + log2_(z)) * kLn2;
 }
 
+constexpr int kManyRows = 2048;
+// Ranges' results of many rows, joined: a row of them for every D / 4 threads, eight ranges at a time.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void tree_join_kernel(const TreeWideArgs a, int chunks) {
+  constexpr int ROWS = group_rows<TreeWideArgs>(), AT_ONCE = 8;
+  constexpr float UNIT = Weight<T>::HALF ? 1.0f / (1 << kWideShift) : 1.0f;
+  const int b = blockIdx.x / chunks;
+  int ranges = a.ranges, base = b * a.units * a.ranges;
+  if (a.by_length) {
+    const int lane = threadIdx.x & 63;
+    const Place p = a.B <= 64 ? place_of_sequence<1>(a, b, lane) : place_of_sequence<kLaneSequences>(a, b, lane);
+    ranges = p.ranges;
+    base = p.base;
+  }
+  const int h = (int)(blockIdx.x % chunks) * (256 / (D / 4)) + threadIdx.x / (D / 4), d4 = threadIdx.x % (D / 4);
+  if (ranges == 1 || h >= a.Hq) return;  // (written already)
+  const int h_in = h % a.G, g = h / a.G;
+  const int64_t at = ((int64_t)base + h_in / ROWS * a.Hkv + g) * ROWS + h_in % ROWS, step = (int64_t)ROWS * a.units;
+  float m = kNone, z = 0.0f;
+  f32x4 acc = (f32x4)(0.0f);
+  for (int i0 = 0; i0 < ranges; i0 += AT_ONCE) {
+    float m1[AT_ONCE], z1[AT_ONCE];
+    f32x4 v[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {  // (ranges behind the last one: that one, without weight)
+      const int64_t from = at + step * min(i0 + k, ranges - 1);
+      m1[k] = a.part_mz[from * 2];
+      z1[k] = a.part_mz[from * 2 + 1];
+      v[k] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + 4 * d4);
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) top = fmaxf(top, m1[k]);
+    const float ref = top == kNone ? 0.0f : top, f0 = exp2_(m - ref);
+    m = top;
+    z *= f0;
+    acc *= f0;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const float f1 = i0 + k < ranges ? exp2_(m1[k] - ref) : 0.0f;
+      z = fmaf(z1[k], f1, z);
+      acc = __builtin_elementwise_fma(v[k], (f32x4)(f1), acc);
+    }
+  }
+  if (__builtin_expect(!finite(acc), 0)) {  // (0 times an infinity is not what it should be)
+    acc = (f32x4)(0.0f);
+    const float ref = m == kNone ? 0.0f : m;
+#pragma unroll 1
+    for (int i = 0; i < ranges; ++i)
+      acc = weighed(acc, 1.0f, *reinterpret_cast<const f32x4*>(a.part_o + (at + step * i) * D + 4 * d4), exp2_(a.part_mz[(at + step * i) * 2] - ref));
+  }
+  const float inv = z == 0.0f ? 0.0f : 1.0f / z;
+  u32x2 w;
+  w[0] = pack2<T>(acc[0] * inv, acc[1] * inv);
+  w[1] = pack2<T>(acc[2] * inv, acc[3] * inv);
+  *reinterpret_cast<u32x2*>(a.out + out_at(a, b, g, h_in, D) + 4 * d4) = w;
+  if (d4 == 0 && a.lse) a.lse[lse_at(a, b, g, h_in)] = z == 0.0f ? kNone : (m + log2_(z * UNIT)) * kLn2;
+}
+
 template <typename T, int D>
 hipError_t launch_wide(const TreeWideArgs& a, int64_t workgroups, hipStream_t s) {
   if (a.cap.cap != 0.0f || a.slopes)
@@ -547,7 +606,14 @@ hipError_t launch_wide(const TreeWideArgs& a, int64_t workgroups, hipStream_t s)
   else
     hipLaunchKernelGGL((tree_wide_kernel<T, D, 0>), dim3((unsigned)workgroups), dim3(256), 0, s, a);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || a.ranges == 0 ? e : launch_join<T, D>(a, s);
+  if (e != hipSuccess || a.ranges == 0) return e;
+  if ((int64_t)a.B * a.Hq < kManyRows) {
+    hipLaunchKernelGGL((decode_long_join_kernel<T, D, 1, TreeWideArgs>), dim3((unsigned)(a.B * a.Hq)), dim3(256), 0, s, a);
+  } else {
+    const int chunks = (a.Hq + 1024 / D - 1) / (1024 / D);
+    hipLaunchKernelGGL((tree_join_kernel<T, D>), dim3((unsigned)(a.B * chunks)), dim3(256), 0, s, a, chunks);
+  }
+  return hipGetLastError();
 }
 
 // More than kFewRows query rows a KV head: the kernel above.  32/8 heads, d 128, behind 100k rows: 32 rows 91 us in decode_long_kernel,
