@@ -18,8 +18,8 @@
 //   values  O^T += V^T P^T, V read column-wise.  The weights are rounded to the type once (decode_long_kernel's second product for
 //           what the rounding left would take the pipe's time here: 24 products a step at d 128 in place of 16).
 // What is left at 64 tokens behind 100k rows: two workgroups a compute unit run at 1.6 GHz under this load, the matrix pipe busy 37 %
-// of it, and 512 ranges' results are 33 MB that are written and read again (13 us in the join).  Capped and biased scores are bound by
-// vector instructions (a batch of 26 tokens with 5000 kept rows each: 47 us + 13).
+// of it, and 512 ranges' results are 33 MB that are written and read again (9 us in the join).  Capped and biased scores are bound by
+// vector instructions (8 sequences of 26 tokens with up to 5000 kept rows: 46 us + 7).
 #include <type_traits>
 
 #include "pkv_long.h"
@@ -540,8 +540,11 @@ __global__ __launch_bounds__(256, (wide_per_unit<D>())) void tree_wide_kernel(co
   if (a.lse && end_half == 0) a.lse[lse_at(a, b, g, end_row)] = z == 0.0f ? kNone : (m - SHIFT + log2_(z)) * kLn2;
 }
 
-constexpr int kManyRows = 2048;
-// Ranges' results of many rows, joined: a row of them for every D / 4 threads, eight ranges at a time.
+constexpr int kFewJoined = 128;  // workgroups, and below decode_long_join_kernel
+// Ranges' results of many rows, joined: a row of them for every D / 4 threads, eight ranges at a time, with nothing to wait for but
+// loads.  32/8 heads, d 128, pages: 64 sequences of 16 tokens behind 2000 rows 126 us, by decode_long_join_kernel, whose workgroups share
+// out a row's ranges and meet, 151; 8 of 26 behind 5000 (28/4 heads) 36.7 and 41.4.  With fewer workgroups than compute units the many
+// ranges of a long cache bound it: behind 100k rows 16 tokens 91 and 87.7, 32 (128 workgroups) 95.7 and 96; behind 4000 rows 22 either way.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void tree_join_kernel(const TreeWideArgs a, int chunks) {
   constexpr int ROWS = group_rows<TreeWideArgs>(), AT_ONCE = 8;
@@ -607,10 +610,10 @@ hipError_t launch_wide(const TreeWideArgs& a, int64_t workgroups, hipStream_t s)
     hipLaunchKernelGGL((tree_wide_kernel<T, D, 0>), dim3((unsigned)workgroups), dim3(256), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.ranges == 0) return e;
-  if ((int64_t)a.B * a.Hq < kManyRows) {
+  const int chunks = (a.Hq + 1024 / D - 1) / (1024 / D);
+  if ((int64_t)a.B * chunks < kFewJoined) {
     hipLaunchKernelGGL((decode_long_join_kernel<T, D, 1, TreeWideArgs>), dim3((unsigned)(a.B * a.Hq)), dim3(256), 0, s, a);
   } else {
-    const int chunks = (a.Hq + 1024 / D - 1) / (1024 / D);
     hipLaunchKernelGGL((tree_join_kernel<T, D>), dim3((unsigned)(a.B * chunks)), dim3(256), 0, s, a, chunks);
   }
   return hipGetLastError();
