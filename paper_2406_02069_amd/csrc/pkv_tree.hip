@@ -2,15 +2,15 @@
 //
 //   out_t = sum_j 2^(s_tj - m_t) V_j / sum_j 2^(s_tj - m_t)  over the rows j that token t sees, m_t a running reference.
 // The T Hq/Hkv query rows of a KV head share its rows of the cache: the more of them, the more products for each byte.  Up to 32 rows
-// HBM bounds (decode_long_kernel, which is described in pkv_decode_long.hip: 8 tokens of 32/8 heads, d 128, behind 100k rows 91 us, 4.5
-// TB/s); from there on feeding the matrix pipe does (tree_wide_kernel: 16 tokens 87 us, 64 147, 128 256).  In both only the steps that
+// HBM bounds (decode_long_kernel, which is described in pkv_decode_long.hip: 8 tokens of 32/8 heads, d 128, behind 100k rows 93 us, 4.4
+// TB/s); from there on feeding the matrix pipe does (tree_wide_kernel: 16 tokens 87 us, 64 145 - 149, 128 256).  In both only the steps that
 // hold drafted tokens look at the tree: 32 of its bits are one word, shifted to the step.
 //
 // tree_wide_kernel: a workgroup is 128 query rows of a KV head x a range of its cache, a wave 32 of the rows against all keys of the
 // range, 32 at a time.  What a wave of decode_long_kernel reads for 16 rows serves 128 here: 64 tokens took 439 us there, 209 at once
 // with this split.
 //   loads   K and V straight into LDS, 8 rows of a step by each wave, two steps ahead in three buffers; a step waits for its own loads
-//           only and for the other waves once.  Rows of a page have one base where pages are of 8 k rows (page size 1: 177 us for the
+//           only and for the other waves once.  Rows of a page have one base where pages are of 8 k rows (page size 1: 179 us for the
 //           64 tokens); page numbers and positions come the same way, for eight steps at a time.
 //   scores  S^T = K Q^T in v_mfma_f32_32x32x16: 32 keys are the rows of A, 32 query rows the columns of B, which stay in registers.
 //           Lane (col, half) ends with 16 keys of row col.
