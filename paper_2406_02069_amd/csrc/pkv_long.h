@@ -17,7 +17,9 @@ constexpr int kWorkgroups = 512;   // at a time on the device: two per compute u
 constexpr int kLaneSequences = 4;  // sequences a lane looks after where ranges go by lengths,
 constexpr int kFlatBatch = 64 * kLaneSequences;  // and so many at most in all
 constexpr int kLeastTiles = 8;     // of a range,
-constexpr int kLeastWide = 12;     // of many query rows (whose results are more to join)
+// and of many query rows, whose results are more to join (32/8 heads, d 128: 64 tokens behind 4000 rows with 8, 12, 16 26.2, 27.6, 29.3 us,
+// 4 sequences of 32 tokens behind 3000 rows 28.5, 27.5, 29.1).
+constexpr int kLeastWide = 12;
 
 // What the kernel is built for: one token over all rows; the same, handing its scores on; drafted tokens; listed blocks of rows.
 // (kTreeWide: drafted tokens whose query rows are many, in pkv_tree.hip's own kernel.)
