@@ -244,6 +244,29 @@ def test_ragged_batches_of_all_sizes(B, Hkv, G, d, T, k_cap, page, window):
     _compare(out, lse, q, K, V, count, new, bits, window=window)
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,d,T,k_cap,page,dtype", [(9, 6, 2, 128, 33, 1700, 16, torch.bfloat16), (70, 5, 1, 64, 9, 900, 0, torch.float16),
+                                                           (3, 7, 1, 128, 59, 4000, 0, torch.float16), (66, 3, 1, 128, 13, 1300, 5, torch.bfloat16)])
+def test_many_rows_of_ragged_ranges(B, Hq, Hkv, d, T, k_cap, page, dtype):
+    # ranges of many rows, joined: sequences of none, one and many ranges, rows that are not there, infinities in some range's values,
+    # and whatever the workspace held
+    print("many rows", B, Hq, Hkv, d, T, k_cap, page, dtype, flush=True)
+    q, (K, V, Kc, Vc, table), tree, bits = _inputs(B, Hq, Hkv, d, T, k_cap, page, dtype, B)
+    count = torch.tensor([k_cap - (k_cap * i // 7) % k_cap for i in range(B)], dtype=torch.int32, device=DEV)
+    count[1], count[2] = 0, T + 40
+    new = torch.tensor([T - i % 4 for i in range(B)], dtype=torch.int32, device=DEV)
+    V[0, 0, 5, 3], V[0, 0, k_cap // 2, 3], V[0, 0, k_cap - T - 9, d - 1], V[2, 0, 20, 6] = math.inf, math.inf, -math.inf, math.nan
+    if page:
+        from tests.cache_ref import paged
+        Vc = paged(V, page, table, Vc.shape[0])
+    for fill in (255, 0):
+        ws = torch.full((1 << 28,), fill, dtype=torch.uint8, device=DEV)
+        out, lse = binding.tree_attention(q, Kc, Vc if page else V, count, tree=tree, new_lens=new, block_table=table, k_cap=k_cap, want_lse=True, workspace=ws)
+        torch.cuda.synchronize()
+        few = list(range(min(B, 9))) + ([B - 1] if B > 9 else [])
+        _compare(out[few], lse[few], q[few], K[few], V[few], count[few], new[few], [bits[b] for b in few])
+        assert not out[1].any() and bool(torch.isposinf(out[0, :Hq // Hkv, 0, 3]).all()) and bool(torch.isneginf(out[0, :Hq // Hkv, 0, d - 1]).all())
+
+
 def test_two_calls_at_once():
     B, Hq, Hkv, d, T, k_cap = 4, 32, 8, 128, 24, 5000
     q, (K, V, Kc, Vc, table), tree, bits = _inputs(B, Hq, Hkv, d, T, k_cap, 16, torch.bfloat16, 31)
