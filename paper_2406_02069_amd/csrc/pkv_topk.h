@@ -126,7 +126,10 @@ __device__ __forceinline__ Cutoff cutoff_of(const K& keys, const Met& own, int k
   tops = before_wave(lds, 0).all;
   uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)min_of_row((uint32_t)lds.sums[lane & 15][1])) + 1;
   const uint32_t high = (uint32_t)__builtin_amdgcn_readfirstlane((int)~min_of_row(~(uint32_t)lds.sums[lane & 15][2])) - 1;
-  if (tops >= k) return {kTop, k, tops == k};
+  if (tops >= k) {
+    __syncthreads();  // (all waves have read lds.sums: equal_before writes there)
+    return {kTop, k, tops == k};
+  }
   int left = k - tops, met = 0;
   uint32_t span = high - low;  // of the part that is looked at, less one
   for (;;) {

@@ -275,6 +275,23 @@ def test_evict_more_protected_rows_than_the_budget():
     _check(K, V, Kc, Vc, table, pos, w, count, 50, 3, 4, (po, wo, co), (torch.zeros_like(pos), torch.zeros_like(w)))
 
 
+@pytest.mark.parametrize("k_cap,budget", [(300, 50), (300, 299), (20000, 700), (70000, 3001)])
+def test_evict_repeated_positions(k_cap, budget):
+    # siblings of a drafted tree share positions: from one row too many that is protected to all of them, wherever they lie
+    print("evict repeated", k_cap, budget, flush=True)
+    K, V, Kc, Vc, table, pos, w, g = _case(1, 4, 64, k_cap, 0, torch.bfloat16, k_cap + 1)
+    K, V = K.clone(), V.clone()
+    some = torch.rand(1, 4, k_cap, generator=g, device=DEV).argsort(2)
+    pos += 4
+    for h, many in enumerate((budget + 1, budget + budget // 2, k_cap - k_cap // 8, k_cap)):
+        pos[0, h, some[0, h, :min(many, k_cap)]] = 2
+    count = torch.tensor([k_cap], dtype=torch.int32, device=DEV)
+    po, wo = torch.zeros_like(pos), torch.zeros_like(w)
+    co = binding.cache_evict(Kc, Vc, count, pos, w, budget, first=4, positions_out=po, weights_out=wo)
+    torch.cuda.synchronize()
+    _check(K, V, Kc, Vc, table, pos, w, count, budget, 0, 4, (po, wo, co), (torch.zeros_like(pos), torch.zeros_like(w)))
+
+
 def test_evict_pages_that_do_not_exist():
     B, Hkv, d, k_cap, page, budget = 2, 2, 64, 160, 16, 64
     K, V, Kc, Vc, table, pos, w, g = _case(B, Hkv, d, k_cap, page, torch.bfloat16, 21)
