@@ -76,8 +76,12 @@ __global__ __launch_bounds__(256) void join_and_weigh_kernel(const WeighArgs a, 
     heads_of_unit<T>(a, b, g, lds_mz);
     __syncthreads();
     float sum[kRowsAtATime];
+    bool saw[kRowsAtATime];  // (rows that no head sees are not written, not even with what they hold)
 #pragma unroll
-    for (int i = 0; i < kRowsAtATime; ++i) sum[i] = 0.0f;
+    for (int i = 0; i < kRowsAtATime; ++i) {
+      sum[i] = 0.0f;
+      saw[i] = false;
+    }
     const float* const s = a.scores + (int64_t)unit * a.G * a.score_row;
 #pragma unroll 2
     for (int h = 0; h < a.G; ++h) {
@@ -86,13 +90,17 @@ __global__ __launch_bounds__(256) void join_and_weigh_kernel(const WeighArgs a, 
 #pragma unroll
       for (int i = 0; i < kRowsAtATime; ++i) x[i] = s[h * a.score_row + min(max(r0 + 256 * i, lo), hi - 1)];
 #pragma unroll
-      for (int i = 0; i < kRowsAtATime; ++i) sum[i] += x[i] == kNone || factor == 0.0f ? 0.0f : exp2_(x[i] - ref) * factor;
+      for (int i = 0; i < kRowsAtATime; ++i) {
+        const bool sees = x[i] != kNone && factor != 0.0f;
+        sum[i] += sees ? exp2_(x[i] - ref) * factor : 0.0f;
+        saw[i] = saw[i] || sees;
+      }
     }
     float* const w = a.weights + b * a.w_sb + g * a.w_sh;
 #pragma unroll
     for (int i = 0; i < kRowsAtATime; ++i) {
       const int r = r0 + 256 * i;
-      if (r >= lo && r < hi) w[r] += sum[i];
+      if (r >= lo && r < hi && saw[i]) w[r] += sum[i];
     }
   }
 }

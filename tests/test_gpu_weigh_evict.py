@@ -121,6 +121,36 @@ def test_nothing_of_the_workspace_reaches_the_weights():
         _compare(out, lse, weights, before, q, K, V, count, None, q_pos, window=100)
 
 
+@pytest.mark.parametrize("k_cap", [900, 12000])
+def test_weights_of_rows_that_are_not_seen_are_not_written(k_cap):
+    # bit by bit: a negative zero plus zero is a positive one.  In front of the window, behind the query, without a position, on a page that
+    # does not exist, behind the last row, and where the query sees nothing
+    print("unseen", k_cap, flush=True)
+    B, Hq, Hkv, d, page = 4, 8, 2, 64, 16
+    g = torch.Generator(device=DEV).manual_seed(k_cap)
+    q = torch.randn(B, Hq, d, generator=g, device=DEV).to(torch.bfloat16)
+    _, _, Kc, Vc, table = make_cache(B, Hkv, k_cap, d, torch.bfloat16, page, g)
+    table[0, k_cap // page - 3] = -1
+    j = torch.arange(k_cap, device=DEV)
+    pos = j.to(torch.int32).expand(B, Hkv, k_cap).contiguous()
+    pos[0, :, k_cap - 30:k_cap - 20] = -1
+    count = torch.tensor([k_cap, k_cap - 7, k_cap, 0], dtype=torch.int32, device=DEV)
+    q_pos = torch.tensor([k_cap - 4, k_cap - 8, -1, 5], dtype=torch.int32, device=DEV)
+    absent = torch.zeros(B, k_cap, dtype=torch.bool, device=DEV)
+    absent[0, (k_cap // page - 3) * page:(k_cap // page - 2) * page] = True
+    for positions, window in ((pos, 0), (pos, 101), (None, 101), (None, 0)):
+        weights = torch.full((B, Hkv, k_cap), -0.0, device=DEV)
+        binding.decode_attention_accumulate(q, Kc, Vc, count, weights, block_table=table, k_cap=k_cap, positions=positions, q_pos=q_pos, window=window)
+        torch.cuda.synchronize()
+        p = pos if positions is not None else j.expand(B, Hkv, k_cap)
+        at = q_pos[:, None, None]
+        seen = (j < count[:, None, None]) & (p >= 0) & (p <= at) & ~absent[:, None]
+        if window:
+            seen &= p > at - window
+        assert bool((weights[seen] > 0).all()) and bool(seen[:2].any(2).all())
+        assert bool((weights[~seen].view(torch.int32) == -2 ** 31).all())
+
+
 def test_weights_from_a_graph_and_two_calls_at_once():
     B, Hq, Hkv, d, k_cap = 2, 32, 8, 128, 6000
     g = torch.Generator(device=DEV).manual_seed(7)
