@@ -831,8 +831,9 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q,
  * Nothing else of weights is written.  Same descriptor, results and errors
  * (PKV_ERR_UNSUPPORTED also B * Hq > 2^23).
  * weights   DEVICE fp32 [B,Hkv,k_cap], 4-byte aligned, with element strides w_sb
- *           and w_sh (>= 0, and >= k_cap where there are several sequences or
- *           heads: their sums do not overlap).
+ *           and w_sh >= 0, in either order.  Sums do not overlap: where there
+ *           are several sequences or heads, the smaller stride is >= k_cap and
+ *           the larger one reaches behind all that the smaller one spans.
  * workspace DEVICE, 256-byte aligned,
  *           >= pkv_decode_accumulate_workspace_bytes(desc) bytes; contents
  *           irrelevant on entry, undefined on exit; concurrent calls need
@@ -886,9 +887,10 @@ typedef struct {
 size_t pkv_evict_workspace_bytes(const pkv_evict_desc* desc);
 
 /*
- * desc        HOST.  What is written has places of its own: po_* and wo_* are >=
- *             k_cap and c_* >= d, where there are several sequences, heads or
- *             rows.
+ * desc        HOST.  What is written has places of its own: of po_*, of wo_* and
+ *             of c_* the smallest stride is >= k_cap (c_*: d) and each larger one
+ *             reaches behind all that the smaller ones span, where there are
+ *             several sequences, heads or rows.
  * K_cache, V_cache
  *             DEVICE, rows of d 16-bit elements, 16-byte aligned, compact or
  *             pools; rows behind the budget keep their content.  Pages that

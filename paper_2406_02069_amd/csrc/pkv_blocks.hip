@@ -347,7 +347,7 @@ int pkv_block_bounds(const pkv_block_desc* desc, const void* K_cache, const int3
   if (rc != PKV_OK) return rc;
   const pkv_block_desc& d = *desc;
   if (!good_strides(d.b_sb, d.b_sh, 0) || !aligned(K_cache, 16) || !aligned(bounds, 16) || !aligned(block_table, 4) || !aligned(count, 4) ||
-      !aligned(new_lens, 4) || (d.page_size > 0 && !block_table) || !apart(d.B, d.Hkv, blocks_of(d) * 2 * d.d, d.b_sb, d.b_sh))
+      !aligned(new_lens, 4) || (d.page_size > 0 && !block_table) || !apart(blocks_of(d) * 2 * d.d, {{d.B, d.b_sb}, {d.Hkv, d.b_sh}}))
     return PKV_ERR_INVALID_ARG;
   BoundsArgs a;
   memset(&a, 0, sizeof(a));

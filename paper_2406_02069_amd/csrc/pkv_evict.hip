@@ -388,8 +388,8 @@ int pkv_cache_evict(const pkv_evict_desc* desc, void* K_cache, void* V_cache, co
       !aligned(weights, 4) || !aligned(positions_out, 4) || !aligned(weights_out, 4) || !aligned(count_out, 4))
     return PKV_ERR_INVALID_ARG;
   if (d.page_size > 0 && !block_table) return PKV_ERR_INVALID_ARG;
-  if (!apart(d.B, d.Hkv, d.k_cap, d.po_sb, d.po_sh) || !apart(d.B, d.Hkv, d.k_cap, d.wo_sb, d.wo_sh)) return PKV_ERR_INVALID_ARG;
-  if (d.page_size == 0 && (!apart(d.B, d.Hkv, d.d, d.c_sb, d.c_sh) || (d.k_cap > 1 && d.c_st < d.d))) return PKV_ERR_INVALID_ARG;
+  if (!apart(d.k_cap, {{d.B, d.po_sb}, {d.Hkv, d.po_sh}}) || !apart(d.k_cap, {{d.B, d.wo_sb}, {d.Hkv, d.wo_sh}})) return PKV_ERR_INVALID_ARG;
+  if (d.page_size == 0 && !apart(d.d, {{d.B, d.c_sb}, {d.Hkv, d.c_sh}, {d.k_cap, d.c_st}})) return PKV_ERR_INVALID_ARG;
   if (positions_out == positions && (d.po_sb != d.p_sb || d.po_sh != d.p_sh)) return PKV_ERR_INVALID_ARG;
   if (weights_out == weights && (d.wo_sb != d.w_sb || d.wo_sh != d.w_sh)) return PKV_ERR_INVALID_ARG;
   if (count_out == count) return PKV_ERR_INVALID_ARG;

@@ -875,8 +875,30 @@ inline int check_long_call(const pkv_decode_long_desc* desc, const void* q, cons
   return PKV_OK;
 }
 
-// Whether places of [B, Hkv, n] with these strides, neighbours in the last dimension, are distinct: what a call writes must be.
-inline bool apart(int64_t B, int64_t Hkv, int64_t n, int64_t sb, int64_t sh) { return (B == 1 || sb >= n) && (Hkv == 1 || sh >= n); }
+// Whether places of a tensor are distinct, as what a call writes must be: `inner` neighbours, and dimensions of `size` places that lie
+// `stride` apart, in any order.  Of those with several places each stride has to reach behind all that the smaller ones span.  (Enough
+// for it; slices and transposes of a contiguous tensor are like that.)
+struct Dim {
+  int64_t size, stride;
+};
+template <int N>
+bool apart(int64_t inner, Dim (&&dims)[N]) {
+  int64_t span = inner;
+  for (int i = 0; i < N; ++i) {
+    for (int k = i + 1; k < N; ++k) {
+      if (dims[k].stride < dims[i].stride) {
+        const Dim d = dims[i];
+        dims[i] = dims[k];
+        dims[k] = d;
+      }
+    }
+    if (dims[i].size <= 1) continue;
+    if (dims[i].stride < span) return false;
+    const int64_t steps = dims[i].size - 1;
+    span = dims[i].stride > (INT64_MAX - span) / steps ? INT64_MAX : span + dims[i].stride * steps;
+  }
+  return true;
+}
 
 inline uint32_t magic_of(int page_size) { return page_size > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint32_t)page_size) : 0xFFFFFFFFu; }
 

@@ -163,7 +163,7 @@ int pkv_decode_attention_accumulate(const pkv_decode_long_desc* desc, const void
   if (rc != PKV_OK) return rc;
   if (check_accumulate_desc(desc) != PKV_OK) return PKV_ERR_UNSUPPORTED;
   const pkv_decode_long_desc& d = *desc;
-  if (!apart(d.B, d.Hkv, d.k_cap, w_sb, w_sh)) return PKV_ERR_INVALID_ARG;
+  if (!apart(d.k_cap, {{d.B, w_sb}, {d.Hkv, w_sh}})) return PKV_ERR_INVALID_ARG;
   const WeighPlan p = plan_of(d);
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < p.all) return PKV_ERR_WORKSPACE;
   WeighArgs a;

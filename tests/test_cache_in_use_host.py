@@ -264,6 +264,28 @@ def test_places_written_twice_refused():
         assert _bounds(_block_desc(**kw)) == I, kw
 
 
+def test_places_that_interleave_refused():
+    # every stride large enough by itself, and two places in one all the same
+    n, c = 8192, 8192 * 128
+    for kw in (dict(B=2, po_sb=n, po_sh=n), dict(B=2, wo_sb=n, wo_sh=n), dict(B=2, wo_sb=4 * n, wo_sh=n), dict(B=2, c_sb=c, c_sh=c), dict(c_sh=128, c_st=128),
+               dict(c_sh=128, c_st=7 * 128), dict(B=2, c_sb=128, c_sh=256, c_st=8 * 128), dict(B=2, po_sh=2 ** 61, po_sb=2 ** 61)):
+        assert _evict(_evict_desc(**kw)) == I, kw
+    for kw in (dict(w_sb=n, w_sh=n), dict(w_sb=7 * n, w_sh=n), dict(w_sb=n, w_sh=2 * n - 1)):
+        assert _weigh(_long_desc(B=2, c_sb=8 * c), **kw) == I, kw
+    for kw in (dict(b_sb=512 * 256, b_sh=512 * 256), dict(b_sb=7 * 512 * 256)):
+        assert _bounds(_block_desc(B=2, **kw)) == I, kw
+
+
+def test_places_of_any_order_taken():
+    # (as far as the workspace, which is not there)
+    n, c = 8192, 8192 * 128
+    for kw in (dict(B=2, po_sb=n, po_sh=2 * n, wo_sb=n + 5, wo_sh=2 * n + 77), dict(B=3, c_sb=128, c_sh=3 * 128, c_st=24 * 128), dict(c_sh=128, c_st=8 * 128),
+               dict(c_sb=0), dict(Hkv=1, c_sh=0, po_sh=0), dict(k_cap=1, budget=1, recent=0, first=0, c_st=0), dict(B=2, po_sb=2 ** 62, wo_sb=2 ** 62)):
+        assert _evict(_evict_desc(**kw), ws=None) == W, kw
+    for kw in (dict(w_sb=n, w_sh=2 * n), dict(w_sb=8 * n, w_sh=n)):
+        assert _weigh(_long_desc(B=2), ws=None, **kw) == W, kw
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     q, K = torch.zeros(1, 8, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 16, 64, dtype=torch.bfloat16)
     n, w, p = torch.zeros(1, dtype=torch.int32), torch.zeros(1, 2, 16), torch.zeros(1, 2, 16, dtype=torch.int32)
