@@ -793,7 +793,8 @@ size_t pkv_tree_workspace_bytes(const pkv_tree_desc* desc);
 /*
  * desc        HOST.  Strides are >= 0 and multiples of 8 (p_*: any >= 0).
  * q, out      DEVICE, of the descriptor's type, 16-byte aligned; out overlaps
- *             nothing, and its rows not one another.
+ *             nothing, and its rows not one another: sorted by size, each of
+ *             its strides reaches behind all that the smaller ones span.
  * K_cache, V_cache
  *             DEVICE, 16-byte aligned: compact with strides c_*, or pools
  *             [num_pages,Hkv,page_size,d] contiguous.

@@ -697,6 +697,7 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q, const void* K_c
       !aligned(slopes, 4) || !aligned(lse_out, 4))
     return PKV_ERR_INVALID_ARG;
   if ((d.page_size > 0 && !block_table) || !positions != !q_pos) return PKV_ERR_INVALID_ARG;
+  if (!apart(d.d, {{d.B, d.o_sb}, {d.Hq, d.o_sh}, {d.T, d.o_st}})) return PKV_ERR_INVALID_ARG;
   const size_t need = pkv_tree_workspace_bytes(desc);
   if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return PKV_ERR_WORKSPACE;
   TreeWideArgs a;

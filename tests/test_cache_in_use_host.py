@@ -274,6 +274,8 @@ def test_places_that_interleave_refused():
         assert _weigh(_long_desc(B=2, c_sb=8 * c), **kw) == I, kw
     for kw in (dict(b_sb=512 * 256, b_sh=512 * 256), dict(b_sb=7 * 512 * 256)):
         assert _bounds(_block_desc(B=2, **kw)) == I, kw
+    for kw in (dict(o_sh=0), dict(o_st=0), dict(o_sh=120), dict(o_sh=128), dict(o_sh=15 * 128), dict(o_st=2048), dict(B=2, o_sb=0), dict(B=2, o_sb=31 * 2048)):
+        assert _tree(_tree_desc(**kw)) == I, kw
 
 
 def test_places_of_any_order_taken():
@@ -284,6 +286,8 @@ def test_places_of_any_order_taken():
         assert _evict(_evict_desc(**kw), ws=None) == W, kw
     for kw in (dict(w_sb=n, w_sh=2 * n), dict(w_sb=8 * n, w_sh=n)):
         assert _weigh(_long_desc(B=2), ws=None, **kw) == W, kw
+    for kw in (dict(o_st=32 * 128, o_sh=128), dict(o_sb=0), dict(T=2, Hq=256, Hkv=8, o_st=256 * 128, o_sh=128), dict(B=2, o_sb=128, o_sh=256, o_st=32 * 256)):
+        assert _tree(_tree_desc(**kw), ws=None) == W, kw
 
 
 def test_binding_refuses_tensors_that_do_not_fit():
