@@ -17,7 +17,7 @@ namespace pkv {
 namespace {
 
 constexpr int kMovedHere = 64;  // rows that the first launch moves by itself
-constexpr int kPairs = 32;      // of a workgroup of the second launch
+constexpr int kPairs = 32;      // of an item of the second launch
 
 struct EvictArgs {
   char *K, *V;
@@ -325,24 +325,29 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs 
   }
 }
 
-// A workgroup: kPairs rows of K and of V, 16 bytes a thread at a time, and its share of the rows that are emptied.
-__global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a, int chunks) {
-  const int unit = blockIdx.x / chunks, chunk = blockIdx.x % chunks, b = unit / a.Hkv, g = unit % a.Hkv;
-  const int moves = a.moves[unit], lanes = a.d / 8, n = min(max(a.count[b], 0), a.k_cap);
-  int32_t* const pos_out = a.positions_out + b * a.po_sb + g * a.po_sh;
-  float* const weight_out = a.weights_out + b * a.wo_sb + g * a.wo_sh;
-  for (int64_t r = a.budget + (int64_t)chunk * 256 + threadIdx.x; r < n; r += (int64_t)chunks * 256) {
-    pos_out[r] = -1;
-    weight_out[r] = 0.0f;
-  }
-  const int32_t *const to = a.pairs + (int64_t)unit * 2 * a.most, *const from = to + a.most;
-  for (int64_t c = chunk; c * kPairs < moves; c += chunks) {
-    for (int i = threadIdx.x; i < kPairs * lanes; i += 256) {
-      const int p = (int)(c * kPairs) + i / lanes;
+// An item: `share` rows of K and of V of a head, 16 bytes a thread at a time, and its share of the rows that are emptied.
+__global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a, int chunks, int share, Items items) {
+  const int lanes = a.d / 8;
+  auto rows_of = [&](int b) { return min(max(a.count[b], 0), a.k_cap); };
+  auto has = [&](int unit, int chunk) {
+    const int moves = a.moves[unit], n = rows_of(unit / a.Hkv);
+    return (int64_t)chunk * share < moves || a.budget + (int64_t)chunk * 256 < n;
+  };
+  each_item(items, blockIdx.x, gridDim.x, has, [&](int unit, int chunk) {
+    const int b = unit / a.Hkv, g = unit % a.Hkv, moves = a.moves[unit], n = rows_of(b);
+    int32_t* const pos_out = a.positions_out + b * a.po_sb + g * a.po_sh;
+    float* const weight_out = a.weights_out + b * a.wo_sb + g * a.wo_sh;
+    for (int64_t r = a.budget + (int64_t)chunk * 256 + threadIdx.x; r < n; r += (int64_t)chunks * 256) {
+      pos_out[r] = -1;
+      weight_out[r] = 0.0f;
+    }
+    const int32_t *const to = a.pairs + (int64_t)unit * 2 * a.most, *const from = to + a.most;
+    for (int i = threadIdx.x; i < share * lanes; i += 256) {
+      const int p = chunk * share + i / lanes;
       if (p >= moves) break;
       move_piece(a, b, g, to[p], from[p], i % lanes);
     }
-  }
+  });
 }
 
 int check_evict_desc(const pkv_evict_desc* desc) {
@@ -419,9 +424,11 @@ int pkv_cache_evict(const pkv_evict_desc* desc, void* K_cache, void* V_cache, co
   hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)units), dim3(kThreads), (size_t)a.in_lds * sizeof(uint32_t), st, a);
   if (hipGetLastError() != hipSuccess) return PKV_ERR_HIP;
   if (!a.second) return PKV_OK;
-  int64_t chunks = (a.most + kPairs - 1) / kPairs;
-  if (chunks > kMaxGrid / units) chunks = kMaxGrid / units;
-  hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(units * chunks)), dim3(256), 0, st, a, (int)chunks);
+  int64_t share = kPairs;
+  while (units * ((a.most + share - 1) / share) > kMostItems) share *= 2;
+  const int chunks = (int)((a.most + share - 1) / share);
+  const Items items = items_of(units, chunks);
+  hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)workgroups_of(items)), dim3(256), 0, st, a, chunks, (int)share, items);
   return hipGetLastError() == hipSuccess ? PKV_OK : PKV_ERR_HIP;
 }
 

@@ -86,6 +86,43 @@ struct Weight {
 
 constexpr int kWideShift = 8;  // kTreeWide, fp16: as pkv_prefill.hip has it
 
+// As many workgroups as a launch whose items follow the room of a cache starts at most: two turns of the device, eight of 256 threads per
+// compute unit.  Most of a large cache's room holds no rows yet, and a workgroup that finds nothing to do still has to be started: one row
+// too many in 64 sequences of 8 heads, room for 4096 rows, 30 us with a workgroup for each item, 16 with these.  A prime, so that the items
+// of one head spread over all of them (one sequence of 64 evicted from 16k rows to 2k: 37 us, with 2048 workgroups 56).  With 2039 and 8191:
+// 15 and 18, 33 and 41; 64 sequences evicted from 4096 rows to 2048 157 and 146, with these 148.
+constexpr int kMostWorkgroups = 4093;
+// The items: `chunks` chunks of each of `units` heads.  Where there are no more than workgroups, neighbours have neighbouring chunks of a head
+// (weights of 100k and 25k rows 121 us, 125 the other way round); otherwise the heads' first chunks come first, which spreads what there is
+// where heads have few (weights of 64 sequences of 2000 rows with room for 16k 83 us, head by head 99).
+struct Items {
+  uint32_t all;           // units * chunks, below 2^31
+  uint32_t minor, magic;  // chunks, or units; magic_of(minor)
+  bool by_head;
+};
+// A workgroup's items, every stride-th from its first one on: work(unit, chunk).  A lane looks whether one of 64 has something to do, so that
+// those that have not cost one look together; all waves of the workgroup come to the same.
+template <typename Has, typename Work>
+__device__ __forceinline__ void each_item(const Items& items, uint32_t first, uint32_t stride, Has has, Work work) {
+  auto major_of = [&](uint32_t item) {
+    const uint32_t m = __umulhi(item, items.magic);
+    return m + (item - m * items.minor >= items.minor);
+  };
+  if (items.by_head) {
+    const uint32_t unit = major_of(first);
+    work((int)unit, (int)(first - unit * items.minor));
+    return;
+  }
+  const uint32_t lane = threadIdx.x & 63;
+  for (uint32_t i0 = first; i0 < items.all; i0 += 64 * stride) {
+    const uint32_t own = min(i0 + lane * stride, items.all - 1), chunk = major_of(own), unit = own - chunk * items.minor;
+    for (uint64_t left = __ballot(i0 + lane * stride < items.all && has((int)unit, (int)chunk)); left != 0; left &= left - 1) {
+      const int l = __builtin_ctzll(left);
+      work(__builtin_amdgcn_readlane((int)unit, l), __builtin_amdgcn_readlane((int)chunk, l));
+    }
+  }
+}
+
 // A wave's reads and writes of its own part of LDS keep their order.
 __device__ __forceinline__ void own_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
@@ -901,6 +938,14 @@ bool apart(int64_t inner, Dim (&&dims)[N]) {
 }
 
 inline uint32_t magic_of(int page_size) { return page_size > 1 ? (uint32_t)(((uint64_t)1 << 32) / (uint32_t)page_size) : 0xFFFFFFFFu; }
+
+inline Items items_of(int64_t units, int64_t chunks) {
+  const bool by_head = units * chunks <= kMostWorkgroups;
+  const int minor = (int)(by_head ? chunks : units);
+  return {(uint32_t)(units * chunks), (uint32_t)minor, magic_of(minor), by_head};
+}
+inline int64_t workgroups_of(const Items& items) { return items.all < kMostWorkgroups ? items.all : kMostWorkgroups; }
+constexpr int64_t kMostItems = ((int64_t)1 << 31) - 1;
 
 // The fields that a descriptor gives; rows: query rows that share a KV head.
 template <typename Desc>
