@@ -830,7 +830,8 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q,
  * over the query heads of its KV head, to a running sum:
  *   weights[b][g][j] += sum_{h of g} softmax_j(s_h)   for every seen row j.
  * Nothing else of weights is written.  Same descriptor, results and errors
- * (PKV_ERR_UNSUPPORTED also B * Hq > 2^23).
+ * (PKV_ERR_UNSUPPORTED also B * Hq > 2^23, or more than 2^31 - 1 times 1024 rows
+ * of all heads).
  * weights   DEVICE fp32 [B,Hkv,k_cap], 4-byte aligned, with element strides w_sb
  *           and w_sh >= 0, in either order.  Sums do not overlap: where there
  *           are several sequences or heads, the smaller stride is >= k_cap and

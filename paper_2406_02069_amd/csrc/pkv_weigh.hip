@@ -61,17 +61,28 @@ __device__ __forceinline__ void heads_of_unit(const WeighArgs& a, int b, int g, 
 
 // The first `joins` workgroups join ranges, HEADS heads each; the others add weights, kChunk rows of a KV head at a time.
 template <typename T, int D, int HEADS>
-__global__ __launch_bounds__(256) void join_and_weigh_kernel(const WeighArgs a, int joins, int chunks, int64_t items) {
+__global__ __launch_bounds__(256) void join_and_weigh_kernel(const WeighArgs a, int joins, Items items) {
   if ((int)blockIdx.x < joins) {
     join_heads<T, D, HEADS>(a);
     return;
   }
   __shared__ float lds_mz[kMostHeads][2];
-  for (int64_t item = (int)blockIdx.x - joins; item < items; item += gridDim.x - joins) {
-    const int unit = (int)(item / chunks), chunk = (int)(item % chunks), b = unit / a.Hkv, g = unit % a.Hkv;
+  struct Rows {
+    int lo, hi;  // visited
+  };
+  auto rows_of = [&](int b) {
     const Tiles tl = tiles_of(a, b);
-    const int lo = tl.first * kTile, hi = min(tl.n, (tl.first + tl.count) * kTile), r0 = chunk * kChunk + threadIdx.x;
-    if (chunk * kChunk >= hi || (chunk + 1) * kChunk <= lo) continue;
+    return Rows{tl.first * kTile, min(tl.n, (tl.first + tl.count) * kTile)};
+  };
+  auto has = [&](int unit, int chunk) {
+    const Rows rows = rows_of(unit / a.Hkv);
+    return chunk * kChunk < rows.hi && (chunk + 1) * kChunk > rows.lo;
+  };
+  each_item(items, blockIdx.x - joins, gridDim.x - joins, has, [&](int unit, int chunk) {
+    const int b = unit / a.Hkv, g = unit % a.Hkv;
+    const Rows rows = rows_of(b);
+    const int lo = rows.lo, hi = rows.hi, r0 = chunk * kChunk + threadIdx.x;
+    if (chunk * kChunk >= hi || (chunk + 1) * kChunk <= lo) return;
     __syncthreads();  // (the last item's have been read)
     heads_of_unit<T>(a, b, g, lds_mz);
     __syncthreads();
@@ -102,27 +113,30 @@ __global__ __launch_bounds__(256) void join_and_weigh_kernel(const WeighArgs a, 
       const int r = r0 + 256 * i;
       if (r >= lo && r < hi && saw[i]) w[r] += sum[i];
     }
-  }
+  });
 }
 
 template <typename T, int D>
-hipError_t launch_weigh(const WeighArgs& a, int64_t workgroups, int chunks, int64_t items, hipStream_t s) {
+hipError_t launch_weigh(const WeighArgs& a, int64_t workgroups, const Items& items, hipStream_t s) {
   const hipError_t e = launch_long<T, D>(a, workgroups, s);
   if (e != hipSuccess) return e;
   const bool four = a.Hq % 4 == 0 && a.B * a.Hq >= 4 * kWorkgroups;  // (as launch_join)
-  const int64_t joins = a.ranges == 0 ? 0 : (int64_t)a.B * a.Hq / (four ? 4 : 1), most = kMaxGrid - joins;
-  const dim3 grid((unsigned)(joins + (items < most ? items : most)));
+  const int64_t joins = a.ranges == 0 ? 0 : (int64_t)a.B * a.Hq / (four ? 4 : 1);
+  const dim3 grid((unsigned)(joins + workgroups_of(items)));
   if (four)
-    hipLaunchKernelGGL((join_and_weigh_kernel<T, D, 4>), grid, dim3(256), 0, s, a, (int)joins, chunks, items);
+    hipLaunchKernelGGL((join_and_weigh_kernel<T, D, 4>), grid, dim3(256), 0, s, a, (int)joins, items);
   else
-    hipLaunchKernelGGL((join_and_weigh_kernel<T, D, 1>), grid, dim3(256), 0, s, a, (int)joins, chunks, items);
+    hipLaunchKernelGGL((join_and_weigh_kernel<T, D, 1>), grid, dim3(256), 0, s, a, (int)joins, items);
   return hipGetLastError();
 }
 
-// (joins and weights share a launch)
+int64_t chunks_of(const pkv_decode_long_desc& d) { return ((int64_t)d.k_cap + kChunk - 1) / kChunk; }
+
+// (joins and weights share a launch; its items are counted in 32 bits)
 int check_accumulate_desc(const pkv_decode_long_desc* desc) {
   const int rc = check_long_desc(desc);
-  return rc == PKV_OK && (int64_t)desc->B * desc->Hq > 1 << 23 ? PKV_ERR_UNSUPPORTED : rc;
+  if (rc != PKV_OK) return rc;
+  return (int64_t)desc->B * desc->Hq > 1 << 23 || (int64_t)desc->B * desc->Hkv * chunks_of(*desc) > kMostItems ? PKV_ERR_UNSUPPORTED : PKV_OK;
 }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -179,13 +193,12 @@ int pkv_decode_attention_accumulate(const pkv_decode_long_desc* desc, const void
   a.weights = weights;
   a.w_sb = w_sb; a.w_sh = w_sh;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const int chunks = (int)((p.score_row + kChunk - 1) / kChunk);
-  const int64_t items = (int64_t)d.B * d.Hkv * chunks;
+  const Items items = items_of((int64_t)d.B * d.Hkv, chunks_of(d));
   hipError_t e;
   if (d.dtype == PKV_BF16)
-    e = d.d == 128 ? launch_weigh<__bf16, 128>(a, p.grid.workgroups, chunks, items, st) : launch_weigh<__bf16, 64>(a, p.grid.workgroups, chunks, items, st);
+    e = d.d == 128 ? launch_weigh<__bf16, 128>(a, p.grid.workgroups, items, st) : launch_weigh<__bf16, 64>(a, p.grid.workgroups, items, st);
   else
-    e = d.d == 128 ? launch_weigh<_Float16, 128>(a, p.grid.workgroups, chunks, items, st) : launch_weigh<_Float16, 64>(a, p.grid.workgroups, chunks, items, st);
+    e = d.d == 128 ? launch_weigh<_Float16, 128>(a, p.grid.workgroups, items, st) : launch_weigh<_Float16, 64>(a, p.grid.workgroups, items, st);
   return e == hipSuccess ? PKV_OK : PKV_ERR_HIP;
 }
 

@@ -110,6 +110,13 @@ def test_weigh_not_built(kw):
     assert _weigh(_long_desc(**kw), table=0x6000, n=1 << 50) == U
 
 
+def test_weigh_of_too_many_rows_refused():
+    for kw in (dict(B=65535, Hkv=128, Hq=128, k_cap=2 ** 18 + 2 ** 11), dict(B=4096, Hkv=512, Hq=512, k_cap=2 ** 20)):
+        assert _weigh(_long_desc(**kw), n=1 << 60) == U, kw
+        assert binding.load().pkv_decode_accumulate_workspace_bytes(_ref(_long_desc(**kw))) == 0
+    assert binding.load().pkv_decode_accumulate_workspace_bytes(_ref(_long_desc(B=4096, Hkv=512, Hq=512, k_cap=2 ** 20 - 1024))) > 0
+
+
 def test_weigh_pointers_and_workspace_refused():
     good = _long_desc()
     need = binding.load().pkv_decode_accumulate_workspace_bytes(_ref(good))
