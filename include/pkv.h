@@ -749,10 +749,10 @@ int pkv_decode_attention_long(const pkv_decode_long_desc* desc, const void* q,
  * itself.  Rows t >= new_b, and rows that see nothing: zero and -inf.
  * Scores, softmax and lse as pkv_decode_attention_long has them, the softmax
  * weights' rounding too, or, where T * Hq/Hkv > 32, as pkv_prefill_attention
- * has it.  A key that a token does not see has no influence on its row beyond
- * rounding, whatever it holds; where a token sees values of V that are not
- * finite, that element of out is their sum.  A page number out of range makes
- * its rows count as absent.
+ * has it: a token's bits depend on how many there are beside it.  A key that a
+ * token does not see has no influence on its row beyond rounding, whatever it
+ * holds; where a token sees values of V that are not finite, that element of
+ * out is their sum.  A page number out of range makes its rows count as absent.
  */
 typedef struct {
   int32_t B, Hq, Hkv; /* Hq % Hkv == 0                                       */
@@ -830,14 +830,16 @@ int pkv_tree_attention(const pkv_tree_desc* desc, const void* q,
  * over the query heads of its KV head, to a running sum:
  *   weights[b][g][j] += sum_{h of g} softmax_j(s_h)   for every seen row j.
  * Nothing else of weights is written.  Same descriptor, results and errors
- * (PKV_ERR_UNSUPPORTED also B * Hq > 2^23, or more than 2^31 - 1 times 1024 rows
- * of all heads).
+ * (PKV_ERR_UNSUPPORTED also B * Hq > 2^23, or B * Hkv * ceil(k_cap / 1024) >=
+ * 2^31).
  * weights   DEVICE fp32 [B,Hkv,k_cap], 4-byte aligned, with element strides w_sb
  *           and w_sh >= 0, in either order.  Sums do not overlap: where there
  *           are several sequences or heads, the smaller stride is >= k_cap and
  *           the larger one reaches behind all that the smaller one spans.
  * workspace DEVICE, 256-byte aligned,
- *           >= pkv_decode_accumulate_workspace_bytes(desc) bytes; contents
+ *           >= pkv_decode_accumulate_workspace_bytes(desc) bytes (the scores,
+ *           4 * B * Hq * k_cap bytes, beside what the attention alone takes: as
+ *           much as the cache itself where d heads share a KV head); contents
  *           irrelevant on entry, undefined on exit; concurrent calls need
  *           distinct ones.
  * A weight is exact to a few 2^-24 of itself times its score's size, and the
@@ -889,10 +891,10 @@ typedef struct {
 size_t pkv_evict_workspace_bytes(const pkv_evict_desc* desc);
 
 /*
- * desc        HOST.  What is written has places of its own: of po_*, of wo_* and
- *             of c_* the smallest stride is >= k_cap (c_*: d) and each larger one
- *             reaches behind all that the smaller ones span, where there are
- *             several sequences, heads or rows.
+ * desc        HOST.  What is written has places of its own: of po_*, of wo_*
+ *             and of c_* the smallest stride is >= k_cap (c_*: d), and each
+ *             larger one reaches behind all that the smaller ones span, where
+ *             there are several sequences, heads or rows.
  * K_cache, V_cache
  *             DEVICE, rows of d 16-bit elements, 16-byte aligned, compact or
  *             pools; rows behind the budget keep their content.  Pages that

@@ -2,12 +2,13 @@
 //
 // Two launches.  The first, a workgroup per (sequence, KV head), finds the smallest weight that stays and pairs the rows behind the
 // budget that stay with the holes before it, the i-th with the i-th by counting both (a prefix sum over waves): sources lie behind all
-// destinations, so that the second can copy the pairs' rows in any order, in place, by as many workgroups as the device holds.
+// destinations, so that the second can copy the pairs' rows in any order, in place, by two turns of workgroups at most.
 // Up to 64 rows are moved by the first already, which is the only one where there can be no more.
 // What bounds it: the first launch is one compute unit's time for a head, a few passes over 4-byte keys (pkv_topk.h) which stand in LDS
 // for up to 32k rows and in L2, through the workspace, beyond; the second the copy.  d 128, 8 heads: one row too many of 2049 in 8
-// sequences 6.7 us, 4 sequences of up to 32k rows to 2k 33 + 11 (keys formed again in each pass: 121), 131072 to 2048 117 (312 with keys
-// formed again), four times that at once 140, 64 sequences of 4096 to 2048 116 (0.5 GB moved).
+// sequences 6.7 us where the cache has room for no more, 10 in room for 4096 (the second launch finds nothing to do); 4 sequences of up to
+// 32k rows to 2k 33 + 12 (keys formed again in each pass: 121), 131072 to 2048 122 (312 with keys formed again), four times that at once 136,
+// 64 sequences of 4096 to 2048 145 (0.5 GB moved).
 #include <string.h>
 
 #include "pkv_long.h"
@@ -67,7 +68,7 @@ struct Unit {
 
 // What becomes of a row that is not moved into: before the budget it stays (holes are filled later), behind it it is emptied.  Where the
 // outputs are the inputs, the former is there already, and the latter waits until the moved rows have been read; where there is a second
-// launch, its many workgroups empty the rows (32k rows to 2k: 33.9 + 11 us without, 32.8 + 11 with).
+// launch, its many workgroups empty the rows (32k rows to 2k, 4 sequences: 33.9 us instead of 32.8 for the first if it does that itself).
 __device__ __forceinline__ void keep_row(const EvictArgs& a, const Unit& u, int r, int32_t p, float w) {
   const bool stays = r < a.budget;
   if (!stays && a.second) return;

@@ -66,7 +66,7 @@ struct TreeWideArgs : TreeArgs {
 };
 template <typename A>
 constexpr bool drafted_mode() { return A::MODE == kTree || A::MODE == kTreeWide; }
-// Query rows of a workgroup, and the factor that its sums carry (2^-).
+// Query rows of a workgroup.
 template <typename A>
 constexpr int group_rows() { return A::MODE == kTreeWide ? 128 : 64; }
 // Listed blocks: place x of the list's rows is row list[x >> shift] << shift | (x & (block - 1)).

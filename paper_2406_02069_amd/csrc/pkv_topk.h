@@ -46,7 +46,8 @@ struct Keys {
 };
 
 // Keys that wait in LDS between the passes over them: up to so many, as far as a cache can hold that many (kernels take the room as
-// dynamic LDS; a workgroup with all of it has a compute unit to itself).  All others are formed again for each pass.
+// dynamic LDS; a workgroup with all of it has a compute unit to itself).  Of more keys, eviction's wait in its workspace, and those of blocks
+// are formed again from the scores for each pass.
 constexpr int kKeysInLds = 32 * kThreads;
 // Raises a kernel's dynamic LDS limit to that, once per device (no allocation).
 inline hipError_t grant_keys(const void* kernel, bool* granted) {

@@ -3,8 +3,8 @@
 //   out_t = sum_j 2^(s_tj - m_t) V_j / sum_j 2^(s_tj - m_t)  over the rows j that token t sees, m_t a running reference.
 // The T Hq/Hkv query rows of a KV head share its rows of the cache: the more of them, the more products for each byte.  Up to 32 rows
 // HBM bounds (decode_long_kernel, which is described in pkv_decode_long.hip: 8 tokens of 32/8 heads, d 128, behind 100k rows 93 us, 4.4
-// TB/s); from there on feeding the matrix pipe does (tree_wide_kernel: 16 tokens 87 us, 64 145 - 149, 128 256).  In both only the steps that
-// hold drafted tokens look at the tree: 32 of its bits are one word, shifted to the step.
+// TB/s); from there on feeding the matrix pipe does (tree_wide_kernel: 16 tokens 88 us, 64 147, 128 258; whole calls, one after the other).
+// In both only the steps that hold drafted tokens look at the tree: 32 of its bits are one word, shifted to the step.
 //
 // tree_wide_kernel: a workgroup is 128 query rows of a KV head x a range of its cache, a wave 32 of the rows against all keys of the
 // range, 32 at a time.  What a wave of decode_long_kernel reads for 16 rows serves 128 here: 64 tokens took 439 us there, 209 at once
@@ -15,11 +15,15 @@
 //   scores  S^T = K Q^T in v_mfma_f32_32x32x16: 32 keys are the rows of A, 32 query rows the columns of B, which stay in registers.
 //           Lane (col, half) ends with 16 keys of row col.
 //   softmax the reference moves when a score exceeds it by 2^6.
-//   values  O^T += V^T P^T, V read column-wise.  The weights are rounded to the type once (decode_long_kernel's second product for
-//           what the rounding left would take the pipe's time here: 24 products a step at d 128 in place of 16).
-// What is left at 64 tokens behind 100k rows: two workgroups a compute unit run at 1.6 GHz under this load, the matrix pipe busy 37 %
-// of it, and 512 ranges' results are 33 MB that are written and read again (9 us in the join).  Capped and biased scores are bound by
-// vector instructions (8 sequences of 26 tokens with up to 5000 kept rows: 46 us + 7).
+//   values  O^T += V^T P^T, V read column-wise.  The weights are rounded to the type once.  decode_long_kernel's second product for what
+//           the rounding left would be 24 products a step at d 128 in place of 16, and the vector work that forms its operand: 9, 32, 64 and
+//           128 tokens behind 100k rows 86, 97, 147 and 258 us as it is, 94, 112, 184 and 335 with it; 8 sequences of 26 tokens and up to
+//           5000 kept rows 53 and 57.  The error of a result, relative to its size, is 2.3e-3 (64 bf16 tokens) and 2.3e-4
+//           (26 fp16 tokens), where rounding the result alone makes 1.7e-3 and 2.0e-4.
+// What is left at 64 tokens behind 100k rows (139 us at 2.0 GHz; 178 where it is called again and again under a profiler, at 1.6 GHz; 9 in
+// the join of 512 ranges' results, 33 MB): vector instructions are issued in 43 % of the cycles, the matrix pipe is busy in 40 %, LDS in
+// 20 % without conflicts, and a wave waits for loads, the barrier or a product for 38 % of its time: two waves a SIMD do not fill one
+// another's gaps.  With biases and kept positions (8 sequences of 26 tokens: 46 us + 7.6) waves wait 57 % of their time, 31 % is vector issue.
 #include <type_traits>
 
 #include "pkv_long.h"
